@@ -286,6 +286,92 @@ int mla_recon_prefill(const mla_recon_cfg *cfg, const void *q, const void *cache
 int mla_recon_fold_uv_into_o(const mla_recon_cfg *cfg, const void *Wo, const void *Wuv,
                              void *Wo_folded, void *hip_stream);
 
+/* ---- serving from a paged latent cache -----------------------------------------------
+ * The cache of one layer in pages that any sequence may own or share: position p of sequence
+ * b lies in row p % page_size of page page_table[b][p / page_size] of the pool.  Rows are
+ * [c^KV | R_p k^PE] of r_kv + G_r d_rope values in the storage dtype, as for mla_recon_decode.
+ *   pool        device [n_pages, page_size, r_kv + G_r d_rope], 16-byte aligned
+ *   page_table  device int32 [batch, max_pages]; only the entries of pages that a call reads
+ *               or writes are looked at, the others may hold anything
+ * page_size is any positive number of rows.  A table entry outside [0, n_pages) names no
+ * page: nothing is written there, and an output that depends on a row there is NaN.  The
+ * struct is a host struct read during the call; what it points to belongs to the caller.
+ * Lengths, offsets and tables are device arrays read by the kernels, so that a captured
+ * graph follows what they hold at each replay. */
+typedef struct {
+  void *pool;
+  const int32_t *page_table;
+  int32_t n_pages, page_size, max_pages;
+} mla_paged_cache;
+
+/* New tokens enter the cache: packed row i with offsets[b] <= i < offsets[b + 1] is the token
+ * of sequence b at position p = start[b] + i - offsets[b].
+ *   rows    [n_rows, r_kv + G_r d_rope], storage dtype: [c^KV | k^PE], k^PE not rotated.  The
+ *           row is written to its place in the pool, k^PE rotated by R_p.  NULL: the pool is
+ *           left as it is (q only)
+ *   q       [n_rows, H, d_nope + d_rope], storage dtype, or NULL: [q^nope | q^rope], not rotated
+ *   q_out   the same shape: [q^nope | R_p q^rope]; may be q itself (rotated in place) and is
+ *           NULL iff q is.  The pool may not overlap any of these, nor q_out rows or another
+ *           part of q
+ *   offsets device int32 [batch + 1], start device int32 [batch] (start[b] >= 0)
+ *   inv_freq device fp32 [G_r, d_rope / 2]
+ * Both dtypes, any G_r (head i takes the frequencies of group i / (H / G_r)).  Angles are taken
+ * in fp64, the rotation in fp32, rounded once.  Packed rows outside [offsets[0], offsets[batch])
+ * are not read and their q_out rows not written; a row whose position lies outside its
+ * sequence's table or on no page is not written (its q_out row is).  Two rows for the same
+ * place of the pool are the caller's error: one of them ends there.
+ * rows, q and q_out 16-byte aligned; at most 8388608 rows, G_r d_rope at most 8192. */
+int mla_recon_cache_append(const mla_recon_cfg *cfg, const mla_paged_cache *cache, const void *rows,
+                           const void *q, void *q_out, int32_t n_rows, const int32_t *offsets,
+                           const int32_t *start, const float *inv_freq, void *hip_stream);
+
+/* mla_recon_decode over a paged cache: one query token per sequence, cfg and its requirements,
+ * q, Wuk (may be NULL if d_nope is 0), Wuv and o as there (cfg->seq is not used).
+ *   max_len an upper bound of the lengths: sequence b attends to its first lengths[b] rows,
+ *           clamped to [0, min(max_len, max_pages page_size)] (0 rows give o = 0)
+ * The work is cut over the rows of all sequences together, so that lengths that differ keep
+ * the whole GPU busy.  ws 16-byte aligned, of mla_recon_decode_paged_workspace_size bytes for
+ * this cfg and max_len (0 = unsupported or invalid). */
+size_t mla_recon_decode_paged_workspace_size(const mla_recon_cfg *cfg, int32_t max_len);
+int mla_recon_decode_paged(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
+                           int32_t max_len, const int32_t *lengths, const void *Wuk,
+                           const void *Wuv, void *o, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Packed prompts, or the next tokens of sequences whose earlier rows are cached, over a paged
+ * cache that already holds the new tokens' rows (mla_recon_cache_append): sequence b has the
+ * query tokens q_offsets[b] .. q_offsets[b + 1] - 1 and kv_offsets[b + 1] - kv_offsets[b]
+ * cached rows; its queries are the last of these positions, and each attends to the rows up
+ * to its own (a query before the first row, where a sequence has more queries than rows,
+ * sees nothing: o = 0).  cfg as for mla_recon_decode (cfg->batch sequences, cfg->seq not used).
+ *   q          [n_q, H, d_nope + d_rope] bf16 (q^rope rotated)
+ *   q_offsets  device int32 [batch + 1], not decreasing, within [0, n_q]
+ *   kv_offsets device int32 [batch + 1], not decreasing, within [0, n_kv]: prefix sums of the
+ *              cached rows of the sequences, n_kv an upper bound of their sum
+ *   Wuk [G_kv d_nope, r_kv] (may be NULL if d_nope is 0), Wuv [G_kv d_k, r_kv] bf16
+ *   o          [n_q, H, d_k] bf16 out; rows of no sequence are left as they were
+ * Keys and values of all n_kv rows are expanded into ws once per call (for single tokens over
+ * long caches mla_recon_decode_paged is the cheaper call).  A row that is not finite (or whose
+ * values are not) makes the outputs of the queries that see it NaN and leaves all others as
+ * they are.  n_q and n_kv at most 1048576.  q, Wuv, o and ws 16-byte aligned, ws of
+ * mla_recon_prefill_paged_workspace_size bytes. */
+size_t mla_recon_prefill_paged_workspace_size(const mla_recon_cfg *cfg, int32_t n_q, int32_t n_kv);
+int mla_recon_prefill_paged(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
+                            const int32_t *q_offsets, const mla_paged_cache *cache, int32_t n_kv,
+                            const int32_t *kv_offsets, const void *Wuk, const void *Wuv, void *o,
+                            void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Pages copied in every layer of a cache, for forking a sequence (its last, partly filled page)
+ * and for compacting a pool: page pairs[2 i + 1] becomes a copy of page pairs[2 i].
+ *   pool    device: layer l's n_pages pages of page_bytes each at pool + l layer_stride (bytes)
+ *   pairs   HOST int32 [n_pairs, 2], read during the call (a captured graph keeps the pairs of
+ *           its capture); all pages within [0, n_pages), no page the destination of two pairs or
+ *           both a destination and a source: MLA_ERR_INVALID_ARG otherwise
+ * pool, page_bytes and layer_stride multiples of 16; layer_stride (of n_layers > 1) at least
+ * n_pages page_bytes; at most 65535 layers and 16 GiB a page.  0 pairs: nothing happens. */
+int mla_recon_cache_copy_pages(void *pool, int32_t n_layers, int64_t layer_stride, int32_t n_pages,
+                               int64_t page_bytes, const int32_t *pairs, int32_t n_pairs,
+                               void *hip_stream);
+
 /* Text of the last error on the calling thread ("" if none). */
 const char *mla_recon_last_error(void);
 

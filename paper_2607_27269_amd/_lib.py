@@ -84,6 +84,13 @@ class AdamwTensor(ctypes.Structure):
                 ("w", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("n", ctypes.c_int64)]
 
 
+class PagedCache(ctypes.Structure):
+    """One layer's paged latent cache (mla_paged_cache): device pointers and sizes."""
+    _fields_ = [("pool", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -117,6 +124,17 @@ def lib() -> ctypes.CDLL:
         L.mla_recon_prefill_workspace_size.restype = sz
         L.mla_recon_prefill.argtypes = [P(Cfg), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.mla_recon_fold_uv_into_o.argtypes = [P(Cfg), vp, vp, vp, vp]
+        L.mla_recon_cache_append.argtypes = [P(Cfg), P(PagedCache), vp, vp, vp, i32, vp, vp, vp, vp]
+        L.mla_recon_decode_paged_workspace_size.argtypes = [P(Cfg), i32]
+        L.mla_recon_decode_paged_workspace_size.restype = sz
+        L.mla_recon_decode_paged.argtypes = [P(Cfg), vp, P(PagedCache), i32, vp, vp, vp, vp, vp, sz,
+                                             vp]
+        L.mla_recon_prefill_paged_workspace_size.argtypes = [P(Cfg), i32, i32]
+        L.mla_recon_prefill_paged_workspace_size.restype = sz
+        L.mla_recon_prefill_paged.argtypes = [P(Cfg), vp, i32, vp, P(PagedCache), i32, vp, vp, vp, vp,
+                                              vp, sz, vp]
+        L.mla_recon_cache_copy_pages.argtypes = [vp, i32, ctypes.c_int64, i32, ctypes.c_int64,
+                                                 P(ctypes.c_int32), i32, vp]
         L.mla_recon_adamw.argtypes = [P(AdamwTensor), i32, i32, i32, ctypes.c_float,
                                       ctypes.c_float, ctypes.c_float, ctypes.c_float,
                                       ctypes.c_float, vp]
@@ -128,7 +146,8 @@ def lib() -> ctypes.CDLL:
                   "mla_recon_student_step", "mla_recon_rel_error", "mla_recon_adamw",
                   "mla_recon_residual_rmsnorm",
                   "mla_recon_decode", "mla_recon_decode_noalloc", "mla_recon_prefill",
-                  "mla_recon_fold_uv_into_o",
+                  "mla_recon_fold_uv_into_o", "mla_recon_cache_append", "mla_recon_decode_paged",
+                  "mla_recon_prefill_paged", "mla_recon_cache_copy_pages",
                   "mla_recon_prof_enable",
                   "mla_recon_prof_read"):
             getattr(L, f).restype = i32
@@ -258,6 +277,45 @@ def mla_recon_prefill(cfg: Cfg, q: int, cache: int, Wuk: int, Wuv: int, Wo: int,
 
 def mla_recon_fold_uv_into_o(cfg: Cfg, Wo: int, Wuv: int, Wo_folded: int, stream: int) -> None:
     _check(lib().mla_recon_fold_uv_into_o(ctypes.byref(cfg), Wo, Wuv, Wo_folded, stream))
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def mla_recon_cache_append(cfg: Cfg, cache: PagedCache, rows: int | None, q: int | None,
+                           q_out: int | None, n_rows: int, offsets: int, start: int, inv_freq: int,
+                           stream: int) -> None:
+    _check(lib().mla_recon_cache_append(ctypes.byref(cfg), _ref(cache), rows, q, q_out, n_rows,
+                                        offsets, start, inv_freq, stream))
+
+
+def mla_recon_decode_paged_workspace_size(cfg: Cfg, max_len: int) -> int:
+    return int(lib().mla_recon_decode_paged_workspace_size(ctypes.byref(cfg), max_len))
+
+
+def mla_recon_decode_paged(cfg: Cfg, q: int, cache: PagedCache, max_len: int, lengths: int, Wuk: int,
+                           Wuv: int, o: int, ws: int, ws_bytes: int, stream: int) -> None:
+    _check(lib().mla_recon_decode_paged(ctypes.byref(cfg), q, _ref(cache), max_len, lengths, Wuk, Wuv,
+                                        o, ws, ws_bytes, stream))
+
+
+def mla_recon_prefill_paged_workspace_size(cfg: Cfg, n_q: int, n_kv: int) -> int:
+    return int(lib().mla_recon_prefill_paged_workspace_size(ctypes.byref(cfg), n_q, n_kv))
+
+
+def mla_recon_prefill_paged(cfg: Cfg, q: int, n_q: int, q_offsets: int, cache: PagedCache, n_kv: int,
+                            kv_offsets: int, Wuk: int, Wuv: int, o: int, ws: int, ws_bytes: int,
+                            stream: int) -> None:
+    _check(lib().mla_recon_prefill_paged(ctypes.byref(cfg), q, n_q, q_offsets, _ref(cache), n_kv,
+                                         kv_offsets, Wuk, Wuv, o, ws, ws_bytes, stream))
+
+
+def mla_recon_cache_copy_pages(pool: int, n_layers: int, layer_stride: int, n_pages: int,
+                               page_bytes: int, pairs, n_pairs: int, stream: int) -> None:
+    """``pairs``: a ctypes pointer to (or array of) the host's 2 n_pairs page numbers."""
+    _check(lib().mla_recon_cache_copy_pages(pool, n_layers, layer_stride, n_pages, page_bytes, pairs,
+                                            n_pairs, stream))
 
 
 def mla_recon_prof_enable(kclass: int, on: bool) -> None:

@@ -4,6 +4,7 @@
 
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -1050,6 +1051,181 @@ int mla_recon_fold_uv_into_o(const mla_recon_cfg* cfg, const void* Wo, const voi
                     (const uint16_t*)Wuv + (size_t)(i / hpg) * dv * rkv, rkv, false,
                     (uint16_t*)Wo_folded + (size_t)i * rkv, (int64_t)H * rkv, DT_BF16, DT_BF16),
                  nullptr, 0, s));
+  return MLA_OK;
+}
+
+// ---- the paged latent cache ------------------------------------------------------------
+static int paged_check(const mla_recon_cfg* cfg, const mla_paged_cache* c, const char* who) {
+  if (!c) return fail(MLA_ERR_INVALID_ARG, "%s: cache is NULL", who);
+  if (!c->pool || !c->page_table)
+    return fail(MLA_ERR_INVALID_ARG, "%s: NULL pool or page table", who);
+  if (c->n_pages < 1 || c->page_size < 1 || c->max_pages < 1)
+    return fail(MLA_ERR_INVALID_ARG, "%s: n_pages, page_size and max_pages must be positive", who);
+  if ((uintptr_t)c->pool % 16)
+    return fail(MLA_ERR_INVALID_ARG, "%s: the pool must be 16-byte aligned", who);
+  if ((double)c->n_pages * c->page_size * (cfg->kv_rank + (double)cfg->s_rope_groups * cfg->rope_dim) >= 2.0e18)
+    return fail(MLA_ERR_INVALID_ARG, "%s: pool too large", who);
+  return MLA_OK;
+}
+
+static PagedPool pool_of(const mla_recon_cfg* cfg, const mla_paged_cache* c) {
+  return PagedPool{c->pool, c->page_table, c->n_pages, c->page_size, c->max_pages,
+                   cfg->kv_rank + cfg->s_rope_groups * cfg->rope_dim};
+}
+
+int mla_recon_cache_append(const mla_recon_cfg* cfg, const mla_paged_cache* cache, const void* rows,
+                           const void* q, void* q_out, int32_t n_rows, const int32_t* offsets,
+                           const int32_t* start, const float* inv_freq, void* hip_stream) {
+  g_err[0] = 0;
+  int rc = check_cfg(cfg);
+  if (rc) return rc;
+  if ((rc = paged_check(cfg, cache, "cache_append"))) return rc;
+  if (n_rows < 0) return fail(MLA_ERR_INVALID_ARG, "cache_append: negative number of rows");
+  if (n_rows > 1 << 23) return fail(MLA_ERR_UNSUPPORTED, "cache_append: at most %d rows per call", 1 << 23);
+  if (!offsets || !start || !inv_freq)
+    return fail(MLA_ERR_INVALID_ARG, "cache_append: NULL pointer argument");
+  if (!rows && !q) return fail(MLA_ERR_INVALID_ARG, "cache_append: neither rows nor q given");
+  if (!q != !q_out) return fail(MLA_ERR_INVALID_ARG, "cache_append: q and q_out go together");
+  if (((uintptr_t)rows | (uintptr_t)q | (uintptr_t)q_out) % 16)
+    return fail(MLA_ERR_INVALID_ARG, "cache_append: rows, q and q_out must be 16-byte aligned");
+  if ((int64_t)cfg->s_rope_groups * cfg->rope_dim > 8192)
+    return fail(MLA_ERR_UNSUPPORTED, "cache_append: %d positional keys of %d values (at most 8192 in all)",
+                cfg->s_rope_groups, cfg->rope_dim);
+  CacheAppend a;
+  a.c = pool_of(cfg, cache);
+  a.B = cfg->batch; a.H = cfg->n_heads; a.dn = cfg->nope_dim; a.dr = cfg->rope_dim;
+  a.rkv = cfg->kv_rank; a.Gr = cfg->s_rope_groups; a.n_rows = n_rows; a.rows = rows; a.q = q;
+  a.q_out = q_out; a.offsets = offsets; a.start = start; a.inv_freq = inv_freq;
+  a.t = cfg->dtype == MLA_FP32 ? DT_F32 : DT_BF16;
+  HIP_TRY(cache_append(a, (hipStream_t)hip_stream));
+  return MLA_OK;
+}
+
+size_t mla_recon_decode_paged_workspace_size(const mla_recon_cfg* cfg, int32_t max_len) {
+  g_err[0] = 0;
+  if (decode_check(cfg, max_len)) return 0;
+  return decode_paged_ws_bytes(cfg->batch, cfg->n_heads, cfg->kv_rank + cfg->rope_dim, cfg->kv_rank,
+                               max_len);
+}
+
+int mla_recon_decode_paged(const mla_recon_cfg* cfg, const void* q, const mla_paged_cache* cache,
+                           int32_t max_len, const int32_t* lengths, const void* Wuk,
+                           const void* Wuv, void* o, void* ws, size_t ws_bytes, void* hip_stream) {
+  g_err[0] = 0;
+  int rc = decode_check(cfg, max_len);
+  if (rc) return rc;
+  if ((rc = paged_check(cfg, cache, "decode_paged"))) return rc;
+  // (no W_UK without non-positional keys)
+  if ((rc = decode_args(cfg, q, cache->pool, lengths, cfg->nope_dim ? Wuk : Wuv, Wuv, o, "decode_paged"))) return rc;
+  if (!ws) return fail(MLA_ERR_INVALID_ARG, "decode_paged: NULL workspace");
+  if ((uintptr_t)ws % 16) return fail(MLA_ERR_INVALID_ARG, "decode_paged: ws must be 16-byte aligned");
+  const size_t need = decode_paged_ws_bytes(cfg->batch, cfg->n_heads, cfg->kv_rank + cfg->rope_dim,
+                                            cfg->kv_rank, max_len);
+  if (ws_bytes < need)
+    return fail(MLA_ERR_WORKSPACE, "decode_paged: workspace too small: %zu < %zu bytes", ws_bytes, need);
+  DecodePaged d;
+  d.c = pool_of(cfg, cache);
+  d.B = cfg->batch; d.H = cfg->n_heads; d.dn = cfg->nope_dim; d.dr = cfg->rope_dim;
+  d.rkv = cfg->kv_rank; d.dv = cfg->head_dim; d.hpg = cfg->n_heads / cfg->s_kv_groups;
+  d.q = q; d.len = lengths; d.Wuk = Wuk; d.Wuv = Wuv; d.scale = cfg->softmax_scale; d.o = o; d.ws = ws;
+  d.max_len = (int)std::min<int64_t>(max_len, (int64_t)cache->page_size * cache->max_pages);
+  HIP_TRY(decode_paged(d, (hipStream_t)hip_stream));
+  return MLA_OK;
+}
+
+constexpr int32_t PREFILL_PAGED_MAX = 1 << 20;
+
+static int prefill_paged_check(const mla_recon_cfg* cfg, int32_t n_q, int32_t n_kv, PrefillPaged* p) {
+  int rc = decode_check(cfg, 1);
+  if (rc) return rc;
+  if (n_q < 0 || n_kv < 0)
+    return fail(MLA_ERR_INVALID_ARG, "prefill_paged: negative number of tokens or rows");
+  if (n_q > PREFILL_PAGED_MAX || n_kv > PREFILL_PAGED_MAX)
+    return fail(MLA_ERR_UNSUPPORTED, "prefill_paged: at most %d tokens and %d cached rows per call",
+                PREFILL_PAGED_MAX, PREFILL_PAGED_MAX);
+  p->B = cfg->batch; p->H = cfg->n_heads; p->G = cfg->s_kv_groups; p->dn = cfg->nope_dim;
+  p->dr = cfg->rope_dim; p->rkv = cfg->kv_rank; p->dv = cfg->head_dim;
+  p->n_q = n_q; p->n_kv = n_kv; p->scale = cfg->softmax_scale;
+  return MLA_OK;
+}
+
+size_t mla_recon_prefill_paged_workspace_size(const mla_recon_cfg* cfg, int32_t n_q, int32_t n_kv) {
+  g_err[0] = 0;
+  PrefillPaged p;
+  if (prefill_paged_check(cfg, n_q, n_kv, &p)) return 0;
+  return prefill_paged_ws_bytes(p);
+}
+
+int mla_recon_prefill_paged(const mla_recon_cfg* cfg, const void* q, int32_t n_q,
+                            const int32_t* q_offsets, const mla_paged_cache* cache, int32_t n_kv,
+                            const int32_t* kv_offsets, const void* Wuk, const void* Wuv, void* o,
+                            void* ws, size_t ws_bytes, void* hip_stream) {
+  g_err[0] = 0;
+  PrefillPaged p;
+  int rc = prefill_paged_check(cfg, n_q, n_kv, &p);
+  if (rc) return rc;
+  if ((rc = paged_check(cfg, cache, "prefill_paged"))) return rc;
+  if (!q || !q_offsets || !kv_offsets || (!Wuk && cfg->nope_dim) || !Wuv || !o || !ws)
+    return fail(MLA_ERR_INVALID_ARG, "prefill_paged: NULL pointer argument");
+  if (((uintptr_t)q | (uintptr_t)Wuv | (uintptr_t)o | (uintptr_t)ws) % 16)
+    return fail(MLA_ERR_INVALID_ARG, "prefill_paged: q, Wuv, o and ws must be 16-byte aligned");
+  const size_t need = prefill_paged_ws_bytes(p);
+  if (ws_bytes < need)
+    return fail(MLA_ERR_WORKSPACE, "prefill_paged: workspace too small: %zu < %zu bytes", ws_bytes, need);
+  if (n_q == 0) return MLA_OK;
+  p.c = pool_of(cfg, cache);
+  p.q = q; p.q_off = q_offsets; p.kv_off = kv_offsets; p.Wuk = Wuk; p.Wuv = Wuv; p.o = o; p.ws = ws;
+  HIP_TRY(prefill_paged(p, (hipStream_t)hip_stream));
+  return MLA_OK;
+}
+
+// Every destination is named once and is no source (a page that is both would be read while it
+// is written): checked against the sorted destinations.
+static int check_pairs(const int32_t* pairs, int32_t n_pairs, int32_t n_pages) {
+  for (int64_t i = 0; i < 2 * (int64_t)n_pairs; ++i)
+    if (pairs[i] < 0 || pairs[i] >= n_pages)
+      return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: pair %d names page %d of %d", (int)(i / 2), pairs[i], n_pages);
+  int32_t few[64];
+  int32_t* dst = n_pairs <= 64 ? few : (int32_t*)malloc((size_t)n_pairs * sizeof(int32_t));
+  if (!dst) return fail(MLA_ERR_HIP, "cache_copy_pages: no host memory for %d pairs", n_pairs);
+  for (int64_t i = 0; i < n_pairs; ++i) dst[i] = pairs[2 * i + 1];
+  std::sort(dst, dst + n_pairs);
+  int32_t twice = -1, both = -1;
+  for (int32_t i = 1; i < n_pairs; ++i)
+    if (dst[i] == dst[i - 1]) twice = dst[i];
+  for (int64_t i = 0; i < n_pairs; ++i)
+    if (std::binary_search(dst, dst + n_pairs, pairs[2 * i])) both = pairs[2 * i];
+  if (dst != few) free(dst);
+  if (twice >= 0)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: page %d is the destination of two pairs", twice);
+  if (both >= 0)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: page %d is a source and a destination", both);
+  return MLA_OK;
+}
+
+int mla_recon_cache_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, int32_t n_pages,
+                               int64_t page_bytes, const int32_t* pairs, int32_t n_pairs,
+                               void* hip_stream) {
+  g_err[0] = 0;
+  if (!pool) return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: NULL pool");
+  if (n_layers < 1 || n_pages < 1 || page_bytes < 1 || n_pairs < 0)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: bad number of layers, pages, bytes or pairs");
+  if (n_layers > 65535) return fail(MLA_ERR_UNSUPPORTED, "cache_copy_pages: at most 65535 layers");
+  if ((uintptr_t)pool % 16 || page_bytes % 16 || layer_stride % 16)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: pool, page_bytes and layer_stride must be multiples of 16");
+  if (page_bytes > ((int64_t)1 << 34) || (double)n_pages * page_bytes > 4.0e18 ||
+      (double)n_layers * (double)layer_stride > 4.0e18)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: pool too large");
+  if (n_layers > 1 && layer_stride < n_pages * page_bytes)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: layers overlap");
+  if (n_pairs == 0) return MLA_OK;
+  if (!pairs) return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: NULL pairs");
+  if (n_pairs > n_pages)
+    return fail(MLA_ERR_INVALID_ARG, "cache_copy_pages: more pairs than pages");
+  int rc = check_pairs(pairs, n_pairs, n_pages);
+  if (rc) return rc;
+  HIP_TRY(cache_copy_pages(pool, n_layers, layer_stride, page_bytes, pairs, n_pairs,
+                           (hipStream_t)hip_stream));
   return MLA_OK;
 }
 

@@ -514,6 +514,17 @@ size_t decode_ws_bytes(int B, int H, int DK, int DVL, int Lmax) {
          al((size_t)B * nsplit * HP * 2 * 4) + al((size_t)B * H * DVL * 2);
 }
 
+hipError_t decode_absorb(const void* q, const void* Wuk, void* qabs, int B, int H, int HP, int hpg,
+                         int dn, int dr, int rkv, hipStream_t s) {
+  if (dn > ABS_DN || rkv % 64) return hipErrorInvalidValue;
+  prof_begin(KC_ELEM, s);
+  absorb_kernel<<<dim3(rkv / 64, (B * hpg + 31) / 32, H / hpg), 128, 0, s>>>(
+      (const bf16_t*)q, (const bf16_t*)Wuk, (bf16_t*)qabs, B, H, HP, hpg, dn, dr, rkv);
+  prof_end(KC_ELEM, s, 2.0 * B * H * dn * rkv, (double)B * H * (rkv + dr + dn + dr) * 2,
+           KLABEL("absorb_kernel"));
+  return hipSuccess;
+}
+
 hipError_t decode_attention(const Decode& d, hipStream_t s) {
   const int DK = d.rkv + d.dr, DVL = d.rkv;
   if (!decode_supported(DK, DVL)) return hipErrorInvalidValue;
@@ -529,13 +540,8 @@ hipError_t decode_attention(const Decode& d, hipStream_t s) {
   float* part_ml = (float*)w;
   w += al((size_t)d.B * nsplit * HP * 2 * 4);
 
-  const int G = d.H / d.hpg;
-  if (d.dn > ABS_DN || d.rkv % 64) return hipErrorInvalidValue;
-  prof_begin(KC_ELEM, s);
-  absorb_kernel<<<dim3(d.rkv / 64, (d.B * d.hpg + 31) / 32, G), 128, 0, s>>>(
-      (const bf16_t*)d.q, (const bf16_t*)d.Wuk, qabs, d.B, d.H, HP, d.hpg, d.dn, d.dr, d.rkv);
-  prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dn * d.rkv, (double)d.B * d.H * (DK + d.dn + d.dr) * 2,
-           KLABEL("absorb_kernel"));
+  hipError_t e = decode_absorb(d.q, d.Wuk, qabs, d.B, d.H, HP, d.hpg, d.dn, d.dr, d.rkv, s);
+  if (e != hipSuccess) return e;
 
   DecodeDev a;
   a.qabs = qabs; a.cache = (const bf16_t*)d.cache; a.ldc = d.ldc;

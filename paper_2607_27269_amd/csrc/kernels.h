@@ -274,6 +274,65 @@ hipError_t uv_project(const void* lat, const void* Wuv, void* o, int rows, int H
 hipError_t prefill_guard(const void* cache, int64_t rows, int rkv, int dr, void* keys, int nk,
                          bool copy_pe, void* v, int nv, void* lat_copy, hipStream_t s);
 
+// The paged latent cache (one layer) and its operators: see paged.hip and paged_attn.hip.
+// Position p of sequence b is row p % page_size of page table[b][p / page_size].
+struct PagedPool {
+  void* pool;                      // [n_pages][page_size][width]
+  const int32_t* table;            // [B][max_pages] device
+  int n_pages, page_size, max_pages, width;
+};
+// New tokens' rows into the pages, the positional keys (and q's rotary part) rotated.
+struct CacheAppend {
+  PagedPool c;
+  int B, H, dn, dr, rkv, Gr;
+  int n_rows;
+  const void* rows;                // [n_rows][width] or null
+  const void* q;                   // [n_rows][H][dn + dr] or null
+  void* q_out;
+  const int32_t* offsets;          // [B + 1] device
+  const int32_t* start;            // [B] device
+  const float* inv_freq;           // [Gr][dr / 2]
+  DType t;
+};
+hipError_t cache_append(const CacheAppend& a, hipStream_t s);
+// page pairs[2 i] -> pages pairs[2 i + 1] (host array) of every layer; bytes multiples of 16
+hipError_t cache_copy_pages(void* pool, int n_layers, int64_t layer_stride, int64_t page_bytes,
+                            const int32_t* pairs, int n_pairs, hipStream_t s);
+
+// Absorbed-form attention of single tokens over a paged cache.
+struct DecodePaged {
+  PagedPool c;
+  int B, H, dn, dr, rkv, dv, hpg;
+  const void* q;                   // [B][H][dn + dr] bf16
+  int max_len;
+  const int32_t* len;              // [B] device
+  const void *Wuk, *Wuv;
+  float scale;
+  void* o;                         // [B][H][dv] bf16
+  void* ws;                        // decode_paged_ws_bytes
+};
+size_t decode_paged_ws_bytes(int B, int H, int DK, int DVL, int max_len);
+hipError_t decode_paged(const DecodePaged& d, hipStream_t s);
+
+// Causal attention of packed query tokens over the cached rows of their sequences.
+struct PrefillPaged {
+  PagedPool c;
+  int B, H, G, dn, dr, rkv, dv;
+  const void* q;                   // [n_q][H][dn + dr] bf16
+  int n_q, n_kv;
+  const int32_t *q_off, *kv_off;   // [B + 1] device
+  const void *Wuk, *Wuv;
+  float scale;
+  void* o;                         // [n_q][H][dv] bf16
+  void* ws;
+};
+size_t prefill_paged_ws_bytes(const PrefillPaged& p);
+hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s);
+
+// The absorbed queries of decoding: qabs [B][HP][rkv + dr] (rows past H are not written).
+hipError_t decode_absorb(const void* q, const void* Wuk, void* qabs, int B, int H, int HP, int hpg,
+                         int dn, int dr, int rkv, hipStream_t s);
+
 // out = a - b elementwise over n elements of dtype t (fp32 arithmetic)
 hipError_t sub_elementwise(const void* a, const void* b, void* out, int64_t n, DType t,
                            hipStream_t s);
