@@ -328,7 +328,8 @@ int mla_recon_cache_append(const mla_recon_cfg *cfg, const mla_paged_cache *cach
 /* mla_recon_decode over a paged cache: one query token per sequence, cfg and its requirements,
  * q, Wuk (may be NULL if d_nope is 0), Wuv and o as there (cfg->seq is not used).
  *   max_len an upper bound of the lengths: sequence b attends to its first lengths[b] rows,
- *           clamped to [0, min(max_len, max_pages page_size)] (0 rows give o = 0)
+ *           clamped to [0, min(max_len, max_pages page_size)] (0 rows give o = 0); batch max_len
+ *           at most 2^35
  * The work is cut over the rows of all sequences together, so that lengths that differ keep
  * the whole GPU busy.  ws 16-byte aligned, of mla_recon_decode_paged_workspace_size bytes for
  * this cfg and max_len (0 = unsupported or invalid). */

@@ -1101,9 +1101,18 @@ int mla_recon_cache_append(const mla_recon_cfg* cfg, const mla_paged_cache* cach
   return MLA_OK;
 }
 
+// (the kernels number the tiles of all sequences with 32 bits)
+static int decode_paged_check(const mla_recon_cfg* cfg, int32_t max_len) {
+  int rc = decode_check(cfg, max_len);
+  if (rc) return rc;
+  if ((int64_t)cfg->batch * max_len > (int64_t)1 << 35)
+    return fail(MLA_ERR_UNSUPPORTED, "decode_paged: at most 2^35 rows (batch times max_len) per call");
+  return MLA_OK;
+}
+
 size_t mla_recon_decode_paged_workspace_size(const mla_recon_cfg* cfg, int32_t max_len) {
   g_err[0] = 0;
-  if (decode_check(cfg, max_len)) return 0;
+  if (decode_paged_check(cfg, max_len)) return 0;
   return decode_paged_ws_bytes(cfg->batch, cfg->n_heads, cfg->kv_rank + cfg->rope_dim, cfg->kv_rank,
                                max_len);
 }
@@ -1112,7 +1121,7 @@ int mla_recon_decode_paged(const mla_recon_cfg* cfg, const void* q, const mla_pa
                            int32_t max_len, const int32_t* lengths, const void* Wuk,
                            const void* Wuv, void* o, void* ws, size_t ws_bytes, void* hip_stream) {
   g_err[0] = 0;
-  int rc = decode_check(cfg, max_len);
+  int rc = decode_paged_check(cfg, max_len);
   if (rc) return rc;
   if ((rc = paged_check(cfg, cache, "decode_paged"))) return rc;
   // (no W_UK without non-positional keys)
