@@ -113,20 +113,21 @@ size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 // every cache row is read once for all heads, 60 operations a byte at 32 heads, and the rows'
 // stream bounds the kernel.
 //
-// * The rows of all sequences, in tiles of 32, form one list; a workgroup takes an equal share
-//   of it, whatever the lengths (one workgroup a CU).  The part of a sequence in a workgroup's
-//   share is a segment; its partial result goes to slot (workgroup + sequence), which no other
-//   segment has: along the list one of the two grows from segment to segment.
-// * Within a segment every wavefront takes every fourth tile by itself: its own LDS buffer, its
-//   own softmax state (running maximum and sum of each head, the weighted latents of all heads in
-//   256 registers), no barrier and no exchange until the segment ends.  While one wavefront waits
-//   for its copies the others multiply: about three of the four 37 KB tiles of a CU are in flight
-//   at any time.
+// * The rows of all sequences, in tiles of 32, form one list; a workgroup (one a CU) takes an
+//   equal share of it, whatever the lengths, and each of its four wavefronts a quarter of the
+//   share, a run of tiles that may cross from sequence to sequence.
+// * A wavefront works on its run by itself: its own LDS buffer, its own softmax state (running
+//   maximum and sum of each head, the weighted latents of all heads in 256 registers), no barrier
+//   and no exchange.  While one wavefront waits for its copies the others multiply: about three of
+//   the four 37 KB tiles of a CU are in flight at any time.
+// * Where a wavefront leaves a sequence it stores the state to slot (wavefront + sequence), which
+//   nobody else has: along the list one of the two grows from state to state.  Where the whole
+//   share lies in one sequence the four states are joined through LDS first and only one is stored
+//   (with long sequences a quarter of the traffic).
 // * S^T = K Q^T has the row in the MFMA row and the head in its column, so a lane owns one head's
 //   state, and the accumulator of S^T is, after the exponential, the B operand of O^T = V^T P^T
 //   (the order of the rows inside a K step is the same on both sides).  V^T comes from the same
 //   LDS tile by transposing reads.
-// * The four states of a segment are joined through LDS in two exchanges of halves.
 constexpr int PD_KT = 32;         // rows per tile
 constexpr int PD_WAVES = 4;
 constexpr float PD_SLACK = 8.f;   // log2 units the running reference maximum may lag
@@ -149,8 +150,15 @@ __device__ __forceinline__ int decode_len(const PagedDecodeDev& a, int b) {
   return min(max(a.len[b], 0), a.max_len);
 }
 __device__ __forceinline__ int tiles_of(int n) { return (n + PD_KT - 1) / PD_KT; }
-// Tiles per workgroup: at least one for each wavefront.
-__device__ __forceinline__ int share_of(int tiles, int nwg) { return max(PD_WAVES, (tiles + nwg - 1) / nwg); }
+// The list's cut: tiles per workgroup (at least one for each wavefront), and the part of
+// workgroup w and of its wavefronts.
+struct ListCut {
+  int total, share;
+  __device__ __forceinline__ ListCut(int tiles, int nwg) : total(tiles), share(max(PD_WAVES, (tiles + nwg - 1) / nwg)) {}
+  __device__ __forceinline__ int lo(int w) const { return (int)min((int64_t)w * share, (int64_t)total); }
+  __device__ __forceinline__ int hi(int w) const { return min(lo(w) + share, total); }
+  __device__ __forceinline__ int per_wave(int w) const { return (hi(w) - lo(w) + PD_WAVES - 1) / PD_WAVES; }
+};
 
 // Matrix products with their accumulators where they are wanted: the weighted latents fill the 256
 // accumulation registers, the tile's logits are in vector registers.  (The compiler puts every
@@ -174,7 +182,7 @@ __device__ __forceinline__ void mfma_a_done(f32x16 (&d)[N]) {
 #pragma unroll
   for (int c = 1; c < N; ++c) asm volatile("" : "+a"(d[c]));
 }
-// v *= f, v[4 g ..] += y on accumulation registers
+// v *= f on accumulation registers
 __device__ __forceinline__ void acc_scale(f32x16& v, float f) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
@@ -185,16 +193,6 @@ __device__ __forceinline__ void acc_scale(f32x16& v, float f) {
     v[e] = x;
   }
 }
-__device__ __forceinline__ void acc_add(f32x16& v, int g, f32x4 y) {
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    float x = v[4 * g + r], t;
-    asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_add_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1"
-                 : "+a"(x), "=&v"(t)
-                 : "v"(y[r]));
-    v[4 * g + r] = x;
-  }
-}
 
 template <int DK, int DVL>
 __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDecodeDev a) {
@@ -203,63 +201,83 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
   constexpr int NCP = (PD_KT * CH + 63) / 64;  // copies (of 64 chunks) of a tile
   constexpr int NKK = DK / 16, NC = DVL / 32;
   static_assert(DK % 16 == 0 && NC % 4 == 0 && CH >= 64 / 4, "decode shape");
-  static_assert(2 * NC * 4096 <= PD_WAVES * NCP * 1024, "two states fit the tiles");
+  static_assert(NC / 2 * 4096 <= NCP * 1024, "half of every state fits the tiles");
+  constexpr int PF = 6;  // operand reads in flight ahead of the products
   __shared__ __attribute__((aligned(1024))) bf16_t tiles[PD_WAVES][NCP * 512];
   __shared__ float ml[PD_WAVES][2][32];
-  __shared__ int scan[64 * PD_WAVES], plan[2];
+  __shared__ int wave_sum[PD_WAVES], plan_b[PD_WAVES], plan_at[PD_WAVES];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int half = lane >> 5, col = lane & 31;
-  const int wg = blockIdx.x, nwg = gridDim.x, h0 = 32 * blockIdx.y;
+  const int wg = blockIdx.x, h0 = 32 * blockIdx.y;
 
   // the list: each thread counts the tiles of a run of sequences, a scan gives their places
   const int run = (a.B + 64 * PD_WAVES - 1) / (64 * PD_WAVES);
   const int b_lo = min(tid * run, a.B), b_hi = min(b_lo + run, a.B);
   int mine = 0;
   for (int b = b_lo; b < b_hi; ++b) mine += tiles_of(decode_len(a, b));
-  scan[tid] = mine;
-  __syncthreads();
-  for (int d = 1; d < 64 * PD_WAVES; d *= 2) {
-    const int v = tid >= d ? scan[tid - d] : 0;
-    __syncthreads();
-    scan[tid] += v;
-    __syncthreads();
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int v = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += v;
   }
-  const int total = scan[64 * PD_WAVES - 1];
-  const int share = share_of(total, nwg);
-  const int t_lo = min((int64_t)wg * share, (int64_t)total), t_hi = min(t_lo + share, total);
-  {
-    int at = scan[tid] - mine;
-    const bool first = wg == 0 && blockIdx.y == 0;
-    if (first || (at <= t_lo && t_lo < at + mine)) {
-      for (int b = b_lo; b < b_hi; ++b) {
-        const int n = tiles_of(decode_len(a, b));
-        if (first) a.tile_off[b] = at;
-        if (at <= t_lo && t_lo < at + n) {
-          plan[0] = b;
-          plan[1] = at;
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < PD_WAVES; ++w) {
+    if (w < wave) upto += wave_sum[w];
+    total += wave_sum[w];
+  }
+  const ListCut cut(total, gridDim.x);
+  const int t_lo = cut.lo(wg), t_hi = cut.hi(wg), per = cut.per_wave(wg);
+  // the sequence of each wavefront's first tile
+  const bool first = wg == 0 && blockIdx.y == 0;
+  int at = upto - mine;
+  if (first || (at < t_hi && at + mine > t_lo)) {
+    for (int b = b_lo; b < b_hi; ++b) {
+      const int n = tiles_of(decode_len(a, b));
+      if (first) a.tile_off[b] = at;
+#pragma unroll
+      for (int w = 0; w < PD_WAVES; ++w) {
+        const int t = t_lo + w * per;
+        if (t < t_hi && at <= t && t < at + n) {
+          plan_b[w] = b;
+          plan_at[w] = at;
         }
-        at += n;
       }
-      if (first && tid == 64 * PD_WAVES - 1) a.tile_off[a.B] = total;
+      at += n;
     }
   }
+  if (first && tid == 0) a.tile_off[a.B] = total;
   __syncthreads();
   if (t_lo >= t_hi) return;
-  int b = __builtin_amdgcn_readfirstlane(plan[0]);
-  int seq0 = __builtin_amdgcn_readfirstlane(plan[1]);  // first tile of sequence b in the list
+
+  int T = t_lo + wave * per;                       // this wavefront's run: tiles [T, T_end)
+  const int T_end = min(T + per, t_hi);
+  int b = 0, seq0 = 0, n = 0, nt = 0;              // the current sequence: first tile, rows, tiles
+  if (T < T_end) {
+    b = __builtin_amdgcn_readfirstlane(plan_b[wave]);
+    seq0 = __builtin_amdgcn_readfirstlane(plan_at[wave]);
+    n = __builtin_amdgcn_readfirstlane(decode_len(a, b));
+    nt = tiles_of(n);
+  }
+  // whether the share lies in one sequence (the same in every wavefront)
+  const int b_first = __builtin_amdgcn_readfirstlane(plan_b[0]);
+  const bool joined = t_hi <= __builtin_amdgcn_readfirstlane(plan_at[0]) + tiles_of(__builtin_amdgcn_readfirstlane(decode_len(a, b_first)));
 
   const uint64_t heads = __ballot(h0 + col < a.H);  // (columns without a head move no reference)
   bf16_t* kt = tiles[wave];
 
-  // row `lane` of tile t of sequence b (the last row again past the end, which gets no weight):
-  // its page's table entry, and its address
-  auto entry = [&](int t, int n) {
-    const int p = min(t * PD_KT + col, n - 1);
-    return a.table[(int64_t)b * a.max_pages + p / a.page_size];
+  // row `col` of tile t (of its sequence) of sequence bb with nn rows; the last row again past the
+  // end, which gets no weight: its page's table entry, and its copies
+  auto entry = [&](int bb, int t, int nn) {
+    const int p = min(t * PD_KT + col, nn - 1);
+    return a.table[(int64_t)bb * a.max_pages + p / a.page_size];
   };
-  auto issue = [&](int t, int n, int page, bool& bad) {
-    const int p = min(t * PD_KT + col, n - 1);
+  auto issue = [&](int t, int nn, int page, bool& bad) {
+    const int p = min(t * PD_KT + col, nn - 1);
     const bool out = page < 0 || page >= a.n_pages;
     bad = __ballot(out) != 0;
     const uint64_t at = (uint64_t)(uintptr_t)(a.pool + ((int64_t)(out ? 0 : page) * a.page_size + p % a.page_size) * DK);
@@ -292,25 +310,21 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
     }
   };
 
-  for (int t0 = t_lo; t0 < t_hi;) {
-    const int n = __builtin_amdgcn_readfirstlane(decode_len(a, b));
-    const int nt = tiles_of(n);
-    if (nt == 0) {
-      ++b;
-      continue;
-    }
-    const int first = t0 - seq0, last = min(t_hi - seq0, nt);  // tiles [first, last) of sequence b
-    const int slot = wg + b;
-
-    int t = first + wave;
-    bool bad = false, any_bad = false;
-    if (t < last) issue(t, n, entry(t, n), bad);
-    bf16x8 qf[NKK];  // this lane's head as B operand fragments (k = 16 kk + 8 half + 0..7)
-    {
-      const bf16_t* qsrc = a.qabs + ((int64_t)b * a.HP + h0 + col) * DK + 8 * half;
+  bool bad = false, any_bad = false;
+  bf16x8 qf[NKK];  // this lane's head as B operand fragments (k = 16 kk + 8 half + 0..7)
+  auto load_q = [&](int bb) __attribute__((always_inline)) {
+    const bf16_t* qsrc = a.qabs + ((int64_t)bb * a.HP + h0 + col) * DK + 8 * half;
 #pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) qf[kk] = *(const bf16x8*)(qsrc + 16 * kk);
-    }
+    for (int kk = 0; kk < NKK; ++kk) qf[kk] = *(const bf16x8*)(qsrc + 16 * kk);
+  };
+  if (T < T_end) issue(T - seq0, n, entry(b, T - seq0, n), bad);
+  else if (!joined) return;
+
+  do {  // a sequence's part of the run
+    const int seg_end = min(T_end, seq0 + nt);
+    int b2 = b, n2 = n, seq2 = seq0;  // the sequence after it
+    any_bad = false;
+    if (T < seg_end) load_q(b);
     f32x16 acc[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -318,18 +332,46 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
       for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
 
-    for (; t < last; t += PD_WAVES) {
+    for (; T < seg_end; ++T) {
       any_bad |= bad;
-      const int next = t + PD_WAVES;
+      const int t = T - seq0;
+      // the tile after this one: the next of the sequence, or the first of the next that has rows
       int page = 0;
-      if (next < last) page = entry(next, n);
+      if (T + 1 < T_end) {
+        if (T + 1 == seg_end) {
+          seq2 += nt;
+          do n2 = __builtin_amdgcn_readfirstlane(decode_len(a, ++b2));
+          while (n2 == 0);
+        }
+        page = entry(b2, T + 1 - seq2, n2);
+      }
       wait_vm<0>();
+      // S^T, the operand reads PF ahead of the products (pinned: the compiler would read each operand
+      // right before its product and wait for it)
       f32x16 s;
-      mfma_v_first(s, *(const bf16x8*)(kt + col * LD + 8 * half), qf[0]);
+      {
+        bf16x8 kf[PF];
+        const bf16_t* kp = kt + col * LD + 8 * half;
 #pragma unroll
-      for (int kk = 1; kk < NKK; ++kk)
-        mfma_v_next(s, *(const bf16x8*)(kt + col * LD + 16 * kk + 8 * half), qf[kk]);
-      mfma_v_done(s);
+        for (int j = 0; j < PF; ++j) kf[j] = *(const bf16x8*)(kp + 16 * j);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) {
+          if (kk == 0) mfma_v_first(s, kf[0], qf[0]);
+          else mfma_v_next(s, kf[kk % PF], qf[kk]);
+          if (kk + PF < NKK) kf[kk % PF] = *(const bf16x8*)(kp + 16 * (kk + PF));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mfma_v_done(s);
+      }
+      // V^T operand of step j = NC u + c: latents 32 c .., rows 16 u + {4 half.., 8 + 4 half..}
+      auto vread = [&](int j) {
+        const int klo = 16 * (j / NC) + 4 * half;
+        return lds_operand_tr(kt, LD, 32 * (j % NC), klo, klo + 8);
+      };
+      bf16x8 vf[PF];
+#pragma unroll
+      for (int j = 0; j < PF; ++j) vf[j] = vread(j);
       // rows past the end (the last tile only; a real branch): no weight
       if ((t + 1) * PD_KT > n) {
         asm volatile("");
@@ -364,66 +406,24 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
         }
         pf[u] = __builtin_bit_cast(bf16x8, w);
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int klo = 16 * u + 4 * half;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) mfma_a(acc[c], lds_operand_tr(kt, LD, 32 * c, klo, klo + 8), pf[u]);
+      for (int j = 0; j < 2 * NC; ++j) {
+        mfma_a(acc[j % NC], vf[j % PF], pf[j / NC]);
+        if (j + PF < 2 * NC) vf[j % PF] = vread(j + PF);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      mfma_a_done(acc);
       // every read of the tile has returned before the next copies may overwrite it
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-      if (next < last) issue(next, n, page, bad);
+      if (T + 1 < T_end) issue(T + 1 - seq2, n2, page, bad);
+      mfma_a_done(acc);
     }
 
-    // join the wavefronts' states: one reference and sum, then the latents
-    float l = pair_sum32(l_run);
-    if (any_bad) l = NAN;  // a row on no page
-    if (half == 0) {
-      ml[wave][0][col] = m_run;
-      ml[wave][1][col] = l;
-    }
-    __syncthreads();  // (and every wavefront is done with its tile)
-    float M = -INFINITY, L = 0.f;
-#pragma unroll
-    for (int w = 0; w < PD_WAVES; ++w) M = fmaxf(M, ml[w][0][col]);
-#pragma unroll
-    for (int w = 0; w < PD_WAVES; ++w) {
-      const float mw = ml[w][0][col];
-      L += ml[w][1][col] * (mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M));
-    }
-    const float f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - M);
-    // wavefronts 2 and 3 hand theirs to 0 and 1, then 1 to 0
-    float* buf = (float*)tiles[0];
-    // (always inlined: a reference to the registers would put them in memory)
-    auto put = [&](float* p) __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *(f32x4*)(p + ((c * 4 + g) * 64 + lane) * 4) =
-              f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
-    };
-    auto add = [&](const float* p) __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) acc_add(acc[c], g, *(const f32x4*)(p + ((c * 4 + g) * 64 + lane) * 4));
-    };
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc_scale(acc[c], f);
-    constexpr int STATE = NC * 1024;  // floats of a wavefront's state
-    if (wave >= 2) put(buf + (wave - 2) * STATE);
-    __syncthreads();
-    if (wave < 2) add(buf + wave * STATE);
-    __syncthreads();
-    if (wave == 1) put(buf);
-    __syncthreads();
-    if (wave == 0) {
-      add(buf);
-      // lane (head col, half) holds latents 32 c + 8 g + 4 half + 0..3
+    if (!joined) {  // leaving the sequence: its state
+      const float l = any_bad ? NAN : pair_sum32(l_run);  // (a row on no page)
       if (h0 + col < a.H) {
-        const int64_t row = (int64_t)slot * a.HP + h0 + col;
+        const int64_t row = ((int64_t)PD_WAVES * wg + wave + b) * a.HP + h0 + col;
+        // lane (head col, half) holds latents 32 c + 8 g + 4 half + 0..3
         float* po = a.part_o + row * DVL + 4 * half;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -432,124 +432,215 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
             *(f32x4*)(po + 32 * c + 8 * g) =
                 f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
         if (half == 0) {
-          a.part_ml[2 * row] = M;
-          a.part_ml[2 * row + 1] = L;
+          a.part_ml[2 * row] = m_run;
+          a.part_ml[2 * row + 1] = l;
+        }
+      }
+      b = b2;
+      n = n2;
+      seq0 = seq2;
+      nt = tiles_of(n);
+      continue;
+    }
+
+    // the four states of one sequence: one reference and sum, then the latents, half of them at a time
+    // through LDS: every wavefront writes its half, then sums a quarter of it
+    const float l = any_bad ? NAN : pair_sum32(l_run);
+    if (half == 0) {
+      ml[wave][0][col] = m_run;
+      ml[wave][1][col] = l;
+    }
+    float* buf = (float*)tiles[0];
+    constexpr int NH = NC / 2;
+    float M = -INFINITY, L = 0.f, f[PD_WAVES];
+    const int64_t row = ((int64_t)PD_WAVES * wg + b_first) * a.HP + h0 + col;
+#pragma unroll
+    for (int ph = 0; ph < 2; ++ph) {
+      __syncthreads();  // (every wavefront is done with its tile, or with the first half)
+      if (ph == 0) {
+#pragma unroll
+        for (int w = 0; w < PD_WAVES; ++w) M = fmaxf(M, ml[w][0][col]);
+#pragma unroll
+        for (int w = 0; w < PD_WAVES; ++w) {
+          const float mw = ml[w][0][col];
+          f[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+          L += ml[w][1][col] * f[w];
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NH; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& v = acc[ph * NH + c];
+          *(f32x4*)(buf + (((wave * NH + c) * 4 + g) * 64 + lane) * 4) = f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+        }
+      __syncthreads();
+#pragma unroll
+      for (int c0 = 0; c0 < NH; c0 += PD_WAVES) {
+        const int c = c0 + wave;
+        if (c < NH) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < PD_WAVES; ++w) v += *(const f32x4*)(buf + (((w * NH + c) * 4 + g) * 64 + lane) * 4) * f[w];
+            if (h0 + col < a.H) *(f32x4*)(a.part_o + row * DVL + 32 * (ph * NH + c) + 8 * g + 4 * half) = v;
+          }
         }
       }
     }
-    t0 = seq0 + last;
-    if (t0 < t_hi) __syncthreads();  // the buffers take tiles again
-    seq0 += nt;
-    ++b;
-  }
+    if (wave == 0 && half == 0 && h0 + col < a.H) {
+      a.part_ml[2 * row] = M;
+      a.part_ml[2 * row + 1] = L;
+    }
+  } while (!joined && T < T_end);
 }
 
-// The segments of a (sequence, head) joined, then W_UV on the matrix cores: lat[d] = sum_s o_s[d]
-// 2^(m_s - M) / sum_s l_s 2^(m_s - M), rounded to bf16, o[e] = sum_d W_UV[g][e][d] lat[d].  A
-// workgroup owns a head and PF_RB sequences; its wavefronts ask for their W_UV rows first, so that
-// the merge hides them.  Segments in the list's order.  Bound by latency.
-constexpr int PF_RB = 8;
-template <int DVL, int DV>
-__global__ __launch_bounds__(256) void paged_finish_kernel(const float* __restrict__ part_o,
-                                                           const float* __restrict__ part_ml,
-                                                           const int32_t* __restrict__ tile_off,
-                                                           const bf16_t* __restrict__ Wuv,
-                                                           bf16_t* __restrict__ o, int B, int H, int HP,
-                                                           int nwg, int hpg) {
-  constexpr int NCG = DVL / 4, NSLOT = 256 / NCG, NK = DVL / 32, NT = DV / 64, LDL = DVL + 8;
-  __shared__ float red[PF_RB][NSLOT][DVL];
-  __shared__ __attribute__((aligned(16))) bf16_t lat[PF_RB * LDL];
-  __shared__ float sM[PF_RB], sInv[PF_RB];
-  __shared__ int s0[PF_RB], sn[PF_RB];
-  const int i = blockIdx.x, b0 = PF_RB * blockIdx.y, nb = min(PF_RB, B - b0);
-  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
-  bf16x8 wf[NT][NK];  // W_UV rows 16 (NT wave + t) + lane % 16, k = 32 kk + 8 (lane / 16) + 0..7
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const bf16_t* wp = Wuv + ((int64_t)(i / hpg) * DV + 16 * (NT * wave + t) + (lane & 15)) * DVL + 8 * (lane >> 4);
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) wf[t][kk] = *(const bf16x8*)(wp + 32 * kk);
-  }
-  const int share = share_of(tile_off[B], nwg);
-  // maxima and sums: a wavefront per sequence and round, a lane takes every 64th segment
-  for (int bb = wave; bb < PF_RB; bb += 4) {
-    int slot = 0, ns = 0;
-    if (bb < nb) {
-      const int t0 = tile_off[b0 + bb], t1 = tile_off[b0 + bb + 1];
-      if (t1 > t0) {
-        slot = t0 / share + b0 + bb;
-        ns = (t1 - 1) / share - t0 / share + 1;
-      }
+// The states of a (sequence, head) joined, then W_UV on the matrix cores: lat[d] = sum_s o_s[d]
+// 2^(m_s - M) / sum_s l_s 2^(m_s - M), o[e] = sum_d W_UV[g][e][d] lat[d].  A workgroup owns a head
+// and RB sequences; its wavefronts ask for their W_UV rows first, so that the merge hides them.
+// States in the list's order.  Bound by latency: RB = 1 where the sequences are few and their
+// states many (8 states of a sequence in flight per thread), 4 where they are many (W_UV read
+// once for four).  The latent enters the product as the sum of two bf16 values, so that it is not
+// rounded between the softmax and W_UV.
+constexpr int PF_THREADS = 512;
+constexpr int PF_MANY = 32;  // sequences from which a workgroup takes four
+
+// Where the states of the sequence with tiles [t0, t1) are: n of them, the first n0 in the slots
+// of its first workgroup (one if that is joined), one for each workgroup inside, the last in those
+// of its last workgroup.
+struct States {
+  int n = 0, n0 = 0, mid = 0, at0 = 0, at_mid = 0, at1 = 0;
+  States() = default;
+  __device__ __forceinline__ States(const ListCut& cut, int b, int t0, int t1) {
+    if (t1 <= t0) return;
+    const int w0 = t0 / cut.share, w1 = (t1 - 1) / cut.share;
+    int v;
+    n0 = part(cut, w0, t0, t1, v);
+    at0 = PD_WAVES * w0 + v + b;
+    n = n0;
+    if (w1 > w0) {
+      mid = w1 - w0 - 1;
+      at_mid = PD_WAVES * (w0 + 1) + b;
+      n += mid + part(cut, w1, t0, t1, v);
+      at1 = PD_WAVES * w1 + v + b;
     }
+  }
+  __device__ __forceinline__ static int part(const ListCut& cut, int w, int t0, int t1, int& v) {
+    const int lo = cut.lo(w), hi = cut.hi(w), per = cut.per_wave(w);
+    v = 0;
+    if (t0 <= lo && hi <= t1) return 1;  // joined
+    v = (max(t0, lo) - lo) / per;
+    return (min(t1, hi) - 1 - lo) / per - v + 1;
+  }
+  __device__ __forceinline__ int slot(int k) const {
+    if (k < n0) return at0 + k;
+    k -= n0;
+    if (k < mid) return at_mid + PD_WAVES * k;
+    return at1 + k - mid;
+  }
+};
+
+template <int DVL, int DV, int RB>
+__global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* __restrict__ part_o,
+                                                                  const float* __restrict__ part_ml,
+                                                                  const int32_t* __restrict__ tile_off,
+                                                                  const bf16_t* __restrict__ Wuv,
+                                                                  bf16_t* __restrict__ o, int B, int H, int HP,
+                                                                  int nwg, int hpg) {
+  constexpr int NCG = DVL / 4, NSLOT = PF_THREADS / NCG, NK = DVL / 32, LDL = DVL + 8, U = 8 / RB;
+  __shared__ float red[RB][NSLOT][DVL];
+  __shared__ __attribute__((aligned(16))) bf16_t lat[2][RB * LDL];  // rounded, and what that lost
+  __shared__ float sM[RB], sInv[RB];
+  const int i = blockIdx.x, b0 = RB * blockIdx.y, nb = min(RB, B - b0);
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  bf16x8 wf[NK];  // W_UV rows 16 wave + lane % 16, k = 32 kk + 8 (lane / 16) + 0..7
+  if (wave < DV / 16) {
+    const bf16_t* wp = Wuv + ((int64_t)(i / hpg) * DV + 16 * wave + (lane & 15)) * DVL + 8 * (lane >> 4);
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) wf[kk] = *(const bf16x8*)(wp + 32 * kk);
+  }
+  const ListCut cut(tile_off[B], nwg);
+  States st[RB];
+  int most = 0;
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    if (r < nb) st[r] = States(cut, b0 + r, tile_off[b0 + r], tile_off[b0 + r + 1]);
+    most = max(most, st[r].n);
+  }
+  // maxima and sums: a wavefront per sequence, a lane takes every 64th state
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    if (wave != r) continue;
     float M = -INFINITY, L = 0.f;
-    for (int sp = lane; sp < ns; sp += 64) {
-      const f32x2 x = *(const f32x2*)(part_ml + 2 * ((int64_t)(slot + sp) * HP + i));
-      const float m1 = fmaxf(M, x[0]);
-      const float ref = m1 == -INFINITY ? 0.f : m1;
+    for (int k = lane; k < st[r].n; k += 64) {
+      const f32x2 x = *(const f32x2*)(part_ml + 2 * ((int64_t)st[r].slot(k) * HP + i));
+      const float m1 = fmaxf(M, x[0]), ref = m1 == -INFINITY ? 0.f : m1;
       L = L * __builtin_amdgcn_exp2f(M - ref) + x[1] * __builtin_amdgcn_exp2f(x[0] - ref);
       M = m1;
     }
     const float Mw = warp_max(M);
     const float Lw = warp_sum(M == -INFINITY ? L : L * __builtin_amdgcn_exp2f(M - Mw));
     if (lane == 0) {
-      s0[bb] = slot;
-      sn[bb] = ns;
-      sM[bb] = Mw == -INFINITY ? 0.f : Mw;
-      sInv[bb] = Lw == 0.f ? 0.f : 1.f / Lw;  // (NaN stays NaN)
+      sM[r] = Mw == -INFINITY ? 0.f : Mw;
+      sInv[r] = Lw == 0.f ? 0.f : 1.f / Lw;  // (NaN stays NaN)
     }
   }
   __syncthreads();
   const int cg = tid % NCG, sl = tid / NCG;
-  for (int bb = 0; bb < nb; ++bb) {
-    const int ns = sn[bb];
-    const float M = sM[bb];
-    const int64_t row0 = (int64_t)s0[bb] * HP + i;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int sp = sl; sp < ns; sp += 8 * NSLOT) {
-      f32x4 x[8];
-      float m[8];
+  f32x4 v[RB];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int64_t rw = row0 + (int64_t)HP * min(sp + u * NSLOT, ns - 1);
-        x[u] = *(const f32x4*)(part_o + rw * DVL + 4 * cg);
-        m[u] = part_ml[2 * rw];
+  for (int r = 0; r < RB; ++r) v[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k0 = sl; k0 < most; k0 += U * NSLOT) {
+    f32x4 x[RB][U];
+    float m[RB][U];
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * NSLOT;
+        m[r][u] = -INFINITY;
+        x[r][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (k < st[r].n) {
+          const int64_t rw = (int64_t)st[r].slot(k) * HP + i;
+          x[r][u] = *(const f32x4*)(part_o + rw * DVL + 4 * cg);
+          m[r][u] = part_ml[2 * rw];
+        }
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (sp + u * NSLOT < ns) v += x[u] * __builtin_amdgcn_exp2f(m[u] - M);
-    }
-    *(f32x4*)&red[bb][sl][4 * cg] = v;
-  }
-  __syncthreads();
-  for (int e = tid; e < nb * NCG; e += 256) {
-    const int bb = e / NCG, c = 4 * (e % NCG);
-    f32x4 v = *(const f32x4*)&red[bb][0][c];
+    for (int r = 0; r < RB; ++r)
 #pragma unroll
-    for (int k = 1; k < NSLOT; ++k) v += *(const f32x4*)&red[bb][k][c];
-    v *= sInv[bb];
-    if (sn[bb] == 0) v = f32x4{0.f, 0.f, 0.f, 0.f};
-    *(u32x2*)(lat + bb * LDL + c) = u32x2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+      for (int u = 0; u < U; ++u) v[r] += x[r][u] * __builtin_amdgcn_exp2f(m[r][u] - sM[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r) *(f32x4*)&red[r][sl][4 * cg] = v[r];
+  __syncthreads();
+  for (int e = tid; e < nb * NCG; e += PF_THREADS) {
+    const int r = e / NCG, c = 4 * (e % NCG);
+    f32x4 w = *(const f32x4*)&red[r][0][c];
+#pragma unroll
+    for (int k = 1; k < NSLOT; ++k) w += *(const f32x4*)&red[r][k][c];
+    w *= sInv[r];
+    const u32x2 hi = {pack2bf(w[0], w[1]), pack2bf(w[2], w[3])};
+    *(u32x2*)(lat[0] + r * LDL + c) = hi;
+    *(u32x2*)(lat[1] + r * LDL + c) =
+        u32x2{pack2bf(w[0] - __uint_as_float(hi[0] << 16), w[1] - __uint_as_float(hi[0] & 0xffff0000u)),
+              pack2bf(w[2] - __uint_as_float(hi[1] << 16), w[3] - __uint_as_float(hi[1] & 0xffff0000u))};
   }
   __syncthreads();
+  if (wave >= DV / 16) return;
   const int n = lane & 15;  // MFMA column: sequence b0 + n
-  const bf16_t* lp = lat + min(n, nb - 1) * LDL + 8 * (lane >> 4);
-  f32x4 acc[NT];
+  const int lp = min(n, nb - 1) * LDL + 8 * (lane >> 4);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-  for (int kk = 0; kk < NK; ++kk) {
-    const bf16x8 lf = *(const bf16x8*)(lp + 32 * kk);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[t][kk], lf, acc[t], 0, 0, 0);
-  }
+    for (int kk = 0; kk < NK; ++kk)
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[kk], *(const bf16x8*)(lat[h] + lp + 32 * kk), acc, 0, 0, 0);
   if (n >= nb) return;
+  bf16_t* op = o + ((int64_t)(b0 + n) * H + i) * DV + 16 * wave + 4 * (lane >> 4);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {  // rows 4 (lane / 16) + 0..3 of each 16-row tile
-    bf16_t* op = o + ((int64_t)(b0 + n) * H + i) * DV + 16 * (NT * wave + t) + 4 * (lane >> 4);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) op[k] = f2bf(acc[t][k]);
-  }
+  for (int k = 0; k < 4; ++k) op[k] = f2bf(acc[k]);  // (o may have any alignment)
 }
 
 // Workgroups over the list, for each block of 32 heads: one a CU in all, and no more than have a
@@ -566,7 +657,7 @@ struct DecodeLayout {
   size_t qabs, part_o, part_ml, tile_off, bytes;
 };
 DecodeLayout decode_layout(int B, int H, int DK, int DVL, int nwg) {
-  const size_t HP = (H + 31) / 32 * 32, slots = (size_t)nwg + B;
+  const size_t HP = (H + 31) / 32 * 32, slots = (size_t)PD_WAVES * nwg + B;
   DecodeLayout l;
   l.qabs = 0;
   l.part_o = l.qabs + al(B * HP * DK * 2);
@@ -606,20 +697,22 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL), (double)d.B * d.max_len * DK * 2,
            KLABEL("paged_decode_kernel"));
   prof_begin(KC_ELEM, s);
-  const dim3 grid(d.H, (d.B + PF_RB - 1) / PF_RB);
-#define X(a_, b_)                                                                                        \
-  if (DK == a_ && DVL == b_) {                                                                           \
-    if (d.dv == 128)                                                                                     \
-      paged_finish_kernel<b_, 128><<<grid, 256, 0, s>>>(a.part_o, a.part_ml, a.tile_off,                 \
-                                                        (const bf16_t*)d.Wuv, (bf16_t*)d.o, d.B, d.H, HP, \
-                                                        nwg, d.hpg);                                     \
-    else                                                                                                 \
-      paged_finish_kernel<b_, 64><<<grid, 256, 0, s>>>(a.part_o, a.part_ml, a.tile_off,                  \
-                                                       (const bf16_t*)d.Wuv, (bf16_t*)d.o, d.B, d.H, HP, \
-                                                       nwg, d.hpg);                                      \
+#define FIN(b_, v_, rb_)                                                                                 \
+  paged_finish_kernel<b_, v_, rb_><<<dim3(d.H, (d.B + rb_ - 1) / rb_), PF_THREADS, 0, s>>>(              \
+      a.part_o, a.part_ml, a.tile_off, (const bf16_t*)d.Wuv, (bf16_t*)d.o, d.B, d.H, HP, nwg, d.hpg)
+#define X(a_, b_)                        \
+  if (DK == a_ && DVL == b_) {           \
+    if (d.dv == 128) {                   \
+      if (d.B < PF_MANY) FIN(b_, 128, 1); \
+      else FIN(b_, 128, 4);              \
+    } else {                             \
+      if (d.B < PF_MANY) FIN(b_, 64, 1);  \
+      else FIN(b_, 64, 4);               \
+    }                                    \
   }
   MLA_PAGED_SHAPES(X)
 #undef X
+#undef FIN
   prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dv * d.rkv, ((double)nwg + d.B) * d.H * (DVL + 2) * 4,
            KLABEL("paged_finish_kernel"));
   return hipGetLastError();
