@@ -92,8 +92,11 @@ struct DecodeDev {
 // H = 32, r_kv = 512; one round of small workgroups), fp32 accumulation.  Measured with the
 // rotary copy: 64 sequences 26 -> 9.0 us, one sequence 13.6 -> 4.1 us (a vector-ALU product and
 // a copy launch before).
+// FRAG: qabs in the order in which the paged decoding reads it, [b][block of 32 heads][16-wide step
+// kk][half][head][8]: a matrix operand is 1 KB in one piece there.
 constexpr int ABS_LD = 96;  // LDS row stride: 4 rows of a transposing read on distinct banks
 constexpr int ABS_DN = 192;
+template <bool FRAG>
 __global__ __launch_bounds__(128) void absorb_kernel(const bf16_t* __restrict__ q,
                                                      const bf16_t* __restrict__ Wuk,
                                                      bf16_t* __restrict__ qabs, int B, int H, int HP,
@@ -126,9 +129,15 @@ __global__ __launch_bounds__(128) void absorb_kernel(const bf16_t* __restrict__ 
     if (16 * kk + 8 * half < dn) w = *(const u32x4*)(qp + 16 * kk);
     qf[kk] = __builtin_bit_cast(bf16x8, w);
   }
+  // where 8 aligned elements c .. of row rc go
+  const int head = g * hpg + rc % hpg;
+  const int64_t fi = ((int64_t)(rc / hpg) * (HP / 32) + head / 32) * (DK / 16) * 512 + head % 32 * 8;
+  auto place = [&](int c) {
+    return FRAG ? qabs + fi + (c >> 4) * 512 + (c >> 3 & 1) * 256 : qabs + qi * DK + c;
+  };
   if (blockIdx.x == 0 && wave == 0 && rr < rows)  // rotary part: dr elements, half a row per lane
     for (int c = 8 * half; c < dr; c += 16)
-      *(u32x4*)(qabs + qi * DK + rkv + c) = *(const u32x4*)(q + bi * dq + dn + c);
+      *(u32x4*)place(rkv + c) = *(const u32x4*)(q + bi * dq + dn + c);
   __syncthreads();
   f32x16 acc;
 #pragma unroll
@@ -140,10 +149,9 @@ __global__ __launch_bounds__(128) void absorb_kernel(const bf16_t* __restrict__ 
           lds_operand_tr(Ws, ABS_LD, 32 * wave, 16 * kk + 8 * half, 16 * kk + 8 * half + 4), qf[kk], acc,
           0, 0, 0);
   if (rr >= rows) return;
-  bf16_t* out = qabs + qi * DK + c0 + 32 * wave + 4 * half;
 #pragma unroll
   for (int e4 = 0; e4 < 4; ++e4)
-    *(u32x2*)(out + 8 * e4) = u32x2{pack2bf(acc[4 * e4], acc[4 * e4 + 1]), pack2bf(acc[4 * e4 + 2], acc[4 * e4 + 3])};
+    *(u32x2*)(place(c0 + 32 * wave + 8 * e4) + 4 * half) = u32x2{pack2bf(acc[4 * e4], acc[4 * e4 + 1]), pack2bf(acc[4 * e4 + 2], acc[4 * e4 + 3])};
 }
 
 template <int DK, int DVL>
@@ -515,11 +523,16 @@ size_t decode_ws_bytes(int B, int H, int DK, int DVL, int Lmax) {
 }
 
 hipError_t decode_absorb(const void* q, const void* Wuk, void* qabs, int B, int H, int HP, int hpg,
-                         int dn, int dr, int rkv, hipStream_t s) {
+                         int dn, int dr, int rkv, bool frag, hipStream_t s) {
   if (dn > ABS_DN || rkv % 64) return hipErrorInvalidValue;
   prof_begin(KC_ELEM, s);
-  absorb_kernel<<<dim3(rkv / 64, (B * hpg + 31) / 32, H / hpg), 128, 0, s>>>(
-      (const bf16_t*)q, (const bf16_t*)Wuk, (bf16_t*)qabs, B, H, HP, hpg, dn, dr, rkv);
+  const dim3 grid(rkv / 64, (B * hpg + 31) / 32, H / hpg);
+  if (frag)
+    absorb_kernel<true><<<grid, 128, 0, s>>>((const bf16_t*)q, (const bf16_t*)Wuk, (bf16_t*)qabs, B, H, HP, hpg,
+                                             dn, dr, rkv);
+  else
+    absorb_kernel<false><<<grid, 128, 0, s>>>((const bf16_t*)q, (const bf16_t*)Wuk, (bf16_t*)qabs, B, H, HP,
+                                              hpg, dn, dr, rkv);
   prof_end(KC_ELEM, s, 2.0 * B * H * dn * rkv, (double)B * H * (rkv + dr + dn + dr) * 2,
            KLABEL("absorb_kernel"));
   return hipSuccess;
@@ -540,7 +553,7 @@ hipError_t decode_attention(const Decode& d, hipStream_t s) {
   float* part_ml = (float*)w;
   w += al((size_t)d.B * nsplit * HP * 2 * 4);
 
-  hipError_t e = decode_absorb(d.q, d.Wuk, qabs, d.B, d.H, HP, d.hpg, d.dn, d.dr, d.rkv, s);
+  hipError_t e = decode_absorb(d.q, d.Wuk, qabs, d.B, d.H, HP, d.hpg, d.dn, d.dr, d.rkv, false, s);
   if (e != hipSuccess) return e;
 
   DecodeDev a;

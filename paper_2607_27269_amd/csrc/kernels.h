@@ -329,9 +329,10 @@ struct PrefillPaged {
 size_t prefill_paged_ws_bytes(const PrefillPaged& p);
 hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s);
 
-// The absorbed queries of decoding: qabs [B][HP][rkv + dr] (rows past H are not written).
+// The absorbed queries of decoding: qabs [B][HP][rkv + dr] (rows past H are not written), or with
+// frag the same values in the order of matrix operands.
 hipError_t decode_absorb(const void* q, const void* Wuk, void* qabs, int B, int H, int HP, int hpg,
-                         int dn, int dr, int rkv, hipStream_t s);
+                         int dn, int dr, int rkv, bool frag, hipStream_t s);
 
 // out = a - b elementwise over n elements of dtype t (fp32 arithmetic)
 hipError_t sub_elementwise(const void* a, const void* b, void* out, int64_t n, DType t,

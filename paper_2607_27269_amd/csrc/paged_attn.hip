@@ -139,7 +139,7 @@ struct PagedDecodeDev {
   int n_pages, page_size, max_pages;
   const int32_t* len;
   int max_len, B, H, HP;
-  const bf16_t* qabs;  // [B][HP][DK]
+  const bf16_t* qabs;  // [B][HP / 32][DK / 16][64 lanes][8]: matrix operands
   float* part_o;       // [slot][HP][DVL], not normalised
   float* part_ml;      // [slot][HP][2]: reference maximum (log2), sum
   int32_t* tile_off;   // [B + 1]: first tile of each sequence in the list
@@ -194,16 +194,41 @@ __device__ __forceinline__ void acc_scale(f32x16& v, float f) {
   }
 }
 
-template <int DK, int DVL>
-__global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDecodeDev a) {
-  constexpr int LD = attn::ld_of(DK);          // padded rows: conflict-free operand reads
-  constexpr int CH = LD / 8, DCH = DK / 8;     // 16-byte chunks of a row, with and without padding
-  constexpr int NCP = (PD_KT * CH + 63) / 64;  // copies (of 64 chunks) of a tile
+// A tile in LDS: 32 rows of CHR 16-byte chunks, not padded; chunk c of row r lies at c ^ swz(r), so
+// that both read patterns are free of bank conflicts: 16 bytes of 16 consecutive rows (S^T), and
+// the transposing reads' 32 bytes of four consecutive rows (V^T; the rows that share banks differ
+// in chunk bit 1).  Without padding a copy's lanes meet the same chunks again after PERIOD copies
+// (ROWS rows), so that the lanes' source offsets are a few registers and a copy of rows that lie
+// together costs no arithmetic.
+template <int DK>
+struct Tile {
+  static constexpr int CHR = DK / 8;
+  static constexpr bool WIDE = DK / 2 % 64 == 32;  // two rows span the banks; else four
+  static constexpr int ROWS = WIDE ? 8 : 16;
+  static constexpr int PERIOD = ROWS * CHR / 64;
+  static constexpr int HALF_COPIES = 16 * CHR / 64;  // copies of 16 rows
+  static constexpr int ELEMS = PD_KT * DK;
+  static_assert(DK / 2 % 64 == 32 || DK / 2 % 64 == 16, "row stride in banks");
+  static_assert(CHR % (WIDE ? 8 : 4) == 0 && ROWS * CHR % 64 == 0, "whole copies");
+  __device__ __forceinline__ static constexpr int swz(int r) {
+    return WIDE ? (r >> 1 & 1) << 1 | (r >> 2 & 1) << 2 | (r >> 3 & 1) : r >> 2 & 3;
+  }
+};
+
+// 1 KB from a uniform address plus the lanes' offsets to the LDS byte address `lds`
+__device__ __forceinline__ void copy_s(uint64_t sbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
+}
+
+template <int DK, int DVL, int OCC>
+__global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedDecodeDev a) {
+  using TL = Tile<DK>;
+  constexpr int CHR = TL::CHR;
   constexpr int NKK = DK / 16, NC = DVL / 32;
-  static_assert(DK % 16 == 0 && NC % 4 == 0 && CH >= 64 / 4, "decode shape");
-  static_assert(NC / 2 * 4096 <= NCP * 1024, "half of every state fits the tiles");
-  constexpr int PF = 6;  // operand reads in flight ahead of the products
-  __shared__ __attribute__((aligned(1024))) bf16_t tiles[PD_WAVES][NCP * 512];
+  static_assert(DK % 16 == 0 && NC % 4 == 0, "decode shape");
+  static_assert(NC / 2 * 2048 <= TL::ELEMS, "half of every state fits the tiles");
+  constexpr int PF = 5;  // operand reads in flight ahead of the products
+  __shared__ __attribute__((aligned(1024))) bf16_t tiles[PD_WAVES][TL::ELEMS];
   __shared__ float ml[PD_WAVES][2][32];
   __shared__ int wave_sum[PD_WAVES], plan_b[PD_WAVES], plan_at[PD_WAVES];
 
@@ -269,60 +294,98 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
 
   const uint64_t heads = __ballot(h0 + col < a.H);  // (columns without a head move no reference)
   bf16_t* kt = tiles[wave];
+  const uint32_t kt_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)kt);
 
-  // row `col` of tile t (of its sequence) of sequence bb with nn rows; the last row again past the
-  // end, which gets no weight: its page's table entry, and its copies
+  // lane offsets: the copies' sources within ROWS rows; the operands in the tile
+  uint32_t voff[TL::PERIOD];
+#pragma unroll
+  for (int k = 0; k < TL::PERIOD; ++k) {
+    const int r = (64 * k + lane) / CHR, pc = (64 * k + lane) % CHR;
+    voff[k] = 16u * (uint32_t)(r * CHR + (pc ^ TL::swz(r)));
+  }
+  const bf16_t* kb[4];  // row col, chunk 2 kk + half for kk % 4 = 0..3
+#pragma unroll
+  for (int j = 0; j < 4; ++j) kb[j] = kt + col * DK + 8 * ((2 * j + half) ^ TL::swz(col));
+  // rows 4 half + (lane % 16) / 4 (+ 8), latents 16 ((lane / 16) % 2) + 4 (lane % 4) (+ 32)
+  const bf16_t* vb[2][2];
+#pragma unroll
+  for (int h8 = 0; h8 < 2; ++h8)
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+      const int r = 8 * h8 + 4 * half + ((lane & 15) >> 2);
+      const int d = 32 * odd + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      vb[h8][odd] = kt + r * DK + 8 * ((d >> 3) ^ TL::swz(r)) + (d & 7);
+    }
+
+  // row `col` of tile t (of its sequence) of sequence bb with nn rows (the last row again past the
+  // end, which gets no weight): its page's table entry, and its address
   auto entry = [&](int bb, int t, int nn) {
     const int p = min(t * PD_KT + col, nn - 1);
     return a.table[(int64_t)bb * a.max_pages + p / a.page_size];
   };
-  auto issue = [&](int t, int nn, int page, bool& bad) {
+  auto address = [&](int t, int nn, int page, bool& bad) {
     const int p = min(t * PD_KT + col, nn - 1);
     const bool out = page < 0 || page >= a.n_pages;
     bad = __ballot(out) != 0;
-    const uint64_t at = (uint64_t)(uintptr_t)(a.pool + ((int64_t)(out ? 0 : page) * a.page_size + p % a.page_size) * DK);
-    const uint32_t lo = (uint32_t)at, hi = (uint32_t)(at >> 32);
-    int ln = lane;  // opaque: the lanes' chunk numbers are cheaper made again than kept in 74 registers
+    return (uint64_t)(uintptr_t)(a.pool + ((int64_t)(out ? 0 : page) * a.page_size + p % a.page_size) * DK);
+  };
+  auto row_address = [&](uint64_t at, int r) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, r) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at >> 32), r) << 32;
+  };
+  // rows 16 g .. 16 g + 15 of a tile whose 16 rows lie together
+  auto issue_half = [&](int g, uint64_t at) __attribute__((always_inline)) {
+    uint64_t base = row_address(at, 16 * g);
+    asm volatile("s_nop 4" : "+s"(base));  // (vector ALU to scalar register to memory operation)
+    uint32_t lds = kt_lds;  // opaque: its sums with constants are cheaper made again than kept
+    asm volatile("" : "+s"(lds));
+#pragma unroll
+    for (int k = 0; k < TL::HALF_COPIES; ++k) {
+      const int q = k / TL::PERIOD;
+      uint32_t v = voff[k % TL::PERIOD];
+      if (TL::WIDE && (q & 1)) asm volatile("v_xor_b32 %0, 16, %0" : "+v"(v));  // (again, not kept)
+      copy_s(base + (uint64_t)(q * TL::ROWS * DK * 2), v, lds + 2 * (16 * g * DK + 512 * k));
+    }
+  };
+  // any tile: copy k fills chunks 64 k .. 64 k + 63, of rows known at compile time
+  auto issue_rows = [&](uint64_t at) __attribute__((always_inline)) {
+    int ln = lane;  // opaque: the lanes' chunk numbers are cheaper made again than kept in registers
     asm volatile("" : "+v"(ln));
-    // copy k fills chunks 64 k .. 64 k + 63 of the padded tile: rows r0 and r0 + 1 (one row's
-    // padding lies between them and takes any chunk), both known at compile time
 #pragma unroll
-    for (int k = 0; k < NCP; ++k) {
-      constexpr int LAST = PD_KT - 1;
-      const int r0 = 64 * k / CH, skip = 64 * k % CH;
+    for (int k = 0; k < 2 * TL::HALF_COPIES; ++k) {
+      const int r0 = 64 * k / CHR, skip = 64 * k % CHR;
       uint64_t src = 0;
-      int c = ln + skip;
+      int c = 0;
 #pragma unroll
-      for (int r = 0; r <= 64 / CH + 1; ++r) {  // the rows that 64 chunks can touch
-        if (r > 0 && r * CH >= skip + 64) break;
-        const int rr = r0 + r < LAST ? r0 + r : LAST;
-        const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)lo, rr) |
-                              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, rr) << 32;
-        const int cc = ln + skip - r * CH;
-        if (r == 0 || cc >= 0) {
+      for (int r = 0; r * CHR < skip + 64; ++r) {  // the rows that 64 chunks touch
+        const uint64_t base = row_address(at, r0 + r);
+        const int pc = ln + skip - r * CHR;
+        if (r == 0 || pc >= 0) {
           src = base;
-          c = cc;
+          c = pc ^ TL::swz(r0 + r);
         }
       }
-      if (c >= DCH) c = 0;
       dma16((const bf16_t*)(uintptr_t)(src + 16u * (uint32_t)c), kt + 512 * k);
       __builtin_amdgcn_sched_barrier(0);  // (or every row's address waits in scalar registers)
     }
   };
+  // whether 16-row halves of whole tiles lie together
+  const bool whole16 = a.page_size % 16 == 0;
 
   bool bad = false, any_bad = false;
   bf16x8 qf[NKK];  // this lane's head as B operand fragments (k = 16 kk + 8 half + 0..7)
   auto load_q = [&](int bb) __attribute__((always_inline)) {
-    const bf16_t* qsrc = a.qabs + ((int64_t)bb * a.HP + h0 + col) * DK + 8 * half;
+    const bf16_t* qsrc = a.qabs + ((int64_t)bb * a.HP + h0) * DK + 8 * lane;
 #pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) qf[kk] = *(const bf16x8*)(qsrc + 16 * kk);
+    for (int kk = 0; kk < NKK; ++kk) qf[kk] = *(const bf16x8*)(qsrc + 512 * kk);
   };
-  if (T < T_end) issue(T - seq0, n, entry(b, T - seq0, n), bad);
+  if (T < T_end) issue_rows(address(T - seq0, n, entry(b, T - seq0, n), bad));
   else if (!joined) return;
 
   do {  // a sequence's part of the run
     const int seg_end = min(T_end, seq0 + nt);
     int b2 = b, n2 = n, seq2 = seq0;  // the sequence after it
+    const int seg_begin = T;
     any_bad = false;
     if (T < seg_end) load_q(b);
     f32x16 acc[NC];
@@ -351,23 +414,24 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
       f32x16 s;
       {
         bf16x8 kf[PF];
-        const bf16_t* kp = kt + col * LD + 8 * half;
+        auto kread = [&](int kk) { return *(const bf16x8*)(kb[kk % 4] + 64 * (kk / 4)); };
 #pragma unroll
-        for (int j = 0; j < PF; ++j) kf[j] = *(const bf16x8*)(kp + 16 * j);
+        for (int j = 0; j < PF; ++j) kf[j] = kread(j);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kk = 0; kk < NKK; ++kk) {
           if (kk == 0) mfma_v_first(s, kf[0], qf[0]);
           else mfma_v_next(s, kf[kk % PF], qf[kk]);
-          if (kk + PF < NKK) kf[kk % PF] = *(const bf16x8*)(kp + 16 * (kk + PF));
+          if (kk + PF < NKK) kf[kk % PF] = kread(kk + PF);
           __builtin_amdgcn_sched_barrier(0);
         }
         mfma_v_done(s);
       }
       // V^T operand of step j = NC u + c: latents 32 c .., rows 16 u + {4 half.., 8 + 4 half..}
       auto vread = [&](int j) {
-        const int klo = 16 * (j / NC) + 4 * half;
-        return lds_operand_tr(kt, LD, 32 * (j % NC), klo, klo + 8);
+        const int c = j % NC, at = 16 * (j / NC) * DK + 64 * (c / 2);
+        const u32x2 lo = lds_read_tr4(vb[0][c & 1] + at), hi = lds_read_tr4(vb[1][c & 1] + at);
+        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
       };
       bf16x8 vf[PF];
 #pragma unroll
@@ -389,8 +453,10 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
         const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
         m_run = m_new;
         l_run *= corr;
+        if (T != seg_begin) {  // (nothing is there yet at the first tile)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
+          for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
+        }
       }
       const float m_use = m_run == -INFINITY ? 0.f : m_run;
       bf16x8 pf[2];  // P rounded to bf16, the matrix cores' operand
@@ -407,15 +473,28 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
         pf[u] = __builtin_bit_cast(bf16x8, w);
       }
       __builtin_amdgcn_sched_barrier(0);
+      // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
+      // reads return in order: that of step NC is there), the others behind the last read
+      const bool more = T + 1 < T_end;
+      uint64_t at = 0;
+      bool together = false;
+      if (more) {
+        at = address(T + 1 - seq2, n2, page, bad);
+        together = whole16 && (T + 2 - seq2) * PD_KT <= n2;
+      }
 #pragma unroll
       for (int j = 0; j < 2 * NC; ++j) {
         mfma_a(acc[j % NC], vf[j % PF], pf[j / NC]);
         if (j + PF < 2 * NC) vf[j % PF] = vread(j + PF);
         __builtin_amdgcn_sched_barrier(0);
+        if (j == NC && together) issue_half(0, at);
       }
       // every read of the tile has returned before the next copies may overwrite it
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-      if (T + 1 < T_end) issue(T + 1 - seq2, n2, page, bad);
+      if (more) {
+        if (together) issue_half(1, at);
+        else issue_rows(at);
+      }
       mfma_a_done(acc);
     }
 
@@ -498,12 +577,11 @@ __global__ __launch_bounds__(64 * PD_WAVES, 1) void paged_decode_kernel(PagedDec
 
 // The states of a (sequence, head) joined, then W_UV on the matrix cores: lat[d] = sum_s o_s[d]
 // 2^(m_s - M) / sum_s l_s 2^(m_s - M), o[e] = sum_d W_UV[g][e][d] lat[d].  A workgroup owns a head
-// and RB sequences; its wavefronts ask for their W_UV rows first, so that the merge hides them.
+// and RB sequences.
 // States in the list's order.  Bound by latency: RB = 1 where the sequences are few and their
-// states many (8 states of a sequence in flight per thread), 4 where they are many (W_UV read
-// once for four).  The latent enters the product as the sum of two bf16 values, so that it is not
+// states many (1024 threads, eight states of the sequence in flight per thread), 4 where they are
+// many (W_UV read once for four).  The latent enters the product as the sum of two bf16 values, so that it is not
 // rounded between the softmax and W_UV.
-constexpr int PF_THREADS = 512;
 constexpr int PF_MANY = 32;  // sequences from which a workgroup takes four
 
 // Where the states of the sequence with tiles [t0, t1) are: n of them, the first n0 in the slots
@@ -541,25 +619,19 @@ struct States {
   }
 };
 
-template <int DVL, int DV, int RB>
-__global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* __restrict__ part_o,
-                                                                  const float* __restrict__ part_ml,
-                                                                  const int32_t* __restrict__ tile_off,
-                                                                  const bf16_t* __restrict__ Wuv,
-                                                                  bf16_t* __restrict__ o, int B, int H, int HP,
-                                                                  int nwg, int hpg) {
-  constexpr int NCG = DVL / 4, NSLOT = PF_THREADS / NCG, NK = DVL / 32, LDL = DVL + 8, U = 8 / RB;
+template <int DVL, int DV, int RB, int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_finish_kernel(const float* __restrict__ part_o,
+                                                               const float* __restrict__ part_ml,
+                                                               const int32_t* __restrict__ tile_off,
+                                                               const bf16_t* __restrict__ Wuv,
+                                                               bf16_t* __restrict__ o, int B, int H, int HP,
+                                                               int nwg, int hpg) {
+  constexpr int NCG = DVL / 4, NSLOT = THREADS / NCG, NK = DVL / 32, LDL = DVL + 8, U = 8 / RB;
   __shared__ float red[RB][NSLOT][DVL];
+  __shared__ float sm[RB][NSLOT], sl[RB][NSLOT];
   __shared__ __attribute__((aligned(16))) bf16_t lat[2][RB * LDL];  // rounded, and what that lost
-  __shared__ float sM[RB], sInv[RB];
   const int i = blockIdx.x, b0 = RB * blockIdx.y, nb = min(RB, B - b0);
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
-  bf16x8 wf[NK];  // W_UV rows 16 wave + lane % 16, k = 32 kk + 8 (lane / 16) + 0..7
-  if (wave < DV / 16) {
-    const bf16_t* wp = Wuv + ((int64_t)(i / hpg) * DV + 16 * wave + (lane & 15)) * DVL + 8 * (lane >> 4);
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) wf[kk] = *(const bf16x8*)(wp + 32 * kk);
-  }
   const ListCut cut(tile_off[B], nwg);
   States st[RB];
   int most = 0;
@@ -568,59 +640,79 @@ __global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* _
     if (r < nb) st[r] = States(cut, b0 + r, tile_off[b0 + r], tile_off[b0 + r + 1]);
     most = max(most, st[r].n);
   }
-  // maxima and sums: a wavefront per sequence, a lane takes every 64th state
-#pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    if (wave != r) continue;
-    float M = -INFINITY, L = 0.f;
-    for (int k = lane; k < st[r].n; k += 64) {
-      const f32x2 x = *(const f32x2*)(part_ml + 2 * ((int64_t)st[r].slot(k) * HP + i));
-      const float m1 = fmaxf(M, x[0]), ref = m1 == -INFINITY ? 0.f : m1;
-      L = L * __builtin_amdgcn_exp2f(M - ref) + x[1] * __builtin_amdgcn_exp2f(x[0] - ref);
-      M = m1;
-    }
-    const float Mw = warp_max(M);
-    const float Lw = warp_sum(M == -INFINITY ? L : L * __builtin_amdgcn_exp2f(M - Mw));
-    if (lane == 0) {
-      sM[r] = Mw == -INFINITY ? 0.f : Mw;
-      sInv[r] = Lw == 0.f ? 0.f : 1.f / Lw;  // (NaN stays NaN)
-    }
-  }
-  __syncthreads();
-  const int cg = tid % NCG, sl = tid / NCG;
+  // DVL / 4 threads, four latents each, times NSLOT slots, each every so-many-th state
+  const int cg = tid % NCG, slot = tid / NCG;
+  float M[RB], L[RB];
   f32x4 v[RB];
 #pragma unroll
-  for (int r = 0; r < RB; ++r) v[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k0 = sl; k0 < most; k0 += U * NSLOT) {
+  for (int r = 0; r < RB; ++r) {
+    M[r] = -INFINITY;
+    L[r] = 0.f;
+    v[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  bf16x8 wf[NK];  // W_UV rows 16 wave + lane % 16, k = 32 kk + 8 (lane / 16) + 0..7
+  for (int k0 = slot, round = 0; round == 0 || k0 < most; k0 += U * NSLOT, ++round) {
     f32x4 x[RB][U];
-    float m[RB][U];
+    f32x2 ml[RB][U];
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int k = k0 + u * NSLOT;
-        m[r][u] = -INFINITY;
+        ml[r][u] = f32x2{-INFINITY, 0.f};
         x[r][u] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (k < st[r].n) {
           const int64_t rw = (int64_t)st[r].slot(k) * HP + i;
           x[r][u] = *(const f32x4*)(part_o + rw * DVL + 4 * cg);
-          m[r][u] = part_ml[2 * rw];
+          ml[r][u] = *(const f32x2*)(part_ml + 2 * rw);
         }
       }
+    if (round == 0 && wave < DV / 16) {  // behind the first states' loads, hidden by the merge
+      const bf16_t* wp = Wuv + ((int64_t)(i / hpg) * DV + 16 * wave + (lane & 15)) * DVL + 8 * (lane >> 4);
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
+      for (int kk = 0; kk < NK; ++kk) wf[kk] = *(const bf16x8*)(wp + 32 * kk);
+    }
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[r] += x[r][u] * __builtin_amdgcn_exp2f(m[r][u] - sM[r]);
+    for (int r = 0; r < RB; ++r) {
+      float m1 = M[r];
+#pragma unroll
+      for (int u = 0; u < U; ++u) m1 = fmaxf(m1, ml[r][u][0]);
+      const float ref = m1 == -INFINITY ? 0.f : m1, c = __builtin_amdgcn_exp2f(M[r] - ref);
+      v[r] *= c;
+      L[r] *= c;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = __builtin_amdgcn_exp2f(ml[r][u][0] - ref);
+        v[r] += x[r][u] * w;
+        L[r] += ml[r][u][1] * w;
+      }
+      M[r] = m1;
+    }
   }
 #pragma unroll
-  for (int r = 0; r < RB; ++r) *(f32x4*)&red[r][sl][4 * cg] = v[r];
+  for (int r = 0; r < RB; ++r) {
+    *(f32x4*)&red[r][slot][4 * cg] = v[r];
+    if (cg == 0) {
+      sm[r][slot] = M[r];
+      sl[r][slot] = L[r];
+    }
+  }
   __syncthreads();
-  for (int e = tid; e < nb * NCG; e += PF_THREADS) {
+  for (int e = tid; e < nb * NCG; e += THREADS) {
     const int r = e / NCG, c = 4 * (e % NCG);
-    f32x4 w = *(const f32x4*)&red[r][0][c];
+    float ref = -INFINITY;
 #pragma unroll
-    for (int k = 1; k < NSLOT; ++k) w += *(const f32x4*)&red[r][k][c];
-    w *= sInv[r];
+    for (int k = 0; k < NSLOT; ++k) ref = fmaxf(ref, sm[r][k]);
+    if (ref == -INFINITY) ref = 0.f;
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NSLOT; ++k) {
+      const float f = __builtin_amdgcn_exp2f(sm[r][k] - ref);
+      w += *(const f32x4*)&red[r][k][c] * f;
+      sum += sl[r][k] * f;
+    }
+    w *= sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
     const u32x2 hi = {pack2bf(w[0], w[1]), pack2bf(w[2], w[3])};
     *(u32x2*)(lat[0] + r * LDL + c) = hi;
     *(u32x2*)(lat[1] + r * LDL + c) =
@@ -667,7 +759,8 @@ DecodeLayout decode_layout(int B, int H, int DK, int DVL, int nwg) {
   return l;
 }
 
-#define MLA_PAGED_SHAPES(X) X(576, 512) X(288, 256) X(160, 128)
+// (DK, DVL, workgroups a CU: what LDS and registers hold)
+#define MLA_PAGED_SHAPES(X) X(576, 512, 1) X(288, 256, 1) X(160, 128, 2)
 
 }  // namespace
 
@@ -686,29 +779,29 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
   a.B = d.B; a.H = d.H; a.HP = HP; a.qabs = (const bf16_t*)(ws + l.qabs);
   a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
   a.tile_off = (int32_t*)(ws + l.tile_off); a.sl2 = d.scale * attn::LOG2E;
-  hipError_t e = decode_absorb(d.q, d.Wuk, ws + l.qabs, d.B, d.H, HP, d.hpg, d.dn, d.dr, d.rkv, s);
+  hipError_t e = decode_absorb(d.q, d.Wuk, ws + l.qabs, d.B, d.H, HP, d.hpg, d.dn, d.dr, d.rkv, true, s);
   if (e != hipSuccess) return e;
   // algorithmic work at full lengths
   prof_begin(KC_ATTN_FWD, s);
-#define X(a_, b_) \
-  if (DK == a_ && DVL == b_) paged_decode_kernel<a_, b_><<<dim3(nwg, HP / 32), 64 * PD_WAVES, 0, s>>>(a);
+#define X(a_, b_, c_) \
+  if (DK == a_ && DVL == b_) paged_decode_kernel<a_, b_, c_><<<dim3(nwg, HP / 32), 64 * PD_WAVES, 0, s>>>(a);
   MLA_PAGED_SHAPES(X)
 #undef X
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL), (double)d.B * d.max_len * DK * 2,
            KLABEL("paged_decode_kernel"));
   prof_begin(KC_ELEM, s);
-#define FIN(b_, v_, rb_)                                                                                 \
-  paged_finish_kernel<b_, v_, rb_><<<dim3(d.H, (d.B + rb_ - 1) / rb_), PF_THREADS, 0, s>>>(              \
+#define FIN(b_, v_, rb_, th_)                                                               \
+  paged_finish_kernel<b_, v_, rb_, th_><<<dim3(d.H, (d.B + rb_ - 1) / rb_), th_, 0, s>>>(   \
       a.part_o, a.part_ml, a.tile_off, (const bf16_t*)d.Wuv, (bf16_t*)d.o, d.B, d.H, HP, nwg, d.hpg)
-#define X(a_, b_)                        \
-  if (DK == a_ && DVL == b_) {           \
-    if (d.dv == 128) {                   \
-      if (d.B < PF_MANY) FIN(b_, 128, 1); \
-      else FIN(b_, 128, 4);              \
-    } else {                             \
-      if (d.B < PF_MANY) FIN(b_, 64, 1);  \
-      else FIN(b_, 64, 4);               \
-    }                                    \
+#define X(a_, b_, c_)                                                     \
+  if (DK == a_ && DVL == b_) {                                            \
+    if (d.dv == 128) {                                                    \
+      if (d.B < PF_MANY) FIN(b_, 128, 1, 1024);                           \
+      else FIN(b_, 128, 4, 512);                                          \
+    } else {                                                              \
+      if (d.B < PF_MANY) FIN(b_, 64, 1, 1024);                            \
+      else FIN(b_, 64, 4, 512);                                           \
+    }                                                                     \
   }
   MLA_PAGED_SHAPES(X)
 #undef X
@@ -733,7 +826,7 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
   a.Wuv = (const bf16_t*)p.Wuv; a.dv = p.dv; a.hpg = hpg; a.o = (bf16_t*)p.o;
   a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv;
   a.sl2 = p.scale * attn::LOG2E;
-  hipError_t e = decode_absorb(p.q, p.Wuk, p.ws, p.n_q, p.H, HP, hpg, p.dn, p.dr, p.rkv, s);
+  hipError_t e = decode_absorb(p.q, p.Wuk, p.ws, p.n_q, p.H, HP, hpg, p.dn, p.dr, p.rkv, false, s);
   if (e != hipSuccess) return e;
   prof_begin(KC_ATTN_FWD, s);
   paged_attn_simple_kernel<<<dim3(p.n_q, p.H), 256, 0, s>>>(a);
