@@ -533,6 +533,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
     constexpr int NH = NC / 2;
     float M = -INFINITY, L = 0.f, f[PD_WAVES];
     const int64_t row = ((int64_t)PD_WAVES * wg + b_first) * a.HP + h0 + col;
+    float* po = a.part_o + row * DVL + 4 * half;
 #pragma unroll
     for (int ph = 0; ph < 2; ++ph) {
       __syncthreads();  // (every wavefront is done with its tile, or with the first half)
@@ -563,7 +564,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < PD_WAVES; ++w) v += *(const f32x4*)(buf + (((w * NH + c) * 4 + g) * 64 + lane) * 4) * f[w];
-            if (h0 + col < a.H) *(f32x4*)(a.part_o + row * DVL + 32 * (ph * NH + c) + 8 * g + 4 * half) = v;
+            if (h0 + col < a.H) *(f32x4*)(po + 32 * (ph * NH + c) + 8 * g) = v;
           }
         }
       }
@@ -576,13 +577,14 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
 }
 
 // The states of a (sequence, head) joined, then W_UV on the matrix cores: lat[d] = sum_s o_s[d]
-// 2^(m_s - M) / sum_s l_s 2^(m_s - M), o[e] = sum_d W_UV[g][e][d] lat[d].  A workgroup owns a head
-// and RB sequences.
-// States in the list's order.  Bound by latency: RB = 1 where the sequences are few and their
-// states many (1024 threads, eight states of the sequence in flight per thread), 4 where they are
-// many (W_UV read once for four).  The latent enters the product as the sum of two bf16 values, so that it is not
-// rounded between the softmax and W_UV.
-constexpr int PF_MANY = 32;  // sequences from which a workgroup takes four
+// 2^(m_s - M) / sum_s l_s 2^(m_s - M), o[e] = sum_d W_UV[g][e][d] lat[d].  A workgroup owns HB heads
+// of a KV group and RB sequences, the columns of the product.  W_UV of the group is copied to LDS,
+// asked for before anything else (read from memory as the matrix operand its rows' 16-byte pieces
+// cost 64 address cycles a KB, 3.4 us for 128 KB; copied 0.9); DVL / 4 threads, four latents each,
+// take a column's states (or every so-many-th of them), eight in flight.  States in the list's
+// order.  The latent enters the product as the sum of two bf16 values, so that it is not rounded
+// between the softmax and W_UV.  Bound by latency: the list's places, the states, the product.
+constexpr int PF_THREADS = 1024;
 
 // Where the states of the sequence with tiles [t0, t1) are: n of them, the first n0 in the slots
 // of its first workgroup (one if that is joined), one for each workgroup inside, the last in those
@@ -619,118 +621,113 @@ struct States {
   }
 };
 
-template <int DVL, int DV, int RB, int THREADS>
-__global__ __launch_bounds__(THREADS) void paged_finish_kernel(const float* __restrict__ part_o,
-                                                               const float* __restrict__ part_ml,
-                                                               const int32_t* __restrict__ tile_off,
-                                                               const bf16_t* __restrict__ Wuv,
-                                                               bf16_t* __restrict__ o, int B, int H, int HP,
-                                                               int nwg, int hpg) {
-  constexpr int NCG = DVL / 4, NSLOT = THREADS / NCG, NK = DVL / 32, LDL = DVL + 8, U = 8 / RB;
-  __shared__ float red[RB][NSLOT][DVL];
-  __shared__ float sm[RB][NSLOT], sl[RB][NSLOT];
-  __shared__ __attribute__((aligned(16))) bf16_t lat[2][RB * LDL];  // rounded, and what that lost
-  const int i = blockIdx.x, b0 = RB * blockIdx.y, nb = min(RB, B - b0);
+template <int DVL, int DV, int HB, int RB>
+__global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* __restrict__ part_o,
+                                                                  const float* __restrict__ part_ml,
+                                                                  const int32_t* __restrict__ tile_off,
+                                                                  const bf16_t* __restrict__ Wuv,
+                                                                  bf16_t* __restrict__ o, int B, int H, int HP,
+                                                                  int nwg, int hpg) {
+  constexpr int NCG = DVL / 4, NCOL = HB * RB, NSLOT = PF_THREADS / NCG / NCOL, U = 8;
+  constexpr int CHW = DVL / 8, NCPW = DV * CHW / 64, NW = PF_THREADS / 64, LDL = DVL + 8;
+  constexpr int RED = NSLOT > 1 ? NCOL * NSLOT * DVL * 4 : 16, LAT = 2 * NCOL * LDL * 2;
+  static_assert(NSLOT >= 1 && NCPW % NW == 0 && NCOL <= 16 && CHW >= 16, "finish shape");
+  __shared__ __attribute__((aligned(1024))) bf16_t Ws[DV * DVL];  // chunk c of row e at c ^ (e % 16)
+  __shared__ __attribute__((aligned(16))) char red_mem[RED];
+  __shared__ __attribute__((aligned(16))) char lat_mem[LAT];
+  __shared__ float sm[NCOL][NSLOT], sl[NCOL][NSLOT];
+  float(*red)[DVL] = (float(*)[DVL])red_mem;                  // [NCOL * NSLOT]
+  bf16_t* lat = (bf16_t*)lat_mem;                             // [2][NCOL][LDL]: rounded, and what that lost
+  const int i0 = HB * blockIdx.x, b0 = RB * blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const bf16_t* Wg = Wuv + (int64_t)(i0 / hpg) * DV * DVL;
+#pragma unroll
+  for (int k0 = 0; k0 < NCPW / NW; ++k0) {
+    const int k = k0 * NW + wave, idx = 64 * k + lane, e = idx / CHW, c = (idx % CHW) ^ (e & 15);
+    dma16(Wg + e * DVL + 8 * c, Ws + 512 * k);
+  }
+  // this thread's column: head i0 + h, sequence b0 + r
+  const int cg = tid % NCG, grp = tid / NCG, col = grp / NSLOT, slot = grp % NSLOT;
+  const int h = col % HB, b = b0 + col / HB;
   const ListCut cut(tile_off[B], nwg);
-  States st[RB];
-  int most = 0;
+  States st;
+  if (b < B) st = States(cut, b, tile_off[b], tile_off[b + 1]);
+  float M = -INFINITY, L = 0.f;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = slot; k0 < st.n; k0 += U * NSLOT) {
+    f32x4 x[U];
+    f32x2 ml[U];
 #pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    if (r < nb) st[r] = States(cut, b0 + r, tile_off[b0 + r], tile_off[b0 + r + 1]);
-    most = max(most, st[r].n);
-  }
-  // DVL / 4 threads, four latents each, times NSLOT slots, each every so-many-th state
-  const int cg = tid % NCG, slot = tid / NCG;
-  float M[RB], L[RB];
-  f32x4 v[RB];
-#pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    M[r] = -INFINITY;
-    L[r] = 0.f;
-    v[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  bf16x8 wf[NK];  // W_UV rows 16 wave + lane % 16, k = 32 kk + 8 (lane / 16) + 0..7
-  for (int k0 = slot, round = 0; round == 0 || k0 < most; k0 += U * NSLOT, ++round) {
-    f32x4 x[RB][U];
-    f32x2 ml[RB][U];
-#pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = k0 + u * NSLOT;
-        ml[r][u] = f32x2{-INFINITY, 0.f};
-        x[r][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (k < st[r].n) {
-          const int64_t rw = (int64_t)st[r].slot(k) * HP + i;
-          x[r][u] = *(const f32x4*)(part_o + rw * DVL + 4 * cg);
-          ml[r][u] = *(const f32x2*)(part_ml + 2 * rw);
-        }
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * NSLOT;
+      ml[u] = f32x2{-INFINITY, 0.f};
+      x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k < st.n) {
+        const int64_t rw = (int64_t)st.slot(k) * HP + i0 + h;
+        x[u] = *(const f32x4*)(part_o + rw * DVL + 4 * cg);
+        ml[u] = *(const f32x2*)(part_ml + 2 * rw);
       }
-    if (round == 0 && wave < DV / 16) {  // behind the first states' loads, hidden by the merge
-      const bf16_t* wp = Wuv + ((int64_t)(i / hpg) * DV + 16 * wave + (lane & 15)) * DVL + 8 * (lane >> 4);
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) wf[kk] = *(const bf16x8*)(wp + 32 * kk);
     }
+    float m1 = M;
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      float m1 = M[r];
+    for (int u = 0; u < U; ++u) m1 = fmaxf(m1, ml[u][0]);
+    const float ref = m1 == -INFINITY ? 0.f : m1, c = __builtin_amdgcn_exp2f(M - ref);
+    v *= c;
+    L *= c;
 #pragma unroll
-      for (int u = 0; u < U; ++u) m1 = fmaxf(m1, ml[r][u][0]);
-      const float ref = m1 == -INFINITY ? 0.f : m1, c = __builtin_amdgcn_exp2f(M[r] - ref);
-      v[r] *= c;
-      L[r] *= c;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float w = __builtin_amdgcn_exp2f(ml[r][u][0] - ref);
-        v[r] += x[r][u] * w;
-        L[r] += ml[r][u][1] * w;
-      }
-      M[r] = m1;
+    for (int u = 0; u < U; ++u) {
+      const float w = __builtin_amdgcn_exp2f(ml[u][0] - ref);
+      v += x[u] * w;
+      L += ml[u][1] * w;
     }
+    M = m1;
   }
-#pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    *(f32x4*)&red[r][slot][4 * cg] = v[r];
+  if (NSLOT > 1) {
+    *(f32x4*)&red[grp][4 * cg] = v;
     if (cg == 0) {
-      sm[r][slot] = M[r];
-      sl[r][slot] = L[r];
+      sm[col][slot] = M;
+      sl[col][slot] = L;
     }
+    __syncthreads();
   }
-  __syncthreads();
-  for (int e = tid; e < nb * NCG; e += THREADS) {
-    const int r = e / NCG, c = 4 * (e % NCG);
-    float ref = -INFINITY;
+  if (slot == 0) {
+    if (NSLOT > 1) {  // the column's slots, in order
+      float ref = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < NSLOT; ++k) ref = fmaxf(ref, sm[r][k]);
-    if (ref == -INFINITY) ref = 0.f;
-    f32x4 w = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
+      for (int k = 0; k < NSLOT; ++k) ref = fmaxf(ref, sm[col][k]);
+      if (ref == -INFINITY) ref = 0.f;
+      v = f32x4{0.f, 0.f, 0.f, 0.f};
+      L = 0.f;
 #pragma unroll
-    for (int k = 0; k < NSLOT; ++k) {
-      const float f = __builtin_amdgcn_exp2f(sm[r][k] - ref);
-      w += *(const f32x4*)&red[r][k][c] * f;
-      sum += sl[r][k] * f;
+      for (int k = 0; k < NSLOT; ++k) {
+        const float f = __builtin_amdgcn_exp2f(sm[col][k] - ref);
+        v += *(const f32x4*)&red[grp + k][4 * cg] * f;
+        L += sl[col][k] * f;
+      }
     }
-    w *= sum == 0.f ? 0.f : 1.f / sum;  // (NaN stays NaN)
-    const u32x2 hi = {pack2bf(w[0], w[1]), pack2bf(w[2], w[3])};
-    *(u32x2*)(lat[0] + r * LDL + c) = hi;
-    *(u32x2*)(lat[1] + r * LDL + c) =
-        u32x2{pack2bf(w[0] - __uint_as_float(hi[0] << 16), w[1] - __uint_as_float(hi[0] & 0xffff0000u)),
-              pack2bf(w[2] - __uint_as_float(hi[1] << 16), w[3] - __uint_as_float(hi[1] & 0xffff0000u))};
+    v *= L == 0.f ? 0.f : 1.f / L;  // (NaN stays NaN)
+    const u32x2 hi = {pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+    *(u32x2*)(lat + col * LDL + 4 * cg) = hi;
+    *(u32x2*)(lat + (NCOL + col) * LDL + 4 * cg) =
+        u32x2{pack2bf(v[0] - __uint_as_float(hi[0] << 16), v[1] - __uint_as_float(hi[0] & 0xffff0000u)),
+              pack2bf(v[2] - __uint_as_float(hi[1] << 16), v[3] - __uint_as_float(hi[1] & 0xffff0000u))};
   }
+  wait_vm<0>();  // W_UV
   __syncthreads();
   if (wave >= DV / 16) return;
-  const int n = lane & 15;  // MFMA column: sequence b0 + n
-  const int lp = min(n, nb - 1) * LDL + 8 * (lane >> 4);
+  // W_UV rows 16 wave + lane % 16 as the A operand, column lane % 16 of the latents as the B operand
+  const int n = lane & 15, q = lane >> 4, e = 16 * wave + n;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int kk = 0; kk < DVL / 32; ++kk) {
+    const bf16x8 wf = *(const bf16x8*)(Ws + e * DVL + 8 * ((4 * kk + q) ^ (e & 15)));
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[kk], *(const bf16x8*)(lat[h] + lp + 32 * kk), acc, 0, 0, 0);
-  if (n >= nb) return;
-  bf16_t* op = o + ((int64_t)(b0 + n) * H + i) * DV + 16 * wave + 4 * (lane >> 4);
+    for (int p = 0; p < 2; ++p)
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          wf, *(const bf16x8*)(lat + (p * NCOL + min(n, NCOL - 1)) * LDL + 32 * kk + 8 * q), acc, 0, 0, 0);
+  }
+  if (n >= NCOL || b0 + n / HB >= B) return;
+  bf16_t* op = o + ((int64_t)(b0 + n / HB) * H + i0 + n % HB) * DV + 16 * wave + 4 * q;
 #pragma unroll
   for (int k = 0; k < 4; ++k) op[k] = f2bf(acc[k]);  // (o may have any alignment)
 }
@@ -790,21 +787,26 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL), (double)d.B * d.max_len * DK * 2,
            KLABEL("paged_decode_kernel"));
   prof_begin(KC_ELEM, s);
-#define FIN(b_, v_, rb_, th_)                                                               \
-  paged_finish_kernel<b_, v_, rb_, th_><<<dim3(d.H, (d.B + rb_ - 1) / rb_), th_, 0, s>>>(   \
+  // one column a workgroup while that is one round on the CUs; else eight that share W_UV
+  const bool few = (int64_t)d.B * d.H <= PD_CUS, heads4 = d.hpg % 4 == 0;
+#define FIN(b_, v_, hb_, rb_)                                                                             \
+  paged_finish_kernel<b_, v_, hb_, rb_><<<dim3(d.H / hb_, (d.B + rb_ - 1) / rb_), PF_THREADS, 0, s>>>(    \
       a.part_o, a.part_ml, a.tile_off, (const bf16_t*)d.Wuv, (bf16_t*)d.o, d.B, d.H, HP, nwg, d.hpg)
-#define X(a_, b_, c_)                                                     \
-  if (DK == a_ && DVL == b_) {                                            \
-    if (d.dv == 128) {                                                    \
-      if (d.B < PF_MANY) FIN(b_, 128, 1, 1024);                           \
-      else FIN(b_, 128, 4, 512);                                          \
-    } else {                                                              \
-      if (d.B < PF_MANY) FIN(b_, 64, 1, 1024);                            \
-      else FIN(b_, 64, 4, 512);                                           \
-    }                                                                     \
+#define FINV(b_, v_)           \
+  if (few) FIN(b_, v_, 1, 1);  \
+  else if (heads4) FIN(b_, v_, 4, 2); \
+  else FIN(b_, v_, 1, 8)
+#define X(a_, b_, c_)          \
+  if (DK == a_ && DVL == b_) { \
+    if (d.dv == 128) {         \
+      FINV(b_, 128);           \
+    } else {                   \
+      FINV(b_, 64);            \
+    }                          \
   }
   MLA_PAGED_SHAPES(X)
 #undef X
+#undef FINV
 #undef FIN
   prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dv * d.rkv, ((double)nwg + d.B) * d.H * (DVL + 2) * 4,
            KLABEL("paged_finish_kernel"));
