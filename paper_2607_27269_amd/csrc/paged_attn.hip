@@ -227,7 +227,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
   constexpr int NKK = DK / 16, NC = DVL / 32;
   static_assert(DK % 16 == 0 && NC % 4 == 0, "decode shape");
   static_assert(NC / 2 * 2048 <= TL::ELEMS, "half of every state fits the tiles");
-  constexpr int PF = 5;  // operand reads in flight ahead of the products
+  constexpr int PF = 5, PV = 3;  // operand reads in flight ahead of the products of S, and of P V
   __shared__ __attribute__((aligned(1024))) bf16_t tiles[PD_WAVES][TL::ELEMS];
   __shared__ float ml[PD_WAVES][2][32];
   __shared__ int wave_sum[PD_WAVES], plan_b[PD_WAVES], plan_at[PD_WAVES];
@@ -433,9 +433,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
         const u32x2 lo = lds_read_tr4(vb[0][c & 1] + at), hi = lds_read_tr4(vb[1][c & 1] + at);
         return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
       };
-      bf16x8 vf[PF];
+      bf16x8 vf[PV];
 #pragma unroll
-      for (int j = 0; j < PF; ++j) vf[j] = vread(j);
+      for (int j = 0; j < PV; ++j) vf[j] = vread(j);
       // rows past the end (the last tile only; a real branch): no weight
       if ((t + 1) * PD_KT > n) {
         asm volatile("");
@@ -459,18 +459,22 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
         }
       }
       const float m_use = m_run == -INFINITY ? 0.f : m_run;
-      bf16x8 pf[2];  // P rounded to bf16, the matrix cores' operand
+      // P as two bf16 operands, rounded and what that lost: a rounding of P alone would add as much
+      // error as that of the output, and the second products hide behind the copies
+      bf16x8 pf[2], pl[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        u32x4 w;
+        u32x4 w, w2;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q], a.sl2, -m_use));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q + 1], a.sl2, -m_use));
           l_run += p0 + p1;
           w[q] = pack2bf(p0, p1);
+          w2[q] = pack2bf(p0 - __uint_as_float(w[q] << 16), p1 - __uint_as_float(w[q] & 0xffff0000u));
         }
         pf[u] = __builtin_bit_cast(bf16x8, w);
+        pl[u] = __builtin_bit_cast(bf16x8, w2);
       }
       __builtin_amdgcn_sched_barrier(0);
       // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
@@ -484,8 +488,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
       }
 #pragma unroll
       for (int j = 0; j < 2 * NC; ++j) {
-        mfma_a(acc[j % NC], vf[j % PF], pf[j / NC]);
-        if (j + PF < 2 * NC) vf[j % PF] = vread(j + PF);
+        mfma_a(acc[j % NC], vf[j % PV], pf[j / NC]);
+        mfma_a(acc[j % NC], vf[j % PV], pl[j / NC]);
+        if (j + PV < 2 * NC) vf[j % PV] = vread(j + PV);
         __builtin_amdgcn_sched_barrier(0);
         if (j == NC && together) issue_half(0, at);
       }
