@@ -93,8 +93,17 @@ struct Attn {
   // c*dv + d] from V column c*dv + d (o_head = 0: dv)
   int n_vchunk = 1;
   int64_t o_head = 0;
+  // attn_fwd_packed only: sequences of different lengths behind one another.  Sequence b has the
+  // queries q_off[b] .. q_off[b + 1] - 1 and the keys and values kv_off[b] .. kv_off[b + 1] - 1
+  // (device [B + 1] each, clamped to n_q and n_kv); its queries stand at the last positions of its
+  // keys and see the keys up to their own position (none: a zero output).  T is not used.
+  const int32_t* q_off = nullptr;
+  const int32_t* kv_off = nullptr;
+  int n_q = 0, n_kv = 0;
 };
 hipError_t attn_fwd(const Attn& a, hipStream_t s);
+// bf16 matrix-core shapes; lse, o_diff, q_cos and value chunks are not for it
+hipError_t attn_fwd_packed(const Attn& a, hipStream_t s);
 
 struct AttnBwd {
   Attn f;                    // forward operands; f.O and f.lse are inputs here

@@ -1,109 +1,12 @@
-// Attention over the paged latent cache (paged.hip) in absorbed form: head i's query against the
-// cache rows is [W_UK[g]^T q^nope_i ; q^rope_i], its output W_UV[g] applied to the
-// attention-weighted latent (g = i / (H / G_kv)).
+// Attention over the paged latent cache (paged.hip): single tokens in absorbed form (head i's query
+// against the cache rows is [W_UK[g]^T q^nope_i ; q^rope_i], its output W_UV[g] applied to the
+// attention-weighted latent, g = i / (H / G_kv)), packed prompts with keys and values written out.
 #include "attn_common.h"
 #include "common.h"
 #include "kernels.h"
 
 namespace mla {
 namespace {
-
-struct PagedAttnDev {
-  const bf16_t* pool;
-  const int32_t* table;
-  int n_pages, page_size, max_pages;
-  int B, H, HP, DK, rkv;
-  const bf16_t* qabs;                // [rows][HP][DK]
-  const bf16_t* Wuv;
-  int dv, hpg;
-  bf16_t* o;                         // [rows][H][dv]
-  const int32_t* len;                // single tokens: [B], row = sequence
-  int max_len;
-  const int32_t *q_off, *kv_off;     // packed tokens: [B + 1]
-  int n_q, n_kv;
-  float sl2;
-};
-
-// A workgroup per (query row, head): each wavefront takes every fourth cache row, 64 lanes over
-// its values, running maximum and sum, the weighted latent in registers; the four states are
-// joined through LDS.
-constexpr int SIMPLE_MAX = 9;  // values of a row per lane: DK <= 576
-__global__ __launch_bounds__(256) void paged_attn_simple_kernel(PagedAttnDev a) {
-  __shared__ float sm[4], sl[4], so[4][512];
-  const int r = blockIdx.x, i = blockIdx.y;
-  const int lane = threadIdx.x & 63, wave = wave_id();
-  int b = r, n;
-  if (a.len) {
-    n = min(max(a.len[b], 0), a.max_len);
-  } else {
-    if (r < max(a.q_off[0], 0) || r >= min(a.q_off[a.B], a.n_q)) return;
-    int lo = 0, hi = a.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.q_off[mid] <= r) lo = mid;
-      else hi = mid - 1;
-    }
-    b = lo;
-    const int kv = min(a.kv_off[b + 1], a.n_kv) - max(a.kv_off[b], 0);
-    n = min(max(kv - (a.q_off[b + 1] - 1 - r), 0), kv);
-  }
-  n = (int)min((int64_t)n, (int64_t)a.page_size * a.max_pages);
-  float q[SIMPLE_MAX], acc[SIMPLE_MAX];
-#pragma unroll
-  for (int k = 0; k < SIMPLE_MAX; ++k) {
-    const int c = lane + 64 * k;
-    q[k] = c < a.DK ? bf2f(a.qabs[((int64_t)r * a.HP + i) * a.DK + c]) : 0.f;
-    acc[k] = 0.f;
-  }
-  float m = -INFINITY, l = 0.f;
-  for (int j = wave; j < n; j += 4) {
-    const int page = a.table[(int64_t)b * a.max_pages + j / a.page_size];
-    const bool bad = page < 0 || page >= a.n_pages;
-    const bf16_t* x = a.pool + ((int64_t)(bad ? 0 : page) * a.page_size + j % a.page_size) * a.DK;
-    float v[SIMPLE_MAX], s = 0.f;
-#pragma unroll
-    for (int k = 0; k < SIMPLE_MAX; ++k) {
-      const int c = lane + 64 * k;
-      v[k] = c < a.DK ? (bad ? NAN : bf2f(x[c])) : 0.f;
-      s += q[k] * v[k];
-    }
-    s = warp_sum(s) * a.sl2;
-    const float m1 = fmaxf(m, s);
-    const float corr = __builtin_amdgcn_exp2f(m - (m1 == -INFINITY ? 0.f : m1));
-    const float p = __builtin_amdgcn_exp2f(s - (m1 == -INFINITY ? 0.f : m1));
-    m = m1;
-    l = l * corr + p;
-#pragma unroll
-    for (int k = 0; k < SIMPLE_MAX; ++k) acc[k] = acc[k] * corr + p * v[k];
-  }
-  if (lane == 0) {
-    sm[wave] = m;
-    sl[wave] = l;
-  }
-#pragma unroll
-  for (int k = 0; k < SIMPLE_MAX; ++k)
-    if (lane + 64 * k < a.rkv) so[wave][lane + 64 * k] = acc[k];
-  __syncthreads();
-  const float M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  float w[4], L = 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    w[k] = sm[k] == -INFINITY && !(sl[k] != sl[k]) ? 0.f : __builtin_amdgcn_exp2f(sm[k] - M);
-    L += w[k] * sl[k];
-  }
-  const float inv = n > 0 ? 1.f / L : 0.f;
-  __syncthreads();
-  for (int c = threadIdx.x; c < a.rkv; c += 256)
-    so[0][c] = (w[0] * so[0][c] + w[1] * so[1][c] + w[2] * so[2][c] + w[3] * so[3][c]) * inv;
-  __syncthreads();
-  for (int e = wave; e < a.dv; e += 4) {
-    const bf16_t* u = a.Wuv + ((int64_t)(i / a.hpg) * a.dv + e) * a.rkv;
-    float v = 0.f;
-    for (int c = lane; c < a.rkv; c += 64) v += bf2f(u[c]) * so[0][c];
-    v = warp_sum(v);
-    if (lane == 0) a.o[((int64_t)r * a.H + i) * a.dv + e] = f2bf(v);
-  }
-}
 
 size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -818,27 +721,133 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ---- prefill --------------------------------------------------------------------------
+// With many queries per cached row the keys W_UK c and values W_UV c are written out once (as for
+// the contiguous cache) and the attention runs on heads of d_nope + d_rope and d_k: gather, one
+// grouped product, attention over the packed sequences.
+namespace {
+
+// The cached rows of all sequences behind one another, a wavefront per row.  Masked keys get P = 0,
+// which keeps a row out of a product only if its values are finite.  So a row that is not finite
+// (or lies on no page) becomes zeros with a NaN positional key: its values and non-positional key
+// are 0 and its logits NaN, for exactly the queries that see it.  So does a row whose finite latent
+// reaches 2^64 and has a value of 2^127 or more (below 2^64 that would take weights of 2^54).
+// Rows of no sequence become zeros.  Bound by memory and, for few rows, by three dependent loads.
+__global__ __launch_bounds__(256) void gather_rows_kernel(PagedPool c, const int32_t* __restrict__ kv_off, int B,
+                                                          int n_kv, int rkv, const bf16_t* __restrict__ Wuv, int nv,
+                                                          bf16_t* __restrict__ out) {
+  const int row = 4 * blockIdx.x + wave_id();
+  if (row >= n_kv) return;
+  const int lane = threadIdx.x & 63, dr = c.width - rkv;
+  bf16_t* dst = out + (int64_t)row * c.width;
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  u32x4 lat = zero, pe = zero;
+  const bool in_lat = 8 * lane < rkv, in_pe = 8 * lane < dr;
+  if (row >= kv_off[0] && row < kv_off[B]) {  // (uniform)
+    int lo = 0, hi = B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (kv_off[mid] <= row) lo = mid;
+      else hi = mid - 1;
+    }
+    const int p = row - kv_off[lo], pg = p / c.page_size;
+    const int page = p >= 0 && pg < c.max_pages ? c.table[(int64_t)lo * c.max_pages + pg] : -1;
+    bool any = page < 0 || page >= c.n_pages;
+    if (!any) {
+      const bf16_t* src = (const bf16_t*)c.pool + ((int64_t)page * c.page_size + p % c.page_size) * c.width;
+      if (in_lat) lat = *(const u32x4*)(src + 8 * lane);
+      if (in_pe) pe = *(const u32x4*)(src + rkv + 8 * lane);
+      uint32_t top = 0u, top_pe = 0u;  // the largest exponents
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        top = max(top, max(lat[q] << 16 & 0x7f800000u, lat[q] & 0x7f800000u));
+        top_pe = max(top_pe, max(pe[q] << 16 & 0x7f800000u, pe[q] & 0x7f800000u));
+      }
+      any = __ballot(max(top, top_pe) == 0x7f800000u) != 0;
+      if (!any && __ballot(top >= (127u + 64u) << 23) != 0) {
+        for (int e = 0; e < nv && !any; ++e) {
+          u32x4 w = zero;
+          if (in_lat) w = *(const u32x4*)(Wuv + (int64_t)e * rkv + 8 * lane);
+          float s = 0.f;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            s += __uint_as_float(lat[q] << 16) * __uint_as_float(w[q] << 16) +
+                 __uint_as_float(lat[q] & 0xffff0000u) * __uint_as_float(w[q] & 0xffff0000u);
+          any = !(fabsf(warp_sum(s)) < 1.7014118e38f);  // 2^127
+        }
+      }
+    }
+    if (any) {
+      lat = zero;
+      pe = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    }
+  }
+  if (in_lat) *(u32x4*)(dst + 8 * lane) = lat;
+  if (in_pe) *(u32x4*)(dst + rkv + 8 * lane) = pe;
+}
+
+struct PrefillLayout {
+  size_t rows, keys, vals, split, split_elems, bytes;
+};
+Gemm expand(const PrefillPaged& p, const void* rows, const void* W, int n, void* out) {
+  Gemm g;
+  g.M = p.n_kv; g.N = n; g.K = p.rkv;
+  g.A = rows; g.lda = p.rkv + p.dr; g.a_kmajor = true;
+  g.B = W; g.ldb = p.rkv; g.b_kmajor = true;
+  g.C = out; g.ldc = n; g.in_t = DT_BF16; g.c_t = DT_BF16; g.alpha = 1.f; g.beta = 0.f;
+  return g;
+}
+PrefillLayout prefill_layout(const PrefillPaged& p) {
+  PrefillLayout l;
+  l.rows = 0;
+  l.keys = l.rows + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
+  l.vals = l.keys + al((size_t)p.n_kv * p.G * p.dn * 2);
+  l.split = l.vals + al((size_t)p.n_kv * p.G * p.dv * 2);
+  l.split_elems = 0;  // partials of the products
+  if (p.n_kv > 0) {
+    if (p.dn > 0) l.split_elems = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dn, nullptr));
+    const size_t v = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dv, nullptr));
+    if (v > l.split_elems) l.split_elems = v;
+  }
+  l.bytes = l.split + al(l.split_elems * 4);
+  return l;
+}
+
+}  // namespace
+
 size_t prefill_paged_ws_bytes(const PrefillPaged& p) {
-  const int HP = (p.H + 31) / 32 * 32;
-  return al((size_t)p.n_q * HP * (p.rkv + p.dr) * 2);
+  const size_t n = prefill_layout(p).bytes;
+  return n > 256 ? n : 256;
 }
 
 hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
-  const int HP = (p.H + 31) / 32 * 32, DK = p.rkv + p.dr, hpg = p.H / p.G;
-  PagedAttnDev a = {};
-  a.pool = (const bf16_t*)p.c.pool; a.table = p.c.table; a.n_pages = p.c.n_pages;
-  a.page_size = p.c.page_size; a.max_pages = p.c.max_pages;
-  a.B = p.B; a.H = p.H; a.HP = HP; a.DK = DK; a.rkv = p.rkv;
-  a.qabs = (const bf16_t*)p.ws;
-  a.Wuv = (const bf16_t*)p.Wuv; a.dv = p.dv; a.hpg = hpg; a.o = (bf16_t*)p.o;
+  const PrefillLayout l = prefill_layout(p);
+  char* ws = (char*)p.ws;
+  void *rows = ws + l.rows, *keys = ws + l.keys, *vals = ws + l.vals;
+  const int W = p.rkv + p.dr, dqk = p.dn + p.dr, nk = p.G * p.dn, nv = p.G * p.dv;
+  if (p.n_kv > 0) {
+    prof_begin(KC_ELEM, s);
+    gather_rows_kernel<<<(p.n_kv + 3) / 4, 256, 0, s>>>(p.c, p.kv_off, p.B, p.n_kv, p.rkv, (const bf16_t*)p.Wuv, nv,
+                                                        (bf16_t*)rows);
+    prof_end(KC_ELEM, s, 0.0, (double)p.n_kv * W * 4, KLABEL("gather_rows_kernel"));
+    Gemm up[2];
+    int n = 0;
+    if (p.dn > 0) up[n++] = expand(p, rows, p.Wuk, nk, keys);
+    up[n++] = expand(p, rows, p.Wuv, nv, vals);
+    const hipError_t e = gemm_group(up, n, (float*)(ws + l.split), l.split_elems, s);
+    if (e != hipSuccess) return e;
+  }
+  Attn a;
+  const bf16_t* kpe = (const bf16_t*)rows + p.rkv;
+  a.B = p.B; a.T = 0; a.H = p.H; a.dqk = dqk; a.dv = p.dv;
+  a.dnope = p.dn > 0 ? p.dn : dqk;  // (no non-positional keys: the positional key is the whole key)
+  a.Q = HeadView{p.q, (int64_t)p.H * dqk, dqk, 1};
+  a.Ka = p.dn > 0 ? HeadView{keys, nk, p.dn, p.H / p.G} : HeadView{kpe, W, 0, p.H};
+  a.Kb = HeadView{kpe, W, 0, p.H};
+  a.V = HeadView{vals, nv, p.dv, p.H / p.G};
+  a.O = p.o; a.o_tok = (int64_t)p.H * p.dv; a.lse = nullptr; a.scale = p.scale; a.t = DT_BF16;
   a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv;
-  a.sl2 = p.scale * attn::LOG2E;
-  hipError_t e = decode_absorb(p.q, p.Wuk, p.ws, p.n_q, p.H, HP, hpg, p.dn, p.dr, p.rkv, false, s);
-  if (e != hipSuccess) return e;
-  prof_begin(KC_ATTN_FWD, s);
-  paged_attn_simple_kernel<<<dim3(p.n_q, p.H), 256, 0, s>>>(a);
-  prof_end(KC_ATTN_FWD, s, 0.0, 0.0, KLABEL("paged_attn_simple_kernel"));
-  return hipGetLastError();
+  return attn_fwd_packed(a, s);
 }
 
 }  // namespace mla
