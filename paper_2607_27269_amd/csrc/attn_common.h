@@ -38,10 +38,6 @@ struct AttnDev {
   const bf16_t* Oref; bf16_t* Odiff;  // optional: Odiff = O - Oref (rounded O), layout of O
   const float* qcos; const float* qsin; int qroff, qnp;  // optional: Q rotated on load
   int nqb;
-  // packed sequences (forward): sequence b's queries are rows q_off[b] .. of Q and O, its keys and
-  // values rows kv_off[b] .. of Ka, Kb and V (offsets clamped to n_q and n_kv)
-  const int32_t *q_off, *kv_off;
-  int n_q, n_kv;
 };
 
 inline AttnDev to_dev(const Attn& a) {
@@ -57,7 +53,6 @@ inline AttnDev to_dev(const Attn& a) {
   d.Oref = (const bf16_t*)a.o_ref; d.Odiff = (bf16_t*)a.o_diff;
   d.qcos = a.q_cos; d.qsin = a.q_sin; d.qroff = a.q_roff; d.qnp = a.q_np;
   d.nqb = 0;
-  d.q_off = a.q_off; d.kv_off = a.kv_off; d.n_q = a.n_q; d.n_kv = a.n_kv;
   return d;
 }
 
@@ -80,15 +75,16 @@ struct KVStage {
   int64_t ka_tok, kb_tok, v_tok;
   int dnope, T;
 
-  // the sequence with keys and values in rows n0 .. n0 + T_ - 1 (voff: first value column)
-  __device__ __forceinline__ void init(const AttnDev& a, int64_t n0, int T_, int i, int voff) {
+  // (voff: first value column)
+  __device__ __forceinline__ void init(const AttnDev& a, int b, int i, int voff) {
     kt.init();
     vt.init();
+    const int64_t n0 = (int64_t)b * a.T;
     ka = a.Ka + n0 * a.ka_tok + (int64_t)(i / a.ka_div) * a.ka_head;
     kb = a.Kb + n0 * a.kb_tok + (int64_t)(i / a.kb_div) * a.kb_head - a.dnope;
     vb = a.V + n0 * a.v_tok + (int64_t)(i / a.v_div) * a.v_head + voff;
     ka_tok = a.ka_tok; kb_tok = a.kb_tok; v_tok = a.v_tok;
-    dnope = a.dnope; T = T_;
+    dnope = a.dnope; T = a.T;
   }
 
   // keys j0 .. j0+BKV-1 into (ks, vs)

@@ -34,13 +34,7 @@ constexpr float RESCALE_SLACK = 8.f;     // log2 units the running reference max
 // HG heads that share their keys and values (a KV group) per workgroup: wavefront w works
 // on head i0 + w % HG and queries 32 (w / HG) .. of the workgroup's 256 / HG per head, so
 // that one K/V tile in LDS serves all HG heads (HG = 1: 256 queries of one head)
-//
-// PACKED: sequences of different lengths behind one another, whose queries stand at the last
-// positions of their keys (diag = keys - queries, negative where there are fewer keys).  Query
-// tiles are numbered without a scan over the lengths: sequence b owns the numbers from
-// q_off[b] / BQH + b, at least as many as it has tiles; the few others are empty.  Later numbers
-// first, so that the heavy (late) tiles of a sequence are not the last to start.
-template <int DQK, int DV, bool LSE, int HG, bool PACKED = false>
+template <int DQK, int DV, bool LSE, int HG>
 __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem) {
   using Stage = KVStage<DQK, DV, FWD_WAVES>;
   constexpr int LDK = Stage::LDK, LDV = Stage::LDV;
@@ -54,35 +48,10 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
   constexpr int BQH = FWD_BQ / HG;  // queries per head
   const int ngr = a.H / HG;
   const int bhc = pid / a.nqb;
-  const int vc = PACKED ? 0 : bhc / (a.B * ngr);  // value chunk; 0 unless nvc > 1
-  const int bh = PACKED ? bhc : bhc % (a.B * ngr);
+  const int vc = bhc / (a.B * ngr), bh = bhc % (a.B * ngr);  // value chunk; 0 unless nvc > 1
   const int qb = a.nqb - 1 - pid % a.nqb;
-  const int i0 = (bh % ngr) * HG;
-  int q0, Tq, Tk, diag = 0;    // first query of the tile in its sequence, queries, keys
-  int64_t nq0, nk0;            // the sequence's first query and key row
-  if constexpr (PACKED) {
-    auto q_at = [&](int b) { return min(max(a.q_off[b], 0), a.n_q); };
-    auto k_at = [&](int b) { return min(max(a.kv_off[b], 0), a.n_kv); };
-    int lo = 0, hi = a.B - 1;  // the last sequence whose numbers start at qb or before
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (q_at(mid) / BQH + mid <= qb) lo = mid;
-      else hi = mid - 1;
-    }
-    const int qs = q_at(lo), ks = k_at(lo);
-    Tq = max(q_at(lo + 1) - qs, 0);
-    Tk = max(k_at(lo + 1) - ks, 0);
-    diag = Tk - Tq;
-    q0 = (qb - (qs / BQH + lo)) * BQH;
-    nq0 = qs;
-    nk0 = ks;
-    if (q0 < 0 || q0 >= Tq) return;
-  } else {
-    const int b = bh / ngr;
-    q0 = qb * BQH;
-    Tq = Tk = a.T;
-    nq0 = nk0 = (int64_t)b * a.T;
-  }
+  const int b = bh / ngr, i0 = (bh % ngr) * HG;
+  const int q0 = qb * BQH;
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5, col = lane & 31;
@@ -92,7 +61,7 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
   // 4 (lane half) + (lane % 16) / 4, column 16 ((lane / 16) % 2) + 4 (lane % 4)
   const int vlane = (4 * half + ((lane & 15) >> 2)) * LDV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   const int my_q = qw0 + col;
-  const int64_t nq = nq0 + min(my_q, Tq - 1);
+  const int64_t nq = (int64_t)b * a.T + min(my_q, a.T - 1);
 
   // this lane's query, as MFMA B operand fragments (d = 16 kk + 8 half + 0..7)
   bf16x8 qf[NKK];
@@ -140,24 +109,12 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
     for (int e = 0; e < 16; ++e) acc_o[c][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
 
-  const int kend = min(Tk, q0 + BQH + diag);
+  const int kend = min(a.T, q0 + BQH);
   const int nkb = (kend + BKV - 1) / BKV;
   // tiles this wavefront sees (a prefix: the causal diagonal cuts its queries last)
-  const int nvis = PACKED ? min(nkb, ((qw0 + 31 + diag) >> 6) + 1) : min(nkb, (qw0 + 31) / BKV + 1);
-  static_assert(BKV == 64, "the shift above");
-  if constexpr (PACKED) {
-    if (kend <= 0) {  // queries before the first key (uniform): they see nothing
-      if (my_q >= Tq) return;
-      bf16_t* zp = a.O + (nq0 + my_q) * a.o_tok + (int64_t)i * a.o_head + 4 * half;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) *(u32x2*)(zp + 32 * c + 8 * g) = u32x2{0u, 0u};
-      return;
-    }
-  }
+  const int nvis = min(nkb, (qw0 + 31) / BKV + 1);
   Stage st;
-  st.init(a, nk0, Tk, i0, vc * DV);  // the group's keys and values
+  st.init(a, b, i0, vc * DV);  // the group's keys and values
   st.issue(0, smem, smem + KS);
   if (nkb > 1) st.issue(BKV, smem + (KS + VS), smem + (KS + VS) + KS);
   wait_all();
@@ -193,11 +150,11 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
     // causal mask on diagonal halves; max of this lane's query (raw logits)
     // (the empty asm keeps this a branch: the compiler would otherwise select per element
     // on every half)
-    if (j0 + 31 > qw0 + diag) {
+    if (j0 + 31 > qw0) {
       asm volatile("");
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (j0 + 8 * (e >> 2) + 4 * half + (e & 3) > my_q + diag) sc[e] = -INFINITY;
+        if (j0 + 8 * (e >> 2) + 4 * half + (e & 3) > my_q) sc[e] = -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -256,7 +213,7 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
     }
     if (kb < nvis) {  // wave-uniform; a second half entirely above the diagonal is skipped
       step(kb, 0, sa, sb);
-      if (kb * BKV + 32 <= qw0 + (PACKED ? diag + 31 : 0)) step(kb, 1, sb, sa);
+      if (kb * BKV + 32 <= qw0) step(kb, 1, sb, sa);
     }
     // tile kb + 2 has landed and nobody reads tile kb's stage any more
     wait_all();
@@ -265,9 +222,9 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
 
   // normalise and store: lane holds query my_q, d = 32c + 8(e/4) + 4 half + e%4
   const float l = pair_sum32(l_run);
-  if (my_q >= Tq) return;
-  const float inv = PACKED && l == 0.f ? 0.f : 1.f / l;  // (l = 0: a query that sees no key)
-  const int64_t ooff = (nq0 + my_q) * a.o_tok + (int64_t)i * a.o_head + vc * DV + 4 * half;
+  if (my_q >= a.T) return;
+  const float inv = 1.f / l;
+  const int64_t ooff = ((int64_t)b * a.T + my_q) * a.o_tok + (int64_t)i * a.o_head + vc * DV + 4 * half;
   bf16_t* op = a.O + ooff;
   // the reference rows first, all loads before any store: interleaved, each load would
   // wait (one in-order memory counter) for every store issued before it
@@ -294,7 +251,7 @@ __device__ __forceinline__ void fwd_tile(const AttnDev& a, int pid, bf16_t* smem
                   pack2bf(lo(w[1]) - lo(r[1]), hi(w[1]) - hi(r[1]))};
       }
     }
-  if (LSE && half == 0) a.lse[(nq0 + my_q) * a.H + i] = (m_run + __log2f(l)) * LN2;
+  if (LSE && half == 0) a.lse[((int64_t)b * a.T + my_q) * a.H + i] = (m_run + __log2f(l)) * LN2;
 }
 
 // one work item per workgroup
@@ -322,14 +279,6 @@ __global__ __launch_bounds__(64 * FWD_WAVES) void attn_fwd_persist_kernel(AttnDe
     if (r > 0) __syncthreads();  // every wavefront is done with the previous item's LDS
     fwd_tile<DQK, DV, LSE, HG>(a, x * per + local, smem);
   }
-}
-
-// packed sequences: one work item per workgroup (their weights differ too much for a fixed walk)
-template <int DQK, int DV, int HG>
-__global__ __launch_bounds__(64 * FWD_WAVES) void attn_fwd_packed_kernel(AttnDev a) {
-  using Stage = KVStage<DQK, DV, FWD_WAVES>;
-  __shared__ __attribute__((aligned(1024))) bf16_t smem[3 * (Stage::KS + Stage::VS)];
-  fwd_tile<DQK, DV, false, HG, true>(a, xcd_remap(blockIdx.x, (a.H / HG) * a.nqb), smem);
 }
 
 template <int DQK, int DV, int HG>
@@ -361,32 +310,13 @@ hipError_t fwd_launch_hg(const Attn& at, hipStream_t s, const char** kernel) {
 
 // four heads per workgroup when they share every key / value source (the head -> group
 // divisors are multiples of 4), else one
-template <int DQK>
-bool share4(const Attn& at) {
-  return at.H % 4 == 0 && at.Ka.div % 4 == 0 && at.V.div % 4 == 0 &&
-         (at.dnope == DQK || at.Kb.div % 4 == 0);
-}
-
 template <int DQK, int DV>
 hipError_t fwd_launch(const Attn& at, hipStream_t s, const char** kernel) {
-  return share4<DQK>(at) ? fwd_launch_hg<DQK, DV, 4>(at, s, kernel)
-                         : fwd_launch_hg<DQK, DV, 1>(at, s, kernel);
+  const bool share4 = at.H % 4 == 0 && at.Ka.div % 4 == 0 && at.V.div % 4 == 0 &&
+                      (at.dnope == DQK || at.Kb.div % 4 == 0);
+  return share4 ? fwd_launch_hg<DQK, DV, 4>(at, s, kernel) : fwd_launch_hg<DQK, DV, 1>(at, s, kernel);
 }
 
-template <int DQK, int DV, int HG>
-hipError_t packed_launch_hg(const Attn& at, hipStream_t s, const char** kernel) {
-  AttnDev d = to_dev(at);
-  d.nqb = at.n_q / (FWD_BQ / HG) + at.B;  // tile numbers of all sequences
-  attn_fwd_packed_kernel<DQK, DV, HG><<<d.H / HG * d.nqb, 64 * FWD_WAVES, 0, s>>>(d);
-  *kernel = KLABEL("attn_fwd_packed_kernel<%d,%d>", DQK, DV);
-  return hipGetLastError();
-}
-
-template <int DQK, int DV>
-hipError_t packed_launch(const Attn& at, hipStream_t s, const char** kernel) {
-  return share4<DQK>(at) ? packed_launch_hg<DQK, DV, 4>(at, s, kernel)
-                         : packed_launch_hg<DQK, DV, 1>(at, s, kernel);
-}
 
 }  // namespace
 
@@ -403,13 +333,6 @@ bool attn_mfma_supported(int dqk, int dv) { return attn::supported(dqk, dv); }
 
 hipError_t attn_fwd_mfma(const Attn& a, hipStream_t s, const char** kernel) {
 #define X(a_, b_) if (a.dqk == a_ && a.dv == b_) return attn::fwd_launch<a_, b_>(a, s, kernel);
-  MLA_MFMA_SHAPES(X)
-#undef X
-  return hipErrorInvalidValue;
-}
-
-hipError_t attn_fwd_packed_mfma(const Attn& a, hipStream_t s, const char** kernel) {
-#define X(a_, b_) if (a.dqk == a_ && a.dv == b_) return attn::packed_launch<a_, b_>(a, s, kernel);
   MLA_MFMA_SHAPES(X)
 #undef X
   return hipErrorInvalidValue;

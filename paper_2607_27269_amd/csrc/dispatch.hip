@@ -103,18 +103,6 @@ hipError_t attn_fwd(const Attn& a, hipStream_t s) {
   return e;
 }
 
-hipError_t attn_fwd_packed(const Attn& a, hipStream_t s) {
-  if (a.t != DT_BF16 || !attn_mfma_supported(a.dqk, a.dv) || a.lse || a.o_diff || a.q_cos || a.n_vchunk != 1)
-    return hipErrorInvalidValue;
-  if (a.n_q == 0) return hipSuccess;
-  prof_begin(KC_ATTN_FWD, s);
-  const char* kname = nullptr;
-  const hipError_t e = attn_fwd_packed_mfma(a, s, &kname);
-  // (the lengths are on the device: no count of the pairs)
-  prof_end(KC_ATTN_FWD, s, 0.0, ((double)a.n_q + a.n_kv) * a.H * (a.dqk + a.dv) * 2, kname);
-  return e;
-}
-
 hipError_t attn_bwd(const AttnBwd& w, hipStream_t s) {
   const Attn& a = w.f;
   if (a.t == DT_BF16 && attn_mfma_supported(a.dqk, a.dv)) return attn_bwd_mfma(w, s);

@@ -93,17 +93,8 @@ struct Attn {
   // c*dv + d] from V column c*dv + d (o_head = 0: dv)
   int n_vchunk = 1;
   int64_t o_head = 0;
-  // attn_fwd_packed only: sequences of different lengths behind one another.  Sequence b has the
-  // queries q_off[b] .. q_off[b + 1] - 1 and the keys and values kv_off[b] .. kv_off[b + 1] - 1
-  // (device [B + 1] each, clamped to n_q and n_kv); its queries stand at the last positions of its
-  // keys and see the keys up to their own position (none: a zero output).  T is not used.
-  const int32_t* q_off = nullptr;
-  const int32_t* kv_off = nullptr;
-  int n_q = 0, n_kv = 0;
 };
 hipError_t attn_fwd(const Attn& a, hipStream_t s);
-// bf16 matrix-core shapes; lse, o_diff, q_cos and value chunks are not for it
-hipError_t attn_fwd_packed(const Attn& a, hipStream_t s);
 
 struct AttnBwd {
   Attn f;                    // forward operands; f.O and f.lse are inputs here
@@ -337,6 +328,23 @@ struct PrefillPaged {
 };
 size_t prefill_paged_ws_bytes(const PrefillPaged& p);
 hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s);
+
+// Causal attention over packed sequences of different lengths (attn_packed.hip): sequence b has the
+// queries q_off[b] .. q_off[b + 1] - 1 and the keys and values kv_off[b] .. kv_off[b + 1] - 1
+// (device [B + 1] each, clamped to n_q and n_kv).  Its queries stand at the last positions of its
+// keys and see the keys up to their own position (none: a zero output).  bf16, the matrix-core
+// shapes; keys and values must be finite where a query that does not see them may meet them.
+struct AttnPacked {
+  int B, H, dqk, dnope, dv;
+  HeadView Q, Ka, Kb, V;           // as in Attn
+  void* O; int64_t o_tok;
+  float scale;
+  const int32_t *q_off, *kv_off;
+  int n_q, n_kv;
+  void* ws;                        // attn_packed_ws_bytes
+};
+size_t attn_packed_ws_bytes(const AttnPacked& a);
+hipError_t attn_fwd_packed(const AttnPacked& a, hipStream_t s);
 
 // The absorbed queries of decoding: qabs [B][HP][rkv + dr] (rows past H are not written), or with
 // frag the same values in the order of matrix operands.

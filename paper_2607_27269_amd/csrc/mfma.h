@@ -47,6 +47,5 @@ struct GemmBatch {
 hipError_t gemm_mfma_causal(const Gemm& g, const GemmBatch& bt, hipStream_t s);
 bool attn_mfma_supported(int dqk, int dv);
 hipError_t attn_fwd_mfma(const Attn& a, hipStream_t s, const char** kernel);
-hipError_t attn_fwd_packed_mfma(const Attn& a, hipStream_t s, const char** kernel);
 hipError_t attn_bwd_mfma(const AttnBwd& w, hipStream_t s);
 }  // namespace mla

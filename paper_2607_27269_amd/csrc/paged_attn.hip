@@ -797,6 +797,20 @@ Gemm expand(const PrefillPaged& p, const void* rows, const void* W, int n, void*
   g.C = out; g.ldc = n; g.in_t = DT_BF16; g.c_t = DT_BF16; g.alpha = 1.f; g.beta = 0.f;
   return g;
 }
+AttnPacked packed_attention(const PrefillPaged& p, const void* rows, const void* keys, const void* vals) {
+  AttnPacked a;
+  const int W = p.rkv + p.dr, dqk = p.dn + p.dr, hpg = p.H / p.G;
+  const bf16_t* kpe = (const bf16_t*)rows + p.rkv;
+  a.B = p.B; a.H = p.H; a.dqk = dqk; a.dv = p.dv;
+  a.dnope = p.dn > 0 ? p.dn : dqk;  // (no non-positional keys: the positional key is the whole key)
+  a.Q = HeadView{p.q, (int64_t)p.H * dqk, dqk, 1};
+  a.Ka = p.dn > 0 ? HeadView{keys, (int64_t)p.G * p.dn, p.dn, hpg} : HeadView{kpe, W, 0, p.H};
+  a.Kb = HeadView{kpe, W, 0, p.H};
+  a.V = HeadView{vals, (int64_t)p.G * p.dv, p.dv, hpg};
+  a.O = p.o; a.o_tok = (int64_t)p.H * p.dv; a.scale = p.scale;
+  a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv; a.ws = nullptr;
+  return a;
+}
 PrefillLayout prefill_layout(const PrefillPaged& p) {
   PrefillLayout l;
   l.rows = 0;
@@ -809,7 +823,8 @@ PrefillLayout prefill_layout(const PrefillPaged& p) {
     const size_t v = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dv, nullptr));
     if (v > l.split_elems) l.split_elems = v;
   }
-  l.bytes = l.split + al(l.split_elems * 4);
+  const size_t parts = attn_packed_ws_bytes(packed_attention(p, nullptr, nullptr, nullptr));
+  l.bytes = l.split + al(l.split_elems * 4 > parts ? l.split_elems * 4 : parts);
   return l;
 }
 
@@ -824,7 +839,7 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
   const PrefillLayout l = prefill_layout(p);
   char* ws = (char*)p.ws;
   void *rows = ws + l.rows, *keys = ws + l.keys, *vals = ws + l.vals;
-  const int W = p.rkv + p.dr, dqk = p.dn + p.dr, nk = p.G * p.dn, nv = p.G * p.dv;
+  const int W = p.rkv + p.dr, nk = p.G * p.dn, nv = p.G * p.dv;
   if (p.n_kv > 0) {
     prof_begin(KC_ELEM, s);
     gather_rows_kernel<<<(p.n_kv + 3) / 4, 256, 0, s>>>(p.c, p.kv_off, p.B, p.n_kv, p.rkv, (const bf16_t*)p.Wuv, nv,
@@ -837,16 +852,8 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
     const hipError_t e = gemm_group(up, n, (float*)(ws + l.split), l.split_elems, s);
     if (e != hipSuccess) return e;
   }
-  Attn a;
-  const bf16_t* kpe = (const bf16_t*)rows + p.rkv;
-  a.B = p.B; a.T = 0; a.H = p.H; a.dqk = dqk; a.dv = p.dv;
-  a.dnope = p.dn > 0 ? p.dn : dqk;  // (no non-positional keys: the positional key is the whole key)
-  a.Q = HeadView{p.q, (int64_t)p.H * dqk, dqk, 1};
-  a.Ka = p.dn > 0 ? HeadView{keys, nk, p.dn, p.H / p.G} : HeadView{kpe, W, 0, p.H};
-  a.Kb = HeadView{kpe, W, 0, p.H};
-  a.V = HeadView{vals, nv, p.dv, p.H / p.G};
-  a.O = p.o; a.o_tok = (int64_t)p.H * p.dv; a.lse = nullptr; a.scale = p.scale; a.t = DT_BF16;
-  a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv;
+  AttnPacked a = packed_attention(p, rows, keys, vals);
+  a.ws = ws + l.split;  // (the products' partials are done with)
   return attn_fwd_packed(a, s);
 }
 
