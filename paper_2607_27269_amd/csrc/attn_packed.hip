@@ -44,11 +44,29 @@ struct PackedDev {
   float* part_ml;  // [nsplit][n_q][H][2]: reference maximum (log2), sum
 };
 
+// A tile of 64 rows in LDS, not padded: 16-byte chunk c of row r lies at c ^ swz(r), so that the reads
+// made of it are free of bank conflicts.  Keys: 16 bytes of 16 consecutive rows.  Values: the
+// transposing reads' 32 bytes of four consecutive rows (pairs of chunks stay pairs).
+template <int D>
+struct KeySwz {
+  static constexpr int BANKS = D / 2 % 64;  // row stride
+  static_assert(BANKS % 16 == 0 && (BANKS != 0 || D % 128 == 0), "row stride in banks");
+  // chunk bits that it changes
+  static constexpr int BITS = BANKS == 0 ? 4 : BANKS == 32 ? 3 : 2;
+  static_assert(D / 8 % (1 << BITS) == 0, "chunks stay in their row");
+  __device__ __forceinline__ static int swz(int r) { return BANKS == 0 ? r & 15 : BANKS == 32 ? r >> 1 & 7 : r >> 2 & 3; }
+};
+template <int D>
+struct ValueSwz {
+  static_assert(D == 64 || D == 128, "row stride in banks");
+  __device__ __forceinline__ static int swz(int r) { return D == 128 ? (r & 3) << 1 : (r >> 1 & 1) << 1; }
+};
+
 // A tile's copies by one wavefront: each lane's source, which moves on by 64 rows a tile.
-template <int D, int LD>
+template <int D, class SWZ>
 struct RowStream {
-  using Map = DmaTile<BKV, D, LD, PA_WAVES>;
-  static constexpr int PER = Map::PER, ELEMS = Map::ALLOC;
+  static constexpr int CHR = D / 8, NBLK = BKV * CHR / 64, PER = (NBLK + PA_WAVES - 1) / PA_WAVES;
+  static constexpr int ELEMS = BKV * D;
   const bf16_t* p[PER];
   int step[PER];  // bytes from row to row
   int row[PER];
@@ -56,13 +74,14 @@ struct RowStream {
   // element (r, c) of the sequence at src(c) + r * tok(c)
   template <class S, class K>
   __device__ __forceinline__ void init(S src, K tok, int64_t row0) {
-    Map m;
-    m.init();
+    const int lane = threadIdx.x & 63, wave = wave_id();
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      row[k] = m.row[k];
-      const int64_t t = tok(m.col[k]);
-      p[k] = src(m.col[k]) + (row0 + row[k]) * t;
+      const int idx = min(wave + k * PA_WAVES, NBLK - 1) * 64 + lane;
+      row[k] = idx / CHR;
+      const int c = 8 * ((idx % CHR) ^ SWZ::swz(row[k]));
+      const int64_t t = tok(c);
+      p[k] = src(c) + (row0 + row[k]) * t;
       step[k] = (int)(2 * t);
     }
   }
@@ -79,7 +98,7 @@ struct RowStream {
         asm volatile("");
         src -= (int64_t)max(j0 + row[k] - last, 0) * step[k];
       }
-      if (Map::NBLK % PA_WAVES == 0 || b < Map::NBLK) dma16((const bf16_t*)src, lds + b * 512);
+      if (NBLK % PA_WAVES == 0 || b < NBLK) dma16((const bf16_t*)src, lds + b * 512);
       p[k] = (const bf16_t*)((const char*)p[k] + (int64_t)BKV * step[k]);
     }
   }
@@ -87,9 +106,9 @@ struct RowStream {
 
 template <int DQK, int DV, int HG, bool SPLIT>
 __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a) {
-  constexpr int LDK = ld_of(DQK), LDV = ld_of(DV);
-  using KS = RowStream<DQK, LDK>;
-  using VS = RowStream<DV, LDV>;
+  using KW = KeySwz<DQK>;
+  using KS = RowStream<DQK, KW>;
+  using VS = RowStream<DV, ValueSwz<DV>>;
   constexpr int NST = 3, STAGE = KS::ELEMS + VS::ELEMS;
   constexpr int NKK = DQK / 16, NC = DV / 32, BQH = PA_BQ / HG;
   constexpr int PK = 4, PV = 4;  // operand reads in flight ahead of the products
@@ -165,9 +184,21 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+v"(qf[kk]));
 
-    const int kofs = col * LDK + 8 * half;
-    // a transposing V read: key row 4 half + (lane % 16) / 4, column 16 ((lane / 16) % 2) + 4 (lane % 4)
-    const int vofs = (4 * half + ((lane & 15) >> 2)) * LDV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    // operand offsets in a stage.  Keys: row col (+ 32), chunk 2 kk + half, one offset for each value of
+    // the changed bits.  Values: rows 4 half + (lane % 16) / 4 (+ 8, 16 ..: the same change), values
+    // 16 ((lane / 16) % 2) + 4 (lane % 4) (+ 32 c: one offset for even and for odd c).
+    constexpr int NKB = (1 << KW::BITS) / 2;
+    int kofs[NKB], vofs[2];
+#pragma unroll
+    for (int j = 0; j < NKB; ++j) kofs[j] = col * DQK + 8 * ((2 * j + half) ^ KW::swz(col));
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+      const int r = 4 * half + ((lane & 15) >> 2), d = 32 * odd + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      vofs[odd] = r * DV + 8 * ((d >> 3) ^ ValueSwz<DV>::swz(r)) + (d & 7);
+    }
+    auto kread = [&](const bf16_t* kt, int kk) {
+      return *(const bf16x8*)(kt + kofs[kk % NKB] + 16 * NKB * (kk / NKB));
+    };
 
     // the logits s of keys j0 .. j0 + 31: masked, and the reference moved if they need it
     auto settle = [&](f32x16& s, int j0) __attribute__((always_inline)) {
@@ -196,15 +227,14 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
     // become sn meanwhile
     auto step = [&](const bf16_t* kn, const bf16_t* vs, f32x16& sc, f32x16& sn) __attribute__((always_inline)) {
       const float m_use = m_run == -INFINITY ? 0.f : m_run;
-      const bf16_t *kp = kn + kofs, *vp = vs + vofs;
       auto vread = [&](int j) {  // step j = NC u + c: keys 16 u .., values 32 c ..
-        const bf16_t* q = vp + 16 * (j / NC) * LDV + 32 * (j % NC);
-        const u32x2 lo = lds_read_tr4(q), hi = lds_read_tr4(q + 8 * LDV);
+        const bf16_t* q = vs + vofs[j % NC % 2] + 16 * (j / NC) * DV + 64 * (j % NC / 2);
+        const u32x2 lo = lds_read_tr4(q), hi = lds_read_tr4(q + 8 * DV);
         return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
       };
       bf16x8 kf[PK], vf[PV];
 #pragma unroll
-      for (int j = 0; j < PK; ++j) kf[j] = *(const bf16x8*)(kp + 16 * j);
+      for (int j = 0; j < PK; ++j) kf[j] = kread(kn, j);
 #pragma unroll
       for (int e = 0; e < 16; ++e) sn[e] = 0.f;
       u32x4 w[2];
@@ -213,7 +243,7 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
         sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk % PK], qf[kk], sn, 0, 0, 0);
-        if (kk + PK < NKK) kf[kk % PK] = *(const bf16x8*)(kp + 16 * (kk + PK));
+        if (kk + PK < NKK) kf[kk % PK] = kread(kn, kk + PK);
         else if (kk + PK - NKK < PV) vf[kk + PK - NKK] = vread(kk + PK - NKK);
 #pragma unroll
         for (int e2 = 8 * kk / NKK; e2 < 8 * (kk + 1) / NKK; ++e2) {  // a share of the 8 pairs
@@ -241,7 +271,7 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       for (int e = 0; e < 16; ++e) sa[e] = 0.f;
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk)
-        sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(smem + kofs + 16 * kk), qf[kk], sa, 0, 0, 0);
+        sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(smem, kk), qf[kk], sa, 0, 0, 0);
       settle(sa, kb0 * BKV);
     }
     for (int kb = kb0; kb < kb1; ++kb) {
@@ -252,11 +282,11 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
         const int cur = __builtin_amdgcn_readfirstlane((kb - kb0) % NST * STAGE);
         const int nxt = __builtin_amdgcn_readfirstlane((kb + 1 - kb0) % NST * STAGE);
         const bf16_t* vs = smem + cur + KS::ELEMS;
-        step(smem + cur + 32 * LDK, vs, sa, sb);
+        step(smem + cur + 32 * DQK, vs, sa, sb);
         if (kb * BKV + 32 <= qw0 + 31 + diag) {  // the second half is not all behind the diagonal
           settle(sb, kb * BKV + 32);
           // (past the last tile the next logits come from a stale stage and are not used)
-          step(smem + nxt, vs + 32 * LDV, sb, sa);
+          step(smem + nxt, vs + 32 * DV, sb, sa);
           if (kb + 1 < nvis) settle(sa, (kb + 1) * BKV);
         }
       }
