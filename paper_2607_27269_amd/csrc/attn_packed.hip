@@ -6,8 +6,8 @@
 // sequence stand at the last positions of its keys: query t sees keys 0 .. t + diag, diag = keys -
 // queries (negative where there are fewer keys: the first queries see none and give 0).
 //
-// The tiles are worked on in the order that the caller gives (the longest first, packed.h), or the
-// last first.
+// Query tiles are numbered without a scan over the lengths: sequence b owns the numbers from
+// q_off[b] / BQH + b, at least as many as it has tiles, and the few others are empty.
 //
 // Keys and values stream through three LDS stages of 64 keys.  S^T = K Q^T has the key in the MFMA row
 // and the query in its column, so a lane owns a query's state and the exponential of its accumulator
@@ -21,7 +21,6 @@
 // each with a result of its own (fp32), and a second launch joins them.
 #include "attn_common.h"
 #include "mfma.h"
-#include "packed.h"
 
 namespace mla {
 namespace attn {
@@ -30,7 +29,6 @@ namespace {
 constexpr int PA_WAVES = 8;
 constexpr int PA_BQ = 32 * PA_WAVES;
 constexpr float PA_SLACK = 8.f;  // log2 units the running reference maximum may lag
-constexpr int PA_GRID = 256;     // a multiple of the 8 XCDs
 
 struct PackedDev {
   int B, H, dnope;
@@ -40,11 +38,8 @@ struct PackedDev {
   const bf16_t* Kb; int64_t kb_tok; int kb_head; int kb_div;
   const bf16_t* V; int64_t v_tok; int v_head; int v_div;
   bf16_t* O; int64_t o_tok;
-  PackedSeqs seqs;
-  int nqb, nsplit;
-  const int32_t* order;  // order_tiles' result, or null
-  int items;             // tiles x parts x head groups
-  int32_t* next;         // a counter for each XCD, 32 apart, 0 at the start
+  const int32_t *q_off, *kv_off;
+  int n_q, n_kv, nqb, nsplit;
   float* part_o;   // [nsplit][n_q][H][DV], not normalised
   float* part_ml;  // [nsplit][n_q][H][2]: reference maximum (log2), sum
 };
@@ -109,26 +104,31 @@ struct RowStream {
   }
 };
 
-// work item `item`: head group item % (H / HG), part of the keys, tile number (or place in the order)
-template <int HG, bool SPLIT>
-__device__ __forceinline__ PackedSeqs::Tile item_tile(const PackedDev& a, int item) {
-  const int nth = item / (a.H / HG) / (SPLIT ? a.nsplit : 1);
-  return a.order ? ordered_tile(a.order, nth) : a.seqs.tile(a.nqb - 1 - nth);
-}
-
 template <int DQK, int DV, int HG, bool SPLIT>
-__device__ __forceinline__ void packed_item(const PackedDev& a, int item, const PackedSeqs::Tile& t, bf16_t* smem) {
+__global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a) {
   using KW = KeySwz<DQK>;
   using KS = RowStream<DQK, KW>;
   using VS = RowStream<DV, ValueSwz<DV>>;
   constexpr int NST = 3, STAGE = KS::ELEMS + VS::ELEMS;
   constexpr int NKK = DQK / 16, NC = DV / 32, BQH = PA_BQ / HG;
   constexpr int PK = 4, PV = 4;  // operand reads in flight ahead of the products
+  __shared__ __attribute__((aligned(1024))) bf16_t smem[NST * STAGE];
 
-  const int ngr = a.H / HG, i0 = item % ngr * HG;
-  const int z = SPLIT ? item / ngr % a.nsplit : 0;
-  if (t.empty()) return;
-  const int qs = t.qs, ks = t.ks, Tq = t.Tq, Tk = t.Tk, diag = Tk - Tq, q0 = t.q0;
+  const int pid = xcd_remap(blockIdx.x, gridDim.x);
+  const int z = SPLIT ? pid % a.nsplit : 0, tile = SPLIT ? pid / a.nsplit : pid;
+  const int qb = a.nqb - 1 - tile % a.nqb, i0 = tile / a.nqb * HG;
+  auto q_at = [&](int b) { return min(max(a.q_off[b], 0), a.n_q); };
+  auto k_at = [&](int b) { return min(max(a.kv_off[b], 0), a.n_kv); };
+  int b = 0;
+  for (int hi = a.B - 1; b < hi;) {  // the last sequence whose numbers start at qb or before
+    const int mid = (b + hi + 1) >> 1;
+    if (q_at(mid) / BQH + mid <= qb) b = mid;
+    else hi = mid - 1;
+  }
+  const int qs = q_at(b), ks = k_at(b);
+  const int Tq = max(q_at(b + 1) - qs, 0), Tk = max(k_at(b + 1) - ks, 0), diag = Tk - Tq;
+  const int q0 = (qb - (qs / BQH + b)) * BQH;
+  if (q0 < 0 || q0 >= Tq) return;
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5, col = lane & 31;
@@ -137,7 +137,8 @@ __device__ __forceinline__ void packed_item(const PackedDev& a, int item, const 
   const int my_q = qw0 + col;
   const int64_t row = (int64_t)qs + my_q;  // of Q and O
 
-  const int nkb = (t.keys(BQH) + BKV - 1) / BKV;
+  const int kend = min(Tk, q0 + BQH + diag);
+  const int nkb = kend > 0 ? (kend + BKV - 1) / BKV : 0;
   const int per = SPLIT ? (nkb + a.nsplit - 1) / a.nsplit : nkb;
   const int kb0 = z * per, kb1 = min(nkb, kb0 + per);
   // tiles that this wavefront sees: [kb0, nvis)
@@ -299,7 +300,7 @@ __device__ __forceinline__ void packed_item(const PackedDev& a, int item, const 
   const float l = pair_sum32(l_run);
   if (my_q >= Tq) return;
   if (SPLIT) {
-    const int64_t at = ((int64_t)z * a.seqs.n_q + row) * a.H + i;
+    const int64_t at = ((int64_t)z * a.n_q + row) * a.H + i;
     if (half == 0) {
       a.part_ml[2 * at] = m_run;
       a.part_ml[2 * at + 1] = l;
@@ -324,50 +325,14 @@ __device__ __forceinline__ void packed_item(const PackedDev& a, int item, const 
   }
 }
 
-// Workgroups (one a CU) fetch their items from a counter for each XCD, the longest first; XCD x has
-// the items x, x + 8, .., so that with a multiple of eight head groups each keeps to its own keys
-// and values.  (One workgroup per item left a fifth of the CUs idle: workgroups are dispatched in
-// order over the parts of an XCD, and the next one waits for its part, not for the first free CU.)
-// Every counter only grows, and a workgroup ends at the first item past the last.
-template <int DQK, int DV, int HG, bool SPLIT>
-__global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a) {
-  __shared__ __attribute__((aligned(1024)))
-  bf16_t smem[3 * (RowStream<DQK, KeySwz<DQK>>::ELEMS + RowStream<DV, ValueSwz<DV>>::ELEMS)];
-  __shared__ int next_item;
-  __shared__ PackedSeqs::Tile next_tile;
-  const int x = blockIdx.x % 8, items = a.items;
-  int item = blockIdx.x;
-  PackedSeqs::Tile t = item_tile<HG, SPLIT>(a, item);
-  if ((int)gridDim.x >= items) {  // one each (uniform)
-    packed_item<DQK, DV, HG, SPLIT>(a, item, t, smem);
-    return;
-  }
-  for (;;) {
-    if (threadIdx.x == 64 * PA_WAVES - 1) {  // the next item, in the shadow of this one's first copies
-      next_item = (int)gridDim.x + x + 8 * atomicAdd(a.next + 32 * x, 1);
-      if (next_item < items) next_tile = item_tile<HG, SPLIT>(a, next_item);
-    }
-    packed_item<DQK, DV, HG, SPLIT>(a, item, t, smem);
-    __syncthreads();
-    item = __builtin_amdgcn_readfirstlane(next_item);
-    if (item >= items) return;
-    t.qs = __builtin_amdgcn_readfirstlane(next_tile.qs);
-    t.ks = __builtin_amdgcn_readfirstlane(next_tile.ks);
-    t.Tq = __builtin_amdgcn_readfirstlane(next_tile.Tq);
-    t.Tk = __builtin_amdgcn_readfirstlane(next_tile.Tk);
-    t.q0 = __builtin_amdgcn_readfirstlane(next_tile.q0);
-    __syncthreads();
-  }
-}
-
 // The parts of every (query, head) joined in order; a thread has four values.  Parts without weight
 // (no key seen: reference -infinity, sum 0) are not read.
 __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedDev a, int dv) {
   const int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x), at = e / dv;
   const int64_t row = at / a.H;
-  if (row >= a.seqs.n_q || row < a.seqs.q_off[0] || row >= a.seqs.q_off[a.B]) return;
+  if (row >= a.n_q || row < a.q_off[0] || row >= a.q_off[a.B]) return;
   const int i = (int)(at % a.H), d = (int)(e % dv);
-  const int64_t stride = (int64_t)a.seqs.n_q * a.H;
+  const int64_t stride = (int64_t)a.n_q * a.H;
   float M = -INFINITY;
   for (int z = 0; z < a.nsplit; ++z) M = fmaxf(M, a.part_ml[2 * (at + z * stride)]);
   float L = 0.f;
@@ -387,10 +352,12 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedDev a, int 
 int heads_per_group(const AttnPacked& a) {
   return a.H % 4 == 0 && a.Ka.div % 4 == 0 && a.V.div % 4 == 0 && (a.dnope == a.dqk || a.Kb.div % 4 == 0) ? 4 : 1;
 }
+// query tile numbers of all sequences
+int tile_numbers(const AttnPacked& a) { return a.n_q / (PA_BQ / heads_per_group(a)) + a.B; }
 // Parts of the keys: where the tiles do not fill the CUs once, as many as fill them twice, each of
 // four or more key tiles of an average sequence.
 int parts_of(const AttnPacked& a) {
-  const int64_t tiles = (int64_t)attn_packed_tiles(a) * (a.H / heads_per_group(a));
+  const int64_t tiles = (int64_t)tile_numbers(a) * (a.H / heads_per_group(a));
   if (tiles >= 256) return 1;
   const int64_t fill = (512 + tiles - 1) / tiles, most = a.n_kv / ((int64_t)a.B * BKV * 4);
   const int64_t n = fill < most ? fill : most;
@@ -399,21 +366,13 @@ int parts_of(const AttnPacked& a) {
 
 template <int DQK, int DV, int HG>
 void launch(const PackedDev& d, hipStream_t s) {
-  const unsigned grid = (unsigned)(d.items < PA_GRID ? d.items : PA_GRID);
+  const unsigned grid = (unsigned)(d.H / HG * d.nqb * d.nsplit);
   if (d.nsplit > 1) attn_packed_kernel<DQK, DV, HG, true><<<grid, 64 * PA_WAVES, 0, s>>>(d);
   else attn_packed_kernel<DQK, DV, HG, false><<<grid, 64 * PA_WAVES, 0, s>>>(d);
 }
 
 }  // namespace
 }  // namespace attn
-
-int attn_packed_bq(const AttnPacked& a) { return attn::PA_BQ / attn::heads_per_group(a); }
-int attn_packed_tiles(const AttnPacked& a) { return a.n_q / attn_packed_bq(a) + a.B; }
-bool attn_packed_ordered(const AttnPacked& a) {
-  const int tiles = attn_packed_tiles(a);
-  return (int64_t)tiles * attn::parts_of(a) * (a.H / attn::heads_per_group(a)) > attn::PA_GRID &&
-         tiles <= ORDER_MAX && a.B <= ORDER_SEQS;
-}
 
 size_t attn_packed_ws_bytes(const AttnPacked& a) {
   const int n = attn::parts_of(a);
@@ -430,9 +389,8 @@ hipError_t attn_fwd_packed(const AttnPacked& a, hipStream_t s) {
   d.Kb = (const bf16_t*)a.Kb.p; d.kb_tok = a.Kb.tok; d.kb_head = (int)a.Kb.head; d.kb_div = a.Kb.div;
   d.V = (const bf16_t*)a.V.p; d.v_tok = a.V.tok; d.v_head = (int)a.V.head; d.v_div = a.V.div;
   d.O = (bf16_t*)a.O; d.o_tok = a.o_tok;
-  d.seqs = PackedSeqs{a.q_off, a.kv_off, a.B, a.n_q, a.n_kv, attn_packed_bq(a)};
-  d.nqb = attn_packed_tiles(a); d.nsplit = attn::parts_of(a); d.order = a.order;
-  d.items = a.H / attn::heads_per_group(a) * d.nqb * d.nsplit; d.next = a.next;
+  d.q_off = a.q_off; d.kv_off = a.kv_off; d.n_q = a.n_q; d.n_kv = a.n_kv;
+  d.nqb = attn::tile_numbers(a); d.nsplit = attn::parts_of(a);
   d.part_o = (float*)a.ws;
   d.part_ml = d.part_o + (size_t)d.nsplit * a.n_q * a.H * a.dv;
   const int hg = attn::heads_per_group(a);

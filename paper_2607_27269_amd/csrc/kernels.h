@@ -342,16 +342,8 @@ struct AttnPacked {
   const int32_t *q_off, *kv_off;
   int n_q, n_kv;
   void* ws;                        // attn_packed_ws_bytes
-  const int32_t* order;            // device: the tiles in the order to work on them (packed.h's
-                                   // order_tiles), or null
-  int32_t* next;                   // device [ATTN_PACKED_COUNTERS], 0 when the kernel starts
 };
-constexpr int ATTN_PACKED_COUNTERS = 256;
 size_t attn_packed_ws_bytes(const AttnPacked& a);
-int attn_packed_bq(const AttnPacked& a);     // queries of a tile
-int attn_packed_tiles(const AttnPacked& a);  // tile numbers of all sequences
-// whether there are so many that their order counts, and no more than order_tiles takes
-bool attn_packed_ordered(const AttnPacked& a);
 hipError_t attn_fwd_packed(const AttnPacked& a, hipStream_t s);
 
 // The absorbed queries of decoding: qabs [B][HP][rkv + dr] (rows past H are not written), or with

@@ -4,7 +4,6 @@
 #include "attn_common.h"
 #include "common.h"
 #include "kernels.h"
-#include "packed.h"
 
 namespace mla {
 namespace {
@@ -734,21 +733,10 @@ namespace {
 // are 0 and its logits NaN, for exactly the queries that see it.  So does a row whose finite latent
 // reaches 2^64 and has a value of 2^127 or more (below 2^64 that would take weights of 2^54).
 // Rows of no sequence become zeros.  Bound by memory and, for few rows, by three dependent loads.
-// The first workgroup clears the attention's counters and puts its query tiles in order meanwhile
-// (order not null).
-__global__ __launch_bounds__(256) void gather_rows_kernel(PagedPool c, PackedSeqs seqs, int rkv,
-                                                          const bf16_t* __restrict__ Wuv, int nv,
-                                                          bf16_t* __restrict__ out, int tiles,
-                                                          int32_t* __restrict__ order,
-                                                          int32_t* __restrict__ next) {
-  if (blockIdx.x == 0) {
-    next[threadIdx.x] = 0;
-    if (order) order_tiles(seqs, tiles, order);
-    return;
-  }
-  const int32_t* kv_off = seqs.kv_off;
-  const int B = seqs.B, n_kv = seqs.n_kv;
-  const int row = 4 * (blockIdx.x - 1) + wave_id();
+__global__ __launch_bounds__(256) void gather_rows_kernel(PagedPool c, const int32_t* __restrict__ kv_off, int B,
+                                                          int n_kv, int rkv, const bf16_t* __restrict__ Wuv, int nv,
+                                                          bf16_t* __restrict__ out) {
+  const int row = 4 * blockIdx.x + wave_id();
   if (row >= n_kv) return;
   const int lane = threadIdx.x & 63, dr = c.width - rkv;
   bf16_t* dst = out + (int64_t)row * c.width;
@@ -799,7 +787,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(PagedPool c, PackedSeq
 }
 
 struct PrefillLayout {
-  size_t rows, keys, vals, order, next, split, split_elems, bytes;
+  size_t rows, keys, vals, split, split_elems, bytes;
 };
 Gemm expand(const PrefillPaged& p, const void* rows, const void* W, int n, void* out) {
   Gemm g;
@@ -821,7 +809,6 @@ AttnPacked packed_attention(const PrefillPaged& p, const void* rows, const void*
   a.V = HeadView{vals, (int64_t)p.G * p.dv, p.dv, hpg};
   a.O = p.o; a.o_tok = (int64_t)p.H * p.dv; a.scale = p.scale;
   a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv; a.ws = nullptr;
-  a.order = nullptr; a.next = nullptr;
   return a;
 }
 PrefillLayout prefill_layout(const PrefillPaged& p) {
@@ -829,9 +816,7 @@ PrefillLayout prefill_layout(const PrefillPaged& p) {
   l.rows = 0;
   l.keys = l.rows + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
   l.vals = l.keys + al((size_t)p.n_kv * p.G * p.dn * 2);
-  l.order = l.vals + al((size_t)p.n_kv * p.G * p.dv * 2);
-  l.next = l.order + al((size_t)ORDER_MAX * ORDER_INTS * 4);
-  l.split = l.next + al((size_t)ATTN_PACKED_COUNTERS * 4);
+  l.split = l.vals + al((size_t)p.n_kv * p.G * p.dv * 2);
   l.split_elems = 0;  // partials of the products
   if (p.n_kv > 0) {
     if (p.dn > 0) l.split_elems = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dn, nullptr));
@@ -855,17 +840,11 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
   char* ws = (char*)p.ws;
   void *rows = ws + l.rows, *keys = ws + l.keys, *vals = ws + l.vals;
   const int W = p.rkv + p.dr, nk = p.G * p.dn, nv = p.G * p.dv;
-  AttnPacked a = packed_attention(p, rows, keys, vals);
-  a.ws = ws + l.split;  // (the products' partials are done with)
-  a.next = (int32_t*)(ws + l.next);
-  const int tiles = attn_packed_tiles(a);
-  if (attn_packed_ordered(a)) a.order = (const int32_t*)(ws + l.order);
-  prof_begin(KC_ELEM, s);
-  gather_rows_kernel<<<1 + (p.n_kv + 3) / 4, 256, 0, s>>>(
-      p.c, PackedSeqs{p.q_off, p.kv_off, p.B, p.n_q, p.n_kv, attn_packed_bq(a)}, p.rkv, (const bf16_t*)p.Wuv, nv,
-      (bf16_t*)rows, tiles, (int32_t*)a.order, a.next);
-  prof_end(KC_ELEM, s, 0.0, (double)p.n_kv * W * 4, KLABEL("gather_rows_kernel"));
   if (p.n_kv > 0) {
+    prof_begin(KC_ELEM, s);
+    gather_rows_kernel<<<(p.n_kv + 3) / 4, 256, 0, s>>>(p.c, p.kv_off, p.B, p.n_kv, p.rkv, (const bf16_t*)p.Wuv, nv,
+                                                        (bf16_t*)rows);
+    prof_end(KC_ELEM, s, 0.0, (double)p.n_kv * W * 4, KLABEL("gather_rows_kernel"));
     Gemm up[2];
     int n = 0;
     if (p.dn > 0) up[n++] = expand(p, rows, p.Wuk, nk, keys);
@@ -873,6 +852,8 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
     const hipError_t e = gemm_group(up, n, (float*)(ws + l.split), l.split_elems, s);
     if (e != hipSuccess) return e;
   }
+  AttnPacked a = packed_attention(p, rows, keys, vals);
+  a.ws = ws + l.split;  // (the products' partials are done with)
   return attn_fwd_packed(a, s);
 }
 
