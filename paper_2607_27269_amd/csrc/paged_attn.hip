@@ -395,15 +395,18 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
         mfma_a(acc[j % NC], vf[j % PV], pl[j / NC]);
         if (j + PV < 2 * NC) vf[j % PV] = vread(j + PV);
         __builtin_amdgcn_sched_barrier(0);
-        if (j == NC && together) issue_half(0, at);
+        if (j == NC) {
+          mfma_a_done(acc);  // (no branch, where the compiler may move registers, before the products' waits)
+          if (together) issue_half(0, at);
+        }
       }
+      mfma_a_done(acc);
       // every read of the tile has returned before the next copies may overwrite it
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
       if (more) {
         if (together) issue_half(1, at);
         else issue_rows(at);
       }
-      mfma_a_done(acc);
     }
 
     if (!joined) {  // leaving the sequence: its state
