@@ -22,7 +22,7 @@ size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 // * A wavefront works on its run by itself: its own LDS buffer, its own softmax state (running
 //   maximum and sum of each head, the weighted latents of all heads in 256 registers), no barrier
 //   and no exchange.  While one wavefront waits for its copies the others multiply: about three of
-//   the four 37 KB tiles of a CU are in flight at any time.
+//   the four 36 KB tiles of a CU are in flight at any time.
 // * Where a wavefront leaves a sequence it stores the state to slot (wavefront + sequence), which
 //   nobody else has: along the list one of the two grows from state to state.  Where the whole
 //   share lies in one sequence the four states are joined through LDS first and only one is stored
@@ -52,7 +52,7 @@ struct PagedDecodeDev {
 __device__ __forceinline__ int decode_len(const PagedDecodeDev& a, int b) {
   return min(max(a.len[b], 0), a.max_len);
 }
-__device__ __forceinline__ int tiles_of(int n) { return (n + PD_KT - 1) / PD_KT; }
+__device__ __forceinline__ int tiles_of(int n) { return (int)(((uint32_t)n + PD_KT - 1) / PD_KT); }  // (n up to 2^31 - 1)
 // The list's cut: tiles per workgroup (at least one for each wavefront), and the part of
 // workgroup w and of its wavefronts.
 struct ListCut {
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
 #pragma unroll
       for (int j = 0; j < PV; ++j) vf[j] = vread(j);
       // rows past the end (the last tile only; a real branch): no weight
-      if ((t + 1) * PD_KT > n) {
+      if (t * PD_KT > n - PD_KT) {
         asm volatile("");
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -387,7 +387,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
       bool together = false;
       if (more) {
         at = address(T + 1 - seq2, n2, page, bad);
-        together = whole16 && (T + 2 - seq2) * PD_KT <= n2;
+        together = whole16 && (T + 1 - seq2) * PD_KT <= n2 - PD_KT;
       }
 #pragma unroll
       for (int j = 0; j < 2 * NC; ++j) {

@@ -320,6 +320,37 @@ def test_decode_position_past_32_bits_of_bytes():
     check_decode(lay, q, [70, 65], Decode(lay, q, [70, 65], 70)())
 
 
+def test_decode_longest_length():
+    """2^31 - 1 rows, the largest length (one page of 65536 rows again and again): the attention over the
+    page's rows, of which one is there 32767 times and the others 32768 times."""
+    lay = Layer(shape("tiny"), [65536], 65536, seed=17, spare=0)
+    lay.table = np.zeros((1, 32768), dtype=np.int64)
+    lay.upload()
+    q = lay.queries(1)
+    n = 2**31 - 1
+    print("[paged] decode 2^31 - 1 rows", flush=True)
+    check_decode(lay, q, [65536], Decode(lay, q, [n], n)())
+
+
+def test_decode_most_sequences():
+    """65535 sequences, the largest batch."""
+    rng = np.random.default_rng(18)
+    lens = rng.integers(0, 4, 65535)
+    lens[[0, 40000, 65534]] = [70, 33, 3]
+    print("[paged] decode 65535 sequences", flush=True)
+    lay = Layer(shape("tiny"), lens, 4, seed=18)
+    q = lay.queries(len(lens))
+    check_decode(lay, q, lens, Decode(lay, q, lens, 70)(), only=set(range(0, 65535, 997)) | {40000, 65533, 65534})
+
+
+def test_decode_without_non_positional_keys():
+    """d_nope = 0: no W_UK, the key is the positional key alone."""
+    lens = [40, 0, 95, 1]
+    lay = Layer(shape("05b", nope_dim=0, rope_dim=64, kv_rank=512), lens, 16, seed=19)
+    q = lay.queries(len(lens))
+    check_decode(lay, q, lens, Decode(lay, q, lens, 95)())
+
+
 # ---- prefill --------------------------------------------------------------------------------
 class Prefill:
     def __init__(self, layer, q, q_off, kv_off, n_kv=None):
@@ -457,6 +488,38 @@ def test_prefill_replays_in_a_graph():
         check_prefill(lay, q, offsets(new), kv, got)
 
 
+def test_prefill_without_cached_rows():
+    """Sequences without rows (their queries see nothing), no cached rows at all."""
+    lay = Layer(shape("8b"), [0, 0], 16, seed=35)
+    q = lay.queries(70)
+    for n_kv in (0, 300):
+        p = Prefill(lay, q, offsets([69, 1]), offsets([0, 0]), n_kv=n_kv)
+        assert not p().any()
+
+
+def test_prefill_on_two_streams_with_their_own_workspaces():
+    import torch
+    new, kv = [200, 3], [1500, 700]
+    lay = Layer(shape("1b"), kv, 64, seed=36)
+    q = lay.queries(203)
+    a = Prefill(lay, q, offsets(new), offsets(kv))
+    b = Prefill(lay, q[::-1], offsets(new), offsets(kv), n_kv=4000)
+    want = a().clone(), b().clone()
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        a.o.zero_(), b.o.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s1):
+            a()
+        with torch.cuda.stream(s2):
+            b()
+        torch.cuda.synchronize()
+        assert torch.equal(a.o, want[0]) and torch.equal(b.o, want[1])
+    check_prefill(lay, q, offsets(new), kv, a.o)
+    check_prefill(lay, q[::-1], offsets(new), kv, b.o)
+
+
 # ---- append -----------------------------------------------------------------------------------
 class Append:
     def __init__(self, cfg, pool, table, rows, q, q_off, start, inv, dtype, in_place=False):
@@ -573,6 +636,40 @@ def test_append_parts_and_padding():
     changed = (got != pool).any(-1)
     assert changed.sum() == (want_pool != pool).any(-1).sum() == 16 + 4
     assert (np.abs(got - want_pool) <= 2.0 ** -8 * np.abs(want_pool) + 1e-6 * 10).all()
+
+
+def test_append_replays_in_a_graph():
+    """A captured call follows offsets, starts, tables and rows as they are at each replay."""
+    import torch
+    cfg, pool, table, rows, q, inv = append_case("1b", "bf16", [40, 40, 40], [40, 40, 40], 16, seed=43)
+    a = Append(cfg, pool, table, rows[:60], q[:60], offsets([20, 20, 20]), [0, 1, 40], inv, "bf16")
+    start_pool = a.pool.clone()
+    a()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a()
+    for new, start in (([20, 20, 20], [0, 1, 40]), ([60, 0, 0], [7, 0, 0]), ([1, 1, 1], [79, 0, 33]), ([0, 18, 42], [0, 62, 5])):
+        a.off.copy_(ints(offsets(new)))
+        a.start.copy_(ints(start))
+        a.table.copy_(a.table.roll(1, 0))
+        a.rows.copy_(a.rows.roll(1, 0))
+        both = []
+        for run in (graph.replay, a, graph.replay):
+            a.pool.copy_(start_pool)
+            a.q_out.fill_(3.0)
+            run()
+            both.append((a.pool.clone(), a.q_out.clone()))
+            torch.cuda.synchronize()
+        for x in both[1:]:
+            assert torch.equal(x[0], both[0][0]) and torch.equal(x[1], both[0][1]), new
+        want_pool, want_q = PO.append(pool, a.table.cpu().numpy(), a.rows.double().cpu().numpy(), q[:60],
+                                      offsets(new), start, inv, kv_rank=cfg.kv_rank, nope_dim=cfg.nope_dim)
+        got = both[0][0].double().cpu().numpy()
+        assert (np.abs(got - want_pool) <= 2.0 ** -8 * np.abs(want_pool) + 1e-6 * 10).all(), new
+        k = sum(new)
+        near(both[0][1][:k], want_q[:k], q[:k], cfg.rope_dim // 2, "bf16")
+        assert (both[0][1][k:] == 3.0).all()
 
 
 # ---- page copies ------------------------------------------------------------------------------
