@@ -350,10 +350,12 @@ int mla_recon_decode_paged(const mla_recon_cfg *cfg, const void *q, const mla_pa
  *              cached rows of the sequences, n_kv an upper bound of their sum
  *   Wuk [G_kv d_nope, r_kv] (may be NULL if d_nope is 0), Wuv [G_kv d_k, r_kv] bf16
  *   o          [n_q, H, d_k] bf16 out; rows of no sequence are left as they were
- * Keys and values of all n_kv rows are expanded into ws once per call (for single tokens over
- * long caches mla_recon_decode_paged is the cheaper call).  A row that is not finite (or one of
- * whose values W_UV c reaches 2^127) makes the outputs of the queries that see it NaN and leaves
- * all others as they are.  n_q and n_kv at most 1048576, n_heads (n_q / 256 + batch) below 2^23.
+ * Keys (bf16) and values (fp16, each row and column scaled by a power of two) of all n_kv rows are
+ * expanded into ws once per call (for single tokens over long caches mla_recon_decode_paged is the
+ * cheaper call).  A row that is not finite (or one with a latent of 2^72 or more) makes the outputs of
+ * the queries that see it NaN and leaves all others as they are; rows whose largest latent is below
+ * 2^-72 lose precision, and W_UV is to be below 2^124.  n_q and n_kv at most 1048576, n_heads (n_q / 256 + batch) below 2^23,
+ * softmax_scale at least 1e-30.
  * q, Wuv, o and ws 16-byte aligned, ws of mla_recon_prefill_paged_workspace_size bytes. */
 size_t mla_recon_prefill_paged_workspace_size(const mla_recon_cfg *cfg, int32_t n_q, int32_t n_kv);
 int mla_recon_prefill_paged(const mla_recon_cfg *cfg, const void *q, int32_t n_q,

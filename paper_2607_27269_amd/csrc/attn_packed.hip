@@ -17,6 +17,15 @@
 // itself the compiler reads an operand right before its product, and the wait for LDS, not the matrix
 // cores, was what a tile cost.  The reference maximum moves only when a block exceeds it by 2^8.
 //
+// The values and the probabilities are fp16 operands: with bf16 ones their two roundings were half of
+// the output's squared error (2.9e-3 of its norm; 2.0e-3 now), at the same rate.  fp16 has the range for it because each
+// row of values is scaled by a power of two 2^-e[n] and each column by another.  The row's goes into the
+// exponent: with x' = x + e[n], P' = 2^(x' - m) is the weight of the scaled row, and P' 2^-e[n] = 2^(x - m)
+// enters the sum, m the reference maximum of x'.  |e| <= 64 keeps both in fp32's range.  P' is at most
+// 2^(PA_SLACK + PA_UP), and what fp16 cannot hold lies 2^-(24 + PA_UP) below a row's largest.  Keys whose e are
+// all 0 (any cache with latents of ordinary size) take a loop without them: 120 us against 130 for the 6
+// ragged sequences of up to 2048 tokens and 32 heads below.
+//
 // Few queries over many keys leave CUs idle: the keys are then cut into nsplit parts per query tile,
 // each with a result of its own (fp32), and a second launch joins them.
 #include "attn_common.h"
@@ -29,6 +38,9 @@ namespace {
 constexpr int PA_WAVES = 8;
 constexpr int PA_BQ = 32 * PA_WAVES;
 constexpr float PA_SLACK = 8.f;  // log2 units the running reference maximum may lag
+constexpr float PA_UP = 7.f;     // P' = 2^PA_UP at the reference
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 struct PackedDev {
   int B, H, dnope;
@@ -36,7 +48,9 @@ struct PackedDev {
   const bf16_t* Q; int64_t q_tok; int q_head;
   const bf16_t* Ka; int64_t ka_tok; int ka_head; int ka_div;
   const bf16_t* Kb; int64_t kb_tok; int kb_head; int kb_div;
-  const bf16_t* V; int64_t v_tok; int v_head; int v_div;
+  const bf16_t* V; int64_t v_tok; int v_head; int v_div;  // (fp16: copied as 16-bit values)
+  const float *key_exp, *v_scale;
+  float bias;  // 1 / sl2
   bf16_t* O; int64_t o_tok;
   const int32_t *q_off, *kv_off;
   int n_q, n_kv, nqb, nsplit;
@@ -61,6 +75,12 @@ struct ValueSwz {
   static_assert(D == 64 || D == 128, "row stride in banks");
   __device__ __forceinline__ static int swz(int r) { return D == 128 ? (r & 3) << 1 : (r >> 1 & 1) << 1; }
 };
+
+// 64 values of 4 bytes from the lanes' addresses to consecutive LDS words
+__device__ __forceinline__ void dma4(const float* src, float* lds) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(l) : "memory");
+}
 
 // A tile's copies by one wavefront: each lane's source, which moves on by 64 rows a tile.
 template <int D, class SWZ>
@@ -113,6 +133,7 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
   constexpr int NKK = DQK / 16, NC = DV / 32, BQH = PA_BQ / HG;
   constexpr int PK = 4, PV = 4;  // operand reads in flight ahead of the products
   __shared__ __attribute__((aligned(1024))) bf16_t smem[NST * STAGE];
+  __shared__ __attribute__((aligned(256))) float kexp[NST][2][BKV];  // e, and 2^-e
 
   const int pid = xcd_remap(blockIdx.x, gridDim.x);
   const int z = SPLIT ? pid % a.nsplit : 0, tile = SPLIT ? pid / a.nsplit : pid;
@@ -175,11 +196,21 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       bf16_t* st = smem + (kb - kb0) % NST * STAGE;
       kst.next(st, kb * BKV, Tk - 1);
       vst.next(st + KS::ELEMS, kb * BKV, Tk - 1);
+      if (wave < 2) dma4(a.key_exp + (int64_t)wave * a.n_kv + ks + min(kb * BKV + lane, Tk - 1), kexp[(kb - kb0) % NST][wave]);
     };
     issue(kb0);
     if (kb0 + 1 < kb1) issue(kb0 + 1);
+    // whether a key has an e other than 0
+    bool any = false;
+    for (int r0 = kb0 * BKV; r0 < min(kb1 * BKV, Tk); r0 += 8 * 64 * PA_WAVES) {
+      float e[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) e[u] = a.key_exp[ks + min(r0 + 64 * PA_WAVES * u + (int)threadIdx.x, Tk - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) any |= e[u] != 0.f;
+    }
     wait_all();
-    __syncthreads();
+    any = __syncthreads_or(any);
     // (in registers from here on: or the compiler's waits for them would also wait for copies)
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+v"(qf[kk]));
@@ -200,6 +231,18 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       return *(const bf16x8*)(kt + kofs[kk % NKB] + 16 * NKB * (kk / NKB));
     };
 
+    // e (w = 0) or 2^-e (w = 1) of keys 8 g + 4 half + 0..3 (+ 32 h) of a stage
+    auto eread = [&](int st, int w, int h, int g) { return *(const f32x4*)&kexp[st][w][32 * h + 8 * g + 4 * half]; };
+    // a logit accumulator starts at e / sl2
+    auto start = [&](f32x16& s, int st, int h, auto any) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 e = {0.f, 0.f, 0.f, 0.f};
+        if (any) e = eread(st, 0, h, g) * a.bias;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s[4 * g + q] = e[q];
+      }
+    };
     // the logits s of keys j0 .. j0 + 31: masked, and the reference moved if they need it
     auto settle = [&](f32x16& s, int j0) __attribute__((always_inline)) {
       if (j0 + 31 > qw0 + diag) {
@@ -223,20 +266,24 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
           for (int e = 0; e < 16; ++e) acc[c][e] *= corr;
       }
     };
-    // half h of a stage: its settled logits sc become P and enter O, the logits of the 32 keys at kn
-    // become sn meanwhile
-    auto step = [&](const bf16_t* kn, const bf16_t* vs, f32x16& sc, f32x16& sn) __attribute__((always_inline)) {
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    // half h of stage st: its settled logits sc become P and enter O, the logits of the 32 keys at kn
+    // (the half behind it, in stage st_n) become sn meanwhile
+    auto step = [&](const bf16_t* kn, const bf16_t* vs, f32x16& sc, f32x16& sn, int st, int h, int st_n, auto any) __attribute__((always_inline)) {
+      const float m_use = (m_run == -INFINITY ? 0.f : m_run) - PA_UP;
       auto vread = [&](int j) {  // step j = NC u + c: keys 16 u .., values 32 c ..
         const bf16_t* q = vs + vofs[j % NC % 2] + 16 * (j / NC) * DV + 64 * (j % NC / 2);
         const u32x2 lo = lds_read_tr4(q), hi = lds_read_tr4(q + 8 * DV);
-        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+        return __builtin_bit_cast(f16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
       };
-      bf16x8 kf[PK], vf[PV];
+      bf16x8 kf[PK];
+      f16x8 vf[PV];
+      f32x4 we[4];
 #pragma unroll
       for (int j = 0; j < PK; ++j) kf[j] = kread(kn, j);
+      start(sn, st_n, 1 - h, any);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sn[e] = 0.f;
+      for (int g = 0; g < 4; ++g)
+        if (any) we[g] = eread(st, 1, h, g);
       u32x4 w[2];
       float l0 = 0.f, l1 = 0.f;
       __builtin_amdgcn_sched_barrier(0);
@@ -249,51 +296,54 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
         for (int e2 = 8 * kk / NKK; e2 < 8 * (kk + 1) / NKK; ++e2) {  // a share of the 8 pairs
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * e2], a.sl2, -m_use));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * e2 + 1], a.sl2, -m_use));
-          l0 += p0;
-          l1 += p1;
-          w[e2 / 4][e2 % 4] = pack2bf(p0, p1);
+          l0 = any ? __builtin_fmaf(p0, we[e2 / 2][2 * e2 % 4], l0) : l0 + p0;
+          l1 = any ? __builtin_fmaf(p1, we[e2 / 2][2 * e2 % 4 + 1], l1) : l1 + p1;
+          w[e2 / 4][e2 % 4] = pack2h(p0, p1);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
       l_run += l0 + l1;
-      const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1])};
+      const f16x8 pf[2] = {__builtin_bit_cast(f16x8, w[0]), __builtin_bit_cast(f16x8, w[1])};
 #pragma unroll
       for (int j = 0; j < 2 * NC; ++j) {
-        acc[j % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % PV], pf[j / NC], acc[j % NC], 0, 0, 0);
+        acc[j % NC] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[j % PV], pf[j / NC], acc[j % NC], 0, 0, 0);
         if (j + PV < 2 * NC) vf[j % PV] = vread(j + PV);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
 
     f32x16 sa, sb;
-    if (kb0 < nvis) {
+    auto run = [&](auto scaled) __attribute__((always_inline)) {
+      if (kb0 < nvis) {
+        start(sa, 0, 0, scaled);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sa[e] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < NKK; ++kk)
-        sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(smem, kk), qf[kk], sa, 0, 0, 0);
-      settle(sa, kb0 * BKV);
-    }
-    for (int kb = kb0; kb < kb1; ++kb) {
-      if (kb + 2 < kb1) issue(kb + 2);
-      if (kb < nvis) {  // (uniform in the wavefront)
-        // stage offsets pass through readfirstlane: opaque to the loop optimiser, which would keep one
-        // induction variable per LDS read
-        const int cur = __builtin_amdgcn_readfirstlane((kb - kb0) % NST * STAGE);
-        const int nxt = __builtin_amdgcn_readfirstlane((kb + 1 - kb0) % NST * STAGE);
-        const bf16_t* vs = smem + cur + KS::ELEMS;
-        step(smem + cur + 32 * DQK, vs, sa, sb);
-        if (kb * BKV + 32 <= qw0 + 31 + diag) {  // the second half is not all behind the diagonal
-          settle(sb, kb * BKV + 32);
-          // (past the last tile the next logits come from a stale stage and are not used)
-          step(smem + nxt, vs + 32 * DV, sb, sa);
-          if (kb + 1 < nvis) settle(sa, (kb + 1) * BKV);
-        }
+        for (int kk = 0; kk < NKK; ++kk)
+          sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(smem, kk), qf[kk], sa, 0, 0, 0);
+        settle(sa, kb0 * BKV);
       }
-      // tile kb + 2 has landed and nobody reads tile kb's stage any more
-      wait_all();
-      __syncthreads();
-    }
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (kb + 2 < kb1) issue(kb + 2);
+        if (kb < nvis) {  // (uniform in the wavefront)
+          // stage offsets pass through readfirstlane: opaque to the loop optimiser, which would keep one
+          // induction variable per LDS read
+          const int st = (kb - kb0) % NST, st_n = (kb + 1 - kb0) % NST;
+          const int cur = __builtin_amdgcn_readfirstlane(st * STAGE), nxt = __builtin_amdgcn_readfirstlane(st_n * STAGE);
+          const bf16_t* vs = smem + cur + KS::ELEMS;
+          step(smem + cur + 32 * DQK, vs, sa, sb, st, 0, st, scaled);
+          if (kb * BKV + 32 <= qw0 + 31 + diag) {  // the second half is not all behind the diagonal
+            settle(sb, kb * BKV + 32);
+            // (past the last tile the next logits come from a stale stage and are not used)
+            step(smem + nxt, vs + 32 * DV, sb, sa, st, 1, st_n, scaled);
+            if (kb + 1 < nvis) settle(sa, (kb + 1) * BKV);
+          }
+        }
+        // tile kb + 2 has landed and nobody reads tile kb's stage any more
+        wait_all();
+        __syncthreads();
+      }
+    };
+    if (any) run(std::true_type{});
+    else run(std::false_type{});
   }
 
   // lane holds query my_q, d = 32 c + 8 g + 4 half + 0..3
@@ -314,14 +364,17 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
         *(f32x4*)(po + 32 * c + 8 * g) =
             f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
   } else {
+    const float* vsc = a.v_scale + (int64_t)(i / a.v_div) * a.v_head + 4 * half;
     const float inv = l == 0.f ? 0.f : 1.f / l;  // (l = 0: a query that sees no key)
     bf16_t* op = a.O + row * a.o_tok + (int64_t)i * DV + 4 * half;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(u32x2*)(op + 32 * c + 8 * g) = u32x2{pack2bf(acc[c][4 * g] * inv, acc[c][4 * g + 1] * inv),
-                                               pack2bf(acc[c][4 * g + 2] * inv, acc[c][4 * g + 3] * inv)};
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]} * inv *
+                        *(const f32x4*)(vsc + 32 * c + 8 * g);
+        *(u32x2*)(op + 32 * c + 8 * g) = u32x2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+      }
   }
 }
 
@@ -344,7 +397,7 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedDev a, int 
     L += ml[1] * w;
     v += *(const f32x4*)(a.part_o + (at + z * stride) * dv + d) * w;
   }
-  v *= L == 0.f ? 0.f : 1.f / L;
+  v *= (L == 0.f ? 0.f : 1.f / L) * *(const f32x4*)(a.v_scale + (int64_t)(i / a.v_div) * a.v_head + d);
   *(u32x2*)(a.O + row * a.o_tok + (int64_t)i * dv + d) = u32x2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
 }
 
@@ -387,6 +440,7 @@ hipError_t attn_fwd_packed(const AttnPacked& a, hipStream_t s) {
   d.Q = (const bf16_t*)a.Q.p; d.q_tok = a.Q.tok; d.q_head = (int)a.Q.head;
   d.Ka = (const bf16_t*)a.Ka.p; d.ka_tok = a.Ka.tok; d.ka_head = (int)a.Ka.head; d.ka_div = a.Ka.div;
   d.Kb = (const bf16_t*)a.Kb.p; d.kb_tok = a.Kb.tok; d.kb_head = (int)a.Kb.head; d.kb_div = a.Kb.div;
+  d.key_exp = a.key_exp; d.v_scale = a.v_scale; d.bias = 1.f / d.sl2;
   d.V = (const bf16_t*)a.V.p; d.v_tok = a.V.tok; d.v_head = (int)a.V.head; d.v_div = a.V.div;
   d.O = (bf16_t*)a.O; d.o_tok = a.o_tok;
   d.q_off = a.q_off; d.kv_off = a.kv_off; d.n_q = a.n_q; d.n_kv = a.n_kv;

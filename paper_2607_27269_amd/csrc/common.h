@@ -35,6 +35,13 @@ __device__ __forceinline__ uint32_t pack2bf(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, b);
 }
 
+// two floats -> packed fp16 pair (lo in bits 0..15), round to nearest even
+__device__ __forceinline__ uint32_t pack2h(float lo, float hi) {
+  typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+  const f32x2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+
 // max / sum of x over the lane pair (l, l ^ 32), from gfx950's v_permlane32_swap (swaps
 // the upper half of one register with the lower half of another: with x in both, each lane
 // then holds its own value and its partner's) - no LDS round trip

@@ -79,6 +79,7 @@ struct GemmDev {
   // with the strides above, column n - split_n
   int split_n;
   bf16_t* c_lo; int64_t ldc_lo, sC1_lo, sC2_lo;
+  int half = 0;       // mix16_t outputs: fp16
 };
 
 // row stride (elements) of an m-major [k][ROWS] tile, read only through the transposing
@@ -362,24 +363,38 @@ struct Loader<false, ROWS, NTHR, BK, true> {
   }
 };
 
+// An output of 16 bits, bf16 or (`half`) fp16 as its product asks; NT products with beta = 0 only.
+struct mix16_t { uint16_t v; };
+template <typename TC> constexpr bool is_mix16 = false;
+template <> constexpr bool is_mix16<mix16_t> = true;
+
 template <typename TC>
-__device__ __forceinline__ void store_out(TC* p, float v);
+__device__ __forceinline__ void store_out(TC* p, float v, bool half);
 template <>
-__device__ __forceinline__ void store_out<float>(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_out<float>(float* p, float v, bool) { *p = v; }
 template <>
-__device__ __forceinline__ void store_out<bf16_t>(bf16_t* p, float v) { *p = f2bf(v); }
+__device__ __forceinline__ void store_out<bf16_t>(bf16_t* p, float v, bool) { *p = f2bf(v); }
+template <>
+__device__ __forceinline__ void store_out<mix16_t>(mix16_t* p, float v, bool half) {
+  p->v = half ? (uint16_t)pack2h(v, v) : (uint16_t)f2bf(v);
+}
 
 // four consecutive outputs: alpha * v + beta * C
 template <typename TC>
-__device__ __forceinline__ void store4(TC* p, f32x4 v, float alpha, float beta);
+__device__ __forceinline__ void store4(TC* p, f32x4 v, float alpha, float beta, bool half);
 template <>
-__device__ __forceinline__ void store4<float>(float* p, f32x4 v, float alpha, float beta) {
+__device__ __forceinline__ void store4<mix16_t>(mix16_t* p, f32x4 v, float alpha, float, bool half) {
+  const f32x4 o = v * alpha;
+  *(u32x2*)p = half ? u32x2{pack2h(o[0], o[1]), pack2h(o[2], o[3])} : u32x2{pack2bf(o[0], o[1]), pack2bf(o[2], o[3])};
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* p, f32x4 v, float alpha, float beta, bool) {
   f32x4 o = v * alpha;
   if (beta != 0.f) o += beta * *(const f32x4*)p;
   *(f32x4*)p = o;
 }
 template <>
-__device__ __forceinline__ void store4<bf16_t>(bf16_t* p, f32x4 v, float alpha, float beta) {
+__device__ __forceinline__ void store4<bf16_t>(bf16_t* p, f32x4 v, float alpha, float beta, bool) {
   f32x4 o = v * alpha;
   if (beta != 0.f) {
     const u32x2 c = *(const u32x2*)p;
@@ -650,12 +665,14 @@ __device__ __forceinline__ void gemm_tile(const GemmDev& g, int wg, int split) {
         }
         TC* p = C + (int64_t)m * g.ldc + n;
         if (vec && n + 4 <= g.N) {
-          store4<TC>(p, v, g.alpha, WB ? g.beta : 0.f);
+          store4<TC>(p, v, g.alpha, WB ? g.beta : 0.f, g.half);
         } else {
           for (int q = 0; q < 4 && n + q < g.N; ++q) {
             float x = g.alpha * v[q];
-            if (WB && g.beta != 0.f) x += g.beta * ld(p + q);
-            store_out<TC>(p + q, x);
+            if constexpr (!is_mix16<TC>) {
+              if (WB && g.beta != 0.f) x += g.beta * ld(p + q);
+            }
+            store_out<TC>(p + q, x, g.half);
           }
         }
       }
@@ -963,12 +980,14 @@ __device__ __forceinline__ void gemm_persist(const GemmDev& g) {
             }
             TC* p = C + cur.coff + (int64_t)m * g.ldc + n;
             if (vec && n + 4 <= g.N) {
-              store4<TC>(p, v, g.alpha, WB ? g.beta : 0.f);
+              store4<TC>(p, v, g.alpha, WB ? g.beta : 0.f, g.half);
             } else {
               for (int q = 0; q < 4 && n + q < g.N; ++q) {
                 float x = g.alpha * v[q];
-                if (WB && g.beta != 0.f) x += g.beta * ld(p + q);
-                store_out<TC>(p + q, x);
+                if constexpr (!is_mix16<TC>) {
+                  if (WB && g.beta != 0.f) x += g.beta * ld(p + q);
+                }
+                store_out<TC>(p + q, x, g.half);
               }
             }
           }
@@ -1095,7 +1114,7 @@ __global__ __launch_bounds__(64 * WM * WN) void attn_ds_gemm_kernel(GemmDev g) {
   [a0] "v"(cu[0]), [a1] "v"(cu[1]), [a2] "v"(cu[2]), [a3] "v"(cu[3]), [b0] "v"(cu[4]),      \
   [b1] "v"(cu[5]), [b2] "v"(cu[6]), [ra] "v"(ra), [rb] "v"(rb)
 
-// Several products of one A (the same rows, K and row strides): column tiles run over the
+// Several products of one A (the same rows, K and row strides; mix16_t outputs: of alike ones): column tiles run over the
 // outputs of the first product, then of the second, .. (g.N, g.B, g.C, g.ldc are not used)
 struct Nt4Group {
   int n;
@@ -1104,6 +1123,9 @@ struct Nt4Group {
   const bf16_t* B[GROUP_MAX];
   void* C[GROUP_MAX];
   int64_t ldc[GROUP_MAX];
+  // mix16_t outputs: an A of its own (same rows, K and row stride) and fp16 or bf16
+  const bf16_t* A[GROUP_MAX];
+  int half[GROUP_MAX];
 };
 
 template <int BN, typename TC, bool SHIFT, bool GROUP>
@@ -1148,6 +1170,7 @@ __device__ __forceinline__ void gemm_nt4(const GemmDev& g, const Nt4Group& gr) {
     m0 = SHIFT ? min(mlo, g.M - BM) : mlo;
     n0 = SHIFT ? min(nlo, (GROUP ? gr.N[pi] : g.N) - BN) : nlo;
   };
+  auto a_of = [&](int pi) { return GROUP && is_mix16<TC> ? gr.A[pi] : g.A; };
   auto b_of = [&](int pi) { return GROUP ? gr.B[pi] : g.B; };
   typename LA::Dma da;
   typename LB::Dma db;
@@ -1178,7 +1201,7 @@ __device__ __forceinline__ void gemm_nt4(const GemmDev& g, const Nt4Group& gr) {
   const int nk = g.ktotal / BKK;  // even
   int m0, n0, mlo, nlo, pi, nm0 = 0, nn0 = 0, nmlo = 0, nnlo = 0, npi = 0;
   tile_of(w, m0, n0, mlo, nlo, pi);
-  const bf16_t* baseA = g.A + (int64_t)m0 * g.lda;
+  const bf16_t* baseA = a_of(pi) + (int64_t)m0 * g.lda;
   const bf16_t* baseB = b_of(pi) + (int64_t)n0 * g.ldb;
   int wnext = w + G;
   bool has_next = wnext < ntiles;
@@ -1186,7 +1209,7 @@ __device__ __forceinline__ void gemm_nt4(const GemmDev& g, const Nt4Group& gr) {
   const bf16_t* nbaseB = baseB;
   if (has_next) {
     tile_of(wnext, nm0, nn0, nmlo, nnlo, npi);
-    nbaseA = g.A + (int64_t)nm0 * g.lda;
+    nbaseA = a_of(npi) + (int64_t)nm0 * g.lda;
     nbaseB = b_of(npi) + (int64_t)nn0 * g.ldb;
   }
   f32x16 acc[TM][TN];
@@ -1355,7 +1378,7 @@ __device__ __forceinline__ void gemm_nt4(const GemmDev& g, const Nt4Group& gr) {
               const f32x4 so = o * lsc;  // masked rows exactly 0 (also where o is not finite)
               o = f32x4{keep ? so[0] : 0.f, keep ? so[1] : 0.f, keep ? so[2] : 0.f, keep ? so[3] : 0.f};
             }
-            if (!SHIFT || (m >= mlo && n >= nlo)) store4<TC>(C + (int64_t)m * ldc + n, o, g.alpha, WB ? g.beta : 0.f);
+            if (!SHIFT || (m >= mlo && n >= nlo)) store4<TC>(C + (int64_t)m * ldc + n, o, g.alpha, WB ? g.beta : 0.f, GROUP && is_mix16<TC> ? gr.half[pi] != 0 : g.half != 0);
           }
         }
       }
@@ -1382,7 +1405,7 @@ __device__ __forceinline__ void gemm_nt4(const GemmDev& g, const Nt4Group& gr) {
     has_next = wnext < ntiles;
     if (has_next) {
       tile_of(wnext, nm0, nn0, nmlo, nnlo, npi);
-      nbaseA = g.A + (int64_t)nm0 * g.lda;
+      nbaseA = a_of(npi) + (int64_t)nm0 * g.lda;
       nbaseB = b_of(npi) + (int64_t)nn0 * g.ldb;
     }
   }
@@ -1404,7 +1427,7 @@ void gemm_nt4_group_kernel(GemmDev g, Nt4Group gr) {
 template <typename TC>
 __global__ void splitk_reduce_kernel(const float* __restrict__ part, int splits, int64_t sstride,
                                      int M, int N, TC* __restrict__ C, int64_t ldc, float alpha,
-                                     float beta) {
+                                     float beta, bool half) {
   int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   int64_t total = (int64_t)M * N;
   if (idx >= total) return;
@@ -1413,8 +1436,10 @@ __global__ void splitk_reduce_kernel(const float* __restrict__ part, int splits,
   for (int z = 0; z < splits; ++z) s += part[(int64_t)z * sstride + idx];
   TC* c = C + (int64_t)m * ldc + n;
   float v = alpha * s;
-  if (beta != 0.f) v += beta * ld(c);
-  store_out<TC>(c, v);
+  if constexpr (!is_mix16<TC>) {
+    if (beta != 0.f) v += beta * ld(c);
+  }
+  store_out<TC>(c, v, half);
 }
 
 // the same, four consecutive outputs per thread (N and ldc multiples of 4), for several sums
@@ -1425,6 +1450,7 @@ struct SumDev {
   void* C;
   int splits, N;
   float alpha, beta;
+  bool half;
 };
 constexpr int SUM_MAX = GROUP_MAX + 1;
 struct SumGroup {
@@ -1442,7 +1468,7 @@ __global__ __launch_bounds__(256) void splitk_reduce4_kernel(SumGroup gr) {
   const int64_t m = idx / d.N;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int z = 0; z < d.splits; ++z) acc += *(const f32x4*)(d.part + z * d.sstride + idx);
-  store4<TC>((TC*)d.C + m * d.ldc + (idx - m * d.N), acc, d.alpha, d.beta);
+  store4<TC>((TC*)d.C + m * d.ldc + (idx - m * d.N), acc, d.alpha, d.beta, d.half);
 }
 
 // Tile shape and split-K factor.
@@ -1571,6 +1597,7 @@ int reserved_splits(const Gemm& g) {
   return best;
 }
 
+#define TC_NAME (sizeof(TC) == 4 ? "fp32" : is_mix16<TC> ? "16 bits" : "bf16")
 template <bool AK, bool BKM, typename TC>
 const char* launch(const GemmDev& d, const Plan& p, hipStream_t s) {
   const int tiles = ((d.M + p.bm - 1) / p.bm) * ((d.N + p.bn - 1) / p.bn);
@@ -1580,17 +1607,17 @@ const char* launch(const GemmDev& d, const Plan& p, hipStream_t s) {
     if (p.kind == TNT256) {
       if (whole) gemm_nt4_persist_kernel<256, TC, false><<<nt_grid, 256, 0, s>>>(d);
       else gemm_nt4_persist_kernel<256, TC, true><<<nt_grid, 256, 0, s>>>(d);
-      return KLABEL("gemm_nt4_persist_kernel<256,256,NT,%s>", sizeof(TC) == 4 ? "fp32" : "bf16");
+      return KLABEL("gemm_nt4_persist_kernel<256,256,NT,%s>", TC_NAME);
     }
     if (p.kind == TNT192) {
       if (whole) gemm_nt4_persist_kernel<192, TC, false><<<nt_grid, 256, 0, s>>>(d);
       else gemm_nt4_persist_kernel<192, TC, true><<<nt_grid, 256, 0, s>>>(d);
-      return KLABEL("gemm_nt4_persist_kernel<256,192,NT,%s>", sizeof(TC) == 4 ? "fp32" : "bf16");
+      return KLABEL("gemm_nt4_persist_kernel<256,192,NT,%s>", TC_NAME);
     }
   }
   const bool persist = d.lscale == nullptr && p.kind != T64;
 #define GL_(name, bm, bn) KLABEL(name "<%d,%d,%s,%s>", bm, bn, AK ? (BKM ? "NT" : "NN") : "TN", \
-                                 sizeof(TC) == 4 ? "fp32" : "bf16")
+                                 TC_NAME)
   if (persist) {
     GemmDev e = d;
     e.nsplit = p.splits;
@@ -1617,7 +1644,7 @@ const char* launch(const GemmDev& d, const Plan& p, hipStream_t s) {
     gemm_mfma_kernel<64, 64, 2, 2, AK, BKM, TC, 64, 4><<<grid, 256, 0, s>>>(d);
     return GL_("gemm_mfma_kernel", 64, 64);
   }
-  if constexpr (AK && BKM) {
+  if constexpr (AK && BKM && !is_mix16<TC>) {
     if (p.kind == T256) {
       gemm_mfma_kernel<256, 256, GWM, GWN, AK, BKM, TC, GBK, GNST><<<grid, 64 * GWM * GWN, 0, s>>>(d);
       return GL_("gemm_mfma_kernel(masked loss)", 256, 256);
@@ -1648,6 +1675,7 @@ static GemmDev dev_of(const Gemm& g) {
   d.B = (const bf16_t*)g.B; d.ldb = g.ldb;
   d.aligned = ((uintptr_t)g.A | (uintptr_t)g.B) % 16 == 0 && g.lda % 8 == 0 && g.ldb % 8 == 0;
   d.C = g.C; d.ldc = g.ldc; d.alpha = g.alpha; d.beta = g.beta;
+  d.half = g.c_t == DT_F16;
   d.mstore = g.M; d.part = nullptr; d.kchunk = 0;
   d.lscale = nullptr; d.lmask = nullptr; d.lpart = nullptr; d.lref = nullptr; d.ldref = 0;
   d.causal = 0; d.rev = 0; d.nbatch = 1; d.zdiv = 1; d.bdiv = 1; d.kgroups = 1;
@@ -1670,7 +1698,7 @@ static void add_sum(SumGroup& gr, const Gemm& g, const float* part, int splits) 
   auto add = [&](const float* p, int64_t n, void* C, float beta) {
     SumDev& d = gr.s[gr.n];
     d.part = p; d.sstride = total; d.ldc = g.ldc; d.C = C; d.splits = splits; d.N = g.N;
-    d.alpha = g.alpha; d.beta = beta;
+    d.alpha = g.alpha; d.beta = beta; d.half = g.c_t == DT_F16;
     d.end = (gr.n ? gr.s[gr.n - 1].end : 0) + n / 4;
     ++gr.n;
   };
@@ -1682,10 +1710,11 @@ static void add_sum(SumGroup& gr, const Gemm& g, const float* part, int splits) 
     add(part, total, g.C, g.beta);
   }
 }
-static hipError_t run_sums(const SumGroup& gr, bool f32, double bytes, hipStream_t s) {
+static hipError_t run_sums(const SumGroup& gr, DType t, double bytes, hipStream_t s) {
   const unsigned grid = (unsigned)((gr.s[gr.n - 1].end + 255) / 256);
   prof_begin(KC_ELEM, s);
-  if (f32) splitk_reduce4_kernel<float><<<grid, 256, 0, s>>>(gr);
+  if (t == DT_F32) splitk_reduce4_kernel<float><<<grid, 256, 0, s>>>(gr);
+  else if (t == DT_F16) splitk_reduce4_kernel<mix16_t><<<grid, 256, 0, s>>>(gr);
   else splitk_reduce4_kernel<bf16_t><<<grid, 256, 0, s>>>(gr);
   prof_end(KC_ELEM, s, 0.0, bytes, KLABEL("splitk_reduce4_kernel"));
   return hipGetLastError();
@@ -1701,6 +1730,7 @@ hipError_t gemm_mfma(const Gemm& g, float* scratch, size_t scratch_elems, hipStr
   const bool two = g.C2 != nullptr;
   if (!g.a_kmajor && g.b_kmajor) return hipErrorInvalidValue;  // (no such product)
   if (two && (!two_ok(g) || !scratch || scratch_elems < (size_t)g.M * g.N)) return hipErrorInvalidValue;
+  if (g.c_t == DT_F16 && (!g.a_kmajor || !g.b_kmajor || g.beta != 0.f)) return hipErrorInvalidValue;
   const Plan p = plan_of(g, scratch ? scratch_elems : 0, ALL_KINDS);
   d.kchunk = p.kchunk;
   d.part = p.splits > 1 || two ? scratch : nullptr;
@@ -1712,7 +1742,8 @@ hipError_t gemm_mfma(const Gemm& g, float* scratch, size_t scratch_elems, hipStr
     if (f32) kname = launch<AK, BK_, float>(d, p, s);                                   \
     else kname = launch<AK, BK_, bf16_t>(d, p, s);                                      \
   }
-  L_(true, true) else L_(true, false) else L_(false, false)
+  if (g.c_t == DT_F16) kname = launch<true, true, mix16_t>(d, p, s);
+  else L_(true, true) else L_(true, false) else L_(false, false)
 #undef L_
   prof_end(kc, s, flops, bytes, kname);
   hipError_t e = hipGetLastError();
@@ -1722,17 +1753,20 @@ hipError_t gemm_mfma(const Gemm& g, float* scratch, size_t scratch_elems, hipStr
     SumGroup gr;
     gr.n = 0;
     add_sum(gr, g, scratch, p.splits);
-    return run_sums(gr, f32, sum_bytes(g, p.splits), s);
+    return run_sums(gr, g.c_t, sum_bytes(g, p.splits), s);
   }
   const int64_t total = (int64_t)g.M * g.N;
   const unsigned grid = (unsigned)((total + 255) / 256);
   prof_begin(KC_ELEM, s);
   if (f32)
     splitk_reduce_kernel<float><<<grid, 256, 0, s>>>(scratch, p.splits, total, g.M, g.N,
-                                                     (float*)g.C, g.ldc, g.alpha, g.beta);
+                                                     (float*)g.C, g.ldc, g.alpha, g.beta, false);
+  else if (g.c_t == DT_F16)
+    splitk_reduce_kernel<mix16_t><<<grid, 256, 0, s>>>(scratch, p.splits, total, g.M, g.N,
+                                                       (mix16_t*)g.C, g.ldc, g.alpha, g.beta, true);
   else
     splitk_reduce_kernel<bf16_t><<<grid, 256, 0, s>>>(scratch, p.splits, total, g.M, g.N,
-                                                      (bf16_t*)g.C, g.ldc, g.alpha, g.beta);
+                                                      (bf16_t*)g.C, g.ldc, g.alpha, g.beta, false);
   prof_end(KC_ELEM, s, 0.0, sum_bytes(g, p.splits), KLABEL("splitk_reduce_kernel"));
   return hipGetLastError();
 }
@@ -1757,8 +1791,11 @@ hipError_t gemm_mfma_group(const Gemm* g, int n, float* scratch, size_t scratch_
   const size_t room = scratch ? scratch_elems : 0;
   double sep = 0.0;
   int kmax = 1;
+  bool halves = false;  // fp16 outputs, beside bf16 ones
+  for (int i = 0; i < n; ++i) halves = halves || g[i].c_t == DT_F16;
   for (int i = 0; i < n; ++i) {
-    if (g[i].a_kmajor != g[0].a_kmajor || g[i].b_kmajor != g[0].b_kmajor || g[i].c_t != g[0].c_t ||
+    if (g[i].a_kmajor != g[0].a_kmajor || g[i].b_kmajor != g[0].b_kmajor ||
+        (g[i].c_t == DT_F32) != (g[0].c_t == DT_F32) || (halves && (layout != 0 || g[i].beta != 0.f)) ||
         (!g[i].a_kmajor && g[i].b_kmajor) || g[i].M <= 0 || g[i].N <= 0)
       return hipErrorNotSupported;
     if (g[i].C2 ? !two_ok(g[i]) : !sum4_ok(g[i])) return hipErrorNotSupported;
@@ -1813,16 +1850,16 @@ hipError_t gemm_mfma_group(const Gemm* g, int n, float* scratch, size_t scratch_
       }
     }
   }
-  // Large products of one A on the four-wavefront kernel: one grid of tiles instead of a partly
+  // Large products of one A (alike ones for mix16_t outputs) on the four-wavefront kernel: one grid of tiles instead of a partly
   // filled last round of each. Measured against the launches it replaces: Q/K/V of 8192 tokens
   // of the 8B layer 339 us, apart 232 + 85 + 85; the five products of h and the two of c^KV of
   // 6002 tokens of the 4096-wide layer with 32 full heads: the whole step 3050 us, before 3125.
   // The rule is the fitted time: where each product fills its rounds by itself, or is too small
   // for 256-row tiles, the launches apart or the smaller tiles come out cheaper.
   int best_bn = 0;
-  bool same_a = layout == 0 && g[0].c_t == DT_BF16;
+  bool same_a = layout == 0 && g[0].c_t != DT_F32;
   for (int i = 0; i < n; ++i)
-    same_a = same_a && g[i].A == g[0].A && g[i].lda == g[0].lda && g[i].M == g[0].M && g[i].K == g[0].K &&
+    same_a = same_a && (halves || g[i].A == g[0].A) && g[i].lda == g[0].lda && g[i].M == g[0].M && g[i].K == g[0].K &&
              g[i].ldb == g[0].ldb && g[i].alpha == g[0].alpha && g[i].beta == 0.f && !g[i].C2;
   for (int bn = 256; same_a && bn >= 192; bn -= 64) {
     const TileCost& c = TILE_COST[0][bn == 256 ? TNT256 : TNT192];
@@ -1854,11 +1891,21 @@ hipError_t gemm_mfma_group(const Gemm* g, int n, float* scratch, size_t scratch_
       gr.B[i] = (const bf16_t*)g[i].B;
       gr.C[i] = g[i].C;
       gr.ldc[i] = g[i].ldc;
+      gr.A[i] = (const bf16_t*)g[i].A;
+      gr.half[i] = g[i].c_t == DT_F16;
     }
     const GemmDev d = dev_of(g[0]);
     const int grid = std::min(tn * ((g[0].M + 255) / 256), NUM_CU);
     prof_begin(kclass, s);
-    if (best_bn == 256) {
+    if (halves) {
+      if (best_bn == 256) {
+        if (whole) gemm_nt4_group_kernel<256, mix16_t, false><<<grid, 256, 0, s>>>(d, gr);
+        else gemm_nt4_group_kernel<256, mix16_t, true><<<grid, 256, 0, s>>>(d, gr);
+      } else {
+        if (whole) gemm_nt4_group_kernel<192, mix16_t, false><<<grid, 256, 0, s>>>(d, gr);
+        else gemm_nt4_group_kernel<192, mix16_t, true><<<grid, 256, 0, s>>>(d, gr);
+      }
+    } else if (best_bn == 256) {
       if (whole) gemm_nt4_group_kernel<256, bf16_t, false><<<grid, 256, 0, s>>>(d, gr);
       else gemm_nt4_group_kernel<256, bf16_t, true><<<grid, 256, 0, s>>>(d, gr);
     } else {
@@ -1901,14 +1948,14 @@ hipError_t gemm_mfma_group(const Gemm* g, int n, float* scratch, size_t scratch_
     gr.end[i] = wgs;
     gr.p[i] = d;
   }
-  const bool f32 = g[0].c_t == DT_F32;
+  const DType t_out = halves ? DT_F16 : g[0].c_t;
   const char* kname = nullptr;
   prof_begin(kclass, s);
 #define T_(bm_, bn_, nst, AK, BK_, TC)                                                            \
   {                                                                                               \
     gemm_group_kernel<bm_, bn_, nst, AK, BK_, TC><<<wgs, 256, 0, s>>>(gr);                        \
     kname = KLABEL("gemm_group_kernel<%d,%d,%s,%s>", bm_, bn_, AK ? (BK_ ? "NT" : "NN") : "TN",   \
-                   sizeof(TC) == 4 ? "fp32" : "bf16");                                            \
+                   sizeof(TC) == 4 ? "fp32" : is_mix16<TC> ? "16 bits" : "bf16");                 \
   }
 #define L_(AK, BK_, TC)                                                                           \
   {                                                                                               \
@@ -1916,13 +1963,13 @@ hipError_t gemm_mfma_group(const Gemm* g, int n, float* scratch, size_t scratch_
     else if (best_tile == 1) T_(128, 64, 3, AK, BK_, TC)                                          \
     else T_(128, 128, 2, AK, BK_, TC)                                                             \
   }
-  if (layout == 0) L_(true, true, bf16_t) else if (layout == 1) L_(true, false, bf16_t) else L_(false, false, float)
+  if (halves) L_(true, true, mix16_t) else if (layout == 0) L_(true, true, bf16_t) else if (layout == 1) L_(true, false, bf16_t) else L_(false, false, float)
 #undef L_
 #undef T_
   prof_end(kclass, s, flops, bytes, kname);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sums.n == 0) return e;
-  return run_sums(sums, f32, sbytes, s);
+  return run_sums(sums, t_out, sbytes, s);
 }
 
 size_t gemm_mfma_masked_sse_parts(const Gemm& g) {

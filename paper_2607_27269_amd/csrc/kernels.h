@@ -8,8 +8,8 @@
 
 namespace mla {
 
-enum DType { DT_BF16 = 0, DT_F32 = 1 };
-inline size_t dsize(DType t) { return t == DT_BF16 ? 2 : 4; }
+enum DType { DT_BF16 = 0, DT_F32 = 1, DT_F16 = 2 };  // DT_F16: outputs of NT products only
+inline size_t dsize(DType t) { return t == DT_F32 ? 4 : 2; }
 
 // Timing classes: one per kernel family (a GEMM layout, an attention kernel, ...).
 enum KClass {
@@ -336,7 +336,13 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s);
 // shapes; keys and values must be finite where a query that does not see them may meet them.
 struct AttnPacked {
   int B, H, dqk, dnope, dv;
-  HeadView Q, Ka, Kb, V;           // as in Attn
+  HeadView Q, Ka, Kb;              // as in Attn
+  // The values in fp16, each row and each column scaled by a power of two: V holds
+  // v[n][d] 2^-key_exp[n] / v_scale[d] (V.head and V.div give head i's columns, v_scale alike),
+  // magnitudes at most 2^15, |key_exp| at most 64.
+  HeadView V;
+  const float* key_exp;            // [2][n_kv]: key_exp, 2^-key_exp
+  const float* v_scale;
   void* O; int64_t o_tok;
   float scale;
   const int32_t *q_off, *kv_off;

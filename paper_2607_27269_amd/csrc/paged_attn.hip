@@ -730,78 +730,122 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
 // grouped product, attention over the packed sequences.
 namespace {
 
-// The cached rows of all sequences behind one another, a wavefront per row.  Masked keys get P = 0,
-// which keeps a row out of a product only if its values are finite.  So a row that is not finite
-// (or lies on no page) becomes zeros with a NaN positional key: its values and non-positional key
-// are 0 and its logits NaN, for exactly the queries that see it.  So does a row whose finite latent
-// reaches 2^64 and has a value of 2^127 or more (below 2^64 that would take weights of 2^54).
+// The cached rows of all sequences behind one another, and what the products need; a wavefront per row.
+//
+// Values are expanded to fp16, whose 11 bits make their rounding an eighth of bf16's, in a range that
+// fits by scaling with powers of two: row n of the latents by 2^-e[n], e a multiple of 16 in [-64, 64] (0
+// where the row's largest value lies in [2^-8, 2^8), which it is brought to), row d of W_UV to a largest
+// value in [1/8, 1/4) (v_scale[d] undoes it).  A scaled value is then below rkv 2^8 / 4 <= 2^15, and
+// typically above 2^-9, in fp16's normal range.  Both scalings are exact in bf16 but for values that
+// vanish beside a row's largest (2^-100).
+//
+// Masked keys get P = 0, which keeps a row out of a product only if its values are finite.  So a row
+// that is not finite, has a latent of 2^72 or more or lies on no page becomes zeros with a NaN positional
+// key: its values and non-positional key are 0 and its logits NaN, for exactly the queries that see it.
 // Rows of no sequence become zeros.  Bound by memory and, for few rows, by three dependent loads.
-__global__ __launch_bounds__(256) void gather_rows_kernel(PagedPool c, const int32_t* __restrict__ kv_off, int B,
-                                                          int n_kv, int rkv, const bf16_t* __restrict__ Wuv, int nv,
-                                                          bf16_t* __restrict__ out) {
-  const int row = 4 * blockIdx.x + wave_id();
-  if (row >= n_kv) return;
-  const int lane = threadIdx.x & 63, dr = c.width - rkv;
-  bf16_t* dst = out + (int64_t)row * c.width;
+constexpr int GATHER_EXP = 64;  // largest |e|
+constexpr int GATHER_TOP = 127 + GATHER_EXP + 8;  // exponent field of the first latent too large
+struct GatherDev {
+  PagedPool c;
+  const int32_t* kv_off;
+  int B, n_kv, rkv, nv;
+  const bf16_t* Wuv;
+  bf16_t* rows;      // [n_kv][width]
+  bf16_t* lat;       // [n_kv][width], scaled latents (rows as far apart as the rows': products of alike operands)
+  float* key_exp;    // [2][n_kv]: e, 2^-e
+  bf16_t* W;         // [nv][rkv], scaled
+  float* v_scale;    // [nv]
+};
+// the largest exponent field among a lane's 8 values
+__device__ __forceinline__ uint32_t top_exponent(u32x4 v) {
+  uint32_t top = 0u;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) top = max(top, max(v[q] << 16 & 0x7f800000u, v[q] & 0x7f800000u));
+  return top >> 23;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x = max(x, __shfl_xor(x, d, 64));
+  return x;
+}
+// 8 values times 2^k (|k| <= 127; in two steps, as 2^-127 is no normal number)
+__device__ __forceinline__ u32x4 scaled(u32x4 v, int k) {
+  const float f = __uint_as_float((uint32_t)(127 + k / 2) << 23), f2 = __uint_as_float((uint32_t)(127 + k - k / 2) << 23);
+  u32x4 o;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    o[q] = pack2bf(__uint_as_float(v[q] << 16) * f * f2, __uint_as_float(v[q] & 0xffff0000u) * f * f2);
+  return o;
+}
+__global__ __launch_bounds__(256) void gather_rows_kernel(GatherDev a) {
+  const int row = 4 * blockIdx.x + wave_id(), lane = threadIdx.x & 63;
+  const PagedPool& c = a.c;
+  const bool in_lat = 8 * lane < a.rkv;
   const u32x4 zero = {0u, 0u, 0u, 0u};
+  const int rows4 = (a.n_kv + 3) / 4 * 4;
+  if (row >= rows4) {  // a row of W_UV
+    const int e = row - rows4;
+    if (e >= a.nv) return;
+    u32x4 w = zero;
+    if (in_lat) w = *(const u32x4*)(a.Wuv + (int64_t)e * a.rkv + 8 * lane);
+    const int k = max(min(wave_max((int)top_exponent(w)) - 127, 124), -100) + 3;
+    if (in_lat) *(u32x4*)(a.W + (int64_t)e * a.rkv + 8 * lane) = scaled(w, -k);
+    if (lane == 0) a.v_scale[e] = __uint_as_float((uint32_t)(127 + k) << 23);
+    return;
+  }
+  if (row >= a.n_kv) return;
+  const int dr = c.width - a.rkv;
+  bf16_t* dst = a.rows + (int64_t)row * c.width;
   u32x4 lat = zero, pe = zero;
-  const bool in_lat = 8 * lane < rkv, in_pe = 8 * lane < dr;
-  if (row >= kv_off[0] && row < kv_off[B]) {  // (uniform)
-    int lo = 0, hi = B - 1;
+  const bool in_pe = 8 * lane < dr;
+  int top = 0;
+  if (row >= a.kv_off[0] && row < a.kv_off[a.B]) {  // (uniform)
+    int lo = 0, hi = a.B - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (kv_off[mid] <= row) lo = mid;
+      if (a.kv_off[mid] <= row) lo = mid;
       else hi = mid - 1;
     }
-    const int p = row - kv_off[lo], pg = p / c.page_size;
+    const int p = row - a.kv_off[lo], pg = p / c.page_size;
     const int page = p >= 0 && pg < c.max_pages ? c.table[(int64_t)lo * c.max_pages + pg] : -1;
     bool any = page < 0 || page >= c.n_pages;
     if (!any) {
       const bf16_t* src = (const bf16_t*)c.pool + ((int64_t)page * c.page_size + p % c.page_size) * c.width;
       if (in_lat) lat = *(const u32x4*)(src + 8 * lane);
-      if (in_pe) pe = *(const u32x4*)(src + rkv + 8 * lane);
-      uint32_t top = 0u, top_pe = 0u;  // the largest exponents
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        top = max(top, max(lat[q] << 16 & 0x7f800000u, lat[q] & 0x7f800000u));
-        top_pe = max(top_pe, max(pe[q] << 16 & 0x7f800000u, pe[q] & 0x7f800000u));
-      }
-      any = __ballot(max(top, top_pe) == 0x7f800000u) != 0;
-      if (!any && __ballot(top >= (127u + 64u) << 23) != 0) {
-        for (int e = 0; e < nv && !any; ++e) {
-          u32x4 w = zero;
-          if (in_lat) w = *(const u32x4*)(Wuv + (int64_t)e * rkv + 8 * lane);
-          float s = 0.f;
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            s += __uint_as_float(lat[q] << 16) * __uint_as_float(w[q] << 16) +
-                 __uint_as_float(lat[q] & 0xffff0000u) * __uint_as_float(w[q] & 0xffff0000u);
-          any = !(fabsf(warp_sum(s)) < 1.7014118e38f);  // 2^127
-        }
-      }
+      if (in_pe) pe = *(const u32x4*)(src + a.rkv + 8 * lane);
+      top = wave_max((int)top_exponent(lat));
+      any = __ballot(top >= GATHER_TOP || top_exponent(pe) == 255u) != 0;
     }
     if (any) {
       lat = zero;
+      top = 0;
       pe = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
     }
   }
-  if (in_lat) *(u32x4*)(dst + 8 * lane) = lat;
-  if (in_pe) *(u32x4*)(dst + rkv + 8 * lane) = pe;
+  const int e = top == 0 ? 0 : max((top - 127 + 8) >> 4 << 4, -GATHER_EXP);
+  if (in_lat) {
+    *(u32x4*)(dst + 8 * lane) = lat;
+    *(u32x4*)(a.lat + (int64_t)row * c.width + 8 * lane) = scaled(lat, -e);
+  }
+  if (in_pe) *(u32x4*)(dst + a.rkv + 8 * lane) = pe;
+  if (lane < 2) a.key_exp[(int64_t)lane * a.n_kv + row] = lane ? __uint_as_float((uint32_t)(127 - e) << 23) : (float)e;
 }
 
 struct PrefillLayout {
-  size_t rows, keys, vals, split, split_elems, bytes;
+  size_t rows, lat, key_exp, W, v_scale, keys, vals, split, split_elems, bytes;
 };
-Gemm expand(const PrefillPaged& p, const void* rows, const void* W, int n, void* out) {
+Gemm expand(const PrefillPaged& p, const void* rows, const void* W, int n, void* out, DType t) {
   Gemm g;
   g.M = p.n_kv; g.N = n; g.K = p.rkv;
   g.A = rows; g.lda = p.rkv + p.dr; g.a_kmajor = true;
   g.B = W; g.ldb = p.rkv; g.b_kmajor = true;
-  g.C = out; g.ldc = n; g.in_t = DT_BF16; g.c_t = DT_BF16; g.alpha = 1.f; g.beta = 0.f;
+  g.C = out; g.ldc = n; g.in_t = DT_BF16; g.c_t = t; g.alpha = 1.f; g.beta = 0.f;
   return g;
 }
-AttnPacked packed_attention(const PrefillPaged& p, const void* rows, const void* keys, const void* vals) {
+AttnPacked packed_attention(const PrefillPaged& p, const PrefillLayout& l, char* ws) {
+  const void *rows = ws + l.rows, *keys = ws + l.keys, *vals = ws + l.vals;
   AttnPacked a;
+  a.key_exp = (const float*)(ws + l.key_exp); a.v_scale = (const float*)(ws + l.v_scale);
   const int W = p.rkv + p.dr, dqk = p.dn + p.dr, hpg = p.H / p.G;
   const bf16_t* kpe = (const bf16_t*)rows + p.rkv;
   a.B = p.B; a.H = p.H; a.dqk = dqk; a.dv = p.dv;
@@ -811,22 +855,27 @@ AttnPacked packed_attention(const PrefillPaged& p, const void* rows, const void*
   a.Kb = HeadView{kpe, W, 0, p.H};
   a.V = HeadView{vals, (int64_t)p.G * p.dv, p.dv, hpg};
   a.O = p.o; a.o_tok = (int64_t)p.H * p.dv; a.scale = p.scale;
-  a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv; a.ws = nullptr;
+  a.q_off = p.q_off; a.kv_off = p.kv_off; a.n_q = p.n_q; a.n_kv = p.n_kv;
+  a.ws = ws + l.split;  // (the products' partials are done with)
   return a;
 }
 PrefillLayout prefill_layout(const PrefillPaged& p) {
   PrefillLayout l;
   l.rows = 0;
-  l.keys = l.rows + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
+  l.lat = l.rows + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
+  l.key_exp = l.lat + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
+  l.W = l.key_exp + al((size_t)p.n_kv * 8);
+  l.v_scale = l.W + al((size_t)p.G * p.dv * p.rkv * 2);
+  l.keys = l.v_scale + al((size_t)p.G * p.dv * 4);
   l.vals = l.keys + al((size_t)p.n_kv * p.G * p.dn * 2);
-  l.split = l.vals + al((size_t)p.n_kv * p.G * p.dv * 2);
   l.split_elems = 0;  // partials of the products
   if (p.n_kv > 0) {
-    if (p.dn > 0) l.split_elems = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dn, nullptr));
-    const size_t v = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dv, nullptr));
+    if (p.dn > 0) l.split_elems = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dn, nullptr, DT_BF16));
+    const size_t v = gemm_scratch_elems(expand(p, nullptr, nullptr, p.G * p.dv, nullptr, DT_F16));
     if (v > l.split_elems) l.split_elems = v;
   }
-  const size_t parts = attn_packed_ws_bytes(packed_attention(p, nullptr, nullptr, nullptr));
+  l.split = l.vals + al((size_t)p.n_kv * p.G * p.dv * 2);
+  const size_t parts = attn_packed_ws_bytes(packed_attention(p, l, nullptr));
   l.bytes = l.split + al(l.split_elems * 4 > parts ? l.split_elems * 4 : parts);
   return l;
 }
@@ -841,23 +890,23 @@ size_t prefill_paged_ws_bytes(const PrefillPaged& p) {
 hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
   const PrefillLayout l = prefill_layout(p);
   char* ws = (char*)p.ws;
-  void *rows = ws + l.rows, *keys = ws + l.keys, *vals = ws + l.vals;
   const int W = p.rkv + p.dr, nk = p.G * p.dn, nv = p.G * p.dv;
+  prof_begin(KC_ELEM, s);
+  GatherDev g;
+  g.c = p.c; g.kv_off = p.kv_off; g.B = p.B; g.n_kv = p.n_kv; g.rkv = p.rkv; g.nv = nv;
+  g.Wuv = (const bf16_t*)p.Wuv; g.rows = (bf16_t*)(ws + l.rows); g.lat = (bf16_t*)(ws + l.lat);
+  g.key_exp = (float*)(ws + l.key_exp); g.W = (bf16_t*)(ws + l.W); g.v_scale = (float*)(ws + l.v_scale);
+  gather_rows_kernel<<<(p.n_kv + 3) / 4 + (nv + 3) / 4, 256, 0, s>>>(g);
+  prof_end(KC_ELEM, s, 0.0, ((double)p.n_kv * (2 * W + p.rkv) + 2.0 * nv * p.rkv) * 2, KLABEL("gather_rows_kernel"));
   if (p.n_kv > 0) {
-    prof_begin(KC_ELEM, s);
-    gather_rows_kernel<<<(p.n_kv + 3) / 4, 256, 0, s>>>(p.c, p.kv_off, p.B, p.n_kv, p.rkv, (const bf16_t*)p.Wuv, nv,
-                                                        (bf16_t*)rows);
-    prof_end(KC_ELEM, s, 0.0, (double)p.n_kv * W * 4, KLABEL("gather_rows_kernel"));
     Gemm up[2];
     int n = 0;
-    if (p.dn > 0) up[n++] = expand(p, rows, p.Wuk, nk, keys);
-    up[n++] = expand(p, rows, p.Wuv, nv, vals);
+    if (p.dn > 0) up[n++] = expand(p, ws + l.rows, p.Wuk, nk, ws + l.keys, DT_BF16);
+    up[n++] = expand(p, ws + l.lat, ws + l.W, nv, ws + l.vals, DT_F16);
     const hipError_t e = gemm_group(up, n, (float*)(ws + l.split), l.split_elems, s);
     if (e != hipSuccess) return e;
   }
-  AttnPacked a = packed_attention(p, rows, keys, vals);
-  a.ws = ws + l.split;  // (the products' partials are done with)
-  return attn_fwd_packed(a, s);
+  return attn_fwd_packed(packed_attention(p, l, ws), s);
 }
 
 }  // namespace mla

@@ -488,6 +488,48 @@ def test_prefill_replays_in_a_graph():
         check_prefill(lay, q, offsets(new), kv, got)
 
 
+@pytest.mark.parametrize("name,new,kv,order", [("8b", [130], [300], 1), ("1b", [200], [200], -1), ("05b", [90, 40], [90, 170], 0),
+                                               ("05b", [20], [4500], 0)])
+def test_prefill_rows_and_weights_of_any_magnitude(name, new, kv, order):
+    """Latents from 2^-69 to 2^69 side by side (ascending, descending or mixed) and rows of W_UV from 2^-40
+    to 2^40: every output to its own precision.  The non-positional queries are 0, so that the logits stay
+    of ordinary size."""
+    print(f"[paged] prefill {name} magnitudes {order}", flush=True)
+    lay = Layer(shape(name), kv, 16, seed=50 + order, poison=False)
+    rkv = lay.cfg.kv_rank
+    for b, n in enumerate(kv):
+        k = lay.rng.choice([-69, -40, -20, -9, 0, 0, 0, 9, 31, 69], n)
+        k = np.sort(k)[::order] if order else k
+        for p in range(n):
+            lay.pool[lay.table[b, p // 16], p % 16, :rkv] *= 2.0 ** k[p]
+    w = 2.0 ** lay.rng.integers(-40, 41, len(lay.Wuv))
+    lay.Wuv = lay.Wuv * w[:, None]
+    lay.upload()
+    q, q_off = lay.queries(sum(new)), offsets(new)
+    q[..., :lay.cfg.nope_dim] = 0
+    got = Prefill(lay, q, q_off, offsets(kv))().double().cpu().numpy()
+    w = np.repeat(w.reshape(lay.cfg.s_kv_groups, -1), lay.cfg.n_heads // lay.cfg.s_kv_groups, axis=0)
+    for b, n in enumerate(kv):
+        lo, hi = int(q_off[b]), int(q_off[b + 1])
+        ref = lay.oracle(q[lo:hi], b, n, n - (hi - lo))
+        for t in range(lo, hi):
+            e = np.linalg.norm((got[t] - ref[t - lo]) / w) / np.linalg.norm(ref[t - lo] / w)
+            assert e <= REL, (b, t, e)
+
+
+def test_prefill_latents_too_large_are_nan_for_the_queries_that_see_them():
+    lay = Layer(shape("05b"), [60], 16, seed=55)
+    lay.pool[lay.table[0, 2], 3, 5] = 2.0 ** 73              # position 35
+    lay.upload()
+    q = lay.queries(60)
+    got = Prefill(lay, q, offsets([60]), offsets([60]))().float().cpu().numpy()
+    assert np.isnan(got[35:]).all()
+    check_prefill(lay, q, offsets([35]), [35], Prefill(lay, q[:35], offsets([35]), offsets([35]))())
+    ref = lay.oracle(q[:35], 0, 35, 0)
+    for t in range(35):
+        assert np.linalg.norm(got[t] - ref[t]) <= REL * np.linalg.norm(ref[t]), t
+
+
 def test_prefill_without_cached_rows():
     """Sequences without rows (their queries see nothing), no cached rows at all."""
     lay = Layer(shape("8b"), [0, 0], 16, seed=35)

@@ -121,3 +121,10 @@ def test_copy_refusals():
     refused(L.MLA_ERR_INVALID_ARG, L.mla_recon_cache_copy_pages, 256, 1, 0, 10, 1024, None, -1, None)
     # nothing to copy: no launch
     L.mla_recon_cache_copy_pages(256, 1, 0, 10, 1024, None, 0, None)
+
+
+def test_prefill_scale_too_small_is_refused():
+    cfg = L.make_cfg(configs.get(1).replace(batch=2, seq=1))
+    cfg.softmax_scale = 1e-31
+    assert L.mla_recon_prefill_paged_workspace_size(cfg, 4, 4) == 0
+    assert "softmax_scale" in L.last_error()
