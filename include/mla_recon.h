@@ -355,7 +355,8 @@ int mla_recon_decode_paged(const mla_recon_cfg *cfg, const void *q, const mla_pa
  * cheaper call).  A row that is not finite (or one with a latent of 2^72 or more) makes the outputs of
  * the queries that see it NaN and leaves all others as they are; rows whose largest latent is below
  * 2^-72 lose precision, and W_UV is to be below 2^124.  n_q and n_kv at most 1048576, n_heads (n_q / 256 + batch) below 2^23,
- * softmax_scale at least 1e-30.
+ * softmax_scale at least 1e-30, (d_nope + d_rope, d_k) one of (64, 64), (96, 64), (128, 64),
+ * (128, 128), (192, 128).
  * q, Wuv, o and ws 16-byte aligned, ws of mla_recon_prefill_paged_workspace_size bytes. */
 size_t mla_recon_prefill_paged_workspace_size(const mla_recon_cfg *cfg, int32_t n_q, int32_t n_kv);
 int mla_recon_prefill_paged(const mla_recon_cfg *cfg, const void *q, int32_t n_q,

@@ -433,6 +433,13 @@ def test_prefill_without_non_positional_keys():
     check_prefill(lay, q, q_off, kv, Prefill(lay, q, q_off, offsets(kv))())
 
 
+def test_prefill_without_non_positional_keys_long():
+    new, kv = [60, 1], [2900, 333]
+    lay = Layer(shape("1b", nope_dim=0), kv, 64, seed=37)
+    q, q_off = lay.queries(sum(new)), offsets(new)
+    check_prefill(lay, q, q_off, kv, Prefill(lay, q, q_off, offsets(kv))())
+
+
 def test_prefill_padded_batch_leaves_rows_of_no_sequence():
     """Rows before the first and behind the last sequence, room for more cached rows than there are."""
     new, kv = [50, 20], [50, 64]

@@ -128,3 +128,9 @@ def test_prefill_scale_too_small_is_refused():
     cfg.softmax_scale = 1e-31
     assert L.mla_recon_prefill_paged_workspace_size(cfg, 4, 4) == 0
     assert "softmax_scale" in L.last_error()
+
+
+def test_prefill_head_widths_without_a_kernel_are_refused():
+    cfg = L.make_cfg(configs.get(3).replace(batch=2, seq=1, nope_dim=0))      # keys of 64, values of 128
+    assert L.mla_recon_prefill_paged_workspace_size(cfg, 4, 4) == 0
+    assert "not supported" in L.last_error()
