@@ -25,9 +25,13 @@
 // The values and the probabilities are fp16 operands: with bf16 ones their two roundings were most of
 // the output's squared error (2.9e-3 of its norm; 2.0 to 2.2e-3 now), at the same rate.  fp16 has the range for it because each
 // row of values is scaled by a power of two 2^-e[n] and each column by another.  The row's goes into the
-// exponent: with x' = x + e[n], P' = 2^(x' - m) is the weight of the scaled row, and P' 2^-e[n] = 2^(x - m)
-// enters the sum, m the reference maximum of x'.  |e| <= 64 keeps both in fp32's range.  P' is at most
-// 2^(PA_SLACK + PA_UP), and what fp16 cannot hold lies 2^-(24 + PA_UP) below a row's largest.  Keys whose e are
+// exponent: with x' = x + e[n], P' = 2^(x' - m) is the weight of the scaled row, m the reference maximum
+// of x'.  P' is at most 2^(PA_SLACK + PA_UP), and what fp16 cannot hold lies 2^-(24 + PA_UP) below a row's
+// largest.  The sum's terms are 2^(x - m), by an exponential of their own: P' 2^-e[n] would be 0 for rows of
+// small latents under a reference that rows of large ones set, where P' is below fp32's range and the term is
+// not.  As |e| <= 64, the row at the reference keeps the sum above 2^(PA_UP - 64), and no term exceeds
+// 2^(PA_UP + PA_SLACK + 64); the reference may move by more than 2^126 at once, so the sum is scaled by two
+// factors.  Keys whose e are
 // all 0 (any cache with latents of ordinary size) take a loop without them: 120 us against 130 for the 6
 // ragged sequences of up to 2048 tokens and 32 heads below.
 //
@@ -54,7 +58,7 @@ struct PackedDev {
   const bf16_t* Ka; int64_t ka_tok; int ka_head; int ka_div;
   const bf16_t* Kb; int64_t kb_tok; int kb_head; int kb_div;
   const bf16_t* V; int64_t v_tok; int v_head; int v_div;  // (fp16: copied as 16-bit values)
-  const float *key_exp, *v_scale;
+  const float *key_exp, *v_scale;  // e of each key, the factor of each column of values
   float bias;  // 1 / sl2
   bf16_t* O; int64_t o_tok;
   const int32_t *q_off, *kv_off;
@@ -80,6 +84,11 @@ struct ValueSwz {
   static_assert(D == 64 || D == 128, "row stride in banks");
   __device__ __forceinline__ static int swz(int r) { return D == 128 ? (r & 3) << 1 : (r >> 1 & 1) << 1; }
 };
+
+// x 2^d, d <= 0, by two factors: one alone is 0 below 2^-126, the product may not be
+__device__ __forceinline__ float scaled_down(float x, float d) {
+  return x * __builtin_amdgcn_exp2f(fmaxf(d, -126.f)) * __builtin_amdgcn_exp2f(fminf(d + 126.f, 0.f));
+}
 
 // 64 values of 4 bytes from the lanes' addresses to consecutive LDS words
 __device__ __forceinline__ void dma4(const float* src, float* lds) {
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
   constexpr int NKK = DQK / 16, NC = DV / 32, BQH = PA_BQ / HG;
   constexpr int PK = 4, PV = 4;  // operand reads in flight ahead of the products
   __shared__ __attribute__((aligned(1024))) bf16_t smem[NST * STAGE];
-  __shared__ __attribute__((aligned(256))) float kexp[NST][2][BKV];  // e, and 2^-e
+  __shared__ __attribute__((aligned(256))) float kexp[NST][BKV];  // e
 
   const int pid = xcd_remap(blockIdx.x, gridDim.x);
   const int z = SPLIT ? pid % a.nsplit : 0, tile = SPLIT ? pid / a.nsplit : pid;
@@ -201,7 +210,7 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       bf16_t* st = smem + (kb - kb0) % NST * STAGE;
       kst.next(st, kb * BKV, Tk - 1);
       vst.next(st + KS::ELEMS, kb * BKV, Tk - 1);
-      if (wave < 2) dma4(a.key_exp + (int64_t)wave * a.n_kv + ks + min(kb * BKV + lane, Tk - 1), kexp[(kb - kb0) % NST][wave]);
+      if (wave == 0) dma4(a.key_exp + ks + min(kb * BKV + lane, Tk - 1), kexp[(kb - kb0) % NST]);
     };
     issue(kb0);
     if (kb0 + 1 < kb1) issue(kb0 + 1);
@@ -236,20 +245,20 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       return *(const bf16x8*)(kt + kofs[kk % NKB] + 16 * NKB * (kk / NKB));
     };
 
-    // e (w = 0) or 2^-e (w = 1) of keys 8 g + 4 half + 0..3 (+ 32 h) of a stage
-    auto eread = [&](int st, int w, int h, int g) { return *(const f32x4*)&kexp[st][w][32 * h + 8 * g + 4 * half]; };
+    // e of keys 8 g + 4 half + 0..3 (+ 32 h) of a stage
+    auto eread = [&](int st, int h, int g) { return *(const f32x4*)&kexp[st][32 * h + 8 * g + 4 * half]; };
     // a logit accumulator starts at e / sl2
     auto start = [&](f32x16& s, int st, int h, auto any) __attribute__((always_inline)) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         f32x4 e = {0.f, 0.f, 0.f, 0.f};
-        if (any) e = eread(st, 0, h, g) * a.bias;
+        if (any) e = eread(st, h, g) * a.bias;
 #pragma unroll
         for (int q = 0; q < 4; ++q) s[4 * g + q] = e[q];
       }
     };
     // the logits s of keys j0 .. j0 + 31: masked, and the reference moved if they need it
-    auto settle = [&](f32x16& s, int j0) __attribute__((always_inline)) {
+    auto settle = [&](f32x16& s, int j0, auto any) __attribute__((always_inline)) {
       if (j0 + 31 > qw0 + diag) {
         asm volatile("");  // (a real branch)
 #pragma unroll
@@ -262,9 +271,9 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       mx = pair_max32(mx) * a.sl2;
       if (__ballot(mx > m_run + PA_SLACK) != 0) {
         const float m_new = fmaxf(m_run, mx);
-        const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        const float d = m_run - (m_new == -INFINITY ? 0.f : m_new), corr = __builtin_amdgcn_exp2f(d);
         m_run = m_new;
-        l_run *= corr;
+        l_run = any ? scaled_down(l_run, d) : l_run * corr;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -282,13 +291,13 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
       };
       bf16x8 kf[PK];
       f16x8 vf[PV];
-      f32x4 we[4];
+      f32x4 ke[4];
 #pragma unroll
       for (int j = 0; j < PK; ++j) kf[j] = kread(kn, j);
       start(sn, st_n, 1 - h, any);
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        if (any) we[g] = eread(st, 1, h, g);
+        if (any) ke[g] = eread(st, h, g);
       u32x4 w[2];
       float l0 = 0.f, l1 = 0.f;
       __builtin_amdgcn_sched_barrier(0);
@@ -299,10 +308,10 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
         else if (kk + PK - NKK < PV) vf[kk + PK - NKK] = vread(kk + PK - NKK);
 #pragma unroll
         for (int e2 = 8 * kk / NKK; e2 < 8 * (kk + 1) / NKK; ++e2) {  // a share of the 8 pairs
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * e2], a.sl2, -m_use));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * e2 + 1], a.sl2, -m_use));
-          l0 = any ? __builtin_fmaf(p0, we[e2 / 2][2 * e2 % 4], l0) : l0 + p0;
-          l1 = any ? __builtin_fmaf(p1, we[e2 / 2][2 * e2 % 4 + 1], l1) : l1 + p1;
+          const float t0 = __builtin_fmaf(sc[2 * e2], a.sl2, -m_use), t1 = __builtin_fmaf(sc[2 * e2 + 1], a.sl2, -m_use);
+          const float p0 = __builtin_amdgcn_exp2f(t0), p1 = __builtin_amdgcn_exp2f(t1);
+          l0 += any ? __builtin_amdgcn_exp2f(t0 - ke[e2 / 2][2 * e2 % 4]) : p0;
+          l1 += any ? __builtin_amdgcn_exp2f(t1 - ke[e2 / 2][2 * e2 % 4 + 1]) : p1;
           w[e2 / 4][e2 % 4] = pack2h(p0, p1);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -324,7 +333,7 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
 #pragma unroll
         for (int kk = 0; kk < NKK; ++kk)
           sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(smem, kk), qf[kk], sa, 0, 0, 0);
-        settle(sa, kb0 * BKV);
+        settle(sa, kb0 * BKV, scaled);
       }
       for (int kb = kb0; kb < kb1; ++kb) {
         if (kb + 2 < kb1) issue(kb + 2);
@@ -336,10 +345,10 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
           const bf16_t* vs = smem + cur + KS::ELEMS;
           step(smem + cur + 32 * DQK, vs, sa, sb, st, 0, st, scaled);
           if (kb * BKV + 32 <= qw0 + 31 + diag) {  // the second half is not all behind the diagonal
-            settle(sb, kb * BKV + 32);
+            settle(sb, kb * BKV + 32, scaled);
             // (past the last tile the next logits come from a stale stage and are not used)
             step(smem + nxt, vs + 32 * DV, sb, sa, st, 1, st_n, scaled);
-            if (kb + 1 < nvis) settle(sa, (kb + 1) * BKV);
+            if (kb + 1 < nvis) settle(sa, (kb + 1) * BKV, scaled);
           }
         }
         // tile kb + 2 has landed and nobody reads tile kb's stage any more
@@ -384,7 +393,8 @@ __global__ __launch_bounds__(64 * PA_WAVES) void attn_packed_kernel(PackedDev a)
 }
 
 // The parts of every (query, head) joined in order; a thread has four values.  Parts without weight
-// (no key seen: reference -infinity, sum 0) are not read.
+// (no key seen: reference -infinity, sum 0) are not read.  References may lie more than 2^126 apart (a part
+// of small latents beside one of large ones).
 __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedDev a, int dv) {
   const int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x), at = e / dv;
   const int64_t row = at / a.H;
@@ -398,9 +408,9 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedDev a, int 
   for (int z = 0; z < a.nsplit; ++z) {
     const f32x2 ml = *(const f32x2*)(a.part_ml + 2 * (at + z * stride));
     if (ml[0] == -INFINITY && ml[1] == 0.f) continue;
-    const float w = __builtin_amdgcn_exp2f(ml[0] - (M == -INFINITY ? 0.f : M));
-    L += ml[1] * w;
-    v += *(const f32x4*)(a.part_o + (at + z * stride) * dv + d) * w;
+    const float down = ml[0] - (M == -INFINITY ? 0.f : M);
+    L += scaled_down(ml[1], down);
+    v += *(const f32x4*)(a.part_o + (at + z * stride) * dv + d) * __builtin_amdgcn_exp2f(down);
   }
   v *= (L == 0.f ? 0.f : 1.f / L) * *(const f32x4*)(a.v_scale + (int64_t)(i / a.v_div) * a.v_head + d);
   *(u32x2*)(a.O + row * a.o_tok + (int64_t)i * dv + d) = u32x2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};

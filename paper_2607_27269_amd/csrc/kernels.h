@@ -341,7 +341,7 @@ struct AttnPacked {
   // v[n][d] 2^-key_exp[n] / v_scale[d] (V.head and V.div give head i's columns, v_scale alike),
   // magnitudes at most 2^15, |key_exp| at most 64.
   HeadView V;
-  const float* key_exp;            // [2][n_kv]: key_exp, 2^-key_exp
+  const float* key_exp;            // [n_kv]
   const float* v_scale;
   void* O; int64_t o_tok;
   float scale;

@@ -760,7 +760,7 @@ struct GatherDev {
   const bf16_t* Wuv;
   bf16_t* rows;      // [n_kv][width]
   bf16_t* lat;       // [n_kv][width], scaled latents (rows as far apart as the rows': products of alike operands)
-  float* key_exp;    // [2][n_kv]: e, 2^-e
+  float* key_exp;    // [n_kv]: e
   bf16_t* W;         // [nv][rkv], scaled
   float* v_scale;    // [nv]
 };
@@ -836,7 +836,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(GatherDev a) {
     *(u32x4*)(a.lat + (int64_t)row * c.width + 8 * lane) = scaled(lat, -e);
   }
   if (in_pe) *(u32x4*)(dst + a.rkv + 8 * lane) = pe;
-  if (lane < 2) a.key_exp[(int64_t)lane * a.n_kv + row] = lane ? __uint_as_float((uint32_t)(127 - e) << 23) : (float)e;
+  if (lane == 0) a.key_exp[row] = (float)e;
 }
 
 struct PrefillLayout {
@@ -872,7 +872,7 @@ PrefillLayout prefill_layout(const PrefillPaged& p) {
   l.rows = 0;
   l.lat = l.rows + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
   l.key_exp = l.lat + al((size_t)p.n_kv * (p.rkv + p.dr) * 2);
-  l.W = l.key_exp + al((size_t)p.n_kv * 8);
+  l.W = l.key_exp + al((size_t)p.n_kv * 4);
   l.v_scale = l.W + al((size_t)p.G * p.dv * p.rkv * 2);
   l.keys = l.v_scale + al((size_t)p.G * p.dv * 4);
   l.vals = l.keys + al((size_t)p.n_kv * p.G * p.dn * 2);
