@@ -332,7 +332,8 @@ int mla_recon_cache_append(const mla_recon_cfg *cfg, const mla_paged_cache *cach
  *           at most 2^35
  * The work is cut over the rows of all sequences together, so that lengths that differ keep
  * the whole GPU busy.  ws 16-byte aligned, of mla_recon_decode_paged_workspace_size bytes for
- * this cfg and max_len (0 = unsupported or invalid). */
+ * this cfg and max_len (0 = unsupported or invalid), or of those for more sequences or a larger
+ * max_len. */
 size_t mla_recon_decode_paged_workspace_size(const mla_recon_cfg *cfg, int32_t max_len);
 int mla_recon_decode_paged(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
                            int32_t max_len, const int32_t *lengths, const void *Wuk,
@@ -357,7 +358,8 @@ int mla_recon_decode_paged(const mla_recon_cfg *cfg, const void *q, const mla_pa
  * 2^-72 lose precision, and W_UV is to be below 2^124.  n_q and n_kv at most 1048576, n_heads (n_q / 256 + batch) below 2^23,
  * softmax_scale at least 1e-30, (d_nope + d_rope, d_k) one of (64, 64), (96, 64), (128, 64),
  * (128, 128), (192, 128).
- * q, Wuv, o and ws 16-byte aligned, ws of mla_recon_prefill_paged_workspace_size bytes. */
+ * q, Wuv, o and ws 16-byte aligned, ws of mla_recon_prefill_paged_workspace_size bytes: the size
+ * for the most tokens, rows and sequences (cfg->batch) of a program's calls serves them all. */
 size_t mla_recon_prefill_paged_workspace_size(const mla_recon_cfg *cfg, int32_t n_q, int32_t n_kv);
 int mla_recon_prefill_paged(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
                             const int32_t *q_offsets, const mla_paged_cache *cache, int32_t n_kv,

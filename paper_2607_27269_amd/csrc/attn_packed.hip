@@ -444,9 +444,21 @@ void launch(const PackedDev& d, hipStream_t s) {
 }  // namespace
 }  // namespace attn
 
+// Enough for the parts of every call of no more queries, keys and sequences.  Fewer keys or more sequences
+// never mean more parts; more queries do mean fewer, at each further query tile: so one sequence, all the
+// keys, and of the query counts up to n_q the last before each further tile.
 size_t attn_packed_ws_bytes(const AttnPacked& a) {
-  const int n = attn::parts_of(a);
-  return n > 1 ? (size_t)n * a.n_q * a.H * (a.dv + 2) * 4 + 256 : 0;
+  AttnPacked c = a;
+  c.B = 1;
+  const int bqh = attn::PA_BQ / attn::heads_per_group(a);
+  size_t rows = 0;
+  for (int64_t end = bqh - 1;; end += bqh) {
+    c.n_q = (int)(end < a.n_q ? end : a.n_q);
+    const int n = attn::parts_of(c);
+    if (n > 1 && (size_t)n * c.n_q > rows) rows = (size_t)n * c.n_q;
+    if (n <= 1 || c.n_q == a.n_q) break;
+  }
+  return rows * a.H * (a.dv + 2) * 4;
 }
 
 hipError_t attn_fwd_packed(const AttnPacked& a, hipStream_t s) {
