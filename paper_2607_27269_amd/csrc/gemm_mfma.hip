@@ -64,7 +64,7 @@ struct GemmDev {
   float alpha, beta;
   int kchunk;         // K elements per split (multiple of BK)
   int nsplit;         // split-K chunks (persistent launch)
-  int aligned;        // rows of A and B 16-byte aligned (gemm_tile)
+  int aligned;        // rows of A and B 16-byte aligned
   int ktotal;
   int mstore;         // rows of C written (M is the row count operand A may be read at)
   // batched causal mode (causal != 0): workgroup z of nbatch works on A + z sA,
@@ -794,7 +794,8 @@ __device__ __forceinline__ void gemm_persist(const GemmDev& g) {
     t.mlo = t.m0;
     t.nlo = t.n0;
     if constexpr (SHIFT) shift_edge<BM, BN, AK, BKM, ATILE>(g, t.m0, t.n0);
-    const bool dma_ok = edge_rows<ATILE>(g) - t.m0 >= BM && g.N - t.n0 >= BN &&
+    // (operands that are not 16-byte aligned go through registers, as in gemm_tile)
+    const bool dma_ok = (ATILE || g.aligned) && edge_rows<ATILE>(g) - t.m0 >= BM && g.N - t.n0 >= BN &&
                         (AK ? (int64_t)BM * g.lda : (int64_t)BK * g.lda) < (1ll << 30) &&
                         (BKM ? (int64_t)BN * g.ldb : (int64_t)BK * g.ldb) < (1ll << 30);
     t.nfull = dma_ok ? (t.kend - t.kbeg) / BK : 0;
