@@ -138,16 +138,18 @@ class PagedLatentCache:
     """The paged latent cache of ``n_layers`` layers of shape ``cfg`` (a configs.LayerConfig).
 
     All layers share one page table: page p of a sequence lies at the same place of every
-    layer's pool [n_pages, page_size, r_kv + G_r d_rope] (storage dtype of cfg)."""
+    layer's pool [n_pages, page_size, r_kv + d_rope], bf16.  Shapes that the attention over pages does not
+    serve (fp32, more than one positional key, other widths) are refused here."""
 
     def __init__(self, cfg, n_layers: int, n_pages: int, page_size: int, device: str = "cuda:0"):
+        # (the library's load fails loudly if it is not built)
+        if L.mla_recon_decode_paged_workspace_size(L.make_cfg(cfg.replace(batch=1, seq=1)), 1) == 0:
+            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
         if not torch.cuda.is_available():
             raise RuntimeError("PagedLatentCache needs a ROCm GPU")
-        L.lib()  # fail loudly if the HIP library is not built
-        self.cfg, self.device = cfg, torch.device(device)
-        self.dtype = torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
+        self.cfg, self.device, self.dtype = cfg, torch.device(device), torch.bfloat16
         self.alloc = PageAllocator(n_pages, page_size)
-        self.width = cfg.kv_rank + cfg.s_rope_groups * cfg.rope_dim
+        self.width = cfg.kv_rank + cfg.rope_dim
         self.pool = torch.zeros(n_layers, n_pages, page_size, self.width, dtype=self.dtype,
                                 device=self.device)
         self._open = None  # the batch that has reserved pages and is not committed
@@ -244,13 +246,13 @@ class Batch:
                              f"is needed, not {x.dtype} {tuple(x.shape)} on {x.device}")
 
     def append(self, layer: int, rows: torch.Tensor, q: torch.Tensor, inv_freq: torch.Tensor) -> torch.Tensor:
-        """Write the new tokens' rows [n_new, r_kv + G_r d_rope] = [c^KV | k^PE], k^PE rotated at its
+        """Write the new tokens' rows [n_new, r_kv + d_rope] = [c^KV | k^PE], k^PE rotated at its
         position, into the pages of ``layer``; returns q [n_new, H, d_nope + d_rope] with its
-        rotary part rotated likewise (a new tensor).  inv_freq [G_r, d_rope / 2] fp32."""
+        rotary part rotated likewise (a new tensor).  inv_freq [1, d_rope / 2] fp32."""
         c, cfg = self.cache, self.cache.cfg
         self._check("rows", rows, (self.n_new, c.width), c.dtype)
         self._check("q", q, (self.n_new, cfg.n_heads, cfg.nope_dim + cfg.rope_dim), c.dtype)
-        self._check("inv_freq", inv_freq, (cfg.s_rope_groups, cfg.rope_dim // 2), torch.float32)
+        self._check("inv_freq", inv_freq, (1, cfg.rope_dim // 2), torch.float32)
         out = torch.empty_like(q)
         with torch.cuda.device(c.device):
             L.mla_recon_cache_append(self.ccfg, self._handle(layer), rows.data_ptr(), q.data_ptr(),
