@@ -9,6 +9,7 @@ otherwise.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -91,6 +92,17 @@ class PagedCache(ctypes.Structure):
                 ("max_pages", ctypes.c_int32)]
 
 
+class _Int32:
+    """An int32 argument.  ctypes' own type would pass the low bits of a larger number on."""
+
+    @classmethod
+    def from_param(cls, v):
+        v = operator.index(v)
+        if not -2**31 <= v < 2**31:
+            raise OverflowError(f"{v} does not fit 32 bits")
+        return ctypes.c_int32(v)
+
+
 _lib = None
 
 
@@ -101,7 +113,7 @@ def lib() -> ctypes.CDLL:
             raise ImportError(f"{LIB_PATH} is missing: build it with "
                               "`python -m paper_2607_27269_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+        vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, _Int32
         P = ctypes.POINTER
         L.mla_recon_workspace_size.argtypes = [P(Cfg)]
         L.mla_recon_workspace_size.restype = sz
@@ -150,14 +162,14 @@ def lib() -> ctypes.CDLL:
                   "mla_recon_prefill_paged", "mla_recon_cache_copy_pages",
                   "mla_recon_prof_enable",
                   "mla_recon_prof_read"):
-            getattr(L, f).restype = i32
+            getattr(L, f).restype = ctypes.c_int32
         L.mla_recon_last_error.argtypes = []
         L.mla_recon_last_error.restype = ctypes.c_char_p
         L.mla_recon_prof_enable.argtypes = [i32, i32]
         L.mla_recon_prof_read.argtypes = [i32, P(ctypes.c_double), P(ctypes.c_int64),
                                           P(ctypes.c_double), P(ctypes.c_double)]
         L.mla_recon_prof_kernels.argtypes = [i32, P(ProfKernel), i32]
-        L.mla_recon_prof_kernels.restype = i32
+        L.mla_recon_prof_kernels.restype = ctypes.c_int32
         _lib = L
     return _lib
 
