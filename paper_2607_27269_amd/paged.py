@@ -198,14 +198,15 @@ class PagedLatentCache:
 
     def batch(self, seqs, counts) -> "Batch":
         """A step that adds counts[i] >= 1 tokens to seqs[i]: pages are reserved (and shared ones
-        copied).  One batch is open at a time."""
+        copied).  One batch is open at a time.  A step larger than the calls of ``Batch.attend`` take (with
+        more than one new token of any sequence: 1048576 cached rows of all its sequences) is refused
+        with nothing changed."""
         self._closed()
-        counts = [int(c) for c in counts]
-        if not seqs or any(c < 1 for c in counts):
-            raise ValueError("a batch has sequences, and one new token or more of each")
-        self._copy(self.alloc.extend(seqs, counts))
-        self._open = Batch(self, list(seqs), counts)
-        return self._open
+        step = Batch(self, list(seqs), [int(c) for c in counts])
+        self._copy(self.alloc.extend(step.seqs, step.counts))
+        step._upload()
+        self._open = step
+        return step
 
 
 class Batch:
@@ -213,24 +214,35 @@ class Batch:
     sequence i follow those of sequence i - 1."""
 
     def __init__(self, cache: PagedLatentCache, seqs, counts):
+        if not seqs or len(seqs) != len(counts) or any(c < 1 for c in counts):
+            raise ValueError("a batch has sequences, and one new token or more of each")
         self.cache, self.seqs, self.counts = cache, seqs, counts
-        a, cfg = cache.alloc, cache.cfg
-        before = [a.length[s] for s in seqs]
-        after = [n + c for n, c in zip(before, counts)]
+        self._before = [cache.alloc.length[s] for s in seqs]
+        self._after = [n + c for n, c in zip(self._before, counts)]
+        self.n_new, self.n_kv, self.max_len = sum(counts), sum(self._after), max(self._after)
+        self.ccfg = L.make_cfg(cache.cfg.replace(batch=len(seqs), seq=1))
+        self.single = all(c == 1 for c in counts)
+        self._ws = None
+        if max(self.max_len, 0 if self.single else self.n_kv) >= 2**31:
+            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, f"a batch over {self.n_kv} rows, {self.max_len} of one sequence")
+        self._ws_bytes = (L.mla_recon_decode_paged_workspace_size(self.ccfg, self.max_len) if self.single else
+                          L.mla_recon_prefill_paged_workspace_size(self.ccfg, self.n_new, self.n_kv))
+        if self._ws_bytes == 0:
+            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
+
+    def _upload(self):
+        """The page table (pages are reserved by now), offsets and lengths, to the GPU."""
+        a, seqs, counts, before, after = self.cache.alloc, self.seqs, self.counts, self._before, self._after
         table = np.full((len(seqs), max(len(a.pages[s]) for s in seqs)), -1, dtype=np.int32)
         for row, s in zip(table, seqs):
             row[:len(a.pages[s])] = a.pages[s]
-        self.n_new, self.n_kv, self.max_len = sum(counts), sum(after), max(after)
         zero = [0]
         # one upload: offsets, starts, offsets of the cached rows, lengths, the table
         parts = [np.cumsum(zero + counts), before, np.cumsum(zero + after), after, table.ravel()]
         flat = torch.from_numpy(np.concatenate([np.asarray(p, dtype=np.int32) for p in parts]))
-        flat = flat.to(cache.device)
+        flat = flat.to(self.cache.device)
         self.offsets, self.start, self.kv_offsets, self.lengths, t = flat.split([len(p) for p in parts])
         self.table = t.view(table.shape)
-        self.ccfg = L.make_cfg(cfg.replace(batch=len(seqs), seq=1))
-        self.single = all(c == 1 for c in counts)
-        self._ws = None
 
     def _handle(self, layer: int) -> L.PagedCache:
         if self.cache._open is not self:
@@ -273,11 +285,7 @@ class Batch:
         o = torch.empty(self.n_new, cfg.n_heads, cfg.head_dim, dtype=c.dtype, device=c.device)
         with torch.cuda.device(c.device):
             if self._ws is None:  # kept for the other layers
-                size = (L.mla_recon_decode_paged_workspace_size(self.ccfg, self.max_len) if self.single else
-                        L.mla_recon_prefill_paged_workspace_size(self.ccfg, self.n_new, self.n_kv))
-                if size == 0:
-                    raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
-                self._ws = torch.empty(size, dtype=torch.uint8, device=c.device)
+                self._ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=c.device)
             stream = torch.cuda.current_stream().cuda_stream
             if self.single:
                 L.mla_recon_decode_paged(self.ccfg, q.data_ptr(), self._handle(layer), self.max_len,

@@ -43,3 +43,32 @@ def test_caches_that_no_attention_serves_are_refused(kw):
     with pytest.raises(L.MlaError) as e:
         PagedLatentCache(configs.get(1).replace(**kw), 1, 4, 16)
     assert e.value.code == L.MLA_ERR_UNSUPPORTED and str(e.value)
+
+
+@pytest.mark.parametrize("page_size,tokens,forks,counts", [
+    (1 << 16, 700_000, 2, [1, 2]),          # 1400003 rows, of which some tokens see more than one new row
+    (1 << 16, 1 << 20, 4096, [1] * 4095 + [2]),   # a little more than 2^32 rows
+    (1 << 16, 10, 1, [(1 << 20) + 1]),      # too many new tokens
+])
+def test_steps_that_no_call_serves_change_nothing(page_size, tokens, forks, counts):
+    """More new tokens, or more cached rows for a step of several tokens a sequence, than a call takes:
+    refused before pages are reserved or copied."""
+    copies = []
+    c = host_cache(6000, page_size, copies=copies)
+    seqs = [grown(c, tokens)]
+    seqs += [c.alloc.fork(seqs[0]) for _ in range(forks - 1)]
+    before = state(c)
+    with pytest.raises(L.MlaError) as e:
+        c.batch(seqs, counts)
+    assert e.value.code == L.MLA_ERR_UNSUPPORTED and str(e.value)
+    assert state(c) == before and not copies
+    c.batch(seqs[:1], [1])                  # single tokens over as many rows are served
+
+
+def test_a_sequence_past_32_bits_is_refused():
+    c = host_cache(40000, 1 << 16)
+    s = grown(c, 2**31 - 1)
+    before = state(c)
+    with pytest.raises(L.MlaError):
+        c.batch([s], [1])
+    assert state(c) == before
