@@ -81,10 +81,11 @@ class PageAllocator:
         self.truncate(seq, 0)
         del self.pages[seq], self.length[seq]
 
-    def extend(self, seqs, counts) -> list[tuple[int, int]]:
+    def extend(self, seqs, counts, copy=None) -> list[tuple[int, int]]:
         """Room for counts[i] more tokens of seqs[i] (lengths stay as they are; pages reserved
         before are kept).  Returns the page pairs (from, to) to copy before anything is written
-        to them.  Raises OutOfPages, having changed nothing, if the pool has too few."""
+        to them; ``copy`` is called with them before anything here has changed (nothing has if it
+        raises).  Raises OutOfPages, having changed nothing, if the pool has too few."""
         seqs, counts = list(seqs), [int(c) for c in counts]
         if len(set(seqs)) != len(seqs) or len(seqs) != len(counts):
             raise ValueError("one count for each of different sequences")
@@ -104,12 +105,13 @@ class PageAllocator:
                     need += 1
         if need > len(self.free_pages):
             raise OutOfPages(f"{need} pages needed, {len(self.free_pages)} free")
-        pairs = []
-        for s, at in shared:
-            old, new = self.pages[s][at], self._take()
-            self.pages[s][at] = new
+        # (the pages that _take gives next)
+        pairs = [(self.pages[s][at], self.free_pages[-1 - i]) for i, (s, at) in enumerate(shared)]
+        if copy is not None:
+            copy(pairs)
+        for (s, at), (old, _) in zip(shared, pairs):
+            self.pages[s][at] = self._take()
             self._release(old)
-            pairs.append((old, new))
         for s, c in zip(seqs, counts):
             for _ in range(-(-(self.length[s] + c) // ps) - len(self.pages[s])):
                 self.pages[s].append(self._take())
@@ -120,12 +122,14 @@ class PageAllocator:
         self.holders[page] = 1
         return page
 
-    def compact(self) -> list[tuple[int, int]]:
+    def compact(self, copy=None) -> list[tuple[int, int]]:
         """Move the pages in use to the front of the pool.  Returns the page pairs (from, to) to
-        copy; afterwards pages >= the number in use are free."""
+        copy (``copy`` as for ``extend``); afterwards pages >= the number in use are free."""
         used = np.flatnonzero(self.holders)
         holes = np.flatnonzero(self.holders[:len(used)] == 0)
         moved = dict(zip(used[used >= len(used)].tolist(), holes.tolist()))
+        if copy is not None:
+            copy(list(moved.items()))
         for pages in self.pages.values():
             pages[:] = [moved.get(p, p) for p in pages]
         for old, new in moved.items():
@@ -192,9 +196,7 @@ class PagedLatentCache:
     def compact(self) -> int:
         """Move the pages in use to the front of the pools; returns how many moved."""
         self._closed()
-        pairs = self.alloc.compact()
-        self._copy(pairs)
-        return len(pairs)
+        return len(self.alloc.compact(self._copy))
 
     def batch(self, seqs, counts) -> "Batch":
         """A step that adds counts[i] >= 1 tokens to seqs[i]: pages are reserved (and shared ones
@@ -203,8 +205,12 @@ class PagedLatentCache:
         with nothing changed."""
         self._closed()
         step = Batch(self, list(seqs), [int(c) for c in counts])
-        self._copy(self.alloc.extend(step.seqs, step.counts))
-        step._upload()
+        self.alloc.extend(step.seqs, step.counts, self._copy)
+        try:
+            step._upload()
+        except BaseException:
+            step._give_back()
+            raise
         self._open = step
         return step
 
@@ -308,6 +314,9 @@ class Batch:
     def abandon(self):
         """Give the batch up: its new tokens do not count, the pages reserved for them go back."""
         self._handle(0)
+        self._give_back()
+        self.cache._open = None
+
+    def _give_back(self):
         for s in self.seqs:
             self.cache.alloc.truncate(s, self.cache.alloc.length[s])
-        self.cache._open = None

@@ -3,7 +3,6 @@ and page tables name copied pages only after the copies were enqueued."""
 import copy
 import os
 
-import numpy as np
 import pytest
 import torch
 
@@ -16,10 +15,11 @@ pytestmark = pytest.mark.skipif(not os.path.exists(L.LIB_PATH),
 
 
 def host_cache(n_pages, page_size, cfg=None, copies=None):
-    """A cache without pools; page copies go to the list `copies`."""
+    """A cache without a GPU's pools; page copies go to the list `copies`."""
     c = object.__new__(PagedLatentCache)
     c.cfg, c.device, c._open = cfg or configs.get(2), torch.device("cpu"), None
     c.alloc = PageAllocator(n_pages, page_size)
+    c.pool = torch.zeros(1, n_pages, 1, 1)
     c._copy = copies.extend if copies is not None else lambda pairs: None
     return c
 
@@ -72,3 +72,49 @@ def test_a_sequence_past_32_bits_is_refused():
     with pytest.raises(L.MlaError):
         c.batch([s], [1])
     assert state(c) == before
+
+
+class Failed(Exception):
+    pass
+
+
+def failing(pairs):
+    if pairs:
+        raise Failed
+
+
+def test_a_failed_page_copy_leaves_the_tables_as_they_were():
+    """Forked sequences grow into a shared page, and a pool is compacted: if the copy fails, no table names
+    the page that did not get one, and the same call can be made again."""
+    copies = []
+    c = host_cache(12, 4, copies=copies)
+    drop, s = grown(c, 8), grown(c, 6)
+    t = c.alloc.fork(s)
+    working, c._copy = c._copy, failing
+    before = state(c)
+    with pytest.raises(Failed):
+        c.batch([s, t], [3, 1])
+    assert state(c) == before
+    c._copy = working
+    step = c.batch([s, t], [3, 1])
+    assert copies == [(c.alloc.pages[t][1], c.alloc.pages[s][1])]
+    step.commit()
+    c.alloc.free(drop)
+    c._copy, before = failing, state(c)
+    with pytest.raises(Failed):
+        c.compact()
+    assert state(c) == before
+    c._copy = working
+    del copies[:]
+    assert c.compact() == len(copies) > 0
+    assert max(p for pages in c.alloc.pages.values() for p in pages) == (c.alloc.holders > 0).sum() - 1
+
+
+def test_a_failed_upload_gives_the_pages_back():
+    c = host_cache(12, 4)
+    s = grown(c, 6)
+    before = (c.alloc.length[s], list(c.alloc.pages[s]), sorted(c.alloc.free_pages))
+    c.device = "no such device"
+    with pytest.raises(RuntimeError):
+        c.batch([s], [9])
+    assert before == (c.alloc.length[s], c.alloc.pages[s], sorted(c.alloc.free_pages)) and c._open is None
