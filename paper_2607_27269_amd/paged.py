@@ -151,11 +151,12 @@ class PagedLatentCache:
             raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
         if not torch.cuda.is_available():
             raise RuntimeError("PagedLatentCache needs a ROCm GPU")
-        self.cfg, self.device, self.dtype = cfg, torch.device(device), torch.bfloat16
+        self.cfg, self.dtype = cfg, torch.bfloat16
         self.alloc = PageAllocator(n_pages, page_size)
         self.width = cfg.kv_rank + cfg.rope_dim
         self.pool = torch.zeros(n_layers, n_pages, page_size, self.width, dtype=self.dtype,
-                                device=self.device)
+                                device=device)
+        self.device = self.pool.device  # (with its index: "cuda" would follow the current device)
         self._open = None  # the batch that has reserved pages and is not committed
 
     def _copy(self, pairs):
