@@ -1152,9 +1152,7 @@ static int prefill_paged_check(const mla_recon_cfg* cfg, int32_t n_q, int32_t n_
   if (n_q > PREFILL_PAGED_MAX || n_kv > PREFILL_PAGED_MAX)
     return fail(MLA_ERR_UNSUPPORTED, "prefill_paged: at most %d tokens and %d cached rows per call",
                 PREFILL_PAGED_MAX, PREFILL_PAGED_MAX);
-  if (!attn_mfma_supported(cfg->nope_dim + cfg->rope_dim, cfg->head_dim))
-    return fail(MLA_ERR_UNSUPPORTED, "prefill_paged: keys of %d values with d_k = %d not supported",
-                cfg->nope_dim + cfg->rope_dim, cfg->head_dim);
+  // (with d_k = 64 or 128, check_cfg leaves the matrix-core widths alone)
   if (cfg->softmax_scale < 1e-30f)
     return fail(MLA_ERR_UNSUPPORTED, "prefill_paged: softmax_scale must be at least 1e-30");
   if ((int64_t)cfg->n_heads * (n_q / 256 + cfg->batch) >= 1 << 23)

@@ -1913,8 +1913,11 @@ hipError_t gemm_mfma_group(const Gemm* g, int n, float* scratch, size_t scratch_
       if (whole) gemm_nt4_group_kernel<192, bf16_t, false><<<grid, 256, 0, s>>>(d, gr);
       else gemm_nt4_group_kernel<192, bf16_t, true><<<grid, 256, 0, s>>>(d, gr);
     }
-    prof_end(kclass, s, flops, bytes, best_bn == 256 ? KLABEL("gemm_nt4_group_kernel<256,256,NT,bf16>")
-                                                     : KLABEL("gemm_nt4_group_kernel<256,192,NT,bf16>"));
+    prof_end(kclass, s, flops, bytes,
+             halves ? (best_bn == 256 ? KLABEL("gemm_nt4_group_kernel<256,256,NT,16 bits>")
+                                      : KLABEL("gemm_nt4_group_kernel<256,192,NT,16 bits>"))
+                    : (best_bn == 256 ? KLABEL("gemm_nt4_group_kernel<256,256,NT,bf16>")
+                                      : KLABEL("gemm_nt4_group_kernel<256,192,NT,bf16>")));
     return hipGetLastError();
   }
   if (best_kc == 0) return hipErrorNotSupported;

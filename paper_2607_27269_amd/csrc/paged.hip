@@ -15,7 +15,6 @@ struct AppendDev {
   const int32_t* table;
   int n_pages, page_size, max_pages, width;
   int B, H, dn, dr, rkv, Gr;
-  int n_rows;
   const void* rows;
   const void* q;
   void* q_out;
@@ -143,7 +142,7 @@ hipError_t cache_append(const CacheAppend& c, hipStream_t s) {
   a.pool = (char*)c.c.pool; a.table = c.c.table; a.n_pages = c.c.n_pages;
   a.page_size = c.c.page_size; a.max_pages = c.c.max_pages; a.width = c.c.width;
   a.B = c.B; a.H = c.H; a.dn = c.dn; a.dr = c.dr; a.rkv = c.rkv; a.Gr = c.Gr;
-  a.n_rows = c.n_rows; a.rows = c.rows; a.q = c.q; a.q_out = c.q_out;
+  a.rows = c.rows; a.q = c.q; a.q_out = c.q_out;
   a.offsets = c.offsets; a.start = c.start; a.inv_freq = c.inv_freq;
   const size_t lds = (size_t)c.Gr * c.dr * 4;
   prof_begin(KC_ELEM, s);
