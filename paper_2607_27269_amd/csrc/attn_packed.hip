@@ -17,10 +17,12 @@
 // itself the compiler reads an operand right before its product and waits for LDS each time.  The
 // reference maximum moves only when a block exceeds it by 2^8.
 //
-// 5505 tokens of 6 sequences, 32 heads of 192 and 128: 123 us, 670 TFLOP/s of the causal pairs; 463 tokens
-// after 13620 cached ones, heads of 128 and 64: 43 us, and 7.6 to join 5 parts.  A tile of 64 keys takes
-// about 2.2 us at any width (matrix cores a third busy, the vector ALU as much): the chain from logits to
-// probabilities to products, not a unit's rate, is what two wavefronts a SIMD do not cover.
+// 5505 tokens of 6 sequences, 32 heads of 192 and 128: 125 us, 660 TFLOP/s of the causal pairs; 463 tokens
+// after 13620 cached ones, heads of 128 and 64: 44 us, and 7.4 to join 5 parts.  With a workgroup on every CU
+// (2048 queries of 32 heads, up to 65536 rows before them) a tile of 64 keys takes 2.4 to 2.9 us at widths
+// 192 and 128, 1.85 at 128 and 64.  No unit is busy all the time: in the first call the matrix cores 36 %, the
+// vector ALU 33 %, LDS 25 % and 7 % more in bank conflicts.  The rest are waits in the chain from logits to
+// probabilities to products, which two wavefronts a SIMD do not cover.
 //
 // The values and the probabilities are fp16 operands: with bf16 ones their two roundings were most of
 // the output's squared error (2.9e-3 of its norm; 2.0 to 2.2e-3 now), at the same rate.  fp16 has the range for it because each
@@ -31,9 +33,8 @@
 // small latents under a reference that rows of large ones set, where P' is below fp32's range and the term is
 // not.  As |e| <= 64, the row at the reference keeps the sum above 2^(PA_UP - 64), and no term exceeds
 // 2^(PA_UP + PA_SLACK + 64); the reference may move by more than 2^126 at once, so the sum is scaled by two
-// factors.  Keys whose e are
-// all 0 (any cache with latents of ordinary size) take a loop without them: 120 us against 130 for the 6
-// ragged sequences of up to 2048 tokens and 32 heads below.
+// factors.  Keys whose e are all 0 (any cache with latents of ordinary size) take a loop without them: 125 us
+// against 144 in the first call above.
 //
 // Few queries over many keys leave CUs idle: the keys are then cut into nsplit parts per query tile,
 // each with a result of its own (fp32), and a second launch joins them.
@@ -67,9 +68,10 @@ struct PackedDev {
   float* part_ml;  // [nsplit][n_q][H][2]: reference maximum (log2), sum
 };
 
-// A tile of 64 rows in LDS, not padded: 16-byte chunk c of row r lies at c ^ swz(r), so that the reads
-// made of it are free of bank conflicts.  Keys: 16 bytes of 16 consecutive rows.  Values: the
-// transposing reads' 32 bytes of four consecutive rows (pairs of chunks stay pairs).
+// A tile of 64 rows in LDS, not padded: 16-byte chunk c of row r lies at c ^ swz(r), which spreads what one
+// read takes over the banks.  Keys: 16 bytes of 16 consecutive rows.  Values: the transposing reads' 32 bytes
+// of four consecutive rows (pairs of chunks stay pairs); each of them still counts two conflict cycles (4.2e6
+// beside 15.0e6 active LDS cycles in 5505 tokens), the keys' reads none.
 template <int D>
 struct KeySwz {
   static constexpr int BANKS = D / 2 % 64;  // row stride
@@ -425,7 +427,9 @@ int heads_per_group(const AttnPacked& a) {
 int tile_numbers(const AttnPacked& a) { return a.n_q / (PA_BQ / heads_per_group(a)) + a.B; }
 // Parts of the keys: where the tiles do not fill the CUs once, as many as fill them twice, each of
 // four or more key tiles of an average sequence.  463 queries of 8 sequences after 13620 rows: 76 us
-// uncut, 41 and 7 to join in parts; 5505 tokens of 6 sequences, 736 tiles, are not cut.
+// uncut, 41 and 7 to join in parts; 5505 tokens of 6 sequences, 736 tiles, are not cut.  The rule knows the
+// average sequence only: four new tokens of each of 64 sequences, one of 100000 rows and the others of 300,
+// are not cut, and the whole call takes 3.4 ms where as many rows spread evenly take 0.68.
 int parts_of(const AttnPacked& a) {
   const int64_t tiles = (int64_t)tile_numbers(a) * (a.H / heads_per_group(a));
   if (tiles >= 256) return 1;

@@ -124,7 +124,8 @@ struct CopyDev {
 };
 
 // Grid (blocks of a page, pairs, layers); bound by memory: 257 pages of 16 layers, 303 MB, 110 us (5.5
-// TB/s read and written, some of the reads from the last-level cache), one page of 16 layers 8.6 us.
+// TB/s read and written, some of the reads from the last-level cache), one page of 16 layers 2.4 us (the call
+// 8.6 to 9.4, append's small ones 7.2: a likely cause is the 3.6 KB of arguments, which few pairs carry too).
 constexpr int COPY_BLOCK = 256 * 16;
 __global__ __launch_bounds__(256) void copy_pages_kernel(CopyDev a) {
   const int64_t at = (int64_t)blockIdx.x * COPY_BLOCK + 16 * threadIdx.x;

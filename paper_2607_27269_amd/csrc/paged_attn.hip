@@ -32,10 +32,16 @@ size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 //   (the order of the rows inside a K step is the same on both sides).  V^T comes from the same
 //   LDS tile by transposing reads.
 //
-// 64 sequences of 4096 rows of 576 values, 32 heads: 65 us, 4.7 TB/s; 2 of 100001 rows 49 us; 109683 rows
+// 64 sequences of 4096 rows of 576 values, 32 heads: 65 us, 4.7 TB/s; 2 of 100001 rows 48 us; 109683 rows
 // of 41 sequences of 1 to 16001 rows 41 us, a few tiles a wavefront and a state stored for each sequence
-// that it meets; 300 rows 8 us.  About 15 us do not depend on the rows: the list, the first
-// copies, the states; a tile of a wavefront takes 2.5 to 3 us when its rows are near, 7.5 us from memory.
+// that it meets.  64 sequences that give each of the 1024 wavefronts 1, 2, 4, 8, 16 or 32 tiles: 20, 26, 35,
+// 64, 120 and 222 us, so 5 to 7 us a tile, and about 15 us for the list, the first copies and the states (8 of
+// them still seen beside many tiles).  With a workgroup or a few those take less: one sequence of 32 to 300
+// rows 11 to 12 us, 8 to 9 with rows of 288 values.
+//
+// Precision: the absorbed queries are bf16 operands, and their rounding is what the output loses beside its
+// own (2.3e-3 of the norm against 1.65e-3); probabilities and weighted latents are held as two bf16 values each,
+// sums and states in fp32.
 constexpr int PD_KT = 32;         // rows per tile
 constexpr int PD_WAVES = 4;
 constexpr float PD_SLACK = 8.f;   // log2 units the running reference maximum may lag
@@ -73,7 +79,9 @@ struct ListCut {
 // product's result on one side, and moved 256 values out and in around each tile for the few that
 // are rescaled.)  The waits are those that the compiler keeps around products it knows: two
 // states after the vector ALU wrote an operand, and the product's passes (19 states at most)
-// before the vector ALU reads a result.
+// before the vector ALU reads a result.  The compiler does not know that latency: that it puts no move or
+// spill of an accumulator there (the kernel of 576-wide rows spills 4 vector and 22 scalar registers) is
+// checked on the built code by tests/test_matrix_waits.py.
 __device__ __forceinline__ void mfma_v_first(f32x16& d, bf16x8 x, bf16x8 y) {
   asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));
 }
@@ -102,12 +110,13 @@ __device__ __forceinline__ void acc_scale(f32x16& v, float f) {
   }
 }
 
-// A tile in LDS: 32 rows of CHR 16-byte chunks, not padded; chunk c of row r lies at c ^ swz(r), so
-// that both read patterns are free of bank conflicts: 16 bytes of 16 consecutive rows (S^T), and
+// A tile in LDS: 32 rows of CHR 16-byte chunks, not padded; chunk c of row r lies at c ^ swz(r), which
+// spreads both read patterns over the banks: 16 bytes of 16 consecutive rows (S^T, no conflicts), and
 // the transposing reads' 32 bytes of four consecutive rows (V^T; the rows that share banks differ
-// in chunk bit 1).  Without padding a copy's lanes meet the same chunks again after PERIOD copies
-// (ROWS rows), so that the lanes' source offsets are a few registers and a copy of rows that lie
-// together costs no arithmetic.
+// in chunk bit 1; two conflict cycles a read are left, 1.0e6 beside 4.1e6 active LDS cycles in 64 x 4096
+// rows).  Without padding a copy's lanes meet the same chunks again after PERIOD copies (ROWS rows), so
+// that the lanes' source offsets are a few registers and a copy of rows that lie together costs no
+// arithmetic.
 template <int DK>
 struct Tile {
   static constexpr int CHR = DK / 8;
@@ -734,7 +743,8 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
 // ---- prefill --------------------------------------------------------------------------
 // With many queries per cached row the keys W_UK c and values W_UV c are written out once (as for
 // the contiguous cache) and the attention runs on heads of d_nope + d_rope and d_k: gather, one
-// grouped product, attention over the packed sequences.
+// grouped product, attention over the packed sequences.  Keys are bf16, whose rounding is most of what the
+// output loses beside its own (2.2e-3 of the norm against 1.65e-3), values and probabilities fp16 (3e-5).
 namespace {
 
 // The cached rows of all sequences behind one another, and what the products need; a wavefront per row.

@@ -12,7 +12,7 @@ work on them.  One model step over some sequences is a ``Batch``::
     batch.commit()                                # the new tokens count as cached
 
 All device work is enqueued on the current HIP stream; calls from more than one stream are the
-caller's to order.
+caller's to order (the layers of a batch share its workspace).
 """
 from __future__ import annotations
 
@@ -282,9 +282,15 @@ class Batch:
 
     def attend(self, layer: int, q: torch.Tensor, Wuk: torch.Tensor, Wuv: torch.Tensor) -> torch.Tensor:
         """The per-head attention outputs [n_new, H, d_k] of the new tokens (q rotated, their rows
-        appended), each over the cached rows of its sequence up to its own: one token of every
-        sequence in absorbed form, more with keys and values written out.  Wuk
-        [G_kv d_nope, r_kv], Wuv [G_kv d_k, r_kv]."""
+        appended), each over the cached rows of its sequence up to its own.  Wuk
+        [G_kv d_nope, r_kv], Wuv [G_kv d_k, r_kv].
+
+        Where every sequence has one new token the call is the absorbed form's (decoding), else keys
+        and values are written out (prefill) for all of the batch.  Single tokens by decoding and by
+        prefill, whole calls of the 8B layer: 64 sequences of 4096 rows 79 and 1197 us, 512 of 16 rows
+        88 and 162, one of 300 rows 21 and 29, 8 of 64 rows 25 and 22 (prefill is ahead in a few short
+        sequences only, by 6 us at most).  One sequence of two tokens among 63 of one, 4096 rows each,
+        makes the step a prefill: 1.3 ms."""
         c, cfg = self.cache, self.cache.cfg
         self._check("q", q, (self.n_new, cfg.n_heads, cfg.nope_dim + cfg.rope_dim), c.dtype)
         self._check("Wuk", Wuk, (cfg.s_kv_groups * cfg.nope_dim, cfg.kv_rank), c.dtype)
