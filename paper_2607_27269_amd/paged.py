@@ -201,9 +201,8 @@ class PagedLatentCache:
 
     def batch(self, seqs, counts) -> "Batch":
         """A step that adds counts[i] >= 1 tokens to seqs[i]: pages are reserved (and shared ones
-        copied).  One batch is open at a time.  A step larger than the calls of ``Batch.attend`` take (with
-        more than one new token of any sequence: 1048576 cached rows of all its sequences) is refused
-        with nothing changed."""
+        copied).  One batch is open at a time.  Sequences past 2^31 - 1 tokens are refused with nothing
+        changed."""
         self._closed()
         step = Batch(self, list(seqs), [int(c) for c in counts])
         self.alloc.extend(step.seqs, step.counts, self._copy)
@@ -230,12 +229,8 @@ class Batch:
         self.ccfg = L.make_cfg(cache.cfg.replace(batch=len(seqs), seq=1))
         self.single = all(c == 1 for c in counts)
         self._ws = None
-        if max(self.max_len, 0 if self.single else self.n_kv) >= 2**31:
-            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, f"a batch over {self.n_kv} rows, {self.max_len} of one sequence")
-        self._ws_bytes = (L.mla_recon_decode_paged_workspace_size(self.ccfg, self.max_len) if self.single else
-                          L.mla_recon_prefill_paged_workspace_size(self.ccfg, self.n_new, self.n_kv))
-        if self._ws_bytes == 0:
-            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
+        if self.max_len >= 2**31:
+            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, f"a sequence of {self.max_len} tokens")
 
     def _upload(self):
         """The page table (pages are reserved by now), offsets and lengths, to the GPU."""
@@ -290,7 +285,8 @@ class Batch:
         prefill, whole calls of the 8B layer: 64 sequences of 4096 rows 79 and 1197 us, 512 of 16 rows
         88 and 162, one of 300 rows 21 and 29, 8 of 64 rows 25 and 22 (prefill is ahead in a few short
         sequences only, by 6 us at most).  One sequence of two tokens among 63 of one, 4096 rows each,
-        makes the step a prefill: 1.3 ms."""
+        makes the step a prefill: 1.3 ms.  A prefill takes 1048576 new tokens and as many cached rows of all
+        its sequences: a larger step is refused here, with nothing enqueued (``append`` serves it)."""
         c, cfg = self.cache, self.cache.cfg
         self._check("q", q, (self.n_new, cfg.n_heads, cfg.nope_dim + cfg.rope_dim), c.dtype)
         self._check("Wuk", Wuk, (cfg.s_kv_groups * cfg.nope_dim, cfg.kv_rank), c.dtype)
@@ -298,7 +294,7 @@ class Batch:
         o = torch.empty(self.n_new, cfg.n_heads, cfg.head_dim, dtype=c.dtype, device=c.device)
         with torch.cuda.device(c.device):
             if self._ws is None:  # kept for the other layers
-                self._ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=c.device)
+                self._ws = torch.empty(self._workspace_bytes(), dtype=torch.uint8, device=c.device)
             stream = torch.cuda.current_stream().cuda_stream
             if self.single:
                 L.mla_recon_decode_paged(self.ccfg, q.data_ptr(), self._handle(layer), self.max_len,
@@ -310,6 +306,15 @@ class Batch:
                                           Wuk.data_ptr(), Wuv.data_ptr(), o.data_ptr(),
                                           self._ws.data_ptr(), self._ws.numel(), stream)
         return o
+
+    def _workspace_bytes(self) -> int:
+        if not self.single and self.n_kv >= 2**31:
+            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, f"a prefill over {self.n_kv} cached rows")
+        size = (L.mla_recon_decode_paged_workspace_size(self.ccfg, self.max_len) if self.single else
+                L.mla_recon_prefill_paged_workspace_size(self.ccfg, self.n_new, self.n_kv))
+        if size == 0:
+            raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
+        return size
 
     def commit(self):
         """The new tokens count as cached."""

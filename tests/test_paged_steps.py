@@ -1,4 +1,4 @@
-"""PagedLatentCache's steps on the host (no GPU): what is refused is refused before anything has changed,
+"""PagedLatentCache's steps on the host (no GPU): what is refused and what fails leaves the books as they were,
 and page tables name copied pages only after the copies were enqueued."""
 import copy
 import os
@@ -46,23 +46,26 @@ def test_caches_that_no_attention_serves_are_refused(kw):
 
 
 @pytest.mark.parametrize("page_size,tokens,forks,counts", [
-    (1 << 16, 700_000, 2, [1, 2]),          # 1400003 rows, of which some tokens see more than one new row
+    (1 << 16, 700_000, 2, [1, 2]),          # 1400003 rows
     (1 << 16, 1 << 20, 4096, [1] * 4095 + [2]),   # a little more than 2^32 rows
     (1 << 16, 10, 1, [(1 << 20) + 1]),      # too many new tokens
 ])
-def test_steps_that_no_call_serves_change_nothing(page_size, tokens, forks, counts):
-    """More new tokens, or more cached rows for a step of several tokens a sequence, than a call takes:
-    refused before pages are reserved or copied."""
-    copies = []
-    c = host_cache(6000, page_size, copies=copies)
+def test_steps_that_only_append_serves(page_size, tokens, forks, counts):
+    """More new tokens, or more cached rows for a step of several tokens a sequence, than the attention
+    takes: their rows can be appended, attend refuses (and does not take their low 32 bits), and the
+    pages go back."""
+    c = host_cache(6000, page_size)
     seqs = [grown(c, tokens)]
     seqs += [c.alloc.fork(seqs[0]) for _ in range(forks - 1)]
-    before = state(c)
+    free = len(c.alloc.free_pages)
+    step = c.batch(seqs, counts)
     with pytest.raises(L.MlaError) as e:
-        c.batch(seqs, counts)
+        step._workspace_bytes()
     assert e.value.code == L.MLA_ERR_UNSUPPORTED and str(e.value)
-    assert state(c) == before and not copies
-    c.batch(seqs[:1], [1])                  # single tokens over as many rows are served
+    step.abandon()
+    assert c._open is None and [c.alloc.length[s] for s in seqs] == [tokens] * forks
+    assert len(c.alloc.free_pages) >= free - (forks - 1)     # (copies of the shared page stay)
+    assert c.batch(seqs[:1], [1])._workspace_bytes() > 0     # single tokens over as many rows are served
 
 
 def test_a_sequence_past_32_bits_is_refused():
