@@ -378,6 +378,80 @@ int mla_recon_cache_copy_pages(void *pool, int32_t n_layers, int64_t layer_strid
                                int64_t page_bytes, const int32_t *pairs, int32_t n_pairs,
                                void *hip_stream);
 
+/* ---- the same cache in eight bits -----------------------------------------------------
+ * MLA_CACHE_E4M3 keeps a row's r_kv latents in e4m3 (OCP: four bits of exponent, three of fraction,
+ * no infinities) times one power of two for the row, and its positional values in bf16: 644 bytes of
+ * the 1152 that 512 latents and 64 positional values take in bf16.  A page is
+ *     page_size rows of r_kv bytes and G_r d_rope bf16 values, then page_size powers of two (fp32),
+ * padded to a multiple of 16 bytes: mla_recon_cache_page_bytes of them, the pages of a pool behind one
+ * another.  A latent x is stored as the e4m3 value nearest to x 2^-e (halves to the even one), e the
+ * least integer in [-80, 120] that brings the row's largest finite latent to 448 or less (-80 for
+ * a row of zeros): off by 2^-4 of itself at most where it is at least 2^-14 of the row's largest, by
+ * 2^-10 2^e below.  A latent that is not finite is stored as NaN.  Latents above 248/256 of the largest
+ * bf16 value may be stored as 2^128.
+ * The calls below take mla_paged_cache with such a pool (mla_recon_cache_copy_pages copies its pages
+ * too); cfg->dtype must be MLA_BF16 for them (rows, queries, weights and outputs). */
+typedef enum {
+  MLA_CACHE_STORAGE = 0,  /* rows of r_kv + G_r d_rope values in the storage dtype         */
+  MLA_CACHE_E4M3 = 1
+} mla_cache_format;
+
+/* Bytes of one page of page_size rows in a format; 0 (and mla_recon_last_error()) if invalid. */
+int64_t mla_recon_cache_page_bytes(const mla_recon_cfg *cfg, int32_t format, int32_t page_size);
+
+/* mla_recon_cache_append into a cache of format MLA_CACHE_E4M3: the same arguments and rules; the
+ * latents are quantised, k^PE is rotated and stored in bf16. */
+int mla_recon_cache_append_e4m3(const mla_recon_cfg *cfg, const mla_paged_cache *cache, const void *rows,
+                                const void *q, void *q_out, int32_t n_rows, const int32_t *offsets,
+                                const int32_t *start, const float *inv_freq, void *hip_stream);
+
+/* Cached rows back into one piece, for another program, another format or a look at them: packed row
+ * i with offsets[b] <= i < offsets[b + 1] becomes the row at position start[b] + i - offsets[b] of
+ * sequence b.
+ *   format  of the cache; MLA_CACHE_STORAGE with both dtypes
+ *   rows    [n_rows, r_kv + G_r d_rope] out, storage dtype, 16-byte aligned: [c^KV | R_p k^PE], latents
+ *           of MLA_CACHE_E4M3 as the values that they stand for (exact in bf16)
+ *   offsets device int32 [batch + 1], not decreasing, start device int32 [batch]
+ * Packed rows outside [offsets[0], offsets[batch]) are left as they were; a row at a position outside
+ * its sequence's table or on no page becomes NaN.  Whether a row was ever written is the caller's to
+ * know.  At most 8388608 rows, G_r d_rope at most 8192. */
+int mla_recon_cache_read(const mla_recon_cfg *cfg, const mla_paged_cache *cache, int32_t format,
+                         void *rows, int32_t n_rows, const int32_t *offsets, const int32_t *start,
+                         void *hip_stream);
+
+/* mla_recon_decode_paged and mla_recon_prefill_paged over a cache of format MLA_CACHE_E4M3: the same
+ * arguments, rules and limits, with workspaces of their own sizes. */
+size_t mla_recon_decode_e4m3_workspace_size(const mla_recon_cfg *cfg, int32_t max_len);
+int mla_recon_decode_e4m3(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
+                          int32_t max_len, const int32_t *lengths, const void *Wuk, const void *Wuv,
+                          void *o, void *ws, size_t ws_bytes, void *hip_stream);
+size_t mla_recon_prefill_e4m3_workspace_size(const mla_recon_cfg *cfg, int32_t n_q, int32_t n_kv);
+int mla_recon_prefill_e4m3(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
+                           const int32_t *q_offsets, const mla_paged_cache *cache, int32_t n_kv,
+                           const int32_t *kv_offsets, const void *Wuk, const void *Wuv, void *o,
+                           void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Decoding for sequences that begin with the same rows (samples of one prompt, users behind one system
+ * prompt): as mla_recon_decode_paged, but the shared rows are read once for a group.
+ * Group g is the sequences group_offsets[g] .. group_offsets[g + 1] - 1; the first shared_len[g] rows
+ * of each of them are the same values, in the same pages or in copies of them.  Which of the copies
+ * is read is not defined.  Sequences of no group, and rows behind the shared ones, are read for
+ * each sequence; where a sequence of a group has fewer rows than shared_len[g] only the rows that all
+ * its sequences with any rows have are read once.  shared_len is clamped to [0, max_len].
+ *   format        of the cache (cfg->dtype must be MLA_BF16)
+ *   n_groups      number of groups, 0 to batch; with 0 the two arrays may be NULL
+ *   group_offsets device int32 [n_groups + 1], not decreasing, within [0, batch]
+ *   shared_len    device int32 [n_groups]
+ * Everything else as for mla_recon_decode_paged.  ws 16-byte aligned, of
+ * mla_recon_decode_shared_workspace_size bytes (0 = unsupported or invalid) for this cfg, max_len and
+ * n_groups, or of those for more sequences, groups or a larger max_len. */
+size_t mla_recon_decode_shared_workspace_size(const mla_recon_cfg *cfg, int32_t format, int32_t max_len,
+                                              int32_t n_groups);
+int mla_recon_decode_shared(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
+                            int32_t format, int32_t max_len, const int32_t *lengths, int32_t n_groups,
+                            const int32_t *group_offsets, const int32_t *shared_len, const void *Wuk,
+                            const void *Wuv, void *o, void *ws, size_t ws_bytes, void *hip_stream);
+
 /* Text of the last error on the calling thread ("" if none). */
 const char *mla_recon_last_error(void);
 

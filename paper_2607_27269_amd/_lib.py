@@ -22,6 +22,8 @@ MLA_ERR_WORKSPACE = -3
 MLA_ERR_HIP = -4
 MLA_BF16 = 0
 MLA_FP32 = 1
+MLA_CACHE_STORAGE = 0
+MLA_CACHE_E4M3 = 1
 # static scratch of mla_recon_decode_noalloc (include/mla_recon.h)
 MLA_DECODE_NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -147,6 +149,20 @@ def lib() -> ctypes.CDLL:
                                               vp, sz, vp]
         L.mla_recon_cache_copy_pages.argtypes = [vp, i32, ctypes.c_int64, i32, ctypes.c_int64,
                                                  P(ctypes.c_int32), i32, vp]
+        L.mla_recon_cache_page_bytes.argtypes = [P(Cfg), i32, i32]
+        L.mla_recon_cache_page_bytes.restype = ctypes.c_int64
+        L.mla_recon_cache_append_e4m3.argtypes = L.mla_recon_cache_append.argtypes
+        L.mla_recon_cache_read.argtypes = [P(Cfg), P(PagedCache), i32, vp, i32, vp, vp, vp]
+        L.mla_recon_decode_e4m3_workspace_size.argtypes = [P(Cfg), i32]
+        L.mla_recon_decode_e4m3_workspace_size.restype = sz
+        L.mla_recon_decode_e4m3.argtypes = L.mla_recon_decode_paged.argtypes
+        L.mla_recon_prefill_e4m3_workspace_size.argtypes = [P(Cfg), i32, i32]
+        L.mla_recon_prefill_e4m3_workspace_size.restype = sz
+        L.mla_recon_prefill_e4m3.argtypes = L.mla_recon_prefill_paged.argtypes
+        L.mla_recon_decode_shared_workspace_size.argtypes = [P(Cfg), i32, i32, i32]
+        L.mla_recon_decode_shared_workspace_size.restype = sz
+        L.mla_recon_decode_shared.argtypes = [P(Cfg), vp, P(PagedCache), i32, i32, vp, i32, vp, vp, vp, vp,
+                                              vp, vp, sz, vp]
         L.mla_recon_adamw.argtypes = [P(AdamwTensor), i32, i32, i32, ctypes.c_float,
                                       ctypes.c_float, ctypes.c_float, ctypes.c_float,
                                       ctypes.c_float, vp]
@@ -160,6 +176,8 @@ def lib() -> ctypes.CDLL:
                   "mla_recon_decode", "mla_recon_decode_noalloc", "mla_recon_prefill",
                   "mla_recon_fold_uv_into_o", "mla_recon_cache_append", "mla_recon_decode_paged",
                   "mla_recon_prefill_paged", "mla_recon_cache_copy_pages",
+                  "mla_recon_cache_append_e4m3", "mla_recon_cache_read", "mla_recon_decode_e4m3",
+                  "mla_recon_prefill_e4m3", "mla_recon_decode_shared",
                   "mla_recon_prof_enable",
                   "mla_recon_prof_read"):
             getattr(L, f).restype = ctypes.c_int32
@@ -328,6 +346,55 @@ def mla_recon_cache_copy_pages(pool: int, n_layers: int, layer_stride: int, n_pa
     """``pairs``: a ctypes pointer to (or array of) the host's 2 n_pairs page numbers."""
     _check(lib().mla_recon_cache_copy_pages(pool, n_layers, layer_stride, n_pages, page_bytes, pairs,
                                             n_pairs, stream))
+
+
+def mla_recon_cache_page_bytes(cfg: Cfg, fmt: int, page_size: int) -> int:
+    return int(lib().mla_recon_cache_page_bytes(ctypes.byref(cfg), fmt, page_size))
+
+
+def mla_recon_cache_append_e4m3(cfg: Cfg, cache: PagedCache, rows: int | None, q: int | None,
+                                q_out: int | None, n_rows: int, offsets: int, start: int, inv_freq: int,
+                                stream: int) -> None:
+    _check(lib().mla_recon_cache_append_e4m3(ctypes.byref(cfg), _ref(cache), rows, q, q_out, n_rows,
+                                             offsets, start, inv_freq, stream))
+
+
+def mla_recon_cache_read(cfg: Cfg, cache: PagedCache, fmt: int, rows: int, n_rows: int, offsets: int,
+                         start: int, stream: int) -> None:
+    _check(lib().mla_recon_cache_read(ctypes.byref(cfg), _ref(cache), fmt, rows, n_rows, offsets, start,
+                                      stream))
+
+
+def mla_recon_decode_e4m3_workspace_size(cfg: Cfg, max_len: int) -> int:
+    return int(lib().mla_recon_decode_e4m3_workspace_size(ctypes.byref(cfg), max_len))
+
+
+def mla_recon_decode_e4m3(cfg: Cfg, q: int, cache: PagedCache, max_len: int, lengths: int, Wuk: int,
+                          Wuv: int, o: int, ws: int, ws_bytes: int, stream: int) -> None:
+    _check(lib().mla_recon_decode_e4m3(ctypes.byref(cfg), q, _ref(cache), max_len, lengths, Wuk, Wuv, o,
+                                       ws, ws_bytes, stream))
+
+
+def mla_recon_prefill_e4m3_workspace_size(cfg: Cfg, n_q: int, n_kv: int) -> int:
+    return int(lib().mla_recon_prefill_e4m3_workspace_size(ctypes.byref(cfg), n_q, n_kv))
+
+
+def mla_recon_prefill_e4m3(cfg: Cfg, q: int, n_q: int, q_offsets: int, cache: PagedCache, n_kv: int,
+                           kv_offsets: int, Wuk: int, Wuv: int, o: int, ws: int, ws_bytes: int,
+                           stream: int) -> None:
+    _check(lib().mla_recon_prefill_e4m3(ctypes.byref(cfg), q, n_q, q_offsets, _ref(cache), n_kv,
+                                        kv_offsets, Wuk, Wuv, o, ws, ws_bytes, stream))
+
+
+def mla_recon_decode_shared_workspace_size(cfg: Cfg, fmt: int, max_len: int, n_groups: int) -> int:
+    return int(lib().mla_recon_decode_shared_workspace_size(ctypes.byref(cfg), fmt, max_len, n_groups))
+
+
+def mla_recon_decode_shared(cfg: Cfg, q: int, cache: PagedCache, fmt: int, max_len: int, lengths: int,
+                            n_groups: int, group_offsets: int | None, shared_len: int | None, Wuk: int,
+                            Wuv: int, o: int, ws: int, ws_bytes: int, stream: int) -> None:
+    _check(lib().mla_recon_decode_shared(ctypes.byref(cfg), q, _ref(cache), fmt, max_len, lengths, n_groups,
+                                         group_offsets, shared_len, Wuk, Wuv, o, ws, ws_bytes, stream))
 
 
 def mla_recon_prof_enable(kclass: int, on: bool) -> None:

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "mla_recon.h"
+#include "cache_rows.h"
 #include "kernels.h"
 #include "mfma.h"
 #include "simt.h"
@@ -1073,12 +1074,37 @@ static PagedPool pool_of(const mla_recon_cfg* cfg, const mla_paged_cache* c) {
                    cfg->kv_rank + cfg->s_rope_groups * cfg->rope_dim};
 }
 
-int mla_recon_cache_append(const mla_recon_cfg* cfg, const mla_paged_cache* cache, const void* rows,
-                           const void* q, void* q_out, int32_t n_rows, const int32_t* offsets,
-                           const int32_t* start, const float* inv_freq, void* hip_stream) {
+static int format_check(const mla_recon_cfg* cfg, int32_t format, const char* who) {
+  if (format != MLA_CACHE_STORAGE && format != MLA_CACHE_E4M3)
+    return fail(MLA_ERR_INVALID_ARG, "%s: unknown cache format %d", who, format);
+  if (format == MLA_CACHE_E4M3 && cfg->dtype != MLA_BF16)
+    return fail(MLA_ERR_UNSUPPORTED, "%s: an e4m3 cache serves bf16 only", who);
+  return MLA_OK;
+}
+
+int64_t mla_recon_cache_page_bytes(const mla_recon_cfg* cfg, int32_t format, int32_t page_size) {
+  g_err[0] = 0;
+  if (check_cfg(cfg) || format_check(cfg, format, "cache_page_bytes")) return 0;
+  if (page_size < 1) {
+    fail(MLA_ERR_INVALID_ARG, "cache_page_bytes: page_size must be positive");
+    return 0;
+  }
+  const int64_t pe = (int64_t)cfg->s_rope_groups * cfg->rope_dim;
+  if (pe + cfg->kv_rank > 1 << 28) {
+    fail(MLA_ERR_INVALID_ARG, "cache_page_bytes: rows too wide");
+    return 0;
+  }
+  if (format == MLA_CACHE_E4M3) return E4m3Page(page_size, cfg->kv_rank, (int)pe).bytes;
+  return page_size * (pe + cfg->kv_rank) * (cfg->dtype == MLA_FP32 ? 4 : 2);
+}
+
+static int append_rows(const mla_recon_cfg* cfg, const mla_paged_cache* cache, bool e4m3, const void* rows,
+                       const void* q, void* q_out, int32_t n_rows, const int32_t* offsets,
+                       const int32_t* start, const float* inv_freq, void* hip_stream) {
   g_err[0] = 0;
   int rc = check_cfg(cfg);
   if (rc) return rc;
+  if (e4m3 && (rc = format_check(cfg, MLA_CACHE_E4M3, "cache_append"))) return rc;
   if ((rc = paged_check(cfg, cache, "cache_append"))) return rc;
   if (n_rows < 0) return fail(MLA_ERR_INVALID_ARG, "cache_append: negative number of rows");
   if (n_rows > 1 << 23) return fail(MLA_ERR_UNSUPPORTED, "cache_append: at most %d rows per call", 1 << 23);
@@ -1096,8 +1122,43 @@ int mla_recon_cache_append(const mla_recon_cfg* cfg, const mla_paged_cache* cach
   a.B = cfg->batch; a.H = cfg->n_heads; a.dn = cfg->nope_dim; a.dr = cfg->rope_dim;
   a.rkv = cfg->kv_rank; a.Gr = cfg->s_rope_groups; a.n_rows = n_rows; a.rows = rows; a.q = q;
   a.q_out = q_out; a.offsets = offsets; a.start = start; a.inv_freq = inv_freq;
-  a.t = cfg->dtype == MLA_FP32 ? DT_F32 : DT_BF16;
+  a.t = cfg->dtype == MLA_FP32 ? DT_F32 : DT_BF16; a.e4m3 = e4m3;
   HIP_TRY(cache_append(a, (hipStream_t)hip_stream));
+  return MLA_OK;
+}
+
+int mla_recon_cache_append(const mla_recon_cfg* cfg, const mla_paged_cache* cache, const void* rows,
+                           const void* q, void* q_out, int32_t n_rows, const int32_t* offsets,
+                           const int32_t* start, const float* inv_freq, void* hip_stream) {
+  return append_rows(cfg, cache, false, rows, q, q_out, n_rows, offsets, start, inv_freq, hip_stream);
+}
+
+int mla_recon_cache_append_e4m3(const mla_recon_cfg* cfg, const mla_paged_cache* cache, const void* rows,
+                                const void* q, void* q_out, int32_t n_rows, const int32_t* offsets,
+                                const int32_t* start, const float* inv_freq, void* hip_stream) {
+  return append_rows(cfg, cache, true, rows, q, q_out, n_rows, offsets, start, inv_freq, hip_stream);
+}
+
+int mla_recon_cache_read(const mla_recon_cfg* cfg, const mla_paged_cache* cache, int32_t format,
+                         void* rows, int32_t n_rows, const int32_t* offsets, const int32_t* start,
+                         void* hip_stream) {
+  g_err[0] = 0;
+  int rc = check_cfg(cfg);
+  if (rc) return rc;
+  if ((rc = format_check(cfg, format, "cache_read"))) return rc;
+  if ((rc = paged_check(cfg, cache, "cache_read"))) return rc;
+  if (n_rows < 0) return fail(MLA_ERR_INVALID_ARG, "cache_read: negative number of rows");
+  if (n_rows > 1 << 23) return fail(MLA_ERR_UNSUPPORTED, "cache_read: at most %d rows per call", 1 << 23);
+  if (!rows || !offsets || !start) return fail(MLA_ERR_INVALID_ARG, "cache_read: NULL pointer argument");
+  if ((uintptr_t)rows % 16) return fail(MLA_ERR_INVALID_ARG, "cache_read: rows must be 16-byte aligned");
+  if ((int64_t)cfg->s_rope_groups * cfg->rope_dim > 8192)
+    return fail(MLA_ERR_UNSUPPORTED, "cache_read: %d positional keys of %d values (at most 8192 in all)",
+                cfg->s_rope_groups, cfg->rope_dim);
+  CacheRead r;
+  r.c = pool_of(cfg, cache);
+  r.B = cfg->batch; r.rkv = cfg->kv_rank; r.n_rows = n_rows; r.rows = rows; r.offsets = offsets;
+  r.start = start; r.t = cfg->dtype == MLA_FP32 ? DT_F32 : DT_BF16; r.e4m3 = format == MLA_CACHE_E4M3;
+  HIP_TRY(cache_read(r, (hipStream_t)hip_stream));
   return MLA_OK;
 }
 
@@ -1142,6 +1203,77 @@ int mla_recon_decode_paged(const mla_recon_cfg* cfg, const void* q, const mla_pa
   return MLA_OK;
 }
 
+// ---- either format, rows that sequences share
+static size_t shared_bytes(const mla_recon_cfg* cfg, int32_t max_len, int32_t n_groups) {
+  return decode_shared_ws_bytes(cfg->batch, cfg->n_heads, cfg->kv_rank + cfg->rope_dim, cfg->kv_rank, max_len, n_groups);
+}
+
+static int decode_shared_check(const mla_recon_cfg* cfg, int32_t format, int32_t max_len, int32_t n_groups, const char* who) {
+  int rc = decode_paged_check(cfg, max_len);
+  if (rc) return rc;
+  if ((rc = format_check(cfg, format, who))) return rc;
+  if (n_groups < 0 || n_groups > cfg->batch)
+    return fail(MLA_ERR_INVALID_ARG, "%s: %d groups of %d sequences", who, n_groups, cfg->batch);
+  return MLA_OK;
+}
+
+static int decode_shared_call(const mla_recon_cfg* cfg, const void* q, const mla_paged_cache* cache, int32_t format,
+                              int32_t max_len, const int32_t* lengths, int32_t n_groups,
+                              const int32_t* group_offsets, const int32_t* shared_len, const void* Wuk,
+                              const void* Wuv, void* o, void* ws, size_t ws_bytes, void* hip_stream, const char* who) {
+  g_err[0] = 0;
+  int rc = decode_shared_check(cfg, format, max_len, n_groups, who);
+  if (rc) return rc;
+  if ((rc = paged_check(cfg, cache, who))) return rc;
+  if ((rc = decode_args(cfg, q, cache->pool, lengths, cfg->nope_dim ? Wuk : Wuv, Wuv, o, who))) return rc;
+  if (n_groups > 0 && (!group_offsets || !shared_len))
+    return fail(MLA_ERR_INVALID_ARG, "%s: NULL group offsets or shared lengths", who);
+  if (!ws) return fail(MLA_ERR_INVALID_ARG, "%s: NULL workspace", who);
+  if ((uintptr_t)ws % 16) return fail(MLA_ERR_INVALID_ARG, "%s: ws must be 16-byte aligned", who);
+  const size_t need = shared_bytes(cfg, max_len, n_groups);
+  if (ws_bytes < need)
+    return fail(MLA_ERR_WORKSPACE, "%s: workspace too small: %zu < %zu bytes", who, ws_bytes, need);
+  DecodeShared p;
+  DecodePaged& d = p.d;
+  d.c = pool_of(cfg, cache);
+  d.B = cfg->batch; d.H = cfg->n_heads; d.dn = cfg->nope_dim; d.dr = cfg->rope_dim;
+  d.rkv = cfg->kv_rank; d.dv = cfg->head_dim; d.hpg = cfg->n_heads / cfg->s_kv_groups;
+  d.q = q; d.len = lengths; d.Wuk = Wuk; d.Wuv = Wuv; d.scale = cfg->softmax_scale; d.o = o; d.ws = ws;
+  d.max_len = (int)std::min<int64_t>(max_len, (int64_t)cache->page_size * cache->max_pages);
+  p.e4m3 = format == MLA_CACHE_E4M3;
+  p.n_groups = n_groups; p.group_off = group_offsets; p.shared_len = shared_len;
+  HIP_TRY(decode_shared(p, (hipStream_t)hip_stream));
+  return MLA_OK;
+}
+
+size_t mla_recon_decode_shared_workspace_size(const mla_recon_cfg* cfg, int32_t format, int32_t max_len,
+                                              int32_t n_groups) {
+  g_err[0] = 0;
+  if (decode_shared_check(cfg, format, max_len, n_groups, "decode_shared")) return 0;
+  return shared_bytes(cfg, max_len, n_groups);
+}
+
+int mla_recon_decode_shared(const mla_recon_cfg* cfg, const void* q, const mla_paged_cache* cache,
+                            int32_t format, int32_t max_len, const int32_t* lengths, int32_t n_groups,
+                            const int32_t* group_offsets, const int32_t* shared_len, const void* Wuk,
+                            const void* Wuv, void* o, void* ws, size_t ws_bytes, void* hip_stream) {
+  return decode_shared_call(cfg, q, cache, format, max_len, lengths, n_groups, group_offsets, shared_len, Wuk, Wuv, o,
+                            ws, ws_bytes, hip_stream, "decode_shared");
+}
+
+size_t mla_recon_decode_e4m3_workspace_size(const mla_recon_cfg* cfg, int32_t max_len) {
+  g_err[0] = 0;
+  if (decode_shared_check(cfg, MLA_CACHE_E4M3, max_len, 0, "decode_e4m3")) return 0;
+  return shared_bytes(cfg, max_len, 0);
+}
+
+int mla_recon_decode_e4m3(const mla_recon_cfg* cfg, const void* q, const mla_paged_cache* cache,
+                          int32_t max_len, const int32_t* lengths, const void* Wuk, const void* Wuv,
+                          void* o, void* ws, size_t ws_bytes, void* hip_stream) {
+  return decode_shared_call(cfg, q, cache, MLA_CACHE_E4M3, max_len, lengths, 0, nullptr, nullptr, Wuk, Wuv, o, ws,
+                            ws_bytes, hip_stream, "decode_e4m3");
+}
+
 constexpr int32_t PREFILL_PAGED_MAX = 1 << 20;
 
 static int prefill_paged_check(const mla_recon_cfg* cfg, int32_t n_q, int32_t n_kv, PrefillPaged* p) {
@@ -1170,10 +1302,10 @@ size_t mla_recon_prefill_paged_workspace_size(const mla_recon_cfg* cfg, int32_t 
   return prefill_paged_ws_bytes(p);
 }
 
-int mla_recon_prefill_paged(const mla_recon_cfg* cfg, const void* q, int32_t n_q,
-                            const int32_t* q_offsets, const mla_paged_cache* cache, int32_t n_kv,
-                            const int32_t* kv_offsets, const void* Wuk, const void* Wuv, void* o,
-                            void* ws, size_t ws_bytes, void* hip_stream) {
+static int prefill_call(const mla_recon_cfg* cfg, bool e4m3, const void* q, int32_t n_q,
+                        const int32_t* q_offsets, const mla_paged_cache* cache, int32_t n_kv,
+                        const int32_t* kv_offsets, const void* Wuk, const void* Wuv, void* o,
+                        void* ws, size_t ws_bytes, void* hip_stream) {
   g_err[0] = 0;
   PrefillPaged p;
   int rc = prefill_paged_check(cfg, n_q, n_kv, &p);
@@ -1189,8 +1321,28 @@ int mla_recon_prefill_paged(const mla_recon_cfg* cfg, const void* q, int32_t n_q
   if (n_q == 0) return MLA_OK;
   p.c = pool_of(cfg, cache);
   p.q = q; p.q_off = q_offsets; p.kv_off = kv_offsets; p.Wuk = Wuk; p.Wuv = Wuv; p.o = o; p.ws = ws;
+  p.e4m3 = e4m3;
   HIP_TRY(prefill_paged(p, (hipStream_t)hip_stream));
   return MLA_OK;
+}
+
+int mla_recon_prefill_paged(const mla_recon_cfg* cfg, const void* q, int32_t n_q,
+                            const int32_t* q_offsets, const mla_paged_cache* cache, int32_t n_kv,
+                            const int32_t* kv_offsets, const void* Wuk, const void* Wuv, void* o,
+                            void* ws, size_t ws_bytes, void* hip_stream) {
+  return prefill_call(cfg, false, q, n_q, q_offsets, cache, n_kv, kv_offsets, Wuk, Wuv, o, ws, ws_bytes, hip_stream);
+}
+
+// (the same workspace: the gathered rows are bf16)
+size_t mla_recon_prefill_e4m3_workspace_size(const mla_recon_cfg* cfg, int32_t n_q, int32_t n_kv) {
+  return mla_recon_prefill_paged_workspace_size(cfg, n_q, n_kv);
+}
+
+int mla_recon_prefill_e4m3(const mla_recon_cfg* cfg, const void* q, int32_t n_q,
+                           const int32_t* q_offsets, const mla_paged_cache* cache, int32_t n_kv,
+                           const int32_t* kv_offsets, const void* Wuk, const void* Wuv, void* o,
+                           void* ws, size_t ws_bytes, void* hip_stream) {
+  return prefill_call(cfg, true, q, n_q, q_offsets, cache, n_kv, kv_offsets, Wuk, Wuv, o, ws, ws_bytes, hip_stream);
 }
 
 // Every destination is named once and is no source (a page that is both would be read while it

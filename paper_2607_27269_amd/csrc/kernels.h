@@ -293,8 +293,20 @@ struct CacheAppend {
   const int32_t* start;            // [B] device
   const float* inv_freq;           // [Gr][dr / 2]
   DType t;
+  bool e4m3;                       // the pool's format is MLA_CACHE_E4M3 (cache_rows.h)
 };
 hipError_t cache_append(const CacheAppend& a, hipStream_t s);
+// Cached rows of either format back as packed rows.
+struct CacheRead {
+  PagedPool c;
+  int B, rkv, n_rows;
+  void* rows;                      // [n_rows][width]
+  const int32_t* offsets;          // [B + 1] device
+  const int32_t* start;            // [B] device
+  DType t;
+  bool e4m3;
+};
+hipError_t cache_read(const CacheRead& c, hipStream_t s);
 // page pairs[2 i] -> pages pairs[2 i + 1] (host array) of every layer; bytes multiples of 16
 hipError_t cache_copy_pages(void* pool, int n_layers, int64_t layer_stride, int64_t page_bytes,
                             const int32_t* pairs, int n_pairs, hipStream_t s);
@@ -314,6 +326,18 @@ struct DecodePaged {
 size_t decode_paged_ws_bytes(int B, int H, int DK, int DVL, int max_len);
 hipError_t decode_paged(const DecodePaged& d, hipStream_t s);
 
+// The same over a cache of either format, the first rows of groups of sequences read once for all of a
+// group (decode_shared.hip).
+struct DecodeShared {
+  DecodePaged d;                   // ws of decode_shared_ws_bytes
+  bool e4m3;
+  int n_groups;
+  const int32_t* group_off;        // [n_groups + 1] device
+  const int32_t* shared_len;       // [n_groups] device
+};
+size_t decode_shared_ws_bytes(int B, int H, int DK, int DVL, int max_len, int n_groups);
+hipError_t decode_shared(const DecodeShared& d, hipStream_t s);
+
 // Causal attention of packed query tokens over the cached rows of their sequences.
 struct PrefillPaged {
   PagedPool c;
@@ -325,6 +349,7 @@ struct PrefillPaged {
   float scale;
   void* o;                         // [n_q][H][dv] bf16
   void* ws;
+  bool e4m3 = false;               // the pool's format
 };
 size_t prefill_paged_ws_bytes(const PrefillPaged& p);
 hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s);

@@ -3,6 +3,7 @@
 // Position p of sequence b lies in row p % page_size of page table[b][p / page_size] of the
 // pool, and the row is [c^KV | R_p k^PE] (Eq. 5's cache).  Row addresses are 64-bit: a pool of
 // 288 GB holds 2.7e8 rows of 1152 bytes.
+#include "cache_rows.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -40,23 +41,13 @@ template <> struct Vec4<float> {
   static __device__ __forceinline__ V down(f32x4 f) { return f; }
 };
 
-// The sequence of packed row i: the largest b with offsets[b] <= i (offsets[0] <= i).
-__device__ __forceinline__ int sequence_of(const int32_t* offsets, int B, int i) {
-  int lo = 0, hi = B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (offsets[mid] <= i) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
 // A workgroup per packed row.  Angles p inv_freq in fp64 turns (one product and one subtraction
 // of whole turns, so a position far into a long cache keeps its fraction), sine and cosine of
 // the fraction in fp32; they are shared by the row's heads through LDS.  Bound by memory: every
 // value is read once and written once: 10981 rows of 6720 values (bf16) 52 us, 5.6 TB/s, where a copy of
 // 1 GiB reaches 5.2; a few rows 4.8 us, a launch.
-template <typename T>
+// E4M3: the first wavefront takes the row's latents, 8 a lane, whose largest gives their power of two.
+template <typename T, bool E4M3>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendDev a) {
   using V = typename Vec4<T>::V;
   extern __shared__ __attribute__((aligned(16))) float trig[];  // [Gr][dr / 2] cosines, then the sines
@@ -87,11 +78,36 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendDev a) {
     if (p >= 0 && pg < a.max_pages) page = a.table[(int64_t)b * a.max_pages + pg];
     if (page >= 0 && page < a.n_pages) {
       const T* x = (const T*)a.rows + (int64_t)row * a.width;
-      T* y = (T*)a.pool + ((int64_t)page * a.page_size + (p - pg * a.page_size)) * a.width;
-      for (int u = tid; u < a.rkv / 4; u += 256) *(V*)(y + 4 * u) = *(const V*)(x + 4 * u);
+      const int r = (int)(p - pg * a.page_size);
+      T* pe;
+      if constexpr (E4M3) {
+        const E4m3Page layout(a.page_size, a.rkv, a.Gr * a.dr);
+        char* y = layout.row(a.pool, page, r);
+        pe = (T*)(y + a.rkv);
+        if (tid < 64) {
+          uint32_t top = 0u;
+          for (int c = 8 * tid; c < a.rkv; c += 512) {
+            const u32x4 v = *(const u32x4*)(x + c);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t lo = v[k] << 16 & 0x7fffffffu, hi = v[k] & 0x7fff0000u;
+              top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+            }
+          }
+#pragma unroll
+          for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+          const int e = e4m3_exponent(top);
+          for (int c = 8 * tid; c < a.rkv; c += 512) *(u32x2*)(y + c) = to_e4m3(*(const u32x4*)(x + c), power_of_two(-e));
+          if (tid == 0) *layout.power(a.pool, page, r) = power_of_two(e);
+        }
+      } else {
+        T* y = (T*)a.pool + ((int64_t)page * a.page_size + r) * a.width;
+        pe = y + a.rkv;
+        for (int u = tid; u < a.rkv / 4; u += 256) *(V*)(y + 4 * u) = *(const V*)(x + 4 * u);
+      }
       for (int u = tid; u < nang / 4; u += 256) {
         const int g = 4 * u / np, d = 4 * u % np;
-        rotate(x + a.rkv + g * a.dr, y + a.rkv + g * a.dr, g, d);
+        rotate(x + a.rkv + g * a.dr, pe + g * a.dr, g, d);
       }
     }
   }
@@ -111,6 +127,48 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendDev a) {
       const int i = u / per;
       rotate(x + i * dq + a.dn, y + i * dq + a.dn, i / hpr, 4 * (u % per));
     }
+  }
+}
+
+// ---- reading rows back ----------------------------------------------------------------
+struct ReadDev {
+  PagedPool c;
+  int B, rkv, pe, n_rows;
+  char* rows;
+  const int32_t* offsets;
+  const int32_t* start;
+};
+
+// A wavefront per packed row, 16 bytes a lane.  Bound by memory.
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(256) void cache_read_kernel(ReadDev a) {
+  const int row = 4 * blockIdx.x + wave_id(), lane = threadIdx.x & 63;
+  const PagedPool& c = a.c;
+  if (row >= a.n_rows || row < a.offsets[0] || row >= a.offsets[a.B]) return;
+  const int b = sequence_of(a.offsets, a.B, row);
+  const int64_t p = (int64_t)a.start[b] + (row - a.offsets[b]), pg = p < 0 ? -1 : p / c.page_size;
+  int page = -1;
+  if (pg >= 0 && pg < c.max_pages) page = c.table[(int64_t)b * c.max_pages + pg];
+  const int r = (int)(p - pg * c.page_size);
+  constexpr int PER = 16 / sizeof(T);  // values of 16 bytes
+  T* y = (T*)a.rows + (int64_t)row * c.width;
+  if (page < 0 || page >= c.n_pages) {
+    const uint32_t nan = sizeof(T) == 4 ? 0x7fc00000u : 0x7fc07fc0u;
+    for (int d = PER * lane; d < c.width; d += 64 * PER) *(u32x4*)(y + d) = u32x4{nan, nan, nan, nan};
+    return;
+  }
+  if constexpr (E4M3) {
+    const E4m3Page layout(c.page_size, a.rkv, a.pe);
+    const char* x = layout.row(c.pool, page, r);
+    const float power = *layout.power(c.pool, page, r);
+    for (int d = 8 * lane; d < a.rkv; d += 512) *(u32x4*)(y + d) = from_e4m3(*(const u32x2*)(x + d), power);
+    for (int d = 8 * lane; d < a.pe; d += 512) {  // (8-byte loads: rows are multiples of 8 bytes)
+      const u32x2 *v = (const u32x2*)(x + a.rkv + 2 * d), lo = v[0], hi = v[1];
+      *(u32x4*)(y + a.rkv + d) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+  } else {
+    const T* x = (const T*)c.pool + ((int64_t)page * c.page_size + r) * c.width;
+    for (int d = PER * lane; d < c.width; d += 64 * PER) *(u32x4*)(y + d) = *(const u32x4*)(x + d);
   }
 }
 
@@ -147,12 +205,35 @@ hipError_t cache_append(const CacheAppend& c, hipStream_t s) {
   a.offsets = c.offsets; a.start = c.start; a.inv_freq = c.inv_freq;
   const size_t lds = (size_t)c.Gr * c.dr * 4;
   prof_begin(KC_ELEM, s);
-  if (c.t == DT_BF16)
-    cache_append_kernel<bf16_t><<<c.n_rows, 256, lds, s>>>(a);
+  if (c.e4m3)
+    cache_append_kernel<bf16_t, true><<<c.n_rows, 256, lds, s>>>(a);
+  else if (c.t == DT_BF16)
+    cache_append_kernel<bf16_t, false><<<c.n_rows, 256, lds, s>>>(a);
   else
-    cache_append_kernel<float><<<c.n_rows, 256, lds, s>>>(a);
+    cache_append_kernel<float, false><<<c.n_rows, 256, lds, s>>>(a);
   const double width = (c.rows ? c.c.width : 0) + (c.q ? (double)c.H * (c.dn + c.dr) : 0.0);
-  prof_end(KC_ELEM, s, 0.0, 2.0 * c.n_rows * width * dsize(c.t), KLABEL("cache_append_kernel"));
+  prof_end(KC_ELEM, s, 0.0,
+           2.0 * c.n_rows * width * dsize(c.t) - (c.e4m3 && c.rows ? (double)c.n_rows * (c.rkv - 4) : 0.0),
+           c.e4m3 ? KLABEL("cache_append_kernel<e4m3>") : KLABEL("cache_append_kernel"));
+  return hipGetLastError();
+}
+
+hipError_t cache_read(const CacheRead& c, hipStream_t s) {
+  if (c.n_rows == 0) return hipSuccess;
+  ReadDev a;
+  a.c = c.c; a.B = c.B; a.rkv = c.rkv; a.pe = c.c.width - c.rkv; a.n_rows = c.n_rows;
+  a.rows = (char*)c.rows; a.offsets = c.offsets; a.start = c.start;
+  const int grid = (c.n_rows + 3) / 4;
+  prof_begin(KC_ELEM, s);
+  if (c.e4m3)
+    cache_read_kernel<bf16_t, true><<<grid, 256, 0, s>>>(a);
+  else if (c.t == DT_BF16)
+    cache_read_kernel<bf16_t, false><<<grid, 256, 0, s>>>(a);
+  else
+    cache_read_kernel<float, false><<<grid, 256, 0, s>>>(a);
+  prof_end(KC_ELEM, s, 0.0,
+           2.0 * c.n_rows * c.c.width * dsize(c.t) - (c.e4m3 ? (double)c.n_rows * (c.rkv - 4) : 0.0),
+           KLABEL("cache_read_kernel"));
   return hipGetLastError();
 }
 

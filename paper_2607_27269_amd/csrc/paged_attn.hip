@@ -2,6 +2,7 @@
 // against the cache rows is [W_UK[g]^T q^nope_i ; q^rope_i], its output W_UV[g] applied to the
 // attention-weighted latent, g = i / (H / G_kv)), packed prompts with keys and values written out.
 #include "attn_common.h"
+#include "cache_rows.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -795,6 +796,7 @@ __device__ __forceinline__ u32x4 scaled(u32x4 v, int k) {
     o[q] = pack2bf(__uint_as_float(v[q] << 16) * f * f2, __uint_as_float(v[q] & 0xffff0000u) * f * f2);
   return o;
 }
+template <bool E4M3>
 __global__ __launch_bounds__(256) void gather_rows_kernel(GatherDev a) {
   const int row = 4 * blockIdx.x + wave_id(), lane = threadIdx.x & 63;
   const PagedPool& c = a.c;
@@ -828,9 +830,17 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(GatherDev a) {
     const int page = p >= 0 && pg < c.max_pages ? c.table[(int64_t)lo * c.max_pages + pg] : -1;
     bool any = page < 0 || page >= c.n_pages;
     if (!any) {
-      const bf16_t* src = (const bf16_t*)c.pool + ((int64_t)page * c.page_size + p % c.page_size) * c.width;
-      if (in_lat) lat = *(const u32x4*)(src + 8 * lane);
-      if (in_pe) pe = *(const u32x4*)(src + a.rkv + 8 * lane);
+      if constexpr (E4M3) {
+        const E4m3Page layout(c.page_size, a.rkv, dr);
+        const char* src = layout.row(c.pool, page, p % c.page_size);
+        const float power = *layout.power(c.pool, page, p % c.page_size);
+        if (in_lat) lat = from_e4m3(*(const u32x2*)(src + 8 * lane), power);
+        if (in_pe) pe = *(const u32x4*)(src + a.rkv + 16 * lane);
+      } else {
+        const bf16_t* src = (const bf16_t*)c.pool + ((int64_t)page * c.page_size + p % c.page_size) * c.width;
+        if (in_lat) lat = *(const u32x4*)(src + 8 * lane);
+        if (in_pe) pe = *(const u32x4*)(src + a.rkv + 8 * lane);
+      }
       top = wave_max((int)top_exponent(lat));
       any = __ballot(top >= GATHER_TOP || top_exponent(pe) == 255u) != 0;
     }
@@ -914,8 +924,12 @@ hipError_t prefill_paged(const PrefillPaged& p, hipStream_t s) {
   g.c = p.c; g.kv_off = p.kv_off; g.B = p.B; g.n_kv = p.n_kv; g.rkv = p.rkv; g.nv = nv;
   g.Wuv = (const bf16_t*)p.Wuv; g.rows = (bf16_t*)(ws + l.rows); g.lat = (bf16_t*)(ws + l.lat);
   g.key_exp = (float*)(ws + l.key_exp); g.W = (bf16_t*)(ws + l.W); g.v_scale = (float*)(ws + l.v_scale);
-  gather_rows_kernel<<<(p.n_kv + 3) / 4 + (nv + 3) / 4, 256, 0, s>>>(g);
-  prof_end(KC_ELEM, s, 0.0, ((double)p.n_kv * (2 * W + p.rkv) + 2.0 * nv * p.rkv) * 2, KLABEL("gather_rows_kernel"));
+  const int grid = (p.n_kv + 3) / 4 + (nv + 3) / 4;
+  if (p.e4m3) gather_rows_kernel<true><<<grid, 256, 0, s>>>(g);
+  else gather_rows_kernel<false><<<grid, 256, 0, s>>>(g);
+  prof_end(KC_ELEM, s, 0.0,
+           ((double)p.n_kv * (2 * W + p.rkv) + 2.0 * nv * p.rkv) * 2 - (p.e4m3 ? (double)p.n_kv * (p.rkv - 4) : 0.0),
+           KLABEL("gather_rows_kernel"));
   if (p.n_kv > 0) {
     Gemm up[2];
     int n = 0;

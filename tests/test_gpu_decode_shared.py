@@ -1,0 +1,216 @@
+"""GPU tests of decoding behind shared prefixes, both cache formats, against float64 over each sequence's own
+rows.  Tolerance: that of decoding (tests/test_gpu_paged.py)."""
+import numpy as np
+import pytest
+
+from test_gpu_cache_e4m3 import E4m3Layer
+from test_gpu_paged import Layer, bf16, check_decode, ints, shape, up
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 4096
+
+
+def make(name, fmt, members, shared, tails, ps, seed, lo=0, hi=0, **kw):
+    """A layer whose groups' sequences have the pages of their first shared[g] rows in common (whole
+    pages; the rest of the shared rows copied), `lo` sequences of no group before and `hi` behind."""
+    lens = [50 + 9 * i for i in range(lo)]
+    lens += [s + tails[k % len(tails)] for k, s in enumerate(s for m, s in zip(members, shared) for _ in range(m))]
+    lens += [20 + 31 * i for i in range(hi)]
+    lay = (E4m3Layer if fmt else Layer)(shape(name, **kw), lens, ps, seed=seed)
+    b = lo
+    for m, s in zip(members, shared):
+        for i in range(b, b + m):
+            lay.table[i, :s // ps] = lay.table[b, :s // ps]
+            for p in range(s // ps * ps, s):
+                src, dst = lay.table[b, p // ps], lay.table[i, p // ps]
+                lay.pool[dst, p % ps] = lay.pool[src, p % ps]
+                if fmt:
+                    lay.codes[dst, p % ps], lay.power[dst, p % ps] = lay.codes[src, p % ps], lay.power[src, p % ps]
+        b += m
+    lay.upload()
+    return lay, lens, np.concatenate([[0], np.cumsum(members)]) + lo
+
+
+class Shared:
+    def __init__(self, lay, q, lens, max_len, offsets, shared, fmt):
+        import torch
+        from paper_2607_27269_amd import _lib as L
+        self.lay, self.max_len, self.fmt, self.c = lay, max_len, int(fmt), lay.handle()
+        self.n = len(shared)
+        self.q, self.lens, self.off, self.shared = up(q), ints(lens), ints(offsets), ints(shared)
+        self.o = torch.full((len(q), lay.cfg.n_heads, lay.cfg.head_dim), 7.0, dtype=torch.bfloat16, device="cuda")
+        self.size = L.mla_recon_decode_shared_workspace_size(self.c[0], self.fmt, max_len, self.n)
+        assert self.size > 0, L.last_error()
+        self.ws = torch.full((self.size + GUARD,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def __call__(self):
+        import torch
+        from paper_2607_27269_amd import _lib as L
+        self.ws[self.size:] = 0xA5
+        L.mla_recon_decode_shared(self.c[0], self.q.data_ptr(), self.c[1], self.fmt, self.max_len, self.lens.data_ptr(),
+                                  self.n, self.off.data_ptr() if self.n else None,
+                                  self.shared.data_ptr() if self.n else None, self.lay.d_Wuk.data_ptr(),
+                                  self.lay.d_Wuv.data_ptr(), self.o.data_ptr(), self.ws.data_ptr(), self.size,
+                                  torch.cuda.current_stream().cuda_stream)
+        return self.o
+
+    def guard(self):
+        assert bool((self.ws[self.size:] == 0xA5).all()), "written behind the workspace"
+
+
+FORMATS = pytest.mark.parametrize("fmt", [False, True], ids=["bf16", "e4m3"])
+
+
+@FORMATS
+@pytest.mark.parametrize("name,members,shared,ps", [
+    ("tiny", [2], [64], 16), ("tiny", [9], [300], 7), ("05b", [4], [1000], 16), ("05b", [1, 3, 2], [65, 31, 500], 32),
+    ("1b", [5, 6], [128, 33], 16), ("8b", [4], [256], 64), ("8b", [3, 1, 13], [700, 90, 95], 24)])
+def test_groups(name, members, shared, ps, fmt):
+    print(f"[shared] {name} {members} x {shared} page {ps} {'e4m3' if fmt else 'bf16'}", flush=True)
+    lay, lens, off = make(name, fmt, members, shared, [1, 40, 3, 70, 32], ps, seed=ps)
+    q = lay.queries(len(lens))
+    d = Shared(lay, q, lens, max(lens), off, shared, fmt)
+    check_decode(lay, q, lens, d())
+    d.guard()
+
+
+@FORMATS
+@pytest.mark.parametrize("H,G", [(1, 1), (14, 2), (33, 1), (40, 8), (64, 2), (128, 128)])
+def test_head_counts(H, G, fmt):
+    print(f"[shared] {H} heads in {G} groups", flush=True)
+    lay, lens, off = make("05b", fmt, [5, 2], [200, 64], [7, 33], 16, seed=H, n_heads=H, s_kv_groups=G, n_kv_groups=G)
+    q = lay.queries(len(lens))
+    d = Shared(lay, q, lens, max(lens), off, [200, 64], fmt)
+    check_decode(lay, q, lens, d())
+    d.guard()
+
+
+@FORMATS
+def test_sequences_of_no_group(fmt):
+    lay, lens, off = make("1b", fmt, [3, 4], [96, 160], [5, 50], 32, seed=3, lo=2, hi=3)
+    q = lay.queries(len(lens))
+    d = Shared(lay, q, lens, max(lens), off, [96, 160], fmt)
+    check_decode(lay, q, lens, d())
+    d.guard()
+
+
+@FORMATS
+def test_no_groups_and_empty_groups(fmt):
+    lay, lens, off = make("05b", fmt, [4], [100], [9, 64], 16, seed=4)
+    q = lay.queries(4)
+    check_decode(lay, q, lens, Shared(lay, q, lens, max(lens), [0], [], fmt)())
+    # groups without sequences, with sequences and without rows, and all of them
+    check_decode(lay, q, lens, Shared(lay, q, lens, max(lens), [0, 0, 4, 4], [70, 100, 5], fmt)())
+    check_decode(lay, q, lens, Shared(lay, q, lens, max(lens), [0, 2, 4], [0, 100], fmt)())
+    check_decode(lay, q, lens, Shared(lay, q, lens, max(lens), [2, 2], [100], fmt)())
+
+
+@FORMATS
+def test_lengths_below_the_shared_rows(fmt):
+    """Sequences with fewer rows than their group shares, none among them; shared lengths past max_len and
+    negative ones."""
+    lay, lens, off = make("8b", fmt, [5], [200], [1, 30], 16, seed=5)
+    q = lay.queries(5)
+    now = [190, 230, 64, 0, 201]
+    check_decode(lay, q, now, Shared(lay, q, now, 230, off, [200], fmt)())
+    check_decode(lay, q, [0] * 5, Shared(lay, q, [0] * 5, 230, off, [200], fmt)())
+    now = [3, 1, 2, 7, 0]
+    check_decode(lay, q, now, Shared(lay, q, now, 230, off, [200], fmt)())
+    check_decode(lay, q, lens, Shared(lay, q, lens, 231, off, [-5], fmt)())
+    same = [200] * 5
+    check_decode(lay, q, same, Shared(lay, q, [200, 201, 2**31 - 1, 230, 210], 200, off, [2**31 - 1], fmt)())
+
+
+@FORMATS
+def test_many_sequences_and_groups(fmt):
+    """More sequences and groups than workgroups."""
+    rng = np.random.default_rng(6)
+    members = rng.integers(1, 4, 300)
+    shared = [int(s) for s in rng.integers(0, 100, 300)]
+    lay, lens, off = make("tiny", fmt, members, shared, [int(t) for t in rng.integers(1, 30, 41)], 8, seed=6)
+    q = lay.queries(len(lens))
+    d = Shared(lay, q, lens, max(lens), off, shared, fmt)
+    check_decode(lay, q, lens, d(), only=set(range(0, len(lens), 17)))
+    d.guard()
+
+
+@FORMATS
+def test_one_large_group(fmt):
+    """One group of 130 sequences behind 2000 rows."""
+    lay, lens, off = make("05b", fmt, [130], [2000], [1, 2, 40], 64, seed=7)
+    q = lay.queries(130)
+    d = Shared(lay, q, lens, max(lens), off, [2000], fmt)
+    check_decode(lay, q, lens, d(), only=set(range(0, 130, 9)) | {129})
+    d.guard()
+
+
+@FORMATS
+def test_bad_pages(fmt):
+    """A shared row on no page: NaN for the group; a row of one sequence's own: for that one."""
+    lay, lens, off = make("1b", fmt, [3, 3], [128, 128], [40], 32, seed=8)
+    lay.table[0:3, 1] = -1
+    lay.table[4, 4] = 10**6
+    lay.upload()
+    q = lay.queries(6)
+    got = Shared(lay, q, lens, max(lens), off, [128, 128], fmt)()
+    check_decode(lay, q, lens, got, only={3, 5})
+    assert np.isnan(got[[0, 1, 2, 4]].float().cpu().numpy()).all()
+
+
+@FORMATS
+def test_large_logits(fmt):
+    """The row with all the weight in the shared part or behind it, logits of about a thousand."""
+    lay, lens, off = make("tiny", fmt, [6], [96], [40], 16, seed=9)
+    q = np.zeros((6, 4, 96))
+    for b, where in enumerate([0, 31, 32, 95, 96, 135]):
+        q[b, :, 64 + b] = 1000.0
+        for p in range(136):
+            lay.pool[lay.table[b, p // 16], p % 16, 128 + b] = 8.0 if p == where else 4.0
+    lay.upload()
+    check_decode(lay, q, lens, Shared(lay, q, lens, 136, off, [96], fmt)())
+
+
+@FORMATS
+def test_repeats_its_bits_and_follows_its_arrays_in_a_graph(fmt):
+    import torch
+    lay, lens, off = make("1b", fmt, [4, 3], [160, 96], [30, 1, 65], 32, seed=10)
+    q = lay.queries(7)
+    d = Shared(lay, q, lens, 300, off, [160, 96], fmt)
+    first = d().clone()
+    d.ws.fill_(0x7B)
+    assert torch.equal(d(), first)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        d()
+    for k, (now, o, s) in enumerate(((lens, off, [160, 96]), ([100] * 4 + [90] * 3, off, [100, 90]),
+                                     (lens, [0, 2, 4], [160, 160]), ([0] * 7, off, [160, 96]), (lens, [0, 0, 0], [5, 5]))):
+        d.lens.copy_(ints(now)), d.off.copy_(ints(o)), d.shared.copy_(ints(s))
+        d.o.fill_(3.0)
+        graph.replay()
+        got = d.o.clone()
+        torch.cuda.synchronize()
+        d.o.fill_(5.0)
+        assert torch.equal(d(), got), k
+        check_decode(lay, q, now, got)
+
+
+@FORMATS
+def test_two_streams_with_their_own_workspaces(fmt):
+    import torch
+    lay, lens, off = make("8b", fmt, [6], [512], [40, 1, 100], 64, seed=11)
+    a = Shared(lay, lay.queries(6), lens, max(lens), off, [512], fmt)
+    b = Shared(lay, lay.queries(6), lens, max(lens), [0, 3, 6], [320, 512], fmt)
+    want = a().clone(), b().clone()
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        a.o.zero_(), b.o.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s1):
+            a()
+        with torch.cuda.stream(s2):
+            b()
+        torch.cuda.synchronize()
+        assert torch.equal(a.o, want[0]) and torch.equal(b.o, want[1])
