@@ -1,0 +1,94 @@
+// The absorbed queries of decoding (decode.hip, decode_shared.hip).
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+
+namespace mla {
+
+// The absorbed queries of the heads of group g: row r = (b, j) of the
+// B hpg rows is head i = g hpg + j of sequence b; qabs[b][i][c] = sum_d q[b][i][d] W_UK[g][d][c]
+// for c < rkv, then the rotary part copied.  A workgroup (two wavefronts) makes 32 rows x 64
+// columns; W_UK's 64 columns are staged in LDS as they lie ([d][c]) and read transposed
+// (MFMA row = c), the query rows come straight from memory (MFMA column = row), so that a
+// lane ends with 4 consecutive c of its row: 8-byte stores.  Bound by latency (W_UK is 1 MB at
+// H = 32, r_kv = 512; one round of small workgroups), fp32 accumulation.  Measured with the
+// rotary copy: 64 sequences 26 -> 9.0 us, one sequence 13.6 -> 4.1 us (a vector-ALU product and
+// a copy launch before).
+// ABS_FRAG: qabs in the order in which the paged decoding reads it, [b][block of 32 heads][16-wide step
+// kk][half][head][8]: a matrix operand is 1 KB in one piece there.
+// ABS_FRAG32: the same order, fp32 (the decoding over an eight-bit cache scales and rounds them itself).
+constexpr int ABS_LD = 96;  // LDS row stride: 4 rows of a transposing read on distinct banks
+constexpr int ABS_DN = 192;
+enum AbsorbOut { ABS_ROWS, ABS_FRAG, ABS_FRAG32 };
+template <AbsorbOut OUT>
+__device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const bf16_t* __restrict__ Wuk,
+                                             void* __restrict__ qabs_, int B, int H, int HP, int hpg, int dn,
+                                             int dr, int rkv, int bx, int by, int g) {
+  using T = typename std::conditional<OUT == ABS_FRAG32, float, bf16_t>::type;
+  T* qabs = (T*)qabs_;
+  __shared__ __attribute__((aligned(16))) bf16_t Ws[ABS_DN * ABS_LD];
+  const int c0 = 64 * bx, r0 = 32 * by;
+  const int DK = rkv + dr, dq = dn + dr, tid = threadIdx.x;
+  const int lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
+  const int dnp = (dn + 15) & ~15;  // d rounded up to the K step, zero filled
+  const bf16_t* Wg = Wuk + (int64_t)g * dn * rkv + c0;
+  if ((uintptr_t)Wuk % 16 == 0) {  // uniform
+    for (int e = tid; e < dnp * 8; e += 128) {
+      const int d = e >> 3, c = 8 * (e & 7);
+      *(u32x4*)(Ws + d * ABS_LD + c) = d < dn ? *(const u32x4*)(Wg + (int64_t)d * rkv + c) : u32x4{0u, 0u, 0u, 0u};
+    }
+  } else {
+    for (int e = tid; e < dnp * 64; e += 128) {
+      const int d = e >> 6, c = e & 63;
+      Ws[d * ABS_LD + c] = d < dn ? Wg[(int64_t)d * rkv + c] : (bf16_t)0;
+    }
+  }
+  const int rows = B * hpg, rr = r0 + col, rc = min(rr, rows - 1);
+  const int64_t bi = (int64_t)(rc / hpg) * H + g * hpg + rc % hpg;           // row of q
+  const int64_t qi = (int64_t)(rc / hpg) * HP + g * hpg + rc % hpg;          // row of qabs
+  const bf16_t* qp = q + bi * dq + 8 * half;
+  bf16x8 qf[ABS_DN / 16];  // this lane's row, asked for before the staging's barrier
+#pragma unroll
+  for (int kk = 0; kk < ABS_DN / 16; ++kk) {
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (16 * kk + 8 * half < dn) w = *(const u32x4*)(qp + 16 * kk);
+    qf[kk] = __builtin_bit_cast(bf16x8, w);
+  }
+  // where 8 aligned elements c .. of row rc go
+  const int head = g * hpg + rc % hpg;
+  const int64_t fi = ((int64_t)(rc / hpg) * (HP / 32) + head / 32) * (DK / 16) * 512 + head % 32 * 8;
+  auto place = [&](int c) {
+    return OUT != ABS_ROWS ? qabs + fi + (c >> 4) * 512 + (c >> 3 & 1) * 256 : qabs + qi * DK + c;
+  };
+  if (bx == 0 && wave == 0 && rr < rows)  // rotary part: dr elements, half a row per lane
+    for (int c = 8 * half; c < dr; c += 16) {
+      const u32x4 v = *(const u32x4*)(q + bi * dq + dn + c);
+      if constexpr (OUT == ABS_FRAG32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *(f32x2*)(place(rkv + c) + 2 * k) = f32x2{__uint_as_float(v[k] << 16), __uint_as_float(v[k] & 0xffff0000u)};
+      } else {
+        *(u32x4*)place(rkv + c) = v;
+      }
+    }
+  __syncthreads();
+  f32x16 acc;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < ABS_DN / 16; ++kk)
+    if (16 * kk < dnp)  // uniform
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          lds_operand_tr(Ws, ABS_LD, 32 * wave, 16 * kk + 8 * half, 16 * kk + 8 * half + 4), qf[kk], acc,
+          0, 0, 0);
+  if (rr >= rows) return;
+#pragma unroll
+  for (int e4 = 0; e4 < 4; ++e4)
+    if constexpr (OUT == ABS_FRAG32)
+      *(f32x4*)(place(c0 + 32 * wave + 8 * e4) + 4 * half) = f32x4{acc[4 * e4], acc[4 * e4 + 1], acc[4 * e4 + 2], acc[4 * e4 + 3]};
+    else
+      *(u32x2*)(place(c0 + 32 * wave + 8 * e4) + 4 * half) = u32x2{pack2bf(acc[4 * e4], acc[4 * e4 + 1]), pack2bf(acc[4 * e4 + 2], acc[4 * e4 + 3])};
+}
+
+}  // namespace mla

@@ -1,126 +1,948 @@
 // Absorbed-form decoding over a paged latent cache of either format, for sequences some of which begin
 // with the same rows.
+#include "absorb.h"
 #include "attn_common.h"
 #include "cache_rows.h"
 #include "common.h"
+#include "decode_parts.h"
 #include "kernels.h"
 
 namespace mla {
 namespace {
 
-struct SharedDev {
-  PagedPool c;
+size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// Attention is that of paged_attn.hip: a block of 32 heads of a sequence (32 queries) is one column block
+// of the matrix products, its state belongs to a wavefront, tiles have 32 rows.  Here the rows of
+// a sequence may begin with ones that its group shares, and there are two lists of tiles:
+//
+// * own rows: the tiles of all query blocks behind what they share, cut as in paged_attn.hip (a wavefront
+//   on a run of its own tiles);
+// * shared rows: a group's query blocks in fours ("quads"), for each quad the tiles of the shared rows.
+//   A workgroup takes a run of these items; its four wavefronts have a query block each and one tile in
+//   LDS for all of them, which is then read from memory once for four blocks and once from the
+//   caches for the group's other quads.
+//
+// The workgroups are divided between the lists by their tiles.  A tile of one block's own rows and
+// an item of four blocks cost a workgroup about the same: the first waits for its copy.
+struct LatentDev {
+  const char* pool;
+  const int32_t* table;
+  int n_pages, page_size, max_pages;
+  int64_t page_bytes;
   const int32_t* len;
-  int max_len, B, H, dn, dr, dv, hpg;
-  const bf16_t *q, *Wuk, *Wuv;
-  bf16_t* o;
+  int max_len, B, H, HB;  // HB: blocks of 32 heads
+  const void* qabs;       // [B HB][DK / 16][64 lanes][8], bf16 or (e4m3) fp32
+  float* part_o;          // [slot][32][DVL], not normalised
+  float* part_ml;         // [slot][32][2]: reference (log2), sum
   float sl2;
+  int nwg;
+  // the lists, made by the plan (one workgroup of the launch before)
+  int n_groups, max_quads;
+  const int32_t* group_off;
+  const int32_t* shared_len;
+  int32_t* head;          // [3]: tiles of shared rows, of own rows, quads
+  int32_t* start;         // [B]: rows that the sequence shares, a multiple of PD_KT
+  int32_t* tile_off;      // [B HB + 1]: first tile of each block's own rows
+  int32_t* quad_x;        // [max_quads]: 4 first block + (blocks - 1)
+  int32_t* quad_item;     // [max_quads + 1]: first item of each quad
+  int32_t* block_quad;    // [B HB]: 4 quad + place in it, or -1
+  int32_t* group_of;      // [B], -1: none
+  int32_t* group_min;     // [n_groups]: shared rows that all have; then how many sequences have rows
+  int32_t* group_cnt;
 };
 
-// A workgroup per (head, sequence): the absorbed query in LDS (fp32), a wavefront per row in turn, each
-// with its own softmax state and weighted latent, joined through LDS, then W_UV.
-template <int DK, int DVL, bool E4M3>
-__global__ __launch_bounds__(256) void decode_simple_kernel(SharedDev a) {
-  constexpr int DR = DK - DVL, NL = (DVL + 63) / 64;
-  __shared__ float qs[DK], lat[4][DVL], ml[4][2];
-  __shared__ int any_bad;
-  const int i = blockIdx.x, b = blockIdx.y, g = i / a.hpg, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
-  const bf16_t* q = a.q + ((int64_t)b * a.H + i) * (a.dn + a.dr);
-  for (int c = tid; c < DVL; c += 256) {
-    float x = 0.f;
-    for (int d = 0; d < a.dn; ++d) x += bf2f(q[d]) * bf2f(a.Wuk[((int64_t)g * a.dn + d) * DVL + c]);
-    qs[c] = x;
-  }
-  for (int c = tid; c < DR; c += 256) qs[DVL + c] = bf2f(q[a.dn + c]);
-  if (tid == 0) any_bad = 0;
-  __syncthreads();
-  const int n = min(max(a.len[b], 0), a.max_len);
-  float m = -INFINITY, l = 0.f, acc[NL];
+__device__ __forceinline__ int len_of(const LatentDev& a, int b) { return min(max(a.len[b], 0), a.max_len); }
+
+// How many workgroups the shared rows get.
+__device__ __forceinline__ int shared_workgroups(int nwg, int shared, int own) {
+  if (shared == 0) return 0;
+  if (own == 0) return nwg;
+  const int64_t n = ((int64_t)nwg * shared + (shared + (int64_t)own) / 2) / (shared + (int64_t)own);
+  return (int)min(max(n, (int64_t)1), (int64_t)nwg - 1);
+}
+// The items of the shared rows in equal runs.
+struct ItemCut {
+  int total, share;
+  __device__ __forceinline__ ItemCut(int items, int nwg) : total(items), share(max(1, nwg > 0 ? (items + nwg - 1) / nwg : 1)) {}
+  __device__ __forceinline__ int lo(int w) const { return (int)min((int64_t)w * share, (int64_t)total); }
+  __device__ __forceinline__ int hi(int w) const { return min(lo(w) + share, total); }
+};
+
+// ---- the plan -------------------------------------------------------------------------
+// Sum over the threads before this one, and over all (NT threads).
+template <int NT>
+__device__ __forceinline__ int scan_before(int mine, int& total) {
+  __shared__ int sums[NT / 64];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  int upto = mine;
 #pragma unroll
-  for (int k = 0; k < NL; ++k) acc[k] = 0.f;
-  const E4m3Page layout(a.c.page_size, DVL, DR);
-  for (int p = wave; p < n; p += 4) {
-    const int page = a.c.table[(int64_t)b * a.c.max_pages + p / a.c.page_size], r = p % a.c.page_size;
-    if (page < 0 || page >= a.c.n_pages) {
-      any_bad = 1;
-      continue;
-    }
-    float x[NL], s = 0.f;
-#pragma unroll
-    for (int k = 0; k < NL; ++k) {
-      const int c = lane + 64 * k;
-      x[k] = 0.f;
-      if (c < DVL) {
-        if constexpr (E4M3)
-          x[k] = __builtin_amdgcn_cvt_pk_f32_fp8((int)(uint8_t)layout.row(a.c.pool, page, r)[c], false)[0] *
-                 *layout.power(a.c.pool, page, r);
-        else
-          x[k] = bf2f(((const bf16_t*)a.c.pool)[((int64_t)page * a.c.page_size + r) * DK + c]);
-        s += x[k] * qs[c];
-      }
-    }
-    if (lane < DR) {
-      const bf16_t* pe = E4M3 ? (const bf16_t*)(layout.row(a.c.pool, page, r) + DVL)
-                              : (const bf16_t*)a.c.pool + ((int64_t)page * a.c.page_size + r) * DK + DVL;
-      s += bf2f(pe[lane]) * qs[DVL + lane];
-    }
-    s = warp_sum(s) * a.sl2;
-    const float m1 = fmaxf(m, s), ref = m1 == -INFINITY ? 0.f : m1;
-    const float f = exp2f(m - ref), w = exp2f(s - ref);  // (NaN stays NaN)
-    l = l * f + w;
-#pragma unroll
-    for (int k = 0; k < NL; ++k) acc[k] = acc[k] * f + x[k] * w;
-    m = m1;
-  }
-#pragma unroll
-  for (int k = 0; k < NL; ++k)
-    if (lane + 64 * k < DVL) lat[wave][lane + 64 * k] = acc[k];
-  if (lane == 0) {
-    ml[wave][0] = m;
-    ml[wave][1] = l;
+  for (int d = 1; d < 64; d *= 2) {
+    const int v = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += v;
   }
   __syncthreads();
-  float M = -INFINITY, L = 0.f, f[4];
-  for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][0]);
-  for (int w = 0; w < 4; ++w) {
-    f[w] = M == -INFINITY ? 1.f : exp2f(ml[w][0] - M);
-    L += ml[w][1] * f[w];
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < wave) upto += sums[w];
+    total += sums[w];
   }
-  const float inv = any_bad ? NAN : n == 0 ? 0.f : 1.f / L;
-  for (int e = tid; e < a.dv; e += 256) {
-    float v = 0.f;
-    for (int c = 0; c < DVL; ++c) {
-      float x = 0.f;
-      for (int w = 0; w < 4; ++w) x += lat[w][c] * f[w];
-      v += x * bf2f(a.Wuv[((int64_t)g * a.dv + e) * DVL + c]);
+  return upto - mine;
+}
+
+__device__ __forceinline__ int agent_load(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// One workgroup of NT threads.  Group offsets that decrease give a plan of no meaning whose indexes
+// are in range.
+template <int NT>
+__device__ void make_plan(const LatentDev& a) {
+  const int tid = threadIdx.x, G = a.n_groups;
+  for (int g = tid; g < G; g += NT) {
+    __hip_atomic_store(a.group_min + g, min(max(a.shared_len[g], 0), a.max_len), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(a.group_cnt + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __threadfence();
+  __syncthreads();
+  // what all sequences of a group that have rows have
+  for (int b = tid; b < a.B; b += NT) {
+    int g = -1;
+    if (G > 0) {
+      g = sequence_of(a.group_off, G, b);
+      if (b < a.group_off[g] || b >= a.group_off[g + 1]) g = -1;
     }
-    a.o[((int64_t)b * a.H + i) * a.dv + e] = f2bf(v * inv);
+    a.group_of[b] = g;
+    const int n = len_of(a, b);
+    if (g >= 0 && n > 0) {
+      atomicMin(a.group_min + g, n);
+      atomicAdd(a.group_cnt + g, 1);
+    }
+    for (int h = 0; h < a.HB; ++h) a.block_quad[b * a.HB + h] = -1;
+  }
+  __threadfence();
+  __syncthreads();
+  // (one block alone gains nothing)
+  auto rows_of = [&](int g) { return agent_load(a.group_cnt + g) * (int64_t)a.HB >= 2 ? agent_load(a.group_min + g) / PD_KT * PD_KT : 0; };
+  // quads and their items
+  const int run = (G + NT - 1) / NT, g_lo = min(tid * run, G), g_hi = min(g_lo + run, G);
+  auto blocks = [&](int g, int& x0) {
+    const int lo = min(max(a.group_off[g], 0), a.B), hi = min(max(a.group_off[g + 1], 0), a.B);
+    x0 = lo * a.HB;
+    return max(hi - lo, 0) * a.HB;
+  };
+  int quads = 0, items = 0, x0, total_q, total_i;
+  for (int g = g_lo; g < g_hi; ++g) {
+    const int q = (blocks(g, x0) + 3) / 4, t = rows_of(g) / PD_KT;
+    if (t > 0) {
+      quads += q;
+      items += q * t;
+    }
+  }
+  int k = scan_before<NT>(quads, total_q), at = scan_before<NT>(items, total_i);
+  for (int g = g_lo; g < g_hi; ++g) {
+    const int n = blocks(g, x0), t = rows_of(g) / PD_KT;
+    if (t == 0) continue;
+    for (int i = 0; i < n; i += 4, ++k, at += t) {
+      if (k >= a.max_quads) break;
+      a.quad_x[k] = 4 * (x0 + i) + min(n - i, 4) - 1;
+      a.quad_item[k] = at;
+      if (k == a.max_quads - 1) a.quad_item[k + 1] = at + t;
+      for (int j = 0; j < min(n - i, 4); ++j)  // (sequences without rows take no part)
+        if (len_of(a, (x0 + i + j) / a.HB) > 0) a.block_quad[x0 + i + j] = 4 * k + j;
+    }
+  }
+  if (tid == 0) {
+    a.head[2] = min(total_q, a.max_quads);
+    if (total_q < a.max_quads) a.quad_item[total_q] = total_i;
+  }
+  // own rows
+  const int runb = (a.B + NT - 1) / NT, b_lo = min(tid * runb, a.B), b_hi = min(b_lo + runb, a.B);
+  int mine = 0, total;
+  for (int b = b_lo; b < b_hi; ++b) {
+    const int g = a.group_of[b], n = len_of(a, b), s = g >= 0 ? min(rows_of(g), n) : 0;
+    a.start[b] = s;
+    mine += tiles_of(n - s) * a.HB;
+  }
+  at = scan_before<NT>(mine, total);
+  for (int b = b_lo; b < b_hi; ++b) {
+    const int n = tiles_of(len_of(a, b) - a.start[b]);
+    for (int h = 0; h < a.HB; ++h, at += n) a.tile_off[b * a.HB + h] = at;
+  }
+  __syncthreads();  // (quad_item is written)
+  if (tid == 0) {
+    a.tile_off[a.B * a.HB] = total;
+    const int q = min(total_q, a.max_quads);
+    a.head[0] = q == 0 ? 0 : a.quad_item[q];
+    a.head[1] = total;
   }
 }
 
-#define MLA_SHARED_SHAPES(X) X(576, 512) X(288, 256) X(160, 128)
+// The absorbed queries (absorb.h), and one workgroup, the first, for the plan.
+constexpr int PREP_THREADS = 128;
+template <bool E4M3>
+__global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev a, const bf16_t* q, const bf16_t* Wuk,
+                                                                      int hpg, int dn, int dr, int rkv) {
+  if (blockIdx.x == 0) {
+    make_plan<PREP_THREADS>(a);
+    return;
+  }
+  const int nx = rkv / 64, ny = (a.B * hpg + 31) / 32, k = blockIdx.x - 1;
+  absorb_block<E4M3 ? ABS_FRAG32 : ABS_FRAG>(q, Wuk, (void*)a.qabs, a.B, a.H, 32 * a.HB, hpg, dn, dr, rkv, k % nx,
+                                             k / nx % ny, k / nx / ny);
+}
+
+// ---- attention ------------------------------------------------------------------------
+__device__ __forceinline__ void mfma_v_first(f32x16& d, f16x8 x, f16x8 y) {
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));
+}
+__device__ __forceinline__ void mfma_v_next(f32x16& d, f16x8 x, f16x8 y) {
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(d) : "v"(x), "v"(y));
+}
+__device__ __forceinline__ void mfma_a(f32x16& d, f16x8 x, f16x8 y) {
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(d) : "v"(x), "v"(y));
+}
+// 8 e4m3 values as fp16 (exact)
+__device__ __forceinline__ f16x8 e4m3_to_f16(uint32_t lo, uint32_t hi) {
+  u32x4 w;
+  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, false));
+  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, true));
+  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false));
+  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true));
+  return __builtin_bit_cast(f16x8, w);
+}
+// LDS transposing read of bytes: in each group of 16 lanes, lane r gives the address of 8 bytes; lane j receives
+// byte j % 8 of what lanes j / 8, j / 8 + 2, .. gave.
+__device__ __forceinline__ u32x2 lds_read_tr8(const char* p) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p));
+}
+// 4 bytes a lane from the lanes' addresses to the LDS byte address `lds`
+__device__ __forceinline__ void copy4(uint64_t src, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(lds) : "memory");
+}
+
+// A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r) (paged_attn.hip), and
+// in eight bits the rows' powers behind them.  S^T reads 16 bytes of 16 consecutive rows, which take
+// different banks; the transposing reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16:
+// 32 bytes of four rows).  In eight bits the rows of those that share banks differ in bits 1 and 3 where two
+// rows span the banks (640 bytes), which go to chunk bits 1 and 2.
+template <int DK, int DVL, bool E4M3>
+struct LatentTile {
+  static constexpr int RB = E4M3 ? DVL + 2 * (DK - DVL) : 2 * DK;  // bytes of a row
+  static constexpr int CHR = RB / 16;
+  static constexpr bool WIDE = RB % 256 == 128;
+  static constexpr int ROWS = WIDE ? 8 : 16;
+  static constexpr int PERIOD = ROWS * CHR / 64;
+  static constexpr int HALF_COPIES = 16 * CHR / 64;
+  static constexpr int BYTES = PD_KT * RB, ALLOC = BYTES + (E4M3 ? 256 : 0);
+  static_assert(RB % 64 == 0 && CHR % (WIDE ? 8 : 4) == 0 && ROWS * CHR % 64 == 0, "whole copies");
+  __device__ __forceinline__ static constexpr int swz(int r) {
+    if (!WIDE) return r >> 2 & 3;
+    return E4M3 ? (r >> 1 & 1) << 1 | (r >> 3 & 1) << 2 | (r >> 2 & 1) : (r >> 1 & 1) << 1 | (r >> 2 & 1) << 2 | (r >> 3 & 1);
+  }
+  static constexpr int XOR8 = 16 * (E4M3 ? 4 : 1);  // what 8 rows further do to an offset (WIDE)
+};
+
+// Eight bits.  A latent is its e4m3 value c times its row's power 2^e.  The products take c (exact in fp16): logits are
+// multiplied by 2^e (before the positional part is added), and a row's weight in the weighted latents is
+// p 2^e = 2^(x + e - m) with x the logit in log2 units and m the running maximum of x + e over the rows.  So weights
+// are at most 2^(SLACK + BIAS) < 2^16 and fp16 holds them with 11 bits down to 2^-22 of the largest (their
+// rounding is an eighth of bf16's, and one operand does where bf16 takes two).  The sum of the p has
+// a reference of its own, the running maximum of x: beside rows of much larger powers 2^(x - m) may be 0
+// where p is not small.  Absorbed queries are fp16 too, each head's brought to [2^8, 2^9) by a power of two.
+constexpr float E8_SLACK = 7.f, E8_BIAS = 8.f;
+
+template <int DK, int DVL, bool E4M3, int OCC>
+__global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(LatentDev a) {
+  using TL = LatentTile<DK, DVL, E4M3>;
+  using QT = typename std::conditional<E4M3, f16x8, bf16x8>::type;
+  constexpr int RB = TL::RB, CHR = TL::CHR, DR = DK - DVL;
+  constexpr int NL = DVL / 16, NR = DR / 16, NC = DVL / 32;
+  constexpr int PF = E4M3 ? 3 : 5, PV = 3;  // operand reads in flight ahead of the products of S, and of P V
+  static_assert(DVL % 128 == 0 && DR % 16 == 0, "decode shape");
+  __shared__ __attribute__((aligned(1024))) char tiles[PD_WAVES][TL::ALLOC];
+  __shared__ float ml[PD_WAVES][2][32];
+  __shared__ int plan_x[PD_WAVES], plan_at[PD_WAVES];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const int half = lane >> 5, col = lane & 31;
+  const int total_s = a.head[0], total_p = a.head[1], VB = a.B * a.HB;
+  const int n_s = __builtin_amdgcn_readfirstlane(shared_workgroups(a.nwg, total_s, total_p));
+  const bool on_shared = (int)blockIdx.x < n_s;
+  const int wg = on_shared ? (int)blockIdx.x : (int)blockIdx.x - n_s;
+
+  // ---- what both lists use ----
+  // lane offsets in a tile: S^T's operand (chunk 2 i + half of row col, i % 4 = 0..3), V^T's
+  int kb[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) kb[j] = col * RB + 16 * ((2 * j + half) ^ TL::swz(col));
+  int vb[4];
+  if constexpr (E4M3) {  // rows 4 half + 0..3, 8 + 4 half + 0..3, latents 16 ((lane / 16) % 2) + 8 (lane % 2) (+ 32 j)
+    const int i = (lane & 15) >> 1, r = 4 * half + (i & 3) + 8 * (i >> 2);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vb[j] = r * RB + 16 * ((2 * j + (lane >> 4 & 1)) ^ TL::swz(r)) + 8 * (lane & 1);
+  } else {  // [8 more rows][32 latents further]: rows 4 half + (lane % 16) / 4, latents 16 ((lane / 16) % 2) + 4 (lane % 4)
+#pragma unroll
+    for (int h8 = 0; h8 < 2; ++h8)
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        const int r = 8 * h8 + 4 * half + ((lane & 15) >> 2);
+        const int d = 32 * odd + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        vb[2 * h8 + odd] = r * RB + 16 * ((d >> 3) ^ TL::swz(r)) + 2 * (d & 7);
+      }
+  }
+  // the row at position p of sequence b (the last of the tile's again past the end, which gets no weight)
+  auto entry = [&](int b, int p) { return a.table[(int64_t)b * a.max_pages + p / a.page_size]; };
+  auto address = [&](int p, int page, bool& bad, uint64_t& power) {
+    const bool out = page < 0 || page >= a.n_pages;
+    bad = __ballot(out) != 0;
+    const uint64_t base = (uint64_t)(uintptr_t)a.pool + (uint64_t)((out ? 0 : page) * a.page_bytes);
+    const int r = p % a.page_size;
+    if constexpr (E4M3) power = base + (uint64_t)((int64_t)a.page_size * RB + 4 * (int64_t)r);
+    return base + (uint64_t)((int64_t)r * RB);
+  };
+  auto row_address = [&](uint64_t at, int r) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, r) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at >> 32), r) << 32;
+  };
+  const bool whole16 = a.page_size % 16 == 0;  // 16-row halves of whole tiles lie together
+
+  auto pin = [](f32x16(&d)[NC]) __attribute__((always_inline)) {  // stays in the accumulation registers here
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+a"(d[c]));
+  };
+
+  // ---- a wavefront's state: 32 queries ----
+  QT qf[NL];             // this lane's head as B operand fragments
+  bf16x8 qr[NR];
+  float qpow = 1.f;      // (eight bits) what the fragments were divided by
+  f32x16 acc[NC];
+  float m_run, mx_run, l_run;
+  bool any_bad;
+  auto begin = [&](int x) __attribute__((always_inline)) {
+    if constexpr (E4M3) {
+      // step 2 i + e holds latents 32 i + 16 half + 8 e + 0..7: the 16 bytes that one LDS read gives
+      const float* src = (const float*)a.qabs + (int64_t)x * 32 * DK + 8 * col;
+      auto place = [&](int i, int e) { return src + (2 * i + half) * 512 + 256 * e; };
+      float top = 0.f;
+#pragma unroll 8
+      for (int s = 0; s < NL; ++s) {
+        const f32x4 u = *(const f32x4*)place(s >> 1, s & 1), v = *(const f32x4*)(place(s >> 1, s & 1) + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(u[k]), fabsf(v[k])));
+      }
+      top = pair_max32(top);
+      const int t = min(max((int)(__float_as_uint(top) >> 23) - 127 - 8, -120), 120);
+      const float down = power_of_two(-t);
+      qpow = power_of_two(t);
+#pragma unroll
+      for (int s = 0; s < NL; ++s) {
+        const f32x4 u = *(const f32x4*)place(s >> 1, s & 1), v = *(const f32x4*)(place(s >> 1, s & 1) + 4);
+        qf[s] = __builtin_bit_cast(f16x8, u32x4{pack2h(u[0] * down, u[1] * down), pack2h(u[2] * down, u[3] * down),
+                                                pack2h(v[0] * down, v[1] * down), pack2h(v[2] * down, v[3] * down)});
+      }
+#pragma unroll
+      for (int s = 0; s < NR; ++s) {
+        const float* p = src + (NL + s) * 512 + 256 * half;
+        const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
+        qr[s] = __builtin_bit_cast(bf16x8, u32x4{pack2bf(u[0], u[1]), pack2bf(u[2], u[3]), pack2bf(v[0], v[1]), pack2bf(v[2], v[3])});
+      }
+    } else {
+      const bf16_t* src = (const bf16_t*)a.qabs + (int64_t)x * 32 * DK + 8 * lane;
+#pragma unroll
+      for (int s = 0; s < NL; ++s) qf[s] = *(const bf16x8*)(src + 512 * s);
+#pragma unroll
+      for (int s = 0; s < NR; ++s) qr[s] = *(const bf16x8*)(src + 512 * (NL + s));
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
+    m_run = mx_run = -INFINITY;
+    l_run = 0.f;
+    any_bad = false;
+  };
+  // One tile at kt, of which `left` rows count.  `heads`: the columns with a head.  `early` is called
+  // when the reads of the first 16 rows (and of all keys) have returned.
+  auto tile = [&](const char* kt, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
+    f32x16 s;
+    if constexpr (E4M3) {
+      u32x4 raw[PF];
+      auto kread = [&](int i) { return *(const u32x4*)(kt + kb[i % 4] + 128 * (i / 4)); };
+#pragma unroll
+      for (int j = 0; j < PF; ++j) raw[j] = kread(j);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NL / 2; ++i) {
+        const u32x4 v = raw[i % PF];
+        const f16x8 k0 = e4m3_to_f16(v[0], v[1]);
+        if (i == 0) mfma_v_first(s, k0, qf[0]);
+        else mfma_v_next(s, k0, qf[2 * i]);
+        const f16x8 k1 = e4m3_to_f16(v[2], v[3]);
+        mfma_v_next(s, k1, qf[2 * i + 1]);
+        if (i + PF < NL / 2 + NR) raw[i % PF] = kread(i + PF);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mfma_v_done(s);
+      const float* pw = (const float*)(kt + TL::BYTES);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 f = *(const f32x4*)(pw + 8 * g + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * g + e] *= f[e] * qpow;
+      }
+#pragma unroll
+      for (int j = 0; j < NR; ++j) {
+        mfma_v_next(s, __builtin_bit_cast(bf16x8, raw[(NL / 2 + j) % PF]), qr[j]);
+        if (j + PF < NR) raw[(NL / 2 + j) % PF] = kread(NL / 2 + j + PF);
+      }
+      mfma_v_done(s);
+    } else {
+      bf16x8 kf[PF];
+      auto kread = [&](int i) { return *(const bf16x8*)(kt + kb[i % 4] + 128 * (i / 4)); };
+#pragma unroll
+      for (int j = 0; j < PF; ++j) kf[j] = kread(j);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kk = 0; kk < NL + NR; ++kk) {
+        if (kk == 0) mfma_v_first(s, kf[0], qf[0]);
+        else mfma_v_next(s, kf[kk % PF], kk < NL ? qf[kk % NL] : qr[kk - NL < 0 ? 0 : kk - NL]);
+        if (kk + PF < NL + NR) kf[kk % PF] = kread(kk + PF);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mfma_v_done(s);
+    }
+    // V^T operand of step j = NC u + c: latents 32 c .., rows 16 u + {4 half.., 8 + 4 half..}
+    auto vread = [&](int j) {
+      const int c = j % NC, u = j / NC;
+      if constexpr (E4M3) {
+        return lds_read_tr8(kt + vb[c % 4] + 128 * (c / 4) + 16 * RB * u);
+      } else {
+        const char* p = kt + 16 * RB * u + 128 * (c / 2);
+        const u32x2 lo = lds_read_tr4((const bf16_t*)(p + vb[c & 1])), hi = lds_read_tr4((const bf16_t*)(p + vb[2 + (c & 1)]));
+        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+      }
+    };
+    typename std::conditional<E4M3, u32x2, bf16x8>::type vf[PV];
+#pragma unroll
+    for (int j = 0; j < PV; ++j) vf[j] = vread(j);
+    if (left < PD_KT) {  // rows past the end: no weight (a real branch)
+      asm volatile("");
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (8 * (e >> 2) + 4 * half + (e & 3) >= left) s[e] = -INFINITY;
+    }
+    QT pf[2];
+    bf16x8 pl[2];
+    if constexpr (E4M3) {
+      float x[16];
+      const float* pw = (const float*)(kt + TL::BYTES);
+      float mx = -INFINITY, my = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const u32x4 f = *(const u32x4*)(pw + 8 * g + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[4 * g + e] = s[4 * g + e] * a.sl2;
+          s[4 * g + e] = x[4 * g + e] + (float)((int)(f[e] >> 23) - 127);
+          mx = fmaxf(mx, x[4 * g + e]);
+          my = fmaxf(my, s[4 * g + e]);
+        }
+      }
+      mx = pair_max32(mx);
+      my = pair_max32(my);
+      // a reference moves only when a tile's maximum exceeds it by more than the slack
+      if ((__ballot(my > m_run + E8_SLACK || mx > mx_run + E8_SLACK) & heads) != 0) {
+        const float m_new = fmaxf(m_run, my), x_new = fmaxf(mx_run, mx);
+        const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        l_run *= __builtin_amdgcn_exp2f(mx_run - (x_new == -INFINITY ? 0.f : x_new));
+        m_run = m_new;
+        mx_run = x_new;
+        if (!first) {  // (nothing is there yet at the first tile)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
+        }
+      }
+      const float m_use = (m_run == -INFINITY ? 0.f : m_run) - E8_BIAS, x_use = mx_run == -INFINITY ? 0.f : mx_run;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        u32x4 w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          w[q] = pack2h(__builtin_amdgcn_exp2f(s[8 * u + 2 * q] - m_use), __builtin_amdgcn_exp2f(s[8 * u + 2 * q + 1] - m_use));
+        pf[u] = __builtin_bit_cast(f16x8, w);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) l_run += __builtin_amdgcn_exp2f(x[e] - x_use);
+    } else {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+      mx = pair_max32(mx) * a.sl2;
+      if ((__ballot(mx > m_run + PD_SLACK) & heads) != 0) {
+        const float m_new = fmaxf(m_run, mx);
+        const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        m_run = m_new;
+        l_run *= corr;
+        if (!first) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
+        }
+      }
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+      // P as two bf16 operands, rounded and what that lost
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        u32x4 w, w2;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q], a.sl2, -m_use));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q + 1], a.sl2, -m_use));
+          l_run += p0 + p1;
+          w[q] = pack2bf(p0, p1);
+          w2[q] = pack2bf(p0 - __uint_as_float(w[q] << 16), p1 - __uint_as_float(w[q] & 0xffff0000u));
+        }
+        pf[u] = __builtin_bit_cast(bf16x8, w);
+        pl[u] = __builtin_bit_cast(bf16x8, w2);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < 2 * NC; ++j) {
+      if constexpr (E4M3) {
+        const f16x8 v = e4m3_to_f16(vf[j % PV][0], vf[j % PV][1]);
+        mfma_a(acc[j % NC], v, pf[j / NC]);
+      } else {
+        mfma_a(acc[j % NC], vf[j % PV], pf[j / NC]);
+        mfma_a(acc[j % NC], vf[j % PV], pl[j / NC]);
+      }
+      if (j + PV < 2 * NC) vf[j % PV] = vread(j + PV);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j == NC) {
+        mfma_a_done(acc);  // (no branch, where the compiler may move registers, before the products' waits)
+        early();
+      }
+    }
+    mfma_a_done(acc);
+    // every read of the tile has returned before copies may overwrite it
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+  };
+  // the reference and sum of the state, as a merge of states takes them
+  auto reference = [&] { return E4M3 ? m_run - E8_BIAS : m_run; };
+  auto sum = [&] {
+    float l = l_run;
+    if constexpr (E4M3) l *= __builtin_amdgcn_exp2f(fminf(mx_run - reference(), 100.f));
+    return any_bad ? NAN : pair_sum32(l);  // (a row on no page)
+  };
+  auto store = [&](int64_t slot, bool has_head) __attribute__((always_inline)) {
+    const float l = sum(), m = reference();
+    if (!has_head) return;
+    const int64_t row = slot * 32 + col;
+    float* po = a.part_o + row * DVL + 4 * half;  // lane (head col, half) holds latents 32 c + 8 g + 4 half + 0..3
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(f32x4*)(po + 32 * c + 8 * g) = f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+    if (half == 0) {
+      a.part_ml[2 * row] = m;
+      a.part_ml[2 * row + 1] = l;
+    }
+  };
+
+  if (on_shared) {
+    // ---- shared rows: items of four query blocks ----
+    const ItemCut cut(total_s, n_s);
+    const int i_lo = cut.lo(wg), i_hi = cut.hi(wg);
+    if (i_lo >= i_hi) return;
+    const int quads = a.head[2];
+    for (int k = tid; k < quads; k += 64 * PD_WAVES)
+      if (a.quad_item[k] <= i_lo && i_lo < a.quad_item[k + 1]) plan_x[0] = k;
+    __syncthreads();
+    int k = __builtin_amdgcn_readfirstlane(plan_x[0]);
+    // this wavefront's copies of a tile: k = wave, wave + 4, .. (the last again where that is past the end)
+    constexpr int ALL = 2 * TL::HALF_COPIES, NJ = (ALL + PD_WAVES - 1) / PD_WAVES;
+    int rc[NJ];  // row and source chunk of the lane's 16 bytes
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int idx = 64 * min(4 * j + wave, ALL - 1) + lane, r = idx / CHR;
+      rc[j] = r << 8 | ((idx % CHR) ^ TL::swz(r));
+    }
+    const uint32_t tiles_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)&tiles[0][0]);
+    auto issue = [&](int buf, uint64_t at, uint64_t power, bool together) __attribute__((always_inline)) {
+      const uint32_t lds = tiles_lds + buf * TL::ALLOC;
+      if constexpr (E4M3) copy4(power, lds + TL::BYTES);
+      const uint64_t lo = row_address(at, 0), hi = row_address(at, 16);
+      auto copy = [&](int j, uint64_t row) __attribute__((always_inline)) {
+        const uint64_t src = row + 16 * (rc[j] & 255);
+        const uint32_t dst = lds + 1024 * min(4 * j + wave, ALL - 1);
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "{m0}"(dst) : "memory");
+      };
+      if (together) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) copy(j, ((rc[j] >> 8) < 16 ? lo : hi) + (uint32_t)((rc[j] >> 8 & 15) * RB));
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const int r = rc[j] >> 8;
+          copy(j, (uint64_t)(uint32_t)__shfl((int)(uint32_t)at, r, 64) | (uint64_t)(uint32_t)__shfl((int)(uint32_t)(at >> 32), r, 64) << 32);
+        }
+      }
+    };
+    for (int i = i_lo; i < i_hi; ++k) {
+      const int q_lo = __builtin_amdgcn_readfirstlane(a.quad_item[k]), q_hi = min(__builtin_amdgcn_readfirstlane(a.quad_item[k + 1]), i_hi);
+      const int qx = __builtin_amdgcn_readfirstlane(a.quad_x[k]), x0 = qx >> 2, nx = (qx & 3) + 1;
+      // (a wavefront without a block works on the last one's, and stores nothing)
+      const int b0 = x0 / a.HB, x = x0 + min(wave, nx - 1);
+      const int h0 = 32 * (x % a.HB);
+      const uint64_t heads = __ballot(h0 + col < a.H);
+      // tile i is copied while the one before is worked on; its table entries were asked for before that
+      int p = (i - q_lo) * PD_KT + col, page = entry(b0, p);
+      bool bad;
+      uint64_t power = 0, at = address(p, page, bad, power);
+      bool bad_now = bad;
+      __syncthreads();  // (the buffers are free)
+      issue(i & 1, at, power, whole16);
+      begin(x);
+      if (i + 1 < q_hi) page = entry(b0, p + PD_KT);
+      bool first = true;
+      for (; i < q_hi; ++i) {
+        pin(acc);
+        wait_vm<0>();
+        __syncthreads();
+        any_bad |= bad_now;
+        if (i + 1 < q_hi) {
+          p += PD_KT;
+          at = address(p, page, bad_now, power);
+          issue((i + 1) & 1, at, power, whole16);
+          if (i + 2 < q_hi) page = entry(b0, p + PD_KT);
+        }
+        tile(&tiles[i & 1][0], PD_KT, heads, first, [] {});
+        first = false;
+      }
+      store((int64_t)4 * (wg + k) + wave, wave < nx && h0 + col < a.H);
+    }
+    return;
+  }
+
+  // ---- own rows: a run of tiles a wavefront ----
+  const ListCut cut(total_p, a.nwg - n_s);
+  const int t_lo = cut.lo(wg), t_hi = cut.hi(wg), per = cut.per_wave(wg);
+  if (t_lo >= t_hi) return;
+  const int64_t slot0 = (int64_t)4 * (n_s + a.max_quads);  // (behind the shared rows')
+  for (int x = tid; x < VB; x += 64 * PD_WAVES) {
+    const int lo = a.tile_off[x], hi = a.tile_off[x + 1];
+#pragma unroll
+    for (int w = 0; w < PD_WAVES; ++w) {
+      const int t = t_lo + w * per;
+      if (t < t_hi && lo <= t && t < hi) {
+        plan_x[w] = x;
+        plan_at[w] = lo;
+      }
+    }
+  }
+  __syncthreads();
+  int T = t_lo + wave * per;                       // this wavefront's run: tiles [T, T_end)
+  const int T_end = min(T + per, t_hi);
+  int x = 0, b = 0, seq0 = 0, s0 = 0, n = 0, nt = 0;  // the current block: first tile, first row, rows, tiles
+  auto sequence = [&](int xx, int& bb, int& ss, int& nn) {
+    bb = xx / a.HB;
+    ss = __builtin_amdgcn_readfirstlane(a.start[bb]);
+    nn = __builtin_amdgcn_readfirstlane(len_of(a, bb));
+  };
+  if (T < T_end) {
+    x = __builtin_amdgcn_readfirstlane(plan_x[wave]);
+    seq0 = __builtin_amdgcn_readfirstlane(plan_at[wave]);
+    sequence(x, b, s0, n);
+    nt = tiles_of(n - s0);
+  }
+  // whether the share lies in one block's rows (the same in every wavefront)
+  const int x_first = __builtin_amdgcn_readfirstlane(plan_x[0]);
+  const bool joined = t_hi <= __builtin_amdgcn_readfirstlane(a.tile_off[x_first + 1]);
+
+  char* kt = tiles[wave];
+  const uint32_t kt_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)kt);
+  uint32_t voff[TL::PERIOD];  // the copies' sources within ROWS rows
+#pragma unroll
+  for (int k = 0; k < TL::PERIOD; ++k) {
+    const int r = (64 * k + lane) / CHR, pc = (64 * k + lane) % CHR;
+    voff[k] = 16u * (uint32_t)(r * CHR + (pc ^ TL::swz(r)));
+  }
+  // rows 16 g .. 16 g + 15 of a tile whose 16 rows lie together
+  auto issue_half = [&](int g, uint64_t at) __attribute__((always_inline)) {
+    uint64_t base = row_address(at, 16 * g);
+    asm volatile("s_nop 4" : "+s"(base));  // (vector ALU to scalar register to memory operation)
+    uint32_t lds = kt_lds;  // opaque: its sums with constants are cheaper made again than kept
+    asm volatile("" : "+s"(lds));
+#pragma unroll
+    for (int k = 0; k < TL::HALF_COPIES; ++k) {
+      const int q = k / TL::PERIOD;
+      uint32_t v = voff[k % TL::PERIOD];
+      if (TL::WIDE && (q & 1)) asm volatile("v_xor_b32 %0, %1, %0" : "+v"(v) : "n"(TL::XOR8));  // (again, not kept)
+      copy_s(base + (uint64_t)(q * TL::ROWS * RB), v, lds + 16 * g * RB + 1024 * k);
+    }
+  };
+  // any tile: copy k fills chunks 64 k .. 64 k + 63, of rows known at compile time
+  auto issue_rows = [&](uint64_t at) __attribute__((always_inline)) {
+    int ln = lane;  // opaque: the lanes' chunk numbers are cheaper made again than kept in registers
+    asm volatile("" : "+v"(ln));
+#pragma unroll
+    for (int k = 0; k < 2 * TL::HALF_COPIES; ++k) {
+      const int r0 = 64 * k / CHR, skip = 64 * k % CHR;
+      uint64_t src = 0;
+      int c = 0;
+#pragma unroll
+      for (int r = 0; r * CHR < skip + 64; ++r) {  // the rows that 64 chunks touch
+        const uint64_t base = row_address(at, r0 + r);
+        const int pc = ln + skip - r * CHR;
+        if (r == 0 || pc >= 0) {
+          src = base;
+          c = pc ^ TL::swz(r0 + r);
+        }
+      }
+      dma16((const bf16_t*)(uintptr_t)(src + 16u * (uint32_t)c), (bf16_t*)(kt + 1024 * k));
+      __builtin_amdgcn_sched_barrier(0);  // (or every row's address waits in scalar registers)
+    }
+  };
+  // position of row col of tile t of a block with rows [ss, nn)
+  auto position = [&](int ss, int nn, int t) { return min(ss + t * PD_KT + col, nn - 1); };
+
+  bool bad = false;
+  uint64_t power = 0;
+  if (T < T_end) {
+    const int p = position(s0, n, T - seq0);
+    const uint64_t at = address(p, entry(b, p), bad, power);
+    if constexpr (E4M3) copy4(power, kt_lds + TL::BYTES);
+    issue_rows(at);
+  } else if (!joined) {
+    return;
+  }
+
+  do {  // a block's part of the run
+    const int seg_end = min(T_end, seq0 + nt);
+    int x2 = x, b2 = b, s2 = s0, n2 = n, seq2 = seq0;  // the block after it
+    const int seg_begin = T, h0 = 32 * (x % a.HB);
+    const uint64_t heads = __ballot(h0 + col < a.H);  // (columns without a head move no reference)
+    begin(x);  // (a wavefront without tiles, in a joined share, has an empty state)
+    for (; T < seg_end; ++T) {
+      any_bad |= bad;
+      const int t = T - seq0;
+      // the tile after this one: the next of the block, or the first of the next that has rows
+      int page = 0, p2 = 0;
+      const bool more = T + 1 < T_end;
+      if (more) {
+        if (T + 1 == seg_end) {
+          seq2 += nt;
+          do sequence(++x2, b2, s2, n2);
+          while (n2 - s2 == 0);
+        }
+        p2 = position(s2, n2, T + 1 - seq2);
+        page = entry(b2, p2);
+      }
+      wait_vm<0>();
+      uint64_t at = 0;
+      bool together = false;
+      tile(kt, n - s0 - t * PD_KT, heads, T == seg_begin, [&]() __attribute__((always_inline)) {
+        // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
+        // reads return in order), the others behind the last read
+        if (more) {
+          at = address(p2, page, bad, power);
+          together = whole16 && (T + 1 - seq2) * PD_KT <= n2 - s2 - PD_KT;
+          if (together) issue_half(0, at);
+        }
+      });
+      if (more) {
+        if constexpr (E4M3) copy4(power, kt_lds + TL::BYTES);
+        if (together) issue_half(1, at);
+        else issue_rows(at);
+      }
+    }
+
+    if (!joined) {  // leaving the block: its state
+      store(slot0 + (int64_t)PD_WAVES * wg + wave + x, h0 + col < a.H);
+      x = x2;
+      b = b2;
+      s0 = s2;
+      n = n2;
+      seq0 = seq2;
+      nt = tiles_of(n - s0);
+      continue;
+    }
+
+    // the four states of one block: one reference and sum, then the latents, a part of them at a time
+    // through LDS: every wavefront writes its part, then sums a quarter of it
+    constexpr int PH = E4M3 ? 4 : 2, NH = NC / PH;
+    static_assert(PD_WAVES * NH * 4096 <= PD_WAVES * TL::ALLOC, "a part of every state fits the tiles");
+    const float l = sum(), ref = reference();
+    if (half == 0) {
+      ml[wave][0][col] = ref;
+      ml[wave][1][col] = l;
+    }
+    float* buf = (float*)tiles[0];
+    float M = -INFINITY, L = 0.f, f[PD_WAVES];
+    const int hj = 32 * (x_first % a.HB);
+    const int64_t row = (slot0 + (int64_t)PD_WAVES * wg + x_first) * 32 + col;
+    float* po = a.part_o + row * DVL + 4 * half;
+#pragma unroll
+    for (int ph = 0; ph < PH; ++ph) {
+      __syncthreads();  // (every wavefront is done with its tile, or with the part before)
+      if (ph == 0) {
+#pragma unroll
+        for (int w = 0; w < PD_WAVES; ++w) M = fmaxf(M, ml[w][0][col]);
+#pragma unroll
+        for (int w = 0; w < PD_WAVES; ++w) {
+          const float mw = ml[w][0][col];
+          f[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+          L += ml[w][1][col] * f[w];
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NH; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& v = acc[ph * NH + c];
+          *(f32x4*)(buf + (((wave * NH + c) * 4 + g) * 64 + lane) * 4) = f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+        }
+      __syncthreads();
+#pragma unroll
+      for (int c0 = 0; c0 < NH; c0 += PD_WAVES) {
+        const int c = c0 + wave;
+        if (c < NH) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < PD_WAVES; ++w) v += *(const f32x4*)(buf + (((w * NH + c) * 4 + g) * 64 + lane) * 4) * f[w];
+            if (hj + col < a.H) *(f32x4*)(po + 32 * (ph * NH + c) + 8 * g) = v;
+          }
+        }
+      }
+    }
+    if (wave == 0 && half == 0 && hj + col < a.H) {
+      a.part_ml[2 * row] = M;
+      a.part_ml[2 * row + 1] = L;
+    }
+  } while (!joined && T < T_end);
+}
+
+// ---- the merge ------------------------------------------------------------------------
+// Where the states of a (sequence, head) are: those of its own rows, then those of the shared ones.
+struct LatentStates {
+  States own;
+  int n = 0, first = 0, pos = 0;  // first: 4 (workgroup + quad) of the shared rows' first state
+  int own_base = 0;
+};
+struct LatentWhere {
+  const int32_t *head, *tile_off, *quad_item, *block_quad;
+  int HB, nwg, max_quads;
+  __device__ __forceinline__ LatentStates states(int b, int h) const {
+    const int x = b * HB + h / 32, shared = head[0], own = head[1];
+    const int n_s = shared_workgroups(nwg, shared, own);
+    LatentStates s;
+    s.own = States(ListCut(own, nwg - n_s), x, tile_off[x], tile_off[x + 1]);
+    s.own_base = 4 * (n_s + max_quads);
+    s.n = s.own.n;
+    const int q = block_quad[x];
+    if (q >= 0) {
+      const ItemCut cut(shared, n_s);
+      const int w0 = quad_item[q >> 2] / cut.share, w1 = (quad_item[(q >> 2) + 1] - 1) / cut.share;
+      s.n += w1 - w0 + 1;
+      s.first = 4 * (w0 + (q >> 2)) + (q & 3);
+    }
+    return s;
+  }
+  __device__ __forceinline__ int64_t row(const LatentStates& s, int k, int h) const {
+    const int64_t slot = k < s.own.n ? (int64_t)s.own_base + s.own.slot(k) : s.first + 4 * (int64_t)(k - s.own.n);
+    return slot * 32 + h % 32;
+  }
+};
+
+struct SharedLayout {
+  size_t qabs, part_o, part_ml, plan, bytes;
+  int max_quads, nwg;
+};
+SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_groups) {
+  const size_t HB = (H + 31) / 32, VB = B * HB;
+  SharedLayout l;
+  l.max_quads = (int)(n_groups == 0 ? 0 : VB / 4 + n_groups);
+  const int64_t tiles = (int64_t)VB * ((max_len + (int64_t)PD_KT - 1) / PD_KT);
+  l.nwg = (int)(tiles < 2 ? 2 : tiles < PD_CUS ? tiles : PD_CUS);
+  const size_t slots = 4 * ((size_t)l.nwg + l.max_quads) + VB;
+  l.qabs = 0;
+  l.part_o = l.qabs + al(VB * 32 * DK * 4);
+  l.part_ml = l.part_o + al(slots * 32 * DVL * 4);
+  l.plan = l.part_ml + al(slots * 32 * 2 * 4);
+  l.bytes = l.plan + al((8 + 2 * (size_t)B + 2 * VB + 1 + 2 * (size_t)l.max_quads + 1 + 2 * (size_t)n_groups) * 4);
+  return l;
+}
+
+// (DK, DVL, workgroups a CU: what LDS and registers hold)
+#define MLA_SHARED_SHAPES(X) X(576, 512, 1) X(288, 256, 1) X(160, 128, 2)
 
 }  // namespace
 
-size_t decode_shared_ws_bytes(int B, int H, int DK, int DVL, int max_len, int n_groups) { return 256; }
+size_t decode_shared_ws_bytes(int B, int H, int DK, int DVL, int max_len, int n_groups) {
+  return shared_layout(B, H, DK, DVL, max_len, n_groups).bytes;
+}
 
 hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   const DecodePaged& d = p.d;
-  const int DK = d.rkv + d.dr, DVL = d.rkv;
-  SharedDev a;
-  a.c = d.c; a.len = d.len; a.max_len = d.max_len; a.B = d.B; a.H = d.H; a.dn = d.dn; a.dr = d.dr;
-  a.dv = d.dv; a.hpg = d.hpg; a.q = (const bf16_t*)d.q; a.Wuk = (const bf16_t*)d.Wuk;
-  a.Wuv = (const bf16_t*)d.Wuv; a.o = (bf16_t*)d.o; a.sl2 = d.scale * attn::LOG2E;
+  const int DK = d.rkv + d.dr, DVL = d.rkv, HB = (d.H + 31) / 32, VB = d.B * HB;
+  if (d.dn > ABS_DN || d.rkv % 64) return hipErrorInvalidValue;
+  const SharedLayout l = shared_layout(d.B, d.H, DK, DVL, d.max_len, p.n_groups);
+  char* ws = (char*)d.ws;
+  LatentDev a;
+  a.pool = (const char*)d.c.pool; a.table = d.c.table; a.n_pages = d.c.n_pages; a.page_size = d.c.page_size;
+  a.max_pages = d.c.max_pages;
+  a.page_bytes = p.e4m3 ? E4m3Page(d.c.page_size, d.rkv, d.dr).bytes : (int64_t)d.c.page_size * DK * 2;
+  a.len = d.len; a.max_len = d.max_len; a.B = d.B; a.H = d.H; a.HB = HB;
+  a.qabs = ws + l.qabs; a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
+  a.sl2 = d.scale * attn::LOG2E; a.nwg = l.nwg;
+  a.n_groups = p.n_groups; a.max_quads = l.max_quads; a.group_off = p.group_off; a.shared_len = p.shared_len;
+  int32_t* at = (int32_t*)(ws + l.plan);
+  a.head = at; at += 8;
+  a.start = at; at += d.B;
+  a.group_of = at; at += d.B;
+  a.tile_off = at; at += VB + 1;
+  a.block_quad = at; at += VB;
+  a.quad_x = at; at += l.max_quads;
+  a.quad_item = at; at += l.max_quads + 1;
+  a.group_min = at; at += p.n_groups;
+  a.group_cnt = at;
+  prof_begin(KC_ELEM, s);
+  const int64_t grid = 1 + (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
+  if (p.e4m3)
+    latent_prepare_kernel<true><<<(unsigned)grid, PREP_THREADS, 0, s>>>(a, (const bf16_t*)d.q, (const bf16_t*)d.Wuk, d.hpg, d.dn, d.dr, d.rkv);
+  else
+    latent_prepare_kernel<false><<<(unsigned)grid, PREP_THREADS, 0, s>>>(a, (const bf16_t*)d.q, (const bf16_t*)d.Wuk, d.hpg, d.dn, d.dr, d.rkv);
+  prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dn * d.rkv, (double)d.B * d.H * (d.rkv + d.dr + d.dn + d.dr) * 2,
+           KLABEL("latent_prepare_kernel"));
+  // algorithmic work at full lengths
   prof_begin(KC_ATTN_FWD, s);
-#define X(a_, b_)                                                                           \
-  if (DK == a_ && DVL == b_) {                                                              \
-    if (p.e4m3) decode_simple_kernel<a_, b_, true><<<dim3(d.H, d.B), 256, 0, s>>>(a);       \
-    else decode_simple_kernel<a_, b_, false><<<dim3(d.H, d.B), 256, 0, s>>>(a);             \
+#define X(a_, b_, c_)                                                                                      \
+  if (DK == a_ && DVL == b_) {                                                                             \
+    if (p.e4m3) latent_decode_kernel<a_, b_, true, c_><<<l.nwg, 64 * PD_WAVES, 0, s>>>(a);                 \
+    else latent_decode_kernel<a_, b_, false, c_><<<l.nwg, 64 * PD_WAVES, 0, s>>>(a);                       \
   }
   MLA_SHARED_SHAPES(X)
 #undef X
-  prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL), (double)d.B * d.max_len * DK * 2,
-           KLABEL("decode_simple_kernel"));
+  prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL),
+           (double)d.B * d.max_len * (p.e4m3 ? d.rkv + 2 * d.dr + 4 : DK * 2), KLABEL("latent_decode_kernel"));
+  prof_begin(KC_ELEM, s);
+  const LatentWhere w{a.head, a.tile_off, a.quad_item, a.block_quad, HB, l.nwg, l.max_quads};
+#define X(a_, b_, c_) \
+  if (DK == a_ && DVL == b_) decode_finish<b_>(d, a.part_o, a.part_ml, w, s);
+  MLA_SHARED_SHAPES(X)
+#undef X
+  prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dv * d.rkv, ((double)l.nwg + d.B) * d.H * (DVL + 2) * 4,
+           KLABEL("paged_finish_kernel"));
   return hipGetLastError();
 }
 

@@ -4,6 +4,7 @@
 #include "attn_common.h"
 #include "cache_rows.h"
 #include "common.h"
+#include "decode_parts.h"
 #include "kernels.h"
 
 namespace mla {
@@ -43,11 +44,6 @@ size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 // Precision: the absorbed queries are bf16 operands, and their rounding is what the output loses beside its
 // own (2.3e-3 of the norm against 1.65e-3); probabilities and weighted latents are held as two bf16 values each,
 // sums and states in fp32.
-constexpr int PD_KT = 32;         // rows per tile
-constexpr int PD_WAVES = 4;
-constexpr float PD_SLACK = 8.f;   // log2 units the running reference maximum may lag
-constexpr int PD_CUS = 256;
-
 struct PagedDecodeDev {
   const bf16_t* pool;
   const int32_t* table;
@@ -64,53 +60,6 @@ struct PagedDecodeDev {
 __device__ __forceinline__ int decode_len(const PagedDecodeDev& a, int b) {
   return min(max(a.len[b], 0), a.max_len);
 }
-__device__ __forceinline__ int tiles_of(int n) { return (int)(((uint32_t)n + PD_KT - 1) / PD_KT); }  // (n up to 2^31 - 1)
-// The list's cut: tiles per workgroup (at least one for each wavefront), and the part of
-// workgroup w and of its wavefronts.
-struct ListCut {
-  int total, share;
-  __device__ __forceinline__ ListCut(int tiles, int nwg) : total(tiles), share(max(PD_WAVES, (tiles + nwg - 1) / nwg)) {}
-  __device__ __forceinline__ int lo(int w) const { return (int)min((int64_t)w * share, (int64_t)total); }
-  __device__ __forceinline__ int hi(int w) const { return min(lo(w) + share, total); }
-  __device__ __forceinline__ int per_wave(int w) const { return (hi(w) - lo(w) + PD_WAVES - 1) / PD_WAVES; }
-};
-
-// Matrix products with their accumulators where they are wanted: the weighted latents fill the 256
-// accumulation registers, the tile's logits are in vector registers.  (The compiler puts every
-// product's result on one side, and moved 256 values out and in around each tile for the few that
-// are rescaled.)  The waits are those that the compiler keeps around products it knows: two
-// states after the vector ALU wrote an operand, and the product's passes (19 states at most)
-// before the vector ALU reads a result.  The compiler does not know that latency: that it puts no move or
-// spill of an accumulator there (the kernel of 576-wide rows spills 4 vector and 22 scalar registers) is
-// checked on the built code by tests/test_matrix_waits.py.
-__device__ __forceinline__ void mfma_v_first(f32x16& d, bf16x8 x, bf16x8 y) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));
-}
-__device__ __forceinline__ void mfma_v_next(f32x16& d, bf16x8 x, bf16x8 y) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(x), "v"(y));
-}
-__device__ __forceinline__ void mfma_v_done(f32x16& d) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(d)); }
-__device__ __forceinline__ void mfma_a(f32x16& d, bf16x8 x, bf16x8 y) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(x), "v"(y));
-}
-template <int N>
-__device__ __forceinline__ void mfma_a_done(f32x16 (&d)[N]) {
-  asm volatile("s_nop 15\n\ts_nop 7" : "+a"(d[0]));
-#pragma unroll
-  for (int c = 1; c < N; ++c) asm volatile("" : "+a"(d[c]));
-}
-// v *= f on accumulation registers
-__device__ __forceinline__ void acc_scale(f32x16& v, float f) {
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    float x = v[e], t;
-    asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1"
-                 : "+a"(x), "=&v"(t)
-                 : "v"(f));
-    v[e] = x;
-  }
-}
-
 // A tile in LDS: 32 rows of CHR 16-byte chunks, not padded; chunk c of row r lies at c ^ swz(r), which
 // spreads both read patterns over the banks: 16 bytes of 16 consecutive rows (S^T, no conflicts), and
 // the transposing reads' 32 bytes of four consecutive rows (V^T; the rows that share banks differ
@@ -132,11 +81,6 @@ struct Tile {
     return WIDE ? (r >> 1 & 1) << 1 | (r >> 2 & 1) << 2 | (r >> 3 & 1) : r >> 2 & 3;
   }
 };
-
-// 1 KB from a uniform address plus the lanes' offsets to the LDS byte address `lds`
-__device__ __forceinline__ void copy_s(uint64_t sbase, uint32_t voff, uint32_t lds) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
-}
 
 template <int DK, int DVL, int OCC>
 __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedDecodeDev a) {
@@ -502,162 +446,6 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
   } while (!joined && T < T_end);
 }
 
-// The states of a (sequence, head) joined, then W_UV on the matrix cores: lat[d] = sum_s o_s[d]
-// 2^(m_s - M) / sum_s l_s 2^(m_s - M), o[e] = sum_d W_UV[g][e][d] lat[d].  A workgroup owns HB heads
-// of a KV group and RB sequences, the columns of the product.  W_UV of the group is copied to LDS,
-// asked for before anything else (read from memory as the matrix operand its rows' 16-byte pieces
-// cost 64 address cycles a KB, 3.4 us for 128 KB; copied 0.9); DVL / 4 threads, four latents each,
-// take a column's states (or every so-many-th of them), eight in flight.  States in the list's
-// order.  The latent enters the product as the sum of two bf16 values, so that it is not rounded
-// between the softmax and W_UV.  Bound by latency: the list's places, the states, the product.
-constexpr int PF_THREADS = 1024;
-
-// Where the states of the sequence with tiles [t0, t1) are: n of them, the first n0 in the slots
-// of its first workgroup (one if that is joined), one for each workgroup inside, the last in those
-// of its last workgroup.
-struct States {
-  int n = 0, n0 = 0, mid = 0, at0 = 0, at_mid = 0, at1 = 0;
-  States() = default;
-  __device__ __forceinline__ States(const ListCut& cut, int b, int t0, int t1) {
-    if (t1 <= t0) return;
-    const int w0 = t0 / cut.share, w1 = (t1 - 1) / cut.share;
-    int v;
-    n0 = part(cut, w0, t0, t1, v);
-    at0 = PD_WAVES * w0 + v + b;
-    n = n0;
-    if (w1 > w0) {
-      mid = w1 - w0 - 1;
-      at_mid = PD_WAVES * (w0 + 1) + b;
-      n += mid + part(cut, w1, t0, t1, v);
-      at1 = PD_WAVES * w1 + v + b;
-    }
-  }
-  __device__ __forceinline__ static int part(const ListCut& cut, int w, int t0, int t1, int& v) {
-    const int lo = cut.lo(w), hi = cut.hi(w), per = cut.per_wave(w);
-    v = 0;
-    if (t0 <= lo && hi <= t1) return 1;  // joined
-    v = (max(t0, lo) - lo) / per;
-    return (min(t1, hi) - 1 - lo) / per - v + 1;
-  }
-  __device__ __forceinline__ int slot(int k) const {
-    if (k < n0) return at0 + k;
-    k -= n0;
-    if (k < mid) return at_mid + PD_WAVES * k;
-    return at1 + k - mid;
-  }
-};
-
-template <int DVL, int DV, int HB, int RB>
-__global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* __restrict__ part_o,
-                                                                  const float* __restrict__ part_ml,
-                                                                  const int32_t* __restrict__ tile_off,
-                                                                  const bf16_t* __restrict__ Wuv,
-                                                                  bf16_t* __restrict__ o, int B, int H, int HP,
-                                                                  int nwg, int hpg) {
-  constexpr int NCG = DVL / 4, NCOL = HB * RB, NSLOT = PF_THREADS / NCG / NCOL, U = 8;
-  constexpr int CHW = DVL / 8, NCPW = DV * CHW / 64, NW = PF_THREADS / 64, LDL = DVL + 8;
-  constexpr int RED = NSLOT > 1 ? NCOL * NSLOT * DVL * 4 : 16, LAT = 2 * NCOL * LDL * 2;
-  static_assert(NSLOT >= 1 && NCPW % NW == 0 && NCOL <= 16 && CHW >= 16, "finish shape");
-  __shared__ __attribute__((aligned(1024))) bf16_t Ws[DV * DVL];  // chunk c of row e at c ^ (e % 16)
-  __shared__ __attribute__((aligned(16))) char red_mem[RED];
-  __shared__ __attribute__((aligned(16))) char lat_mem[LAT];
-  __shared__ float sm[NCOL][NSLOT], sl[NCOL][NSLOT];
-  float(*red)[DVL] = (float(*)[DVL])red_mem;                  // [NCOL * NSLOT]
-  bf16_t* lat = (bf16_t*)lat_mem;                             // [2][NCOL][LDL]: rounded, and what that lost
-  const int i0 = HB * blockIdx.x, b0 = RB * blockIdx.y;
-  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
-  const bf16_t* Wg = Wuv + (int64_t)(i0 / hpg) * DV * DVL;
-#pragma unroll
-  for (int k0 = 0; k0 < NCPW / NW; ++k0) {
-    const int k = k0 * NW + wave, idx = 64 * k + lane, e = idx / CHW, c = (idx % CHW) ^ (e & 15);
-    dma16(Wg + e * DVL + 8 * c, Ws + 512 * k);
-  }
-  // this thread's column: head i0 + h, sequence b0 + r
-  const int cg = tid % NCG, grp = tid / NCG, col = grp / NSLOT, slot = grp % NSLOT;
-  const int h = col % HB, b = b0 + col / HB;
-  const ListCut cut(tile_off[B], nwg);
-  States st;
-  if (b < B) st = States(cut, b, tile_off[b], tile_off[b + 1]);
-  float M = -INFINITY, L = 0.f;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = slot; k0 < st.n; k0 += U * NSLOT) {
-    f32x4 x[U];
-    f32x2 ml[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + u * NSLOT;
-      ml[u] = f32x2{-INFINITY, 0.f};
-      x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (k < st.n) {
-        const int64_t rw = (int64_t)st.slot(k) * HP + i0 + h;
-        x[u] = *(const f32x4*)(part_o + rw * DVL + 4 * cg);
-        ml[u] = *(const f32x2*)(part_ml + 2 * rw);
-      }
-    }
-    float m1 = M;
-#pragma unroll
-    for (int u = 0; u < U; ++u) m1 = fmaxf(m1, ml[u][0]);
-    const float ref = m1 == -INFINITY ? 0.f : m1, c = __builtin_amdgcn_exp2f(M - ref);
-    v *= c;
-    L *= c;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float w = __builtin_amdgcn_exp2f(ml[u][0] - ref);
-      v += x[u] * w;
-      L += ml[u][1] * w;
-    }
-    M = m1;
-  }
-  if (NSLOT > 1) {
-    *(f32x4*)&red[grp][4 * cg] = v;
-    if (cg == 0) {
-      sm[col][slot] = M;
-      sl[col][slot] = L;
-    }
-    __syncthreads();
-  }
-  if (slot == 0) {
-    if (NSLOT > 1) {  // the column's slots, in order
-      float ref = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < NSLOT; ++k) ref = fmaxf(ref, sm[col][k]);
-      if (ref == -INFINITY) ref = 0.f;
-      v = f32x4{0.f, 0.f, 0.f, 0.f};
-      L = 0.f;
-#pragma unroll
-      for (int k = 0; k < NSLOT; ++k) {
-        const float f = __builtin_amdgcn_exp2f(sm[col][k] - ref);
-        v += *(const f32x4*)&red[grp + k][4 * cg] * f;
-        L += sl[col][k] * f;
-      }
-    }
-    v *= L == 0.f ? 0.f : 1.f / L;  // (NaN stays NaN)
-    const u32x2 hi = {pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
-    *(u32x2*)(lat + col * LDL + 4 * cg) = hi;
-    *(u32x2*)(lat + (NCOL + col) * LDL + 4 * cg) =
-        u32x2{pack2bf(v[0] - __uint_as_float(hi[0] << 16), v[1] - __uint_as_float(hi[0] & 0xffff0000u)),
-              pack2bf(v[2] - __uint_as_float(hi[1] << 16), v[3] - __uint_as_float(hi[1] & 0xffff0000u))};
-  }
-  wait_vm<0>();  // W_UV
-  __syncthreads();
-  if (wave >= DV / 16) return;
-  // W_UV rows 16 wave + lane % 16 as the A operand, column lane % 16 of the latents as the B operand
-  const int n = lane & 15, q = lane >> 4, e = 16 * wave + n;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int kk = 0; kk < DVL / 32; ++kk) {
-    const bf16x8 wf = *(const bf16x8*)(Ws + e * DVL + 8 * ((4 * kk + q) ^ (e & 15)));
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          wf, *(const bf16x8*)(lat + (p * NCOL + min(n, NCOL - 1)) * LDL + 32 * kk + 8 * q), acc, 0, 0, 0);
-  }
-  if (n >= NCOL || b0 + n / HB >= B) return;
-  bf16_t* op = o + ((int64_t)(b0 + n / HB) * H + i0 + n % HB) * DV + 16 * wave + 4 * q;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) op[k] = f2bf(acc[k]);  // (o may have any alignment)
-}
-
 // Workgroups over the list, for each block of 32 heads: one a CU in all, and no more than have a
 // tile for each wavefront at the largest lengths.
 int decode_workgroups(int B, int H, int max_len) {
@@ -713,29 +501,10 @@ hipError_t decode_paged(const DecodePaged& d, hipStream_t s) {
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL), (double)d.B * d.max_len * DK * 2,
            KLABEL("paged_decode_kernel"));
   prof_begin(KC_ELEM, s);
-  // One column a workgroup while that is one round on the CUs, else eight that share W_UV (four heads of two
-  // sequences, or one of eight where a group's heads are no multiple of four): 64 columns of many states
-  // 9.7 us by one, 38 by eight; 2048 columns 36 us by one, 8.2 by eight.
-  const bool few = (int64_t)d.B * d.H <= PD_CUS, heads4 = d.hpg % 4 == 0;
-#define FIN(b_, v_, hb_, rb_)                                                                             \
-  paged_finish_kernel<b_, v_, hb_, rb_><<<dim3(d.H / hb_, (d.B + rb_ - 1) / rb_), PF_THREADS, 0, s>>>(    \
-      a.part_o, a.part_ml, a.tile_off, (const bf16_t*)d.Wuv, (bf16_t*)d.o, d.B, d.H, HP, nwg, d.hpg)
-#define FINV(b_, v_)           \
-  if (few) FIN(b_, v_, 1, 1);  \
-  else if (heads4) FIN(b_, v_, 4, 2); \
-  else FIN(b_, v_, 1, 8)
-#define X(a_, b_, c_)          \
-  if (DK == a_ && DVL == b_) { \
-    if (d.dv == 128) {         \
-      FINV(b_, 128);           \
-    } else {                   \
-      FINV(b_, 64);            \
-    }                          \
-  }
+#define X(a_, b_, c_) \
+  if (DK == a_ && DVL == b_) decode_finish<b_>(d, a.part_o, a.part_ml, ListWhere{a.tile_off, d.B, HP, nwg}, s);
   MLA_PAGED_SHAPES(X)
 #undef X
-#undef FINV
-#undef FIN
   prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dv * d.rkv, ((double)nwg + d.B) * d.H * (DVL + 2) * 4,
            KLABEL("paged_finish_kernel"));
   return hipGetLastError();
