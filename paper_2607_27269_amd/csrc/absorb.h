@@ -1,7 +1,5 @@
 // The absorbed queries of decoding (decode.hip, decode_shared.hip).
 #pragma once
-#include <type_traits>
-
 #include "common.h"
 
 namespace mla {
@@ -17,16 +15,17 @@ namespace mla {
 // a copy launch before).
 // ABS_FRAG: qabs in the order in which the paged decoding reads it, [b][block of 32 heads][16-wide step
 // kk][half][head][8]: a matrix operand is 1 KB in one piece there.
-// ABS_FRAG32: the same order, fp32 (the decoding over an eight-bit cache scales and rounds them itself).
+// ABS_F16: fp16 for the decoding over an eight-bit cache, as [b][block of heads][step][half][head][8]: step 2 i + e
+// of half h holds latents 32 i + 16 h + 8 e + 0..7.  32 latents of a head are brought to [2^8, 2^9) by a power of
+// two, whose exponent is written to exps [b][block of heads][head][rkv / 32]; the rotary part stays bf16.
 constexpr int ABS_LD = 96;  // LDS row stride: 4 rows of a transposing read on distinct banks
 constexpr int ABS_DN = 192;
-enum AbsorbOut { ABS_ROWS, ABS_FRAG, ABS_FRAG32 };
+enum AbsorbOut { ABS_ROWS, ABS_FRAG, ABS_F16 };
+constexpr int ABS_MIN_EXP = -126, ABS_MAX_EXP = 120;
 template <AbsorbOut OUT>
 __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const bf16_t* __restrict__ Wuk,
-                                             void* __restrict__ qabs_, int B, int H, int HP, int hpg, int dn,
-                                             int dr, int rkv, int bx, int by, int g) {
-  using T = typename std::conditional<OUT == ABS_FRAG32, float, bf16_t>::type;
-  T* qabs = (T*)qabs_;
+                                             bf16_t* __restrict__ qabs, int8_t* __restrict__ exps, int B, int H,
+                                             int HP, int hpg, int dn, int dr, int rkv, int bx, int by, int g) {
   __shared__ __attribute__((aligned(16))) bf16_t Ws[ABS_DN * ABS_LD];
   const int c0 = 64 * bx, r0 = 32 * by;
   const int DK = rkv + dr, dq = dn + dr, tid = threadIdx.x;
@@ -62,16 +61,8 @@ __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const
     return OUT != ABS_ROWS ? qabs + fi + (c >> 4) * 512 + (c >> 3 & 1) * 256 : qabs + qi * DK + c;
   };
   if (bx == 0 && wave == 0 && rr < rows)  // rotary part: dr elements, half a row per lane
-    for (int c = 8 * half; c < dr; c += 16) {
-      const u32x4 v = *(const u32x4*)(q + bi * dq + dn + c);
-      if constexpr (OUT == ABS_FRAG32) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *(f32x2*)(place(rkv + c) + 2 * k) = f32x2{__uint_as_float(v[k] << 16), __uint_as_float(v[k] & 0xffff0000u)};
-      } else {
-        *(u32x4*)place(rkv + c) = v;
-      }
-    }
+    for (int c = 8 * half; c < dr; c += 16)
+      *(u32x4*)place(rkv + c) = *(const u32x4*)(q + bi * dq + dn + c);
   __syncthreads();
   f32x16 acc;
 #pragma unroll
@@ -82,13 +73,25 @@ __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           lds_operand_tr(Ws, ABS_LD, 32 * wave, 16 * kk + 8 * half, 16 * kk + 8 * half + 4), qf[kk], acc,
           0, 0, 0);
+  if constexpr (OUT == ABS_F16) {
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(acc[e]));
+    top = pair_max32(top);  // (the lane pair has the row's 32 latents of this wavefront)
+    const int t = min(max((int)(__float_as_uint(top) >> 23) - 135, ABS_MIN_EXP), ABS_MAX_EXP), i = c0 / 32 + wave;
+    const float down = __uint_as_float((uint32_t)(127 - t) << 23);
+    if (rr >= rows) return;
+    if (half == 0) exps[qi * (rkv / 32) + i] = (int8_t)t;
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4)
+      *(u32x2*)(qabs + fi + (2 * i + (e4 & 1)) * 512 + (e4 >> 1) * 256 + 4 * half) =
+          u32x2{pack2h(acc[4 * e4] * down, acc[4 * e4 + 1] * down), pack2h(acc[4 * e4 + 2] * down, acc[4 * e4 + 3] * down)};
+    return;
+  }
   if (rr >= rows) return;
 #pragma unroll
   for (int e4 = 0; e4 < 4; ++e4)
-    if constexpr (OUT == ABS_FRAG32)
-      *(f32x4*)(place(c0 + 32 * wave + 8 * e4) + 4 * half) = f32x4{acc[4 * e4], acc[4 * e4 + 1], acc[4 * e4 + 2], acc[4 * e4 + 3]};
-    else
-      *(u32x2*)(place(c0 + 32 * wave + 8 * e4) + 4 * half) = u32x2{pack2bf(acc[4 * e4], acc[4 * e4 + 1]), pack2bf(acc[4 * e4 + 2], acc[4 * e4 + 3])};
+    *(u32x2*)(place(c0 + 32 * wave + 8 * e4) + 4 * half) = u32x2{pack2bf(acc[4 * e4], acc[4 * e4 + 1]), pack2bf(acc[4 * e4 + 2], acc[4 * e4 + 3])};
 }
 
 }  // namespace mla

@@ -87,9 +87,9 @@ struct DecodeDev {
 template <AbsorbOut OUT>
 __global__ __launch_bounds__(128) void absorb_kernel(const bf16_t* __restrict__ q,
                                                      const bf16_t* __restrict__ Wuk,
-                                                     void* __restrict__ qabs, int B, int H, int HP,
+                                                     bf16_t* __restrict__ qabs, int B, int H, int HP,
                                                      int hpg, int dn, int dr, int rkv) {
-  absorb_block<OUT>(q, Wuk, qabs, B, H, HP, hpg, dn, dr, rkv, blockIdx.x, blockIdx.y, blockIdx.z);
+  absorb_block<OUT>(q, Wuk, qabs, nullptr, B, H, HP, hpg, dn, dr, rkv, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 template <int DK, int DVL>
@@ -466,10 +466,10 @@ hipError_t decode_absorb(const void* q, const void* Wuk, void* qabs, int B, int 
   prof_begin(KC_ELEM, s);
   const dim3 grid(rkv / 64, (B * hpg + 31) / 32, H / hpg);
   if (frag)
-    absorb_kernel<ABS_FRAG><<<grid, 128, 0, s>>>((const bf16_t*)q, (const bf16_t*)Wuk, qabs, B, H, HP, hpg,
+    absorb_kernel<ABS_FRAG><<<grid, 128, 0, s>>>((const bf16_t*)q, (const bf16_t*)Wuk, (bf16_t*)qabs, B, H, HP, hpg,
                                              dn, dr, rkv);
   else
-    absorb_kernel<ABS_ROWS><<<grid, 128, 0, s>>>((const bf16_t*)q, (const bf16_t*)Wuk, qabs, B, H, HP,
+    absorb_kernel<ABS_ROWS><<<grid, 128, 0, s>>>((const bf16_t*)q, (const bf16_t*)Wuk, (bf16_t*)qabs, B, H, HP,
                                               hpg, dn, dr, rkv);
   prof_end(KC_ELEM, s, 2.0 * B * H * dn * rkv, (double)B * H * (rkv + dr + dn + dr) * 2,
            KLABEL("absorb_kernel"));

@@ -35,7 +35,8 @@ struct LatentDev {
   int64_t page_bytes;
   const int32_t* len;
   int max_len, B, H, HB;  // HB: blocks of 32 heads
-  const void* qabs;       // [B HB][DK / 16][64 lanes][8], bf16 or (e4m3) fp32
+  const bf16_t* qabs;     // [B HB][DK / 16][64 lanes][8], bf16 or (e4m3, the latents) fp16
+  const int8_t* qexp;     // e4m3: [B HB][32][DVL / 32], exponents of the queries' powers of two
   float* part_o;          // [slot][32][DVL], not normalised
   float* part_ml;         // [slot][32][2]: reference (log2), sum
   float sl2;
@@ -51,8 +52,7 @@ struct LatentDev {
   int32_t* quad_item;     // [max_quads + 1]: first item of each quad
   int32_t* block_quad;    // [B HB]: 4 quad + place in it, or -1
   int32_t* group_of;      // [B], -1: none
-  int32_t* group_min;     // [n_groups]: shared rows that all have; then how many sequences have rows
-  int32_t* group_cnt;
+  int32_t* group;         // [5 n_groups]: scratch of the plan
 };
 
 __device__ __forceinline__ int len_of(const LatentDev& a, int b) { return min(max(a.len[b], 0), a.max_len); }
@@ -105,9 +105,13 @@ __device__ __forceinline__ int agent_load(const int32_t* p) {
 template <int NT>
 __device__ void make_plan(const LatentDev& a) {
   const int tid = threadIdx.x, G = a.n_groups;
+  // per group: the shared rows that all its sequences have, how many have rows; then its first quad, item, and tiles
+  constexpr int IN_LDS = 512;
+  __shared__ int32_t group_lds[5 * IN_LDS];
+  int32_t *group_min = G <= IN_LDS ? group_lds : a.group, *group_cnt = group_min + G, *group = group_cnt + G;
   for (int g = tid; g < G; g += NT) {
-    __hip_atomic_store(a.group_min + g, min(max(a.shared_len[g], 0), a.max_len), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(a.group_cnt + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(group_min + g, min(max(a.shared_len[g], 0), a.max_len), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(group_cnt + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __threadfence();
   __syncthreads();
@@ -121,15 +125,14 @@ __device__ void make_plan(const LatentDev& a) {
     a.group_of[b] = g;
     const int n = len_of(a, b);
     if (g >= 0 && n > 0) {
-      atomicMin(a.group_min + g, n);
-      atomicAdd(a.group_cnt + g, 1);
+      atomicMin(group_min + g, n);
+      atomicAdd(group_cnt + g, 1);
     }
-    for (int h = 0; h < a.HB; ++h) a.block_quad[b * a.HB + h] = -1;
   }
   __threadfence();
   __syncthreads();
   // (one block alone gains nothing)
-  auto rows_of = [&](int g) { return agent_load(a.group_cnt + g) * (int64_t)a.HB >= 2 ? agent_load(a.group_min + g) / PD_KT * PD_KT : 0; };
+  auto rows_of = [&](int g) { return agent_load(group_cnt + g) * (int64_t)a.HB >= 2 ? agent_load(group_min + g) / PD_KT * PD_KT : 0; };
   // quads and their items
   const int run = (G + NT - 1) / NT, g_lo = min(tid * run, G), g_hi = min(g_lo + run, G);
   auto blocks = [&](int g, int& x0) {
@@ -147,28 +150,45 @@ __device__ void make_plan(const LatentDev& a) {
   }
   int k = scan_before<NT>(quads, total_q), at = scan_before<NT>(items, total_i);
   for (int g = g_lo; g < g_hi; ++g) {
-    const int n = blocks(g, x0), t = rows_of(g) / PD_KT;
-    if (t == 0) continue;
-    for (int i = 0; i < n; i += 4, ++k, at += t) {
-      if (k >= a.max_quads) break;
-      a.quad_x[k] = 4 * (x0 + i) + min(n - i, 4) - 1;
-      a.quad_item[k] = at;
-      if (k == a.max_quads - 1) a.quad_item[k + 1] = at + t;
-      for (int j = 0; j < min(n - i, 4); ++j)  // (sequences without rows take no part)
-        if (len_of(a, (x0 + i + j) / a.HB) > 0) a.block_quad[x0 + i + j] = 4 * k + j;
+    const int n = blocks(g, x0), t = rows_of(g) / PD_KT, q = (n + 3) / 4;
+    group[3 * g] = k;
+    group[3 * g + 1] = at;
+    group[3 * g + 2] = t;
+    if (t > 0) {
+      k += q;
+      at += q * t;
     }
   }
   if (tid == 0) {
     a.head[2] = min(total_q, a.max_quads);
-    if (total_q < a.max_quads) a.quad_item[total_q] = total_i;
+    a.quad_item[min(total_q, a.max_quads)] = total_i;  // (again below, where the quads do not fit)
   }
+  __threadfence();
+  __syncthreads();
   // own rows
   const int runb = (a.B + NT - 1) / NT, b_lo = min(tid * runb, a.B), b_hi = min(b_lo + runb, a.B);
   int mine = 0, total;
   for (int b = b_lo; b < b_hi; ++b) {
-    const int g = a.group_of[b], n = len_of(a, b), s = g >= 0 ? min(rows_of(g), n) : 0;
+    const int g = a.group_of[b], n = len_of(a, b);
+    int s = 0, k0 = 0, at0 = 0, first = 0, blocks_of = 0;
+    if (g >= 0) {
+      k0 = agent_load(group + 3 * g);
+      at0 = agent_load(group + 3 * g + 1);
+      s = min(agent_load(group + 3 * g + 2) * PD_KT, n);
+      blocks_of = blocks(g, first);
+    }
     a.start[b] = s;
     mine += tiles_of(n - s) * a.HB;
+    for (int h = 0; h < a.HB; ++h) {
+      const int x = b * a.HB + h, j = x - first, q = k0 + j / 4, t = g >= 0 ? agent_load(group + 3 * g + 2) : 0;
+      const bool in = t > 0 && j >= 0 && q < a.max_quads;
+      a.block_quad[x] = in && n > 0 ? 4 * q + j % 4 : -1;  // (sequences without rows take no part)
+      if (in && j % 4 == 0) {
+        a.quad_x[q] = 4 * x + min(blocks_of - j, 4) - 1;
+        a.quad_item[q] = at0 + j / 4 * t;
+        if (q == a.max_quads - 1) a.quad_item[q + 1] = at0 + (j / 4 + 1) * t;
+      }
+    }
   }
   at = scan_before<NT>(mine, total);
   for (int b = b_lo; b < b_hi; ++b) {
@@ -179,7 +199,7 @@ __device__ void make_plan(const LatentDev& a) {
   if (tid == 0) {
     a.tile_off[a.B * a.HB] = total;
     const int q = min(total_q, a.max_quads);
-    a.head[0] = q == 0 ? 0 : a.quad_item[q];
+    a.head[0] = q == 0 ? 0 : agent_load(a.quad_item + q);
     a.head[1] = total;
   }
 }
@@ -194,8 +214,8 @@ __global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev 
     return;
   }
   const int nx = rkv / 64, ny = (a.B * hpg + 31) / 32, k = blockIdx.x - 1;
-  absorb_block<E4M3 ? ABS_FRAG32 : ABS_FRAG>(q, Wuk, (void*)a.qabs, a.B, a.H, 32 * a.HB, hpg, dn, dr, rkv, k % nx,
-                                             k / nx % ny, k / nx / ny);
+  absorb_block<E4M3 ? ABS_F16 : ABS_FRAG>(q, Wuk, (bf16_t*)a.qabs, (int8_t*)a.qexp, a.B, a.H, 32 * a.HB, hpg, dn, dr,
+                                          rkv, k % nx, k / nx % ny, k / nx / ny);
 }
 
 // ---- attention ------------------------------------------------------------------------
@@ -223,13 +243,7 @@ __device__ __forceinline__ u32x2 lds_read_tr8(const char* p) {
   typedef int i32x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p));
 }
-// 4 bytes a lane from the lanes' addresses to the LDS byte address `lds`
-__device__ __forceinline__ void copy4(uint64_t src, uint32_t lds) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(lds) : "memory");
-}
-
-// A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r) (paged_attn.hip), and
-// in eight bits the rows' powers behind them.  S^T reads 16 bytes of 16 consecutive rows, which take
+// A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r) (paged_attn.hip).  S^T reads 16 bytes of 16 consecutive rows, which take
 // different banks; the transposing reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16:
 // 32 bytes of four rows).  In eight bits the rows of those that share banks differ in bits 1 and 3 where two
 // rows span the banks (640 bytes), which go to chunk bits 1 and 2.
@@ -241,7 +255,7 @@ struct LatentTile {
   static constexpr int ROWS = WIDE ? 8 : 16;
   static constexpr int PERIOD = ROWS * CHR / 64;
   static constexpr int HALF_COPIES = 16 * CHR / 64;
-  static constexpr int BYTES = PD_KT * RB, ALLOC = BYTES + (E4M3 ? 256 : 0);
+  static constexpr int BYTES = PD_KT * RB;
   static_assert(RB % 64 == 0 && CHR % (WIDE ? 8 : 4) == 0 && ROWS * CHR % 64 == 0, "whole copies");
   __device__ __forceinline__ static constexpr int swz(int r) {
     if (!WIDE) return r >> 2 & 3;
@@ -267,9 +281,13 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   constexpr int NL = DVL / 16, NR = DR / 16, NC = DVL / 32;
   constexpr int PF = E4M3 ? 3 : 5, PV = 3;  // operand reads in flight ahead of the products of S, and of P V
   static_assert(DVL % 128 == 0 && DR % 16 == 0, "decode shape");
-  __shared__ __attribute__((aligned(1024))) char tiles[PD_WAVES][TL::ALLOC];
-  __shared__ float ml[PD_WAVES][2][32];
-  __shared__ int plan_x[PD_WAVES], plan_at[PD_WAVES];
+  // In eight bits a wavefront has two tiles, all of the LDS at 576 values; what is small lies in a second tile: of
+  // wavefront 0 (the plan, before the copies) and of the wavefront itself (reference and sum, after its tiles).
+  constexpr int NBUF = E4M3 ? 2 : 1, SMALL = NBUF * PD_WAVES * TL::BYTES - (E4M3 ? PD_WAVES * TL::BYTES : 0);
+  __shared__ __attribute__((aligned(1024))) char tiles[NBUF * PD_WAVES * TL::BYTES + (E4M3 ? 0 : 1088)];
+  int* plan_x = (int*)(tiles + SMALL + (E4M3 ? 0 : 1024));  // [PD_WAVES], then plan_at
+  int* plan_at = plan_x + PD_WAVES;
+  auto ml = [&](int w) { return (float*)(tiles + SMALL + w * (E4M3 ? TL::BYTES : 256)); };  // [2][32]
 
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int half = lane >> 5, col = lane & 31;
@@ -300,12 +318,12 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   }
   // the row at position p of sequence b (the last of the tile's again past the end, which gets no weight)
   auto entry = [&](int b, int p) { return a.table[(int64_t)b * a.max_pages + p / a.page_size]; };
-  auto address = [&](int p, int page, bool& bad, uint64_t& power) {
+  auto address = [&](int p, int page, bool& bad, float& power) {
     const bool out = page < 0 || page >= a.n_pages;
     bad = __ballot(out) != 0;
     const uint64_t base = (uint64_t)(uintptr_t)a.pool + (uint64_t)((out ? 0 : page) * a.page_bytes);
     const int r = p % a.page_size;
-    if constexpr (E4M3) power = base + (uint64_t)((int64_t)a.page_size * RB + 4 * (int64_t)r);
+    if constexpr (E4M3) power = *(const float*)(uintptr_t)(base + (uint64_t)((int64_t)a.page_size * RB + 4 * (int64_t)r));
     return base + (uint64_t)((int64_t)r * RB);
   };
   auto row_address = [&](uint64_t at, int r) {
@@ -327,39 +345,33 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   float m_run, mx_run, l_run;
   bool any_bad;
   auto begin = [&](int x) __attribute__((always_inline)) {
-    if constexpr (E4M3) {
-      // step 2 i + e holds latents 32 i + 16 half + 8 e + 0..7: the 16 bytes that one LDS read gives
-      const float* src = (const float*)a.qabs + (int64_t)x * 32 * DK + 8 * col;
-      auto place = [&](int i, int e) { return src + (2 * i + half) * 512 + 256 * e; };
-      float top = 0.f;
-#pragma unroll 8
-      for (int s = 0; s < NL; ++s) {
-        const f32x4 u = *(const f32x4*)place(s >> 1, s & 1), v = *(const f32x4*)(place(s >> 1, s & 1) + 4);
+    const bf16_t* src = a.qabs + (int64_t)x * 32 * DK + 8 * lane;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(u[k]), fabsf(v[k])));
+    for (int s = 0; s < NL; ++s) qf[s] = *(const QT*)(src + 512 * s);
+#pragma unroll
+    for (int s = 0; s < NR; ++s) qr[s] = *(const bf16x8*)(src + 512 * (NL + s));
+    if constexpr (E4M3) {  // one power for the head's queries
+      const int8_t* e = a.qexp + ((int64_t)x * 32 + col) * NC;
+      int t[NC], top = ABS_MIN_EXP;
+#pragma unroll
+      for (int i = 0; i < NC; i += 4) {
+        const uint32_t w = *(const uint32_t*)(e + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          t[i + k] = (int)(w << (24 - 8 * k)) >> 24;
+          top = max(top, t[i + k]);
+        }
       }
-      top = pair_max32(top);
-      const int t = min(max((int)(__float_as_uint(top) >> 23) - 127 - 8, -120), 120);
-      const float down = power_of_two(-t);
-      qpow = power_of_two(t);
+      qpow = power_of_two(min(top, ABS_MAX_EXP));
 #pragma unroll
-      for (int s = 0; s < NL; ++s) {
-        const f32x4 u = *(const f32x4*)place(s >> 1, s & 1), v = *(const f32x4*)(place(s >> 1, s & 1) + 4);
-        qf[s] = __builtin_bit_cast(f16x8, u32x4{pack2h(u[0] * down, u[1] * down), pack2h(u[2] * down, u[3] * down),
-                                                pack2h(v[0] * down, v[1] * down), pack2h(v[2] * down, v[3] * down)});
+      for (int i = 0; i < NC; ++i) {
+        const _Float16 f = (_Float16)power_of_two(max(t[i] - top, -30));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          qf[2 * i][k] *= f;
+          qf[2 * i + 1][k] *= f;
+        }
       }
-#pragma unroll
-      for (int s = 0; s < NR; ++s) {
-        const float* p = src + (NL + s) * 512 + 256 * half;
-        const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
-        qr[s] = __builtin_bit_cast(bf16x8, u32x4{pack2bf(u[0], u[1]), pack2bf(u[2], u[3]), pack2bf(v[0], v[1]), pack2bf(v[2], v[3])});
-      }
-    } else {
-      const bf16_t* src = (const bf16_t*)a.qabs + (int64_t)x * 32 * DK + 8 * lane;
-#pragma unroll
-      for (int s = 0; s < NL; ++s) qf[s] = *(const bf16x8*)(src + 512 * s);
-#pragma unroll
-      for (int s = 0; s < NR; ++s) qr[s] = *(const bf16x8*)(src + 512 * (NL + s));
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -369,11 +381,15 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     l_run = 0.f;
     any_bad = false;
   };
-  // One tile at kt, of which `left` rows count.  `heads`: the columns with a head.  `early` is called
+  // One tile at kt, of which `left` rows count; power: of row col (eight bits).  `heads`: the columns with a head.  `early` is called
   // when the reads of the first 16 rows (and of all keys) have returned.
-  auto tile = [&](const char* kt, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
+  auto tile = [&](const char* kt, float power, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
     f32x16 s;
+    float pw[16];  // powers of the rows of s: 8 (e / 4) + 4 half + e % 4
     if constexpr (E4M3) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        pw[e] = __int_as_float(__builtin_amdgcn_ds_bpermute(16 * half + 32 * (e >> 2) + 4 * (e & 3), __float_as_int(power)));
       u32x4 raw[PF];
       auto kread = [&](int i) { return *(const u32x4*)(kt + kb[i % 4] + 128 * (i / 4)); };
 #pragma unroll
@@ -391,13 +407,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         __builtin_amdgcn_sched_barrier(0);
       }
       mfma_v_done(s);
-      const float* pw = (const float*)(kt + TL::BYTES);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 f = *(const f32x4*)(pw + 8 * g + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * g + e] *= f[e] * qpow;
-      }
+      for (int e = 0; e < 16; ++e) s[e] *= pw[e] * qpow;
 #pragma unroll
       for (int j = 0; j < NR; ++j) {
         mfma_v_next(s, __builtin_bit_cast(bf16x8, raw[(NL / 2 + j) % PF]), qr[j]);
@@ -443,18 +454,13 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     bf16x8 pl[2];
     if constexpr (E4M3) {
       float x[16];
-      const float* pw = (const float*)(kt + TL::BYTES);
       float mx = -INFINITY, my = -INFINITY;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const u32x4 f = *(const u32x4*)(pw + 8 * g + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[4 * g + e] = s[4 * g + e] * a.sl2;
-          s[4 * g + e] = x[4 * g + e] + (float)((int)(f[e] >> 23) - 127);
-          mx = fmaxf(mx, x[4 * g + e]);
-          my = fmaxf(my, s[4 * g + e]);
-        }
+      for (int e = 0; e < 16; ++e) {
+        x[e] = s[e] * a.sl2;
+        s[e] = x[e] + (float)((int)(__float_as_uint(pw[e]) >> 23) - 127);
+        mx = fmaxf(mx, x[e]);
+        my = fmaxf(my, s[e]);
       }
       mx = pair_max32(mx);
       my = pair_max32(my);
@@ -575,10 +581,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       const int idx = 64 * min(4 * j + wave, ALL - 1) + lane, r = idx / CHR;
       rc[j] = r << 8 | ((idx % CHR) ^ TL::swz(r));
     }
-    const uint32_t tiles_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)&tiles[0][0]);
-    auto issue = [&](int buf, uint64_t at, uint64_t power, bool together) __attribute__((always_inline)) {
-      const uint32_t lds = tiles_lds + buf * TL::ALLOC;
-      if constexpr (E4M3) copy4(power, lds + TL::BYTES);
+    const uint32_t tiles_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tiles);
+    auto issue = [&](int buf, uint64_t at, bool together) __attribute__((always_inline)) {
+      const uint32_t lds = tiles_lds + buf * TL::BYTES;
       const uint64_t lo = row_address(at, 0), hi = row_address(at, 16);
       auto copy = [&](int j, uint64_t row) __attribute__((always_inline)) {
         const uint64_t src = row + 16 * (rc[j] & 255);
@@ -605,27 +610,30 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       const uint64_t heads = __ballot(h0 + col < a.H);
       // tile i is copied while the one before is worked on; its table entries were asked for before that
       int p = (i - q_lo) * PD_KT + col, page = entry(b0, p);
-      bool bad;
-      uint64_t power = 0, at = address(p, page, bad, power);
-      bool bad_now = bad;
+      bool bad = false, bad_next = false;
+      float power = 1.f, power_next = 1.f;
+      uint64_t at = address(p, page, bad, power);
       __syncthreads();  // (the buffers are free)
-      issue(i & 1, at, power, whole16);
+      issue(i & 1, at, whole16);
       begin(x);
       if (i + 1 < q_hi) page = entry(b0, p + PD_KT);
       bool first = true;
       for (; i < q_hi; ++i) {
         pin(acc);
         wait_vm<0>();
+        asm volatile("" : "+v"(page), "+v"(power));  // (what was loaded is there: no wait for it below, behind the next copies)
         __syncthreads();
-        any_bad |= bad_now;
+        any_bad |= bad;
         if (i + 1 < q_hi) {
           p += PD_KT;
-          at = address(p, page, bad_now, power);
-          issue((i + 1) & 1, at, power, whole16);
+          at = address(p, page, bad_next, power_next);
+          issue((i + 1) & 1, at, whole16);
           if (i + 2 < q_hi) page = entry(b0, p + PD_KT);
         }
-        tile(&tiles[i & 1][0], PD_KT, heads, first, [] {});
+        tile(tiles + (i & 1) * TL::BYTES, power, PD_KT, heads, first, [] {});
         first = false;
+        power = power_next;
+        bad = bad_next;
       }
       store((int64_t)4 * (wg + k) + wave, wave < nx && h0 + col < a.H);
     }
@@ -649,7 +657,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     }
   }
   __syncthreads();
-  int T = t_lo + wave * per;                       // this wavefront's run: tiles [T, T_end)
+  const int t_first = t_lo + wave * per;
+  int T = t_first;                                 // this wavefront's run: tiles [T, T_end)
   const int T_end = min(T + per, t_hi);
   int x = 0, b = 0, seq0 = 0, s0 = 0, n = 0, nt = 0;  // the current block: first tile, first row, rows, tiles
   auto sequence = [&](int xx, int& bb, int& ss, int& nn) {
@@ -667,7 +676,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   const int x_first = __builtin_amdgcn_readfirstlane(plan_x[0]);
   const bool joined = t_hi <= __builtin_amdgcn_readfirstlane(a.tile_off[x_first + 1]);
 
-  char* kt = tiles[wave];
+  char* kt = tiles + wave * TL::BYTES;
   const uint32_t kt_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)kt);
   uint32_t voff[TL::PERIOD];  // the copies' sources within ROWS rows
 #pragma unroll
@@ -676,7 +685,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     voff[k] = 16u * (uint32_t)(r * CHR + (pc ^ TL::swz(r)));
   }
   // rows 16 g .. 16 g + 15 of a tile whose 16 rows lie together
-  auto issue_half = [&](int g, uint64_t at) __attribute__((always_inline)) {
+  auto issue_half = [&](int g, uint64_t at, uint32_t kt_lds) __attribute__((always_inline)) {
     uint64_t base = row_address(at, 16 * g);
     asm volatile("s_nop 4" : "+s"(base));  // (vector ALU to scalar register to memory operation)
     uint32_t lds = kt_lds;  // opaque: its sums with constants are cheaper made again than kept
@@ -690,7 +699,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     }
   };
   // any tile: copy k fills chunks 64 k .. 64 k + 63, of rows known at compile time
-  auto issue_rows = [&](uint64_t at) __attribute__((always_inline)) {
+  auto issue_rows = [&](uint64_t at, char* kt) __attribute__((always_inline)) {
     int ln = lane;  // opaque: the lanes' chunk numbers are cheaper made again than kept in registers
     asm volatile("" : "+v"(ln));
 #pragma unroll
@@ -715,12 +724,11 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   auto position = [&](int ss, int nn, int t) { return min(ss + t * PD_KT + col, nn - 1); };
 
   bool bad = false;
-  uint64_t power = 0;
+  float power = 1.f;
+  if constexpr (E4M3) __syncthreads();  // (the plan has been read: copies may overwrite it)
   if (T < T_end) {
     const int p = position(s0, n, T - seq0);
-    const uint64_t at = address(p, entry(b, p), bad, power);
-    if constexpr (E4M3) copy4(power, kt_lds + TL::BYTES);
-    issue_rows(at);
+    issue_rows(address(p, entry(b, p), bad, power), kt);
   } else if (!joined) {
     return;
   }
@@ -733,7 +741,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     begin(x);  // (a wavefront without tiles, in a joined share, has an empty state)
     for (; T < seg_end; ++T) {
       any_bad |= bad;
-      const int t = T - seq0;
+      const int t = T - seq0, left = n - s0 - t * PD_KT;
       // the tile after this one: the next of the block, or the first of the next that has rows
       int page = 0, p2 = 0;
       const bool more = T + 1 < T_end;
@@ -746,22 +754,38 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         p2 = position(s2, n2, T + 1 - seq2);
         page = entry(b2, p2);
       }
+      const bool together = more && whole16 && (T + 1 - seq2) * PD_KT <= n2 - s2 - PD_KT;
       wait_vm<0>();
-      uint64_t at = 0;
-      bool together = false;
-      tile(kt, n - s0 - t * PD_KT, heads, T == seg_begin, [&]() __attribute__((always_inline)) {
-        // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
-        // reads return in order), the others behind the last read
+      if constexpr (E4M3) {
+        // the other buffer takes the next tile, asked for before this one is worked on
+        float power_next = 1.f;
+        asm volatile("" : "+v"(page), "+v"(power));  // (loaded: no wait for them behind the copies)
+        const int now = __builtin_amdgcn_readfirstlane((T - t_first) & 1), next = (now ^ 1) * PD_WAVES * TL::BYTES;
         if (more) {
-          at = address(p2, page, bad, power);
-          together = whole16 && (T + 1 - seq2) * PD_KT <= n2 - s2 - PD_KT;
-          if (together) issue_half(0, at);
+          const uint64_t at = address(p2, page, bad, power_next);
+          if (together) {
+            issue_half(0, at, kt_lds + next);
+            issue_half(1, at, kt_lds + next);
+          } else {
+            issue_rows(at, kt + next);
+          }
         }
-      });
-      if (more) {
-        if constexpr (E4M3) copy4(power, kt_lds + TL::BYTES);
-        if (together) issue_half(1, at);
-        else issue_rows(at);
+        tile(kt + now * PD_WAVES * TL::BYTES, power, left, heads, T == seg_begin, [] {});
+        power = power_next;
+      } else {
+        uint64_t at = 0;
+        tile(kt, 1.f, left, heads, T == seg_begin, [&]() __attribute__((always_inline)) {
+          // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
+          // reads return in order), the others behind the last read
+          if (more) {
+            at = address(p2, page, bad, power);
+            if (together) issue_half(0, at, kt_lds);
+          }
+        });
+        if (more) {
+          if (together) issue_half(1, at, kt_lds);
+          else issue_rows(at, kt);
+        }
       }
     }
 
@@ -779,13 +803,13 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     // the four states of one block: one reference and sum, then the latents, a part of them at a time
     // through LDS: every wavefront writes its part, then sums a quarter of it
     constexpr int PH = E4M3 ? 4 : 2, NH = NC / PH;
-    static_assert(PD_WAVES * NH * 4096 <= PD_WAVES * TL::ALLOC, "a part of every state fits the tiles");
+    static_assert(PD_WAVES * NH * 4096 <= PD_WAVES * TL::BYTES, "a part of every state fits the (first) tiles");
     const float l = sum(), ref = reference();
     if (half == 0) {
-      ml[wave][0][col] = ref;
-      ml[wave][1][col] = l;
+      ml(wave)[col] = ref;
+      ml(wave)[32 + col] = l;
     }
-    float* buf = (float*)tiles[0];
+    float* buf = (float*)tiles;
     float M = -INFINITY, L = 0.f, f[PD_WAVES];
     const int hj = 32 * (x_first % a.HB);
     const int64_t row = (slot0 + (int64_t)PD_WAVES * wg + x_first) * 32 + col;
@@ -795,12 +819,12 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       __syncthreads();  // (every wavefront is done with its tile, or with the part before)
       if (ph == 0) {
 #pragma unroll
-        for (int w = 0; w < PD_WAVES; ++w) M = fmaxf(M, ml[w][0][col]);
+        for (int w = 0; w < PD_WAVES; ++w) M = fmaxf(M, ml(w)[col]);
 #pragma unroll
         for (int w = 0; w < PD_WAVES; ++w) {
-          const float mw = ml[w][0][col];
+          const float mw = ml(w)[col];
           f[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
-          L += ml[w][1][col] * f[w];
+          L += ml(w)[32 + col] * f[w];
         }
       }
 #pragma unroll
@@ -865,7 +889,7 @@ struct LatentWhere {
 };
 
 struct SharedLayout {
-  size_t qabs, part_o, part_ml, plan, bytes;
+  size_t qabs, qexp, part_o, part_ml, plan, bytes;
   int max_quads, nwg;
 };
 SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_groups) {
@@ -876,10 +900,11 @@ SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_gro
   l.nwg = (int)(tiles < 2 ? 2 : tiles < PD_CUS ? tiles : PD_CUS);
   const size_t slots = 4 * ((size_t)l.nwg + l.max_quads) + VB;
   l.qabs = 0;
-  l.part_o = l.qabs + al(VB * 32 * DK * 4);
+  l.qexp = l.qabs + al(VB * 32 * DK * 2);
+  l.part_o = l.qexp + al(VB * 32 * (DVL / 32));
   l.part_ml = l.part_o + al(slots * 32 * DVL * 4);
   l.plan = l.part_ml + al(slots * 32 * 2 * 4);
-  l.bytes = l.plan + al((8 + 2 * (size_t)B + 2 * VB + 1 + 2 * (size_t)l.max_quads + 1 + 2 * (size_t)n_groups) * 4);
+  l.bytes = l.plan + al((8 + 2 * (size_t)B + 2 * VB + 1 + 2 * (size_t)l.max_quads + 1 + 5 * (size_t)n_groups) * 4);
   return l;
 }
 
@@ -903,7 +928,7 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.max_pages = d.c.max_pages;
   a.page_bytes = p.e4m3 ? E4m3Page(d.c.page_size, d.rkv, d.dr).bytes : (int64_t)d.c.page_size * DK * 2;
   a.len = d.len; a.max_len = d.max_len; a.B = d.B; a.H = d.H; a.HB = HB;
-  a.qabs = ws + l.qabs; a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
+  a.qabs = (const bf16_t*)(ws + l.qabs); a.qexp = (const int8_t*)(ws + l.qexp); a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
   a.sl2 = d.scale * attn::LOG2E; a.nwg = l.nwg;
   a.n_groups = p.n_groups; a.max_quads = l.max_quads; a.group_off = p.group_off; a.shared_len = p.shared_len;
   int32_t* at = (int32_t*)(ws + l.plan);
@@ -914,8 +939,7 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.block_quad = at; at += VB;
   a.quad_x = at; at += l.max_quads;
   a.quad_item = at; at += l.max_quads + 1;
-  a.group_min = at; at += p.n_groups;
-  a.group_cnt = at;
+  a.group = at;
   prof_begin(KC_ELEM, s);
   const int64_t grid = 1 + (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
   if (p.e4m3)
