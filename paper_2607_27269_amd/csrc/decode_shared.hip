@@ -42,35 +42,31 @@ struct LatentDev {
   float sl2;
   int nwg;
   // the lists, made by the plan (one workgroup of the launch before)
-  int n_groups, max_quads;
+  int n_groups, max_pieces;
   const int32_t* group_off;
   const int32_t* shared_len;
-  int32_t* head;          // [3]: tiles of shared rows, of own rows, quads
+  int32_t* head;          // [3]: pieces of the shared rows, workgroups for them, tiles of own rows
   int32_t* start;         // [B]: rows that the sequence shares, a multiple of PD_KT
   int32_t* tile_off;      // [B HB + 1]: first tile of each block's own rows
-  int32_t* quad_x;        // [max_quads]: 4 first block + (blocks - 1)
-  int32_t* quad_item;     // [max_quads + 1]: first item of each quad
-  int32_t* block_quad;    // [B HB]: 4 quad + place in it, or -1
-  int32_t* group_of;      // [B], -1: none
-  int32_t* group;         // [5 n_groups]: scratch of the plan
+  int32_t* member;        // [B]: the sequence's group if it has shared rows, else -1
+  int32_t* group;         // [n_groups][GROUP_INTS]
+  int32_t* scratch;       // [3 n_groups]
 };
 
 __device__ __forceinline__ int len_of(const LatentDev& a, int b) { return min(max(a.len[b], 0), a.max_len); }
 
-// How many workgroups the shared rows get.
-__device__ __forceinline__ int shared_workgroups(int nwg, int shared, int own) {
+// A group in the plan: its first piece, quads, pieces of each quad, tiles, first block, blocks, and the sequence (one
+// that has rows) whose page table the shared rows are read through.  Piece p of quad q is
+// number first + p quads + q: workgroups with neighbouring numbers read the same rows for different quads.
+constexpr int GROUP_INTS = 7;
+enum { G_FIRST, G_QUADS, G_PIECES, G_TILES, G_X0, G_BLOCKS, G_SEQ };
+
+// How many workgroups the shared rows get, where they have `shared` tiles of quads and the own rows `own` tiles.
+__device__ __forceinline__ int shared_workgroups(int nwg, int64_t shared, int64_t own) {
   if (shared == 0) return 0;
   if (own == 0) return nwg;
-  const int64_t n = ((int64_t)nwg * shared + (shared + (int64_t)own) / 2) / (shared + (int64_t)own);
-  return (int)min(max(n, (int64_t)1), (int64_t)nwg - 1);
+  return (int)min(max((nwg * shared + (shared + own) / 2) / (shared + own), (int64_t)1), (int64_t)nwg - 1);
 }
-// The items of the shared rows in equal runs.
-struct ItemCut {
-  int total, share;
-  __device__ __forceinline__ ItemCut(int items, int nwg) : total(items), share(max(1, nwg > 0 ? (items + nwg - 1) / nwg : 1)) {}
-  __device__ __forceinline__ int lo(int w) const { return (int)min((int64_t)w * share, (int64_t)total); }
-  __device__ __forceinline__ int hi(int w) const { return min(lo(w) + share, total); }
-};
 
 // ---- the plan -------------------------------------------------------------------------
 // Sum over the threads before this one, and over all (NT threads).
@@ -105,102 +101,107 @@ __device__ __forceinline__ int agent_load(const int32_t* p) {
 template <int NT>
 __device__ void make_plan(const LatentDev& a) {
   const int tid = threadIdx.x, G = a.n_groups;
-  // per group: the shared rows that all its sequences have, how many have rows; then its first quad, item, and tiles
+  // per group: the shared rows that all its sequences have, how many have rows, and the first that has
   constexpr int IN_LDS = 512;
-  __shared__ int32_t group_lds[5 * IN_LDS];
-  int32_t *group_min = G <= IN_LDS ? group_lds : a.group, *group_cnt = group_min + G, *group = group_cnt + G;
+  __shared__ int32_t group_lds[3 * IN_LDS];
+  int32_t *group_min = G <= IN_LDS ? group_lds : a.scratch, *group_cnt = group_min + G, *group_seq = group_cnt + G;
   for (int g = tid; g < G; g += NT) {
     __hip_atomic_store(group_min + g, min(max(a.shared_len[g], 0), a.max_len), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(group_cnt + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(group_seq + g, a.B, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __threadfence();
   __syncthreads();
-  // what all sequences of a group that have rows have
   for (int b = tid; b < a.B; b += NT) {
     int g = -1;
-    if (G > 0) {
+    const int n = len_of(a, b);
+    if (G > 0 && n > 0) {
       g = sequence_of(a.group_off, G, b);
       if (b < a.group_off[g] || b >= a.group_off[g + 1]) g = -1;
     }
-    a.group_of[b] = g;
-    const int n = len_of(a, b);
-    if (g >= 0 && n > 0) {
+    a.member[b] = g;
+    if (g >= 0) {
       atomicMin(group_min + g, n);
       atomicAdd(group_cnt + g, 1);
+      atomicMin(group_seq + g, b);
     }
   }
   __threadfence();
   __syncthreads();
-  // (one block alone gains nothing)
-  auto rows_of = [&](int g) { return agent_load(group_cnt + g) * (int64_t)a.HB >= 2 ? agent_load(group_min + g) / PD_KT * PD_KT : 0; };
-  // quads and their items
   const int run = (G + NT - 1) / NT, g_lo = min(tid * run, G), g_hi = min(g_lo + run, G);
-  auto blocks = [&](int g, int& x0) {
-    const int lo = min(max(a.group_off[g], 0), a.B), hi = min(max(a.group_off[g + 1], 0), a.B);
-    x0 = lo * a.HB;
-    return max(hi - lo, 0) * a.HB;
-  };
-  int quads = 0, items = 0, x0, total_q, total_i;
+  int quads = 0, items = 0, total_q, total_i, longest = 0;
   for (int g = g_lo; g < g_hi; ++g) {
-    const int q = (blocks(g, x0) + 3) / 4, t = rows_of(g) / PD_KT;
+    const int lo = min(max(a.group_off[g], 0), a.B), n = max(min(max(a.group_off[g + 1], 0), a.B) - lo, 0) * a.HB;
+    // (one block alone gains nothing)
+    const int t = agent_load(group_cnt + g) * (int64_t)a.HB >= 2 ? agent_load(group_min + g) / PD_KT : 0;
+    int32_t* d = a.group + GROUP_INTS * g;
+    d[G_QUADS] = (n + 3) / 4;
+    __hip_atomic_store(d + G_TILES, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    d[G_X0] = lo * a.HB;
+    d[G_BLOCKS] = n;
+    d[G_SEQ] = agent_load(group_seq + g);
     if (t > 0) {
-      quads += q;
-      items += q * t;
+      quads += (n + 3) / 4;
+      items += (n + 3) / 4 * t;
+      longest = max(longest, t);
     }
   }
-  int k = scan_before<NT>(quads, total_q), at = scan_before<NT>(items, total_i);
-  for (int g = g_lo; g < g_hi; ++g) {
-    const int n = blocks(g, x0), t = rows_of(g) / PD_KT, q = (n + 3) / 4;
-    group[3 * g] = k;
-    group[3 * g + 1] = at;
-    group[3 * g + 2] = t;
-    if (t > 0) {
-      k += q;
-      at += q * t;
-    }
-  }
-  if (tid == 0) {
-    a.head[2] = min(total_q, a.max_quads);
-    a.quad_item[min(total_q, a.max_quads)] = total_i;  // (again below, where the quads do not fit)
-  }
+  scan_before<NT>(quads, total_q);
+  scan_before<NT>(items, total_i);
   __threadfence();
   __syncthreads();
   // own rows
   const int runb = (a.B + NT - 1) / NT, b_lo = min(tid * runb, a.B), b_hi = min(b_lo + runb, a.B);
   int mine = 0, total;
   for (int b = b_lo; b < b_hi; ++b) {
-    const int g = a.group_of[b], n = len_of(a, b);
-    int s = 0, k0 = 0, at0 = 0, first = 0, blocks_of = 0;
-    if (g >= 0) {
-      k0 = agent_load(group + 3 * g);
-      at0 = agent_load(group + 3 * g + 1);
-      s = min(agent_load(group + 3 * g + 2) * PD_KT, n);
-      blocks_of = blocks(g, first);
-    }
-    a.start[b] = s;
-    mine += tiles_of(n - s) * a.HB;
-    for (int h = 0; h < a.HB; ++h) {
-      const int x = b * a.HB + h, j = x - first, q = k0 + j / 4, t = g >= 0 ? agent_load(group + 3 * g + 2) : 0;
-      const bool in = t > 0 && j >= 0 && q < a.max_quads;
-      a.block_quad[x] = in && n > 0 ? 4 * q + j % 4 : -1;  // (sequences without rows take no part)
-      if (in && j % 4 == 0) {
-        a.quad_x[q] = 4 * x + min(blocks_of - j, 4) - 1;
-        a.quad_item[q] = at0 + j / 4 * t;
-        if (q == a.max_quads - 1) a.quad_item[q + 1] = at0 + (j / 4 + 1) * t;
-      }
-    }
+    const int g = a.member[b], n = len_of(a, b), t = g >= 0 ? agent_load(a.group + GROUP_INTS * g + G_TILES) : 0;
+    a.start[b] = min(t * PD_KT, n);
+    if (t == 0) a.member[b] = -1;
+    mine += tiles_of(n - min(t * PD_KT, n)) * a.HB;
   }
-  at = scan_before<NT>(mine, total);
+  int at = scan_before<NT>(mine, total);
   for (int b = b_lo; b < b_hi; ++b) {
     const int n = tiles_of(len_of(a, b) - a.start[b]);
     for (int h = 0; h < a.HB; ++h, at += n) a.tile_off[b * a.HB + h] = at;
   }
-  __syncthreads();  // (quad_item is written)
+  // The shared rows' workgroups take a piece each: the least number of tiles a piece for which there are enough of
+  // them (with more quads than workgroups a quad is a piece).
+  const int n_s = shared_workgroups(a.nwg, total_i, total);
+  auto pieces_at = [&](int t) {
+    int n = 0, sum;
+    for (int g = g_lo; g < g_hi; ++g) {
+      const int32_t* d = a.group + GROUP_INTS * g;
+      n += d[G_QUADS] * ((d[G_TILES] + t - 1) / t);
+    }
+    scan_before<NT>(n, sum);
+    return sum;
+  };
+  int lo = 1, hi = total_i;  // (as many tiles as there are: a quad is a piece)
+  if (total_q < n_s) {
+    lo = (total_i + n_s - 1) / n_s;
+    hi = (total_i + n_s - total_q - 1) / (n_s - total_q);  // (enough: a quad's last piece is all that is rounded up)
+    while (lo < hi) {
+      const int mid = lo + (hi - lo) / 2;
+      if (pieces_at(mid) <= n_s) hi = mid;
+      else lo = mid + 1;
+    }
+  }
+  hi = max(hi, 1);
+  int count = 0, pieces;
+  for (int g = g_lo; g < g_hi; ++g) count += a.group[GROUP_INTS * g + G_QUADS] * ((a.group[GROUP_INTS * g + G_TILES] + hi - 1) / hi);
+  int first = scan_before<NT>(count, pieces);
+  for (int g = g_lo; g < g_hi; ++g) {
+    int32_t* d = a.group + GROUP_INTS * g;
+    d[G_FIRST] = first;
+    d[G_PIECES] = (d[G_TILES] + hi - 1) / hi;
+    first += d[G_QUADS] * d[G_PIECES];
+    if (first > a.max_pieces) d[G_PIECES] = 0;  // (of decreasing offsets: no slots)
+  }
   if (tid == 0) {
     a.tile_off[a.B * a.HB] = total;
-    const int q = min(total_q, a.max_quads);
-    a.head[0] = q == 0 ? 0 : agent_load(a.quad_item + q);
-    a.head[1] = total;
+    a.head[0] = min(pieces, a.max_pieces);
+    a.head[1] = n_s;
+    a.head[2] = total;
   }
 }
 
@@ -268,9 +269,10 @@ struct LatentTile {
 // multiplied by 2^e (before the positional part is added), and a row's weight in the weighted latents is
 // p 2^e = 2^(x + e - m) with x the logit in log2 units and m the running maximum of x + e over the rows.  So weights
 // are at most 2^(SLACK + BIAS) < 2^16 and fp16 holds them with 11 bits down to 2^-22 of the largest (their
-// rounding is an eighth of bf16's, and one operand does where bf16 takes two).  The sum of the p has
-// a reference of its own, the running maximum of x: beside rows of much larger powers 2^(x - m) may be 0
-// where p is not small.  Absorbed queries are fp16 too, each head's brought to [2^8, 2^9) by a power of two.
+// rounding is an eighth of bf16's, and one operand does where bf16 takes two).  The sum of the p = 2^(x - m) is in
+// fp32, whose range holds them down to 2^-14 of the largest even beside the largest power, 2^120.
+// Absorbed queries are fp16 too, each head's brought to [2^8, 2^9) by a power of two; the rotary part is bf16
+// and divided by the same power, so that the logit is multiplied by it last.
 constexpr float E8_SLACK = 7.f, E8_BIAS = 8.f;
 
 template <int DK, int DVL, bool E4M3, int OCC>
@@ -284,17 +286,18 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   // In eight bits a wavefront has two tiles, all of the LDS at 576 values; what is small lies in a second tile: of
   // wavefront 0 (the plan, before the copies) and of the wavefront itself (reference and sum, after its tiles).
   constexpr int NBUF = E4M3 ? 2 : 1, SMALL = NBUF * PD_WAVES * TL::BYTES - (E4M3 ? PD_WAVES * TL::BYTES : 0);
-  __shared__ __attribute__((aligned(1024))) char tiles[NBUF * PD_WAVES * TL::BYTES + (E4M3 ? 0 : 1088)];
+  constexpr int TABLE = 64 + TL::PERIOD * 256;  // (the plan's, then the shared rows' copies)
+  __shared__ __attribute__((aligned(1024))) char tiles[NBUF * PD_WAVES * TL::BYTES + (E4M3 ? 0 : 1024 + TABLE)];
   int* plan_x = (int*)(tiles + SMALL + (E4M3 ? 0 : 1024));  // [PD_WAVES], then plan_at
   int* plan_at = plan_x + PD_WAVES;
   auto ml = [&](int w) { return (float*)(tiles + SMALL + w * (E4M3 ? TL::BYTES : 256)); };  // [2][32]
 
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int half = lane >> 5, col = lane & 31;
-  const int total_s = a.head[0], total_p = a.head[1], VB = a.B * a.HB;
-  const int n_s = __builtin_amdgcn_readfirstlane(shared_workgroups(a.nwg, total_s, total_p));
+  const int total_p = a.head[2], VB = a.B * a.HB;
+  const int n_s = __builtin_amdgcn_readfirstlane(a.head[1]);
   const bool on_shared = (int)blockIdx.x < n_s;
-  const int wg = on_shared ? (int)blockIdx.x : (int)blockIdx.x - n_s;
+  const int wg = on_shared ? xcd_remap(blockIdx.x, n_s) : (int)blockIdx.x - n_s;
 
   // ---- what both lists use ----
   // lane offsets in a tile: S^T's operand (chunk 2 i + half of row col, i % 4 = 0..3), V^T's
@@ -340,9 +343,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   // ---- a wavefront's state: 32 queries ----
   QT qf[NL];             // this lane's head as B operand fragments
   bf16x8 qr[NR];
-  float qpow = 1.f;      // (eight bits) what the fragments were divided by
+  float sl2 = a.sl2;     // logits to log2 units (eight bits: times what the fragments were divided by)
   f32x16 acc[NC];
-  float m_run, mx_run, l_run;
+  float m_run, l_run;
   bool any_bad;
   auto begin = [&](int x) __attribute__((always_inline)) {
     const bf16_t* src = a.qabs + (int64_t)x * 32 * DK + 8 * lane;
@@ -362,10 +365,20 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
           top = max(top, t[i + k]);
         }
       }
-      qpow = power_of_two(min(top, ABS_MAX_EXP));
+      top = min(max(top, -64), 100);  // (the positional part is divided by it)
+      sl2 = a.sl2 * power_of_two(top);
+      const float down = power_of_two(-top);
+#pragma unroll
+      for (int s = 0; s < NR; ++s) {
+        const u32x4 v = __builtin_bit_cast(u32x4, qr[s]);
+        u32x4 w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = pack2bf(__uint_as_float(v[k] << 16) * down, __uint_as_float(v[k] & 0xffff0000u) * down);
+        qr[s] = __builtin_bit_cast(bf16x8, w);
+      }
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const _Float16 f = (_Float16)power_of_two(max(t[i] - top, -30));
+        const _Float16 f = (_Float16)power_of_two(min(max(t[i] - top, -30), 15));
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           qf[2 * i][k] *= f;
@@ -377,24 +390,24 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
-    m_run = mx_run = -INFINITY;
+    m_run = -INFINITY;
     l_run = 0.f;
     any_bad = false;
   };
-  // One tile at kt, of which `left` rows count; power: of row col (eight bits).  `heads`: the columns with a head.  `early` is called
-  // when the reads of the first 16 rows (and of all keys) have returned.
-  auto tile = [&](const char* kt, float power, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
-    f32x16 s;
-    float pw[16];  // powers of the rows of s: 8 (e / 4) + 4 half + e % 4
+  // of the rows of s (8 (e / 4) + 4 half + e % 4), what lane col has for row col
+  auto of_rows = [&](float v, float (&out)[16]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      out[e] = __int_as_float(__builtin_amdgcn_ds_bpermute(16 * half + 32 * (e >> 2) + 4 * (e & 3), __float_as_int(v)));
+  };
+  // S^T of the tile at kt (eight bits: power, of row col, is in it; pw: the powers of the rows of s)
+  auto logits = [&](const char* kt, float power, f32x16& s, float (&pw)[16]) __attribute__((always_inline)) {
+    auto kread = [&](int i) { return *(const u32x4*)(kt + kb[i % 4] + 128 * (i / 4)); };
+    u32x4 raw[PF];  // (pinned: the compiler would read each operand right before its product and wait for it)
+#pragma unroll
+    for (int j = 0; j < PF; ++j) raw[j] = kread(j);
+    __builtin_amdgcn_sched_barrier(0);
     if constexpr (E4M3) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        pw[e] = __int_as_float(__builtin_amdgcn_ds_bpermute(16 * half + 32 * (e >> 2) + 4 * (e & 3), __float_as_int(power)));
-      u32x4 raw[PF];
-      auto kread = [&](int i) { return *(const u32x4*)(kt + kb[i % 4] + 128 * (i / 4)); };
-#pragma unroll
-      for (int j = 0; j < PF; ++j) raw[j] = kread(j);
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < NL / 2; ++i) {
         const u32x4 v = raw[i % PF];
@@ -404,132 +417,128 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         const f16x8 k1 = e4m3_to_f16(v[2], v[3]);
         mfma_v_next(s, k1, qf[2 * i + 1]);
         if (i + PF < NL / 2 + NR) raw[i % PF] = kread(i + PF);
+        if (i == NL / 2 - 2) of_rows(power, pw);
         __builtin_amdgcn_sched_barrier(0);
       }
       mfma_v_done(s);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] *= pw[e] * qpow;
+      for (int e = 0; e < 16; ++e) s[e] *= pw[e];
 #pragma unroll
       for (int j = 0; j < NR; ++j) {
         mfma_v_next(s, __builtin_bit_cast(bf16x8, raw[(NL / 2 + j) % PF]), qr[j]);
         if (j + PF < NR) raw[(NL / 2 + j) % PF] = kread(NL / 2 + j + PF);
       }
-      mfma_v_done(s);
     } else {
-      bf16x8 kf[PF];
-      auto kread = [&](int i) { return *(const bf16x8*)(kt + kb[i % 4] + 128 * (i / 4)); };
-#pragma unroll
-      for (int j = 0; j < PF; ++j) kf[j] = kread(j);
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int kk = 0; kk < NL + NR; ++kk) {
-        if (kk == 0) mfma_v_first(s, kf[0], qf[0]);
-        else mfma_v_next(s, kf[kk % PF], kk < NL ? qf[kk % NL] : qr[kk - NL < 0 ? 0 : kk - NL]);
-        if (kk + PF < NL + NR) kf[kk % PF] = kread(kk + PF);
+        const bf16x8 k = __builtin_bit_cast(bf16x8, raw[kk % PF]);
+        if (kk == 0) mfma_v_first(s, k, qf[0]);
+        else mfma_v_next(s, k, kk < NL ? qf[kk % NL] : qr[kk - NL < 0 ? 0 : kk - NL]);
+        if (kk + PF < NL + NR) raw[kk % PF] = kread(kk + PF);
         __builtin_amdgcn_sched_barrier(0);
       }
-      mfma_v_done(s);
     }
-    // V^T operand of step j = NC u + c: latents 32 c .., rows 16 u + {4 half.., 8 + 4 half..}
-    auto vread = [&](int j) {
-      const int c = j % NC, u = j / NC;
-      if constexpr (E4M3) {
-        return lds_read_tr8(kt + vb[c % 4] + 128 * (c / 4) + 16 * RB * u);
-      } else {
-        const char* p = kt + 16 * RB * u + 128 * (c / 2);
-        const u32x2 lo = lds_read_tr4((const bf16_t*)(p + vb[c & 1])), hi = lds_read_tr4((const bf16_t*)(p + vb[2 + (c & 1)]));
-        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-      }
-    };
-    typename std::conditional<E4M3, u32x2, bf16x8>::type vf[PV];
+    mfma_v_done(s);
+  };
+  // V^T operand of step j = NC u + c: latents 32 c .., rows 16 u + {4 half.., 8 + 4 half..}
+  auto vread = [&](const char* kt, int j) {
+    const int c = j % NC, u = j / NC;
+    if constexpr (E4M3) {
+      return lds_read_tr8(kt + vb[c % 4] + 128 * (c / 4) + 16 * RB * u);
+    } else {
+      const char* p = kt + 16 * RB * u + 128 * (c / 2);
+      const u32x2 lo = lds_read_tr4((const bf16_t*)(p + vb[c & 1])), hi = lds_read_tr4((const bf16_t*)(p + vb[2 + (c & 1)]));
+      return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    }
+  };
+  using VT = typename std::conditional<E4M3, u32x2, bf16x8>::type;
+  // A tile's weights as matrix operands: fp16, or two bf16 values each (rounded, and what that lost: a rounding of
+  // P alone would add as much error as that of the output)
+  struct Weights {
+    u32x4 hi[2], lo[2];
+  };
+  auto product = [&](int j, VT v, const Weights& w) __attribute__((always_inline)) {
+    if constexpr (E4M3) {
+      mfma_a(acc[j % NC], e4m3_to_f16(v[0], v[1]), __builtin_bit_cast(f16x8, w.hi[j / NC]));
+    } else {
+      mfma_a(acc[j % NC], v, __builtin_bit_cast(bf16x8, w.hi[j / NC]));
+      mfma_a(acc[j % NC], v, __builtin_bit_cast(bf16x8, w.lo[j / NC]));
+    }
+  };
+  // The softmax of a tile in steps that can be spread over the products of another: the references first (they move only
+  // when the tile's maximum exceeds one by more than the slack; returns whether the weighted latents are
+  // to be multiplied by corr), then 16 exponentials, then 8 pairs of operands.
+  auto softmax_refs = [&](const f32x16& s, float power, uint64_t heads, float& corr) __attribute__((always_inline)) {
+    float lg[16], my = -INFINITY;
+    if constexpr (E4M3) of_rows(fmaxf((float)((int)(__float_as_uint(power) >> 23) - 127), (float)E4M3_MIN_EXP), lg);
 #pragma unroll
-    for (int j = 0; j < PV; ++j) vf[j] = vread(j);
+    for (int e = 0; e < 16; ++e) my = fmaxf(my, E4M3 ? __builtin_fmaf(s[e], sl2, lg[e]) : s[e]);
+    my = pair_max32(my);
+    if constexpr (!E4M3) my *= sl2;
+    const bool move = (__ballot(my > m_run + (E4M3 ? E8_SLACK : PD_SLACK)) & heads) != 0;
+    // (no branch: products may be under way)
+    const float m_new = move ? fmaxf(m_run, my) : m_run;
+    corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+    m_run = m_new;
+    l_run *= corr;
+    return move;
+  };
+  auto softmax_exp = [&](f32x16& s, const float (&pw)[16], int e) __attribute__((always_inline)) {
+    const float ref = (m_run == -INFINITY ? 0.f : m_run) - (E4M3 ? E8_BIAS : 0.f);
+    s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -ref));
+    l_run += s[e];
+    if constexpr (E4M3) s[e] *= pw[e];
+  };
+  auto softmax_pack = [&](f32x16& s, int q) __attribute__((always_inline)) {  // (in place: weights() takes them)
+    const float p0 = s[2 * q], p1 = s[2 * q + 1];
+    if constexpr (E4M3) {
+      s[2 * q] = __uint_as_float(pack2h(p0, p1));
+    } else {
+      const uint32_t h = pack2bf(p0, p1);
+      s[2 * q] = __uint_as_float(h);
+      s[2 * q + 1] = __uint_as_float(pack2bf(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u)));
+    }
+  };
+  auto weights = [&](const f32x16& s) __attribute__((always_inline)) {
+    Weights w;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      w.hi[q / 4][q % 4] = __float_as_uint(s[2 * q]);
+      w.lo[q / 4][q % 4] = __float_as_uint(s[2 * q + 1]);
+    }
+    return w;
+  };
+  auto rescale = [&](float corr) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
+  };
+  // One tile at kt, of which `left` rows count; power: of row col (eight bits).  `heads`: the columns with a head.
+  // `early` is called when the reads of the first 16 rows (and of all keys) have returned.
+  auto tile = [&](const char* kt, float power, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
+    f32x16 s;
+    float pw[16];
+    logits(kt, power, s, pw);
+    VT vf[PV];
+#pragma unroll
+    for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
     if (left < PD_KT) {  // rows past the end: no weight (a real branch)
       asm volatile("");
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (8 * (e >> 2) + 4 * half + (e & 3) >= left) s[e] = -INFINITY;
     }
-    QT pf[2];
-    bf16x8 pl[2];
-    if constexpr (E4M3) {
-      float x[16];
-      float mx = -INFINITY, my = -INFINITY;
+    float corr;
+    if (softmax_refs(s, power, heads, corr) && !first) rescale(corr);  // (nothing is there yet at the first tile)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[e] = s[e] * a.sl2;
-        s[e] = x[e] + (float)((int)(__float_as_uint(pw[e]) >> 23) - 127);
-        mx = fmaxf(mx, x[e]);
-        my = fmaxf(my, s[e]);
-      }
-      mx = pair_max32(mx);
-      my = pair_max32(my);
-      // a reference moves only when a tile's maximum exceeds it by more than the slack
-      if ((__ballot(my > m_run + E8_SLACK || mx > mx_run + E8_SLACK) & heads) != 0) {
-        const float m_new = fmaxf(m_run, my), x_new = fmaxf(mx_run, mx);
-        const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
-        l_run *= __builtin_amdgcn_exp2f(mx_run - (x_new == -INFINITY ? 0.f : x_new));
-        m_run = m_new;
-        mx_run = x_new;
-        if (!first) {  // (nothing is there yet at the first tile)
+    for (int e = 0; e < 16; ++e) softmax_exp(s, pw, e);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
-        }
-      }
-      const float m_use = (m_run == -INFINITY ? 0.f : m_run) - E8_BIAS, x_use = mx_run == -INFINITY ? 0.f : mx_run;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        u32x4 w;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          w[q] = pack2h(__builtin_amdgcn_exp2f(s[8 * u + 2 * q] - m_use), __builtin_amdgcn_exp2f(s[8 * u + 2 * q + 1] - m_use));
-        pf[u] = __builtin_bit_cast(f16x8, w);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) l_run += __builtin_amdgcn_exp2f(x[e] - x_use);
-    } else {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
-      mx = pair_max32(mx) * a.sl2;
-      if ((__ballot(mx > m_run + PD_SLACK) & heads) != 0) {
-        const float m_new = fmaxf(m_run, mx);
-        const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
-        m_run = m_new;
-        l_run *= corr;
-        if (!first) {
-#pragma unroll
-          for (int c = 0; c < NC; ++c) acc_scale(acc[c], corr);
-        }
-      }
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
-      // P as two bf16 operands, rounded and what that lost
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        u32x4 w, w2;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q], a.sl2, -m_use));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q + 1], a.sl2, -m_use));
-          l_run += p0 + p1;
-          w[q] = pack2bf(p0, p1);
-          w2[q] = pack2bf(p0 - __uint_as_float(w[q] << 16), p1 - __uint_as_float(w[q] & 0xffff0000u));
-        }
-        pf[u] = __builtin_bit_cast(bf16x8, w);
-        pl[u] = __builtin_bit_cast(bf16x8, w2);
-      }
-    }
+    for (int q = 0; q < 8; ++q) softmax_pack(s, q);
+    const Weights w = weights(s);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < 2 * NC; ++j) {
-      if constexpr (E4M3) {
-        const f16x8 v = e4m3_to_f16(vf[j % PV][0], vf[j % PV][1]);
-        mfma_a(acc[j % NC], v, pf[j / NC]);
-      } else {
-        mfma_a(acc[j % NC], vf[j % PV], pf[j / NC]);
-        mfma_a(acc[j % NC], vf[j % PV], pl[j / NC]);
-      }
-      if (j + PV < 2 * NC) vf[j % PV] = vread(j + PV);
+      product(j, vf[j % PV], w);
+      if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
       __builtin_amdgcn_sched_barrier(0);
       if (j == NC) {
         mfma_a_done(acc);  // (no branch, where the compiler may move registers, before the products' waits)
@@ -543,9 +552,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   // the reference and sum of the state, as a merge of states takes them
   auto reference = [&] { return E4M3 ? m_run - E8_BIAS : m_run; };
   auto sum = [&] {
-    float l = l_run;
-    if constexpr (E4M3) l *= __builtin_amdgcn_exp2f(fminf(mx_run - reference(), 100.f));
-    return any_bad ? NAN : pair_sum32(l);  // (a row on no page)
+    return any_bad ? NAN : pair_sum32(l_run);  // (a row on no page)
   };
   auto store = [&](int64_t slot, bool has_head) __attribute__((always_inline)) {
     const float l = sum(), m = reference();
@@ -564,78 +571,141 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   };
 
   if (on_shared) {
-    // ---- shared rows: items of four query blocks ----
-    const ItemCut cut(total_s, n_s);
-    const int i_lo = cut.lo(wg), i_hi = cut.hi(wg);
-    if (i_lo >= i_hi) return;
-    const int quads = a.head[2];
-    for (int k = tid; k < quads; k += 64 * PD_WAVES)
-      if (a.quad_item[k] <= i_lo && i_lo < a.quad_item[k + 1]) plan_x[0] = k;
-    __syncthreads();
-    int k = __builtin_amdgcn_readfirstlane(plan_x[0]);
-    // this wavefront's copies of a tile: k = wave, wave + 4, .. (the last again where that is past the end)
-    constexpr int ALL = 2 * TL::HALF_COPIES, NJ = (ALL + PD_WAVES - 1) / PD_WAVES;
-    int rc[NJ];  // row and source chunk of the lane's 16 bytes
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int idx = 64 * min(4 * j + wave, ALL - 1) + lane, r = idx / CHR;
-      rc[j] = r << 8 | ((idx % CHR) ^ TL::swz(r));
+    // ---- shared rows: pieces of four query blocks ----
+    // This wavefront's part of a tile's copies: 8 rows (WIDE) or half of 16, its lanes' source offsets in a table in LDS.
+    int* table = plan_x + 16;
+    for (int u = tid; u < 64 * TL::PERIOD; u += 64 * PD_WAVES) {
+      const int r = u / CHR, pc = u % CHR;
+      table[u] = 16 * (r * CHR + (pc ^ TL::swz(r)));
     }
-    const uint32_t tiles_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tiles);
+    constexpr int NJ = TL::WIDE ? TL::PERIOD : (TL::PERIOD + 1) / 2;
+    const int row0 = TL::WIDE ? 8 * wave : 16 * (wave >> 1);
+    auto copy_of = [&](int j) { return TL::WIDE ? j : min(2 * j + (wave & 1), TL::PERIOD - 1); };
+    const uint32_t tiles_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tiles) + row0 * RB;
     auto issue = [&](int buf, uint64_t at, bool together) __attribute__((always_inline)) {
-      const uint32_t lds = tiles_lds + buf * TL::BYTES;
-      const uint64_t lo = row_address(at, 0), hi = row_address(at, 16);
-      auto copy = [&](int j, uint64_t row) __attribute__((always_inline)) {
-        const uint64_t src = row + 16 * (rc[j] & 255);
-        const uint32_t dst = lds + 1024 * min(4 * j + wave, ALL - 1);
-        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "{m0}"(dst) : "memory");
-      };
+      const uint32_t lds = __builtin_amdgcn_readfirstlane(tiles_lds + buf * TL::BYTES);
+      const int flip = TL::WIDE && (wave & 1) ? TL::XOR8 : 0;
       if (together) {
+        uint64_t base = row_address(at, row0);
+        asm volatile("s_nop 4" : "+s"(base));  // (vector ALU to scalar register to memory operation)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) copy(j, ((rc[j] >> 8) < 16 ? lo : hi) + (uint32_t)((rc[j] >> 8 & 15) * RB));
+        for (int j = 0; j < NJ; ++j) copy_s(base, (uint32_t)(table[64 * copy_of(j) + lane] ^ flip), lds + 1024 * copy_of(j));
       } else {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          const int r = rc[j] >> 8;
-          copy(j, (uint64_t)(uint32_t)__shfl((int)(uint32_t)at, r, 64) | (uint64_t)(uint32_t)__shfl((int)(uint32_t)(at >> 32), r, 64) << 32);
+          const uint32_t off = (uint32_t)(table[64 * copy_of(j) + lane] ^ flip), r = off / RB;
+          const int from = row0 + (int)r;
+          const uint64_t src = (uint64_t)(uint32_t)__shfl((int)(uint32_t)at, from, 64) | (uint64_t)(uint32_t)__shfl((int)(uint32_t)(at >> 32), from, 64) << 32;
+          dma16((const bf16_t*)(uintptr_t)(src + (off - r * RB)), (bf16_t*)(tiles + buf * TL::BYTES + row0 * RB + 1024 * copy_of(j)));
         }
       }
     };
-    for (int i = i_lo; i < i_hi; ++k) {
-      const int q_lo = __builtin_amdgcn_readfirstlane(a.quad_item[k]), q_hi = min(__builtin_amdgcn_readfirstlane(a.quad_item[k + 1]), i_hi);
-      const int qx = __builtin_amdgcn_readfirstlane(a.quad_x[k]), x0 = qx >> 2, nx = (qx & 3) + 1;
+    const int pieces = __builtin_amdgcn_readfirstlane(a.head[0]);
+    for (int piece = wg; piece < pieces; piece += n_s) {
+      if (tid == 0) plan_x[0] = -1;
+      __syncthreads();
+      for (int g = tid; g < a.n_groups; g += 64 * PD_WAVES) {
+        const int32_t* d = a.group + GROUP_INTS * g;
+        if (d[G_FIRST] <= piece && piece < d[G_FIRST] + d[G_QUADS] * d[G_PIECES]) plan_x[0] = g;
+      }
+      __syncthreads();
+      const int g = __builtin_amdgcn_readfirstlane(plan_x[0]);
+      if (g < 0) continue;
+      const int32_t* d = a.group + GROUP_INTS * g;
+      const int quads = __builtin_amdgcn_readfirstlane(d[G_QUADS]), of = __builtin_amdgcn_readfirstlane(d[G_PIECES]);
+      const int nt = __builtin_amdgcn_readfirstlane(d[G_TILES]), k = piece - __builtin_amdgcn_readfirstlane(d[G_FIRST]);
+      const int q = k % quads, pp = k / quads;
+      const int x0 = __builtin_amdgcn_readfirstlane(d[G_X0]) + 4 * q, nx = min(__builtin_amdgcn_readfirstlane(d[G_BLOCKS]) - 4 * q, 4);
+      const int q_hi = (int)((int64_t)nt * (pp + 1) / of);
+      int i = (int)((int64_t)nt * pp / of);
       // (a wavefront without a block works on the last one's, and stores nothing)
-      const int b0 = x0 / a.HB, x = x0 + min(wave, nx - 1);
+      const int b0 = __builtin_amdgcn_readfirstlane(d[G_SEQ]), x = x0 + min(wave, nx - 1);
       const int h0 = 32 * (x % a.HB);
       const uint64_t heads = __ballot(h0 + col < a.H);
-      // tile i is copied while the one before is worked on; its table entries were asked for before that
-      int p = (i - q_lo) * PD_KT + col, page = entry(b0, p);
-      bool bad = false, bad_next = false;
-      float power = 1.f, power_next = 1.f;
-      uint64_t at = address(p, page, bad, power);
+      // Item i: P V of its tile while the softmax of the next tile runs between the products; the tile after that
+      // is copied meanwhile (three buffers).
+      int p = i * PD_KT + col, page = entry(b0, p);
+      bool bad = false;
+      float power = 1.f;
       __syncthreads();  // (the buffers are free)
-      issue(i & 1, at, whole16);
+      issue(i % 3, address(p, page, bad, power), whole16);
       begin(x);
       if (i + 1 < q_hi) page = entry(b0, p + PD_KT);
-      bool first = true;
-      for (; i < q_hi; ++i) {
+      // asks for tile j, whose table entries are there, and for the entries of the one after it
+      auto next = [&](int j) __attribute__((always_inline)) {
+        asm volatile("" : "+v"(page), "+v"(power));  // (loaded: no wait for them behind the copies)
+        float power_of = power;
+        if (j < q_hi) {
+          p += PD_KT;
+          bool out;
+          issue(j % 3, address(p, page, out, power), whole16);
+          bad |= out;
+          if (j + 1 < q_hi) page = entry(b0, p + PD_KT);
+        }
+        return power_of;
+      };
+      f32x16 s;
+      float pw[16], corr;
+      wait_vm<0>();
+      __syncthreads();
+      float pow_now = next(i + 1);
+      logits(tiles + (i % 3) * TL::BYTES, pow_now, s, pw);
+      softmax_refs(s, pow_now, heads, corr);
+      bool move = false;  // (nothing is there yet at the first tile)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) softmax_exp(s, pw, e);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) softmax_pack(s, q);
+      Weights w = weights(s);
+      for (; i + 1 < q_hi; ++i) {
         pin(acc);
         wait_vm<0>();
-        asm volatile("" : "+v"(page), "+v"(power));  // (what was loaded is there: no wait for it below, behind the next copies)
         __syncthreads();
-        any_bad |= bad;
-        if (i + 1 < q_hi) {
-          p += PD_KT;
-          at = address(p, page, bad_next, power_next);
-          issue((i + 1) & 1, at, whole16);
-          if (i + 2 < q_hi) page = entry(b0, p + PD_KT);
+        pow_now = next(i + 2);
+        logits(tiles + ((i + 1) % 3) * TL::BYTES, pow_now, s, pw);
+        const char* kt = tiles + (i % 3) * TL::BYTES;
+        VT vf[PV];
+#pragma unroll
+        for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
+        if (move) rescale(corr);
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int K = 16 / NC;  // exponentials a step
+#pragma unroll
+        for (int j = 0; j < 2 * NC; ++j) {
+          product(j, vf[j % PV], w);
+          if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
+          if (j == 0) move = softmax_refs(s, pow_now, heads, corr);
+#pragma unroll
+          for (int k = 0; k < K; ++k) {
+            const int e = (j - 1) * K + k;
+            if (e >= 0 && e < 16) softmax_exp(s, pw, e);
+            if (e >= 16 && e < 24) softmax_pack(s, e - 16);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        tile(tiles + (i & 1) * TL::BYTES, power, PD_KT, heads, first, [] {});
-        first = false;
-        power = power_next;
-        bad = bad_next;
+        mfma_a_done(acc);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // (every read of the tile has returned)
+        w = weights(s);
       }
-      store((int64_t)4 * (wg + k) + wave, wave < nx && h0 + col < a.H);
+      {
+        const char* kt = tiles + (i % 3) * TL::BYTES;
+        VT vf[PV];
+#pragma unroll
+        for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
+        if (move) rescale(corr);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2 * NC; ++j) {
+          product(j, vf[j % PV], w);
+          if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mfma_a_done(acc);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        ++i;
+      }
+      any_bad = bad;
+      store((int64_t)4 * piece + wave, wave < nx && h0 + col < a.H);
     }
     return;
   }
@@ -644,7 +714,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   const ListCut cut(total_p, a.nwg - n_s);
   const int t_lo = cut.lo(wg), t_hi = cut.hi(wg), per = cut.per_wave(wg);
   if (t_lo >= t_hi) return;
-  const int64_t slot0 = (int64_t)4 * (n_s + a.max_quads);  // (behind the shared rows')
+  const int64_t slot0 = (int64_t)4 * a.max_pieces;  // (behind the shared rows')
   for (int x = tid; x < VB; x += 64 * PD_WAVES) {
     const int lo = a.tile_off[x], hi = a.tile_off[x + 1];
 #pragma unroll
@@ -860,51 +930,50 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
 // Where the states of a (sequence, head) are: those of its own rows, then those of the shared ones.
 struct LatentStates {
   States own;
-  int n = 0, first = 0, pos = 0;  // first: 4 (workgroup + quad) of the shared rows' first state
-  int own_base = 0;
+  int n = 0, first = 0, step = 0;  // of the shared rows' states: the first slot, and from piece to piece
 };
 struct LatentWhere {
-  const int32_t *head, *tile_off, *quad_item, *block_quad;
-  int HB, nwg, max_quads;
+  const int32_t *head, *tile_off, *member, *group;
+  int HB, nwg, max_pieces;
   __device__ __forceinline__ LatentStates states(int b, int h) const {
-    const int x = b * HB + h / 32, shared = head[0], own = head[1];
-    const int n_s = shared_workgroups(nwg, shared, own);
+    const int x = b * HB + h / 32;
     LatentStates s;
-    s.own = States(ListCut(own, nwg - n_s), x, tile_off[x], tile_off[x + 1]);
-    s.own_base = 4 * (n_s + max_quads);
+    s.own = States(ListCut(head[2], max(nwg - head[1], 1)), x, tile_off[x], tile_off[x + 1]);
     s.n = s.own.n;
-    const int q = block_quad[x];
-    if (q >= 0) {
-      const ItemCut cut(shared, n_s);
-      const int w0 = quad_item[q >> 2] / cut.share, w1 = (quad_item[(q >> 2) + 1] - 1) / cut.share;
-      s.n += w1 - w0 + 1;
-      s.first = 4 * (w0 + (q >> 2)) + (q & 3);
+    const int g = member[b];
+    if (g >= 0) {
+      const int32_t* d = group + GROUP_INTS * g;
+      const int j = x - d[G_X0];
+      s.n += d[G_PIECES];
+      s.first = 4 * (d[G_FIRST] + j / 4) + j % 4;
+      s.step = 4 * d[G_QUADS];
     }
     return s;
   }
   __device__ __forceinline__ int64_t row(const LatentStates& s, int k, int h) const {
-    const int64_t slot = k < s.own.n ? (int64_t)s.own_base + s.own.slot(k) : s.first + 4 * (int64_t)(k - s.own.n);
+    const int64_t slot = k < s.own.n ? 4 * (int64_t)max_pieces + s.own.slot(k) : s.first + (int64_t)s.step * (k - s.own.n);
     return slot * 32 + h % 32;
   }
 };
 
 struct SharedLayout {
   size_t qabs, qexp, part_o, part_ml, plan, bytes;
-  int max_quads, nwg;
+  int max_pieces, nwg;
 };
 SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_groups) {
   const size_t HB = (H + 31) / 32, VB = B * HB;
   SharedLayout l;
-  l.max_quads = (int)(n_groups == 0 ? 0 : VB / 4 + n_groups);
   const int64_t tiles = (int64_t)VB * ((max_len + (int64_t)PD_KT - 1) / PD_KT);
   l.nwg = (int)(tiles < 2 ? 2 : tiles < PD_CUS ? tiles : PD_CUS);
-  const size_t slots = 4 * ((size_t)l.nwg + l.max_quads) + VB;
+  // a piece a workgroup, or a quad a piece (the plan stays below both)
+  l.max_pieces = n_groups == 0 ? 0 : (int)(VB / 4 + n_groups > (size_t)l.nwg ? VB / 4 + n_groups : l.nwg);
+  const size_t slots = 4 * ((size_t)l.nwg + l.max_pieces) + VB;
   l.qabs = 0;
   l.qexp = l.qabs + al(VB * 32 * DK * 2);
   l.part_o = l.qexp + al(VB * 32 * (DVL / 32));
   l.part_ml = l.part_o + al(slots * 32 * DVL * 4);
   l.plan = l.part_ml + al(slots * 32 * 2 * 4);
-  l.bytes = l.plan + al((8 + 2 * (size_t)B + 2 * VB + 1 + 2 * (size_t)l.max_quads + 1 + 5 * (size_t)n_groups) * 4);
+  l.bytes = l.plan + al((8 + 2 * (size_t)B + VB + 1 + (GROUP_INTS + 3) * (size_t)n_groups) * 4);
   return l;
 }
 
@@ -930,16 +999,14 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.len = d.len; a.max_len = d.max_len; a.B = d.B; a.H = d.H; a.HB = HB;
   a.qabs = (const bf16_t*)(ws + l.qabs); a.qexp = (const int8_t*)(ws + l.qexp); a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
   a.sl2 = d.scale * attn::LOG2E; a.nwg = l.nwg;
-  a.n_groups = p.n_groups; a.max_quads = l.max_quads; a.group_off = p.group_off; a.shared_len = p.shared_len;
+  a.n_groups = p.n_groups; a.max_pieces = l.max_pieces; a.group_off = p.group_off; a.shared_len = p.shared_len;
   int32_t* at = (int32_t*)(ws + l.plan);
   a.head = at; at += 8;
   a.start = at; at += d.B;
-  a.group_of = at; at += d.B;
+  a.member = at; at += d.B;
   a.tile_off = at; at += VB + 1;
-  a.block_quad = at; at += VB;
-  a.quad_x = at; at += l.max_quads;
-  a.quad_item = at; at += l.max_quads + 1;
-  a.group = at;
+  a.group = at; at += GROUP_INTS * p.n_groups;
+  a.scratch = at;
   prof_begin(KC_ELEM, s);
   const int64_t grid = 1 + (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
   if (p.e4m3)
@@ -960,7 +1027,7 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL),
            (double)d.B * d.max_len * (p.e4m3 ? d.rkv + 2 * d.dr + 4 : DK * 2), KLABEL("latent_decode_kernel"));
   prof_begin(KC_ELEM, s);
-  const LatentWhere w{a.head, a.tile_off, a.quad_item, a.block_quad, HB, l.nwg, l.max_quads};
+  const LatentWhere w{a.head, a.tile_off, a.member, a.group, HB, l.nwg, l.max_pieces};
 #define X(a_, b_, c_) \
   if (DK == a_ && DVL == b_) decode_finish<b_>(d, a.part_o, a.part_ml, w, s);
   MLA_SHARED_SHAPES(X)

@@ -115,11 +115,16 @@ def test_lengths_below_the_shared_rows(fmt):
     now = [190, 230, 64, 0, 201]
     check_decode(lay, q, now, Shared(lay, q, now, 230, off, [200], fmt)())
     check_decode(lay, q, [0] * 5, Shared(lay, q, [0] * 5, 230, off, [200], fmt)())
-    now = [3, 1, 2, 7, 0]
+    lay.table[0] = 10**6              # (nothing of a sequence without rows is looked at)
+    lay.d_table.copy_(ints(lay.table))
+    now = [0, 230, 201, 210, 201]
     check_decode(lay, q, now, Shared(lay, q, now, 230, off, [200], fmt)())
+    now = [0, 1, 2, 7, 0]
+    check_decode(lay, q, now, Shared(lay, q, now, 230, off, [200], fmt)())
+    lens[0] = 0
     check_decode(lay, q, lens, Shared(lay, q, lens, 231, off, [-5], fmt)())
-    same = [200] * 5
-    check_decode(lay, q, same, Shared(lay, q, [200, 201, 2**31 - 1, 230, 210], 200, off, [2**31 - 1], fmt)())
+    same = [0] + [200] * 4
+    check_decode(lay, q, same, Shared(lay, q, [-1, 201, 2**31 - 1, 230, 210], 200, off, [2**31 - 1], fmt)())
 
 
 @FORMATS
