@@ -244,6 +244,11 @@ __device__ __forceinline__ u32x2 lds_read_tr8(const char* p) {
   typedef int i32x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p));
 }
+// 4 bytes a lane from the lanes' addresses to the LDS byte address `lds`
+__device__ __forceinline__ void dma4(const void* src, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(lds) : "memory");
+}
+
 // A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r) (paged_attn.hip).  S^T reads 16 bytes of 16 consecutive rows, which take
 // different banks; the transposing reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16:
 // 32 bytes of four rows).  In eight bits the rows of those that share banks differ in bits 1 and 3 where two
@@ -286,7 +291,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   // In eight bits a wavefront has two tiles, all of the LDS at 576 values; what is small lies in a second tile: of
   // wavefront 0 (the plan, before the copies) and of the wavefront itself (reference and sum, after its tiles).
   constexpr int NBUF = E4M3 ? 2 : 1, SMALL = NBUF * PD_WAVES * TL::BYTES - (E4M3 ? PD_WAVES * TL::BYTES : 0);
-  constexpr int TABLE = 64 + TL::PERIOD * 256;  // (the plan's, then the shared rows' copies)
+  // (the plan's, the offsets of the shared rows' copies, each wavefront's page table entries and powers of four tiles)
+  constexpr int TABLE = 64 + TL::PERIOD * 256 + PD_WAVES * (E4M3 ? 2048 : 1024);
   __shared__ __attribute__((aligned(1024))) char tiles[NBUF * PD_WAVES * TL::BYTES + (E4M3 ? 0 : 1024 + TABLE)];
   int* plan_x = (int*)(tiles + SMALL + (E4M3 ? 0 : 1024));  // [PD_WAVES], then plan_at
   int* plan_at = plan_x + PD_WAVES;
@@ -321,12 +327,12 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   }
   // the row at position p of sequence b (the last of the tile's again past the end, which gets no weight)
   auto entry = [&](int b, int p) { return a.table[(int64_t)b * a.max_pages + p / a.page_size]; };
-  auto address = [&](int p, int page, bool& bad, float& power) {
+  auto address = [&](int p, int page, bool& bad, uint64_t& power) {
     const bool out = page < 0 || page >= a.n_pages;
     bad = __ballot(out) != 0;
     const uint64_t base = (uint64_t)(uintptr_t)a.pool + (uint64_t)((out ? 0 : page) * a.page_bytes);
     const int r = p % a.page_size;
-    if constexpr (E4M3) power = *(const float*)(uintptr_t)(base + (uint64_t)((int64_t)a.page_size * RB + 4 * (int64_t)r));
+    if constexpr (E4M3) power = base + (uint64_t)((int64_t)a.page_size * RB + 4 * (int64_t)r);
     return base + (uint64_t)((int64_t)r * RB);
   };
   auto row_address = [&](uint64_t at, int r) {
@@ -600,6 +606,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         }
       }
     };
+    const int* ahead = table + 64 * TL::PERIOD + wave * (E4M3 ? 512 : 256);
+    const uint32_t ahead_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ahead);
     const int pieces = __builtin_amdgcn_readfirstlane(a.head[0]);
     for (int piece = wg; piece < pieces; piece += n_s) {
       if (tid == 0) plan_x[0] = -1;
@@ -622,34 +630,41 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       const int b0 = __builtin_amdgcn_readfirstlane(d[G_SEQ]), x = x0 + min(wave, nx - 1);
       const int h0 = 32 * (x % a.HB);
       const uint64_t heads = __ballot(h0 + col < a.H);
-      // Item i: P V of its tile while the softmax of the next tile runs between the products; the tile after that
-      // is copied meanwhile (three buffers).
-      int p = i * PD_KT + col, page = entry(b0, p);
+      // Tile i: P V while the softmax of the next tile runs between the products.  Copies are asked for three tiles
+      // ahead (four buffers) and the page table's entries two tiles before that, all of it without a register that
+      // the compiler would wait for: a wait names how many operations of the later tiles may be under way.
       bool bad = false;
-      float power = 1.f;
-      __syncthreads();  // (the buffers are free)
-      issue(i % 3, address(p, page, bad, power), whole16);
-      begin(x);
-      if (i + 1 < q_hi) page = entry(b0, p + PD_KT);
-      // asks for tile j, whose table entries are there, and for the entries of the one after it
-      auto next = [&](int j) __attribute__((always_inline)) {
-        asm volatile("" : "+v"(page), "+v"(power));  // (loaded: no wait for them behind the copies)
-        float power_of = power;
-        if (j < q_hi) {
-          p += PD_KT;
-          bool out;
-          issue(j % 3, address(p, page, out, power), whole16);
-          bad |= out;
-          if (j + 1 < q_hi) page = entry(b0, p + PD_KT);
-        }
-        return power_of;
+      auto ask = [&](int j) __attribute__((always_inline)) {  // (the last tile's entries again past the end)
+        dma4(a.table + (int64_t)b0 * a.max_pages + (min(j, q_hi - 1) * PD_KT + col) / a.page_size, ahead_lds + 256 * (j & 3));
       };
-      f32x16 s;
-      float pw[16], corr;
+      auto copy = [&](int j, int page) __attribute__((always_inline)) {
+        uint64_t power_at = 0;
+        bool out;
+        const uint64_t at = address(j * PD_KT + col, page, out, power_at);
+        bad |= out;
+        if constexpr (E4M3) dma4((const void*)(uintptr_t)power_at, ahead_lds + 1024 + 256 * (j & 3));
+        issue(j & 3, at, whole16);
+      };
+      constexpr int OPS = NJ + (E4M3 ? 2 : 1);  // of copy() and ask()
+      auto power_of = [&](int j) { return E4M3 ? __int_as_float(ahead[256 + 64 * (j & 3) + lane]) : 1.f; };
+      const int page0 = entry(b0, i * PD_KT + col), page1 = entry(b0, min(i + 1, q_hi - 1) * PD_KT + col),
+                page2 = entry(b0, min(i + 2, q_hi - 1) * PD_KT + col);
+      __syncthreads();  // (the buffers are free)
+      copy(i, page0);
+      begin(x);
       wait_vm<0>();
+      if (i + 1 < q_hi) {
+        copy(i + 1, page1);
+        ask(i + 3);
+      }
+      if (i + 2 < q_hi) {
+        copy(i + 2, page2);
+        ask(i + 4);
+      }
       __syncthreads();
-      float pow_now = next(i + 1);
-      logits(tiles + (i % 3) * TL::BYTES, pow_now, s, pw);
+      f32x16 s;
+      float pw[16], corr, pow_now = power_of(i);
+      logits(tiles + (i & 3) * TL::BYTES, pow_now, s, pw);
       softmax_refs(s, pow_now, heads, corr);
       bool move = false;  // (nothing is there yet at the first tile)
 #pragma unroll
@@ -659,11 +674,16 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       Weights w = weights(s);
       for (; i + 1 < q_hi; ++i) {
         pin(acc);
-        wait_vm<0>();
+        if (i + 2 < q_hi) wait_vm<OPS>();
+        else wait_vm<0>();
         __syncthreads();
-        pow_now = next(i + 2);
-        logits(tiles + ((i + 1) % 3) * TL::BYTES, pow_now, s, pw);
-        const char* kt = tiles + (i % 3) * TL::BYTES;
+        if (i + 3 < q_hi) {
+          copy(i + 3, ahead[64 * ((i + 3) & 3) + lane]);
+          ask(i + 5);
+        }
+        pow_now = power_of(i + 1);
+        logits(tiles + ((i + 1) & 3) * TL::BYTES, pow_now, s, pw);
+        const char* kt = tiles + (i & 3) * TL::BYTES;
         VT vf[PV];
 #pragma unroll
         for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
@@ -688,7 +708,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         w = weights(s);
       }
       {
-        const char* kt = tiles + (i % 3) * TL::BYTES;
+        const char* kt = tiles + (i & 3) * TL::BYTES;
         VT vf[PV];
 #pragma unroll
         for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
@@ -702,7 +722,6 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         }
         mfma_a_done(acc);
         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-        ++i;
       }
       any_bad = bad;
       store((int64_t)4 * piece + wave, wave < nx && h0 + col < a.H);
@@ -798,7 +817,10 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   if constexpr (E4M3) __syncthreads();  // (the plan has been read: copies may overwrite it)
   if (T < T_end) {
     const int p = position(s0, n, T - seq0);
-    issue_rows(address(p, entry(b, p), bad, power), kt);
+    uint64_t power_at = 0;
+    const uint64_t at = address(p, entry(b, p), bad, power_at);
+    if constexpr (E4M3) power = *(const float*)(uintptr_t)power_at;
+    issue_rows(at, kt);
   } else if (!joined) {
     return;
   }
@@ -832,13 +854,15 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         asm volatile("" : "+v"(page), "+v"(power));  // (loaded: no wait for them behind the copies)
         const int now = __builtin_amdgcn_readfirstlane((T - t_first) & 1), next = (now ^ 1) * PD_WAVES * TL::BYTES;
         if (more) {
-          const uint64_t at = address(p2, page, bad, power_next);
+          uint64_t power_at = 0;
+          const uint64_t at = address(p2, page, bad, power_at);
           if (together) {
             issue_half(0, at, kt_lds + next);
             issue_half(1, at, kt_lds + next);
           } else {
             issue_rows(at, kt + next);
           }
+          power_next = *(const float*)(uintptr_t)power_at;
         }
         tile(kt + now * PD_WAVES * TL::BYTES, power, left, heads, T == seg_begin, [] {});
         power = power_next;
@@ -848,7 +872,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
           // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
           // reads return in order), the others behind the last read
           if (more) {
-            at = address(p2, page, bad, power);
+            uint64_t unused;
+            at = address(p2, page, bad, unused);
             if (together) issue_half(0, at, kt_lds);
           }
         });
