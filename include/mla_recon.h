@@ -420,7 +420,9 @@ int mla_recon_cache_read(const mla_recon_cfg *cfg, const mla_paged_cache *cache,
                          void *hip_stream);
 
 /* mla_recon_decode_paged and mla_recon_prefill_paged over a cache of format MLA_CACHE_E4M3: the same
- * arguments, rules and limits, with workspaces of their own sizes. */
+ * arguments and rules, with workspaces of their own sizes; decoding takes batch ceil(n_heads / 32) max_len up
+ * to 2^35.  (Beside rows with latents of 2^118 and more, softmax weights below 2^-14 of the largest may
+ * be lost.) */
 size_t mla_recon_decode_e4m3_workspace_size(const mla_recon_cfg *cfg, int32_t max_len);
 int mla_recon_decode_e4m3(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
                           int32_t max_len, const int32_t *lengths, const void *Wuk, const void *Wuv,
@@ -442,7 +444,7 @@ int mla_recon_prefill_e4m3(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
  *   n_groups      number of groups, 0 to batch; with 0 the two arrays may be NULL
  *   group_offsets device int32 [n_groups + 1], not decreasing, within [0, batch]
  *   shared_len    device int32 [n_groups]
- * Everything else as for mla_recon_decode_paged.  ws 16-byte aligned, of
+ * Everything else as for mla_recon_decode_paged, but batch ceil(n_heads / 32) max_len is at most 2^35.  ws 16-byte aligned, of
  * mla_recon_decode_shared_workspace_size bytes (0 = unsupported or invalid) for this cfg, max_len and
  * n_groups, or of those for more sequences, groups or a larger max_len. */
 size_t mla_recon_decode_shared_workspace_size(const mla_recon_cfg *cfg, int32_t format, int32_t max_len,

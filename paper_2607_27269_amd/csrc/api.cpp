@@ -1214,6 +1214,10 @@ static int decode_shared_check(const mla_recon_cfg* cfg, int32_t format, int32_t
   if ((rc = format_check(cfg, format, who))) return rc;
   if (n_groups < 0 || n_groups > cfg->batch)
     return fail(MLA_ERR_INVALID_ARG, "%s: %d groups of %d sequences", who, n_groups, cfg->batch);
+  // (tiles of all blocks of 32 heads are numbered with 32 bits)
+  const int64_t blocks = (int64_t)cfg->batch * ((cfg->n_heads + (int64_t)31) / 32);
+  if (blocks > 1 << 24 || blocks * max_len > (int64_t)1 << 35)
+    return fail(MLA_ERR_UNSUPPORTED, "%s: at most 2^35 rows (batch times blocks of 32 heads times max_len) per call", who);
   return MLA_OK;
 }
 

@@ -11,6 +11,11 @@ work on them.  One model step over some sequences is a ``Batch``::
         o = batch.attend(layer, q, Wuk, Wuv)          # prefill or decode
     batch.commit()                                # the new tokens count as cached
 
+The pools hold bf16 rows or, with ``format="e4m3"``, rows whose latents take eight bits (about half
+the bytes, so twice the tokens and a quicker decoding; a latent is off by up to 2^-4 of itself).
+Forked sequences share pages: a step of single tokens made with ``share=True`` attends to the
+pages that neighbours in the batch have in common once for all of them.
+
 All device work is enqueued on the current HIP stream; calls from more than one stream are the
 caller's to order (the layers of a batch share its workspace).
 """
@@ -138,24 +143,56 @@ class PageAllocator:
         return list(moved.items())
 
 
+def shared_prefixes(table: np.ndarray, page_size: int, least_rows: int) -> list[tuple[int, int, int]]:
+    """Groups (first sequence, sequences, shared rows) of neighbours in a page table whose rows begin
+    with the same pages.  A sequence joins its neighbour's group unless fewer rows would then be spared
+    (those of all but one); a group has two sequences at least, and shares least_rows at least."""
+    if len(table) < 2:
+        return []
+    differ = (table[1:] != table[:-1]) | (table[1:] < 0)
+    alike = np.where(differ.any(1), differ.argmax(1), table.shape[1])   # pages in common with the one before
+    groups, first, pages = [], 0, 0
+    for i, n in enumerate(list(alike) + [0], start=1):
+        n = int(n)
+        if n and (i == first + 1 or (i - first) * min(n, pages) >= (i - first - 1) * pages):
+            pages = n if i == first + 1 else min(n, pages)
+            continue
+        if i - first >= 2 and pages * page_size >= least_rows:
+            groups.append((first, i - first, pages * page_size))
+        first = i
+    return groups
+
+
 class PagedLatentCache:
     """The paged latent cache of ``n_layers`` layers of shape ``cfg`` (a configs.LayerConfig).
 
     All layers share one page table: page p of a sequence lies at the same place of every
-    layer's pool [n_pages, page_size, r_kv + d_rope], bf16.  Shapes that the attention over pages does not
+    layer's pool: [n_pages, page_size, r_kv + d_rope] in bf16, or [n_pages, bytes of a page] where
+    ``format`` is "e4m3".  Shapes that the attention over pages does not
     serve (fp32, more than one positional key, other widths) are refused here."""
 
-    def __init__(self, cfg, n_layers: int, n_pages: int, page_size: int, device: str = "cuda:0"):
+    format = "bf16"
+
+    def __init__(self, cfg, n_layers: int, n_pages: int, page_size: int, device: str = "cuda:0",
+                 format: str = "bf16"):
+        if format not in ("bf16", "e4m3"):
+            raise ValueError(f"format {format!r}: bf16 or e4m3")
         # (the library's load fails loudly if it is not built)
-        if L.mla_recon_decode_paged_workspace_size(L.make_cfg(cfg.replace(batch=1, seq=1)), 1) == 0:
+        ccfg = L.make_cfg(cfg.replace(batch=1, seq=1))
+        if L.mla_recon_decode_paged_workspace_size(ccfg, 1) == 0:
             raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
         if not torch.cuda.is_available():
             raise RuntimeError("PagedLatentCache needs a ROCm GPU")
-        self.cfg, self.dtype = cfg, torch.bfloat16
+        self.cfg, self.dtype, self.format = cfg, torch.bfloat16, format
         self.alloc = PageAllocator(n_pages, page_size)
         self.width = cfg.kv_rank + cfg.rope_dim
-        self.pool = torch.zeros(n_layers, n_pages, page_size, self.width, dtype=self.dtype,
-                                device=device)
+        if format == "e4m3":
+            self.pool = torch.zeros(n_layers, n_pages,
+                                    L.mla_recon_cache_page_bytes(ccfg, L.MLA_CACHE_E4M3, page_size),
+                                    dtype=torch.uint8, device=device)
+        else:
+            self.pool = torch.zeros(n_layers, n_pages, page_size, self.width, dtype=self.dtype,
+                                    device=device)
         self.device = self.pool.device  # (with its index: "cuda" would follow the current device)
         self._open = None  # the batch that has reserved pages and is not committed
 
@@ -199,12 +236,41 @@ class PagedLatentCache:
         self._closed()
         return len(self.alloc.compact(self._copy))
 
-    def batch(self, seqs, counts) -> "Batch":
+    def _handle(self, layer: int, table: torch.Tensor) -> L.PagedCache:
+        pool = self.pool[layer]
+        return L.PagedCache(pool.data_ptr(), table.data_ptr(), pool.shape[0], self.alloc.page_size,
+                            table.shape[1])
+
+    @property
+    def _format(self) -> int:
+        return L.MLA_CACHE_E4M3 if self.format == "e4m3" else L.MLA_CACHE_STORAGE
+
+    def read(self, layer: int, seq: int, start: int = 0, count: int | None = None) -> torch.Tensor:
+        """Cached rows start .. start + count - 1 of a sequence (default: all from start), as one bf16 tensor
+        [count, r_kv + d_rope] = [c^KV | k^PE rotated]: for another cache, or a look at what is stored."""
+        have = self.alloc.length[seq]
+        count = have - start if count is None else int(count)
+        if start < 0 or count < 0 or start + count > have:
+            raise ValueError(f"rows {start} .. {start + count - 1} of the {have} of sequence {seq}")
+        out = torch.empty(count, self.width, dtype=self.dtype, device=self.device)
+        if count == 0:
+            return out
+        pages = self.alloc.pages[seq]
+        flat = torch.from_numpy(np.asarray([0, count, start] + pages, dtype=np.int32)).to(self.device)
+        offsets, first, table = flat.split([2, 1, len(pages)])
+        with torch.cuda.device(self.device):
+            L.mla_recon_cache_read(L.make_cfg(self.cfg.replace(batch=1, seq=1)),
+                                   self._handle(layer, table.view(1, -1)), self._format, out.data_ptr(), count,
+                                   offsets.data_ptr(), first.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        return out
+
+    def batch(self, seqs, counts, share: bool = False) -> "Batch":
         """A step that adds counts[i] >= 1 tokens to seqs[i]: pages are reserved (and shared ones
         copied).  One batch is open at a time.  Sequences past 2^31 - 1 tokens are refused with nothing
-        changed."""
+        changed.  share: where every sequence has one new token, pages that neighbours in seqs have in
+        common are attended to once for all of them (put forks of one sequence next to each other)."""
         self._closed()
-        step = Batch(self, list(seqs), [int(c) for c in counts])
+        step = Batch(self, list(seqs), [int(c) for c in counts], share)
         self.alloc.extend(step.seqs, step.counts, self._copy)
         try:
             step._upload()
@@ -219,7 +285,11 @@ class Batch:
     """One model step over some sequences of a PagedLatentCache: the packed new tokens of
     sequence i follow those of sequence i - 1."""
 
-    def __init__(self, cache: PagedLatentCache, seqs, counts):
+    # Rows that a group has to share to be worth it: 4 sequences of the 8B layer behind 64 shared rows 23 us
+    # shared and 22 apart, behind 256 24 and 28
+    SHARE_ROWS = 128
+
+    def __init__(self, cache: PagedLatentCache, seqs, counts, share: bool = False):
         if not seqs or len(seqs) != len(counts) or any(c < 1 for c in counts):
             raise ValueError("a batch has sequences, and one new token or more of each")
         self.cache, self.seqs, self.counts = cache, seqs, counts
@@ -228,6 +298,7 @@ class Batch:
         self.n_new, self.n_kv, self.max_len = sum(counts), sum(self._after), max(self._after)
         self.ccfg = L.make_cfg(cache.cfg.replace(batch=len(seqs), seq=1))
         self.single = all(c == 1 for c in counts)
+        self.share, self.groups = share and self.single, []
         self._ws = None
         if self.max_len >= 2**31:
             raise L.MlaError(L.MLA_ERR_UNSUPPORTED, f"a sequence of {self.max_len} tokens")
@@ -238,20 +309,33 @@ class Batch:
         table = np.full((len(seqs), max(len(a.pages[s]) for s in seqs)), -1, dtype=np.int32)
         for row, s in zip(table, seqs):
             row[:len(a.pages[s])] = a.pages[s]
+        if self.share:
+            # (pages in common are full: a shared page that is not has been copied)
+            self.groups = shared_prefixes(table, a.page_size, self.SHARE_ROWS)
         zero = [0]
         # one upload: offsets, starts, offsets of the cached rows, lengths, the table
         parts = [np.cumsum(zero + counts), before, np.cumsum(zero + after), after, table.ravel()]
+        if self.groups:  # all sequences between the groups' ends: those between two groups are groups without rows
+            bounds, shared = [self.groups[0][0]], []
+            for first, n, rows in self.groups:
+                if first > bounds[-1]:
+                    bounds.append(first)
+                    shared.append(0)
+                bounds.append(first + n)
+                shared.append(rows)
+            self.n_groups = len(shared)
+            parts += [bounds, shared]
         flat = torch.from_numpy(np.concatenate([np.asarray(p, dtype=np.int32) for p in parts]))
         flat = flat.to(self.cache.device)
-        self.offsets, self.start, self.kv_offsets, self.lengths, t = flat.split([len(p) for p in parts])
+        self.offsets, self.start, self.kv_offsets, self.lengths, t, *g = flat.split([len(p) for p in parts])
+        if self.groups:
+            self.group_offsets, self.shared_len = g
         self.table = t.view(table.shape)
 
     def _handle(self, layer: int) -> L.PagedCache:
         if self.cache._open is not self:
             raise RuntimeError("this batch is not open")
-        pool = self.cache.pool[layer]
-        return L.PagedCache(pool.data_ptr(), self.table.data_ptr(), pool.shape[0], pool.shape[1],
-                            self.table.shape[1])
+        return self.cache._handle(layer, self.table)
 
     def _check(self, name, x, shape, dtype):
         if tuple(x.shape) != shape or x.dtype != dtype or x.device != self.cache.pool.device \
@@ -268,17 +352,18 @@ class Batch:
         self._check("q", q, (self.n_new, cfg.n_heads, cfg.nope_dim + cfg.rope_dim), c.dtype)
         self._check("inv_freq", inv_freq, (1, cfg.rope_dim // 2), torch.float32)
         out = torch.empty_like(q)
+        append = L.mla_recon_cache_append_e4m3 if c.format == "e4m3" else L.mla_recon_cache_append
         with torch.cuda.device(c.device):
-            L.mla_recon_cache_append(self.ccfg, self._handle(layer), rows.data_ptr(), q.data_ptr(),
-                                     out.data_ptr(), self.n_new, self.offsets.data_ptr(),
-                                     self.start.data_ptr(), inv_freq.data_ptr(),
-                                     torch.cuda.current_stream().cuda_stream)
+            append(self.ccfg, self._handle(layer), rows.data_ptr(), q.data_ptr(), out.data_ptr(), self.n_new,
+                   self.offsets.data_ptr(), self.start.data_ptr(), inv_freq.data_ptr(),
+                   torch.cuda.current_stream().cuda_stream)
         return out
 
     def attend(self, layer: int, q: torch.Tensor, Wuk: torch.Tensor, Wuv: torch.Tensor) -> torch.Tensor:
         """The per-head attention outputs [n_new, H, d_k] of the new tokens (q rotated, their rows
         appended), each over the cached rows of its sequence up to its own.  Wuk
-        [G_kv d_nope, r_kv], Wuv [G_kv d_k, r_kv].
+        [G_kv d_nope, r_kv], Wuv [G_kv d_k, r_kv].  Of a step made with share=True the results are
+        those of the step without it up to rounding.
 
         Where every sequence has one new token the call is the absorbed form's (decoding), else keys
         and values are written out (prefill) for all of the batch.  Single tokens by decoding and by
@@ -296,22 +381,35 @@ class Batch:
             if self._ws is None:  # kept for the other layers
                 self._ws = torch.empty(self._workspace_bytes(), dtype=torch.uint8, device=c.device)
             stream = torch.cuda.current_stream().cuda_stream
-            if self.single:
-                L.mla_recon_decode_paged(self.ccfg, q.data_ptr(), self._handle(layer), self.max_len,
-                                         self.lengths.data_ptr(), Wuk.data_ptr(), Wuv.data_ptr(),
-                                         o.data_ptr(), self._ws.data_ptr(), self._ws.numel(), stream)
-            else:
-                L.mla_recon_prefill_paged(self.ccfg, q.data_ptr(), self.n_new, self.offsets.data_ptr(),
-                                          self._handle(layer), self.n_kv, self.kv_offsets.data_ptr(),
-                                          Wuk.data_ptr(), Wuv.data_ptr(), o.data_ptr(),
+            e4m3 = c.format == "e4m3"
+            if self.groups:
+                L.mla_recon_decode_shared(self.ccfg, q.data_ptr(), self._handle(layer), c._format, self.max_len,
+                                          self.lengths.data_ptr(), self.n_groups, self.group_offsets.data_ptr(),
+                                          self.shared_len.data_ptr(), Wuk.data_ptr(), Wuv.data_ptr(), o.data_ptr(),
                                           self._ws.data_ptr(), self._ws.numel(), stream)
+            elif self.single:
+                decode = L.mla_recon_decode_e4m3 if e4m3 else L.mla_recon_decode_paged
+                decode(self.ccfg, q.data_ptr(), self._handle(layer), self.max_len, self.lengths.data_ptr(),
+                       Wuk.data_ptr(), Wuv.data_ptr(), o.data_ptr(), self._ws.data_ptr(), self._ws.numel(), stream)
+            else:
+                prefill = L.mla_recon_prefill_e4m3 if e4m3 else L.mla_recon_prefill_paged
+                prefill(self.ccfg, q.data_ptr(), self.n_new, self.offsets.data_ptr(), self._handle(layer), self.n_kv,
+                        self.kv_offsets.data_ptr(), Wuk.data_ptr(), Wuv.data_ptr(), o.data_ptr(),
+                        self._ws.data_ptr(), self._ws.numel(), stream)
         return o
 
     def _workspace_bytes(self) -> int:
         if not self.single and self.n_kv >= 2**31:
             raise L.MlaError(L.MLA_ERR_UNSUPPORTED, f"a prefill over {self.n_kv} cached rows")
-        size = (L.mla_recon_decode_paged_workspace_size(self.ccfg, self.max_len) if self.single else
-                L.mla_recon_prefill_paged_workspace_size(self.ccfg, self.n_new, self.n_kv))
+        e4m3 = self.cache.format == "e4m3"
+        if self.groups:
+            size = L.mla_recon_decode_shared_workspace_size(self.ccfg, self.cache._format, self.max_len, self.n_groups)
+        elif self.single:
+            size = (L.mla_recon_decode_e4m3_workspace_size if e4m3 else
+                    L.mla_recon_decode_paged_workspace_size)(self.ccfg, self.max_len)
+        else:
+            size = (L.mla_recon_prefill_e4m3_workspace_size if e4m3 else
+                    L.mla_recon_prefill_paged_workspace_size)(self.ccfg, self.n_new, self.n_kv)
         if size == 0:
             raise L.MlaError(L.MLA_ERR_UNSUPPORTED, L.last_error())
         return size

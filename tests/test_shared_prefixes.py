@@ -1,0 +1,84 @@
+"""Which sequences of a step share their first pages (paged.shared_prefixes, Batch), on the host."""
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_27269_amd import _lib as L
+from paper_2607_27269_amd.paged import Batch, PagedLatentCache, shared_prefixes
+from test_paged_steps import grown, host_cache
+
+
+def table(*rows):
+    out = np.full((len(rows), max(map(len, rows))), -1, dtype=np.int32)
+    for t, r in zip(out, rows):
+        t[:len(r)] = r
+    return out
+
+
+@pytest.mark.parametrize("rows,groups", [
+    ([[1, 2, 3]], []),
+    ([[1, 2, 3], [4, 5]], []),
+    ([[1, 2, 3], [1, 2, 4]], [(0, 2, 32)]),
+    ([[1, 2], [1, 2]], [(0, 2, 32)]),
+    ([[1, 2, 3], [1, 2, 4], [5], [6, 7, 8, 9], [6, 7, 8, 1], [6, 7, 8]], [(0, 2, 32), (3, 3, 48)]),
+    ([[0, 1, 2, 3, 9], [0, 1, 2, 3, 8], [0, 1, 5], [0, 6]], [(0, 3, 32)]),   # 4 pages spared, 2 x 2, 3 x 1
+    ([[0, 1, 2, 3, 9], [0, 1, 2, 3, 8], [0, 5], [0, 6]], [(0, 2, 64), (2, 2, 16)]),
+    ([[1], [2], [3], [3]], [(2, 2, 16)]),
+    ([[-1, -1], [-1, -1]], []),
+])
+def test_groups_of_a_table(rows, groups):
+    assert shared_prefixes(table(*rows), 16, 1) == groups
+
+
+def test_few_shared_rows_are_not_worth_it():
+    t = table([1, 2, 3], [1, 2, 4])
+    assert shared_prefixes(t, 16, 33) == [] and shared_prefixes(t, 16, 32) == [(0, 2, 32)]
+
+
+def test_the_first_and_last_rows_hold_for_any_table():
+    """Random tables: groups are disjoint, in order, and share what they say."""
+    rng = np.random.default_rng(0)
+    for _ in range(300):
+        t = rng.integers(0, 2, (rng.integers(1, 12), rng.integers(1, 6))).astype(np.int32)
+        t[rng.random(t.shape) < 0.05] = -1
+        end = 0
+        for first, n, rows in shared_prefixes(t, 4, 1):
+            assert first >= end and n >= 2 and rows % 4 == 0
+            end = first + n
+            part = t[first:end, :rows // 4]
+            assert (part == part[0]).all() and (part >= 0).all()
+        assert end <= len(t)
+
+
+@pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libmlarecon.so not built")
+def test_a_step_shares_full_pages_only():
+    """Forks of a sequence with a partly filled last page: each that grows has its own copy of that page;
+    sequences between two groups are a group without shared rows."""
+    c = host_cache(200, 16)
+    a = grown(c, 16 * 9 + 3)
+    b = c.alloc.fork(a)
+    alone = grown(c, 20)
+    d = grown(c, 16 * 8)
+    e = c.alloc.fork(d)
+    step = c.batch([a, b, alone, d, e], [1] * 5, share=True)
+    assert step.groups == [(0, 2, 144), (3, 2, 128)]
+    assert step.group_offsets.tolist() == [0, 2, 3, 5] and step.shared_len.tolist() == [144, 0, 128]
+    assert step.n_groups == 3 and step.lengths.tolist() == [148, 148, 21, 129, 129]
+    step.abandon()
+    step = c.batch([alone, a, d, b], [1] * 4, share=True)       # no neighbours
+    assert not step.groups
+    step.abandon()
+    step = c.batch([a, b], [1, 2], share=True)                  # not single tokens
+    assert not step.groups
+    step.abandon()
+    step = c.batch([alone, a, b], [1] * 3)
+    assert not step.groups
+    step.abandon()
+
+
+def test_unknown_formats_are_refused():
+    from paper_2607_27269_amd import configs
+    with pytest.raises(ValueError):
+        PagedLatentCache(configs.get(1), 1, 4, 16, format="fp8")
