@@ -32,6 +32,8 @@ struct LatentDev {
   const char* pool;
   const int32_t* table;
   int n_pages, page_size, max_pages;
+  uint32_t div_mul;       // p / page_size = (2 p div_mul >> 32) >> div_shift for p below 2^31
+  int div_shift;
   int64_t page_bytes;
   const int32_t* len;
   int max_len, B, H, HB;  // HB: blocks of 32 heads
@@ -66,6 +68,10 @@ __device__ __forceinline__ int shared_workgroups(int nwg, int64_t shared, int64_
   if (shared == 0) return 0;
   if (own == 0) return nwg;
   return (int)min(max((nwg * shared + (shared + own) / 2) / (shared + own), (int64_t)1), (int64_t)nwg - 1);
+}
+
+__device__ __forceinline__ int page_of(const LatentDev& a, int p) {
+  return (int)(__umulhi(2u * (uint32_t)p, a.div_mul) >> a.div_shift);
 }
 
 // ---- the plan -------------------------------------------------------------------------
@@ -220,15 +226,24 @@ __global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev 
 }
 
 // ---- attention ------------------------------------------------------------------------
-__device__ __forceinline__ void mfma_v_first(f32x16& d, f16x8 x, f16x8 y) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));
-}
-__device__ __forceinline__ void mfma_v_next(f32x16& d, f16x8 x, f16x8 y) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(d) : "v"(x), "v"(y));
-}
-__device__ __forceinline__ void mfma_a(f32x16& d, f16x8 x, f16x8 y) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(d) : "v"(x), "v"(y));
-}
+// The products here have no wait for operands: these come from LDS, or were converted a product before
+// (tests/test_latent_waits.py looks at the built code).
+#define MLA_PRODUCTS(T, op)                                                                                       \
+  __device__ __forceinline__ void pv_first(f32x16& d, T x, T y) {                                                 \
+    asm volatile("v_mfma_f32_32x32x16_" op " %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));                         \
+  }                                                                                                               \
+  __device__ __forceinline__ void pv_next(f32x16& d, T x, T y) {                                                  \
+    asm volatile("v_mfma_f32_32x32x16_" op " %0, %1, %2, %0" : "+v"(d) : "v"(x), "v"(y));                         \
+  }                                                                                                               \
+  __device__ __forceinline__ void pa_next(f32x16& d, T x, T y) {                                                  \
+    asm volatile("v_mfma_f32_32x32x16_" op " %0, %1, %2, %0" : "+a"(d) : "v"(x), "v"(y));                         \
+  }
+MLA_PRODUCTS(bf16x8, "bf16")
+MLA_PRODUCTS(f16x8, "f16")
+#undef MLA_PRODUCTS
+// operands of coming products, written by the vector ALU here at the latest: two wait states
+template <class T>
+__device__ __forceinline__ void operand_written(T& x) { asm volatile("s_nop 1" : "+v"(x)); }
 // 8 e4m3 values as fp16 (exact)
 __device__ __forceinline__ f16x8 e4m3_to_f16(uint32_t lo, uint32_t hi) {
   u32x4 w;
@@ -286,7 +301,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   using QT = typename std::conditional<E4M3, f16x8, bf16x8>::type;
   constexpr int RB = TL::RB, CHR = TL::CHR, DR = DK - DVL;
   constexpr int NL = DVL / 16, NR = DR / 16, NC = DVL / 32;
-  constexpr int PF = E4M3 ? 3 : 5, PV = 3;  // operand reads in flight ahead of the products of S, and of P V
+  constexpr int PF = E4M3 ? 5 : 5, PV = E4M3 ? 5 : 3;  // operand reads in flight ahead of the products of S, and of P V
   static_assert(DVL % 128 == 0 && DR % 16 == 0, "decode shape");
   // In eight bits a wavefront has two tiles, all of the LDS at 576 values; what is small lies in a second tile: of
   // wavefront 0 (the plan, before the copies) and of the wavefront itself (reference and sum, after its tiles).
@@ -326,12 +341,12 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       }
   }
   // the row at position p of sequence b (the last of the tile's again past the end, which gets no weight)
-  auto entry = [&](int b, int p) { return a.table[(int64_t)b * a.max_pages + p / a.page_size]; };
+  auto entry = [&](int b, int p) { return a.table[(int64_t)b * a.max_pages + page_of(a, p)]; };
   auto address = [&](int p, int page, bool& bad, uint64_t& power) {
     const bool out = page < 0 || page >= a.n_pages;
     bad = __ballot(out) != 0;
     const uint64_t base = (uint64_t)(uintptr_t)a.pool + (uint64_t)((out ? 0 : page) * a.page_bytes);
-    const int r = p % a.page_size;
+    const int r = p - page_of(a, p) * a.page_size;
     if constexpr (E4M3) power = base + (uint64_t)((int64_t)a.page_size * RB + 4 * (int64_t)r);
     return base + (uint64_t)((int64_t)r * RB);
   };
@@ -400,46 +415,59 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     l_run = 0.f;
     any_bad = false;
   };
-  // of the rows of s (8 (e / 4) + 4 half + e % 4), what lane col has for row col
-  auto of_rows = [&](float v, float (&out)[16]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      out[e] = __int_as_float(__builtin_amdgcn_ds_bpermute(16 * half + 32 * (e >> 2) + 4 * (e & 3), __float_as_int(v)));
-  };
-  // S^T of the tile at kt (eight bits: power, of row col, is in it; pw: the powers of the rows of s)
-  auto logits = [&](const char* kt, float power, f32x16& s, float (&pw)[16]) __attribute__((always_inline)) {
+  // S^T of the tile at kt.  Eight bits: the rows' powers are in it; pw takes those of the rows of s
+  // (8 (e / 4) + 4 half + e % 4) from powers(e), the address of four of them, once the tile's last read is asked for.
+  auto logits = [&](const char* kt, f32x16& s, float (&pw)[16], auto powers) __attribute__((always_inline)) {
     auto kread = [&](int i) { return *(const u32x4*)(kt + kb[i % 4] + 128 * (i / 4)); };
     u32x4 raw[PF];  // (pinned: the compiler would read each operand right before its product and wait for it)
 #pragma unroll
     for (int j = 0; j < PF; ++j) raw[j] = kread(j);
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (E4M3) {
+      f16x8 k0 = e4m3_to_f16(raw[0][0], raw[0][1]), k1 = e4m3_to_f16(raw[0][2], raw[0][3]);
+      asm volatile("" : "+v"(k0));
+      operand_written(k1);
 #pragma unroll
       for (int i = 0; i < NL / 2; ++i) {
-        const u32x4 v = raw[i % PF];
-        const f16x8 k0 = e4m3_to_f16(v[0], v[1]);
-        if (i == 0) mfma_v_first(s, k0, qf[0]);
-        else mfma_v_next(s, k0, qf[2 * i]);
-        const f16x8 k1 = e4m3_to_f16(v[2], v[3]);
-        mfma_v_next(s, k1, qf[2 * i + 1]);
+        const u32x4 v = raw[(i + 1) % PF];
+        if (i == 0) pv_first(s, k0, qf[0]);
+        else pv_next(s, k0, qf[2 * i]);
+        if (i + 1 < NL / 2) {
+          k0 = e4m3_to_f16(v[0], v[1]);
+          operand_written(k0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        pv_next(s, k1, qf[2 * i + 1]);
+        if (i + 1 < NL / 2) {
+          k1 = e4m3_to_f16(v[2], v[3]);
+          operand_written(k1);
+        }
         if (i + PF < NL / 2 + NR) raw[i % PF] = kread(i + PF);
-        if (i == NL / 2 - 2) of_rows(power, pw);
+        if (i == NL / 2 - 2) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const f32x4 v4 = *powers(e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) pw[e + k] = v4[k];
+          }
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
       mfma_v_done(s);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] *= pw[e];
+      operand_written(s);
 #pragma unroll
       for (int j = 0; j < NR; ++j) {
-        mfma_v_next(s, __builtin_bit_cast(bf16x8, raw[(NL / 2 + j) % PF]), qr[j]);
-        if (j + PF < NR) raw[(NL / 2 + j) % PF] = kread(NL / 2 + j + PF);
+        pv_next(s, __builtin_bit_cast(bf16x8, raw[(NL / 2 + j) % PF]), qr[j]);
       }
+      static_assert(NR <= PF - 1, "the positional part is read before the powers are");
     } else {
 #pragma unroll
       for (int kk = 0; kk < NL + NR; ++kk) {
         const bf16x8 k = __builtin_bit_cast(bf16x8, raw[kk % PF]);
-        if (kk == 0) mfma_v_first(s, k, qf[0]);
-        else mfma_v_next(s, k, kk < NL ? qf[kk % NL] : qr[kk - NL < 0 ? 0 : kk - NL]);
+        if (kk == 0) pv_first(s, k, qf[0]);
+        else pv_next(s, k, kk < NL ? qf[kk % NL] : qr[kk - NL < 0 ? 0 : kk - NL]);
         if (kk + PF < NL + NR) raw[kk % PF] = kread(kk + PF);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -463,24 +491,50 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   struct Weights {
     u32x4 hi[2], lo[2];
   };
-  auto product = [&](int j, VT v, const Weights& w) __attribute__((always_inline)) {
+  // P V of the tile at kt; step(j) is called behind the products of step j.  Operands are read PV steps ahead and
+  // converted one.
+  auto weighted = [&](const char* kt, const Weights& w, auto step) __attribute__((always_inline)) {
+    VT vf[PV];
+#pragma unroll
+    for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
+    f16x8 v;
     if constexpr (E4M3) {
-      mfma_a(acc[j % NC], e4m3_to_f16(v[0], v[1]), __builtin_bit_cast(f16x8, w.hi[j / NC]));
-    } else {
-      mfma_a(acc[j % NC], v, __builtin_bit_cast(bf16x8, w.hi[j / NC]));
-      mfma_a(acc[j % NC], v, __builtin_bit_cast(bf16x8, w.lo[j / NC]));
+      v = e4m3_to_f16(vf[0][0], vf[0][1]);
+      operand_written(v);
     }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < 2 * NC; ++j) {
+      if constexpr (E4M3) {
+        pa_next(acc[j % NC], v, __builtin_bit_cast(f16x8, w.hi[j / NC]));
+        if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
+        if (j + 1 < 2 * NC) {
+          v = e4m3_to_f16(vf[(j + 1) % PV][0], vf[(j + 1) % PV][1]);
+          operand_written(v);
+        }
+      } else {
+        pa_next(acc[j % NC], vf[j % PV], __builtin_bit_cast(bf16x8, w.hi[j / NC]));
+        pa_next(acc[j % NC], vf[j % PV], __builtin_bit_cast(bf16x8, w.lo[j / NC]));
+        if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
+      }
+      step(j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    mfma_a_done(acc);
+    // every read of the tile has returned before copies may overwrite it
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
   };
   // The softmax of a tile in steps that can be spread over the products of another: the references first (they move only
   // when the tile's maximum exceeds one by more than the slack; returns whether the weighted latents are
   // to be multiplied by corr), then 16 exponentials, then 8 pairs of operands.
-  auto softmax_refs = [&](const f32x16& s, float power, uint64_t heads, float& corr) __attribute__((always_inline)) {
-    float lg[16], my = -INFINITY;
-    if constexpr (E4M3) of_rows(fmaxf((float)((int)(__float_as_uint(power) >> 23) - 127), (float)E4M3_MIN_EXP), lg);
+  auto softmax_refs = [&](const f32x16& s, const float (&pw)[16], uint64_t heads, float& corr) __attribute__((always_inline)) {
+    float my = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) my = fmaxf(my, E4M3 ? __builtin_fmaf(s[e], sl2, lg[e]) : s[e]);
+    for (int e = 0; e < 16; ++e)  // (a power's exponent from its bits; that of a row never written counts as -80)
+      my = fmaxf(my, E4M3 ? __builtin_fmaf((float)max(__float_as_uint(pw[e]), (uint32_t)(127 + E4M3_MIN_EXP) << 23), 0x1p-23f, s[e] * sl2) : s[e]);
     my = pair_max32(my);
-    if constexpr (!E4M3) my *= sl2;
+    if constexpr (E4M3) my -= 127.f;
+    else my *= sl2;
     const bool move = (__ballot(my > m_run + (E4M3 ? E8_SLACK : PD_SLACK)) & heads) != 0;
     // (no branch: products may be under way)
     const float m_new = move ? fmaxf(m_run, my) : m_run;
@@ -512,6 +566,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       w.hi[q / 4][q % 4] = __float_as_uint(s[2 * q]);
       w.lo[q / 4][q % 4] = __float_as_uint(s[2 * q + 1]);
     }
+    if constexpr (!E4M3) asm volatile("" : "+v"(w.lo[0]), "+v"(w.lo[1]));
+    asm volatile("" : "+v"(w.hi[0]));
+    operand_written(w.hi[1]);
     return w;
   };
   auto rescale = [&](float corr) __attribute__((always_inline)) {
@@ -520,13 +577,16 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   };
   // One tile at kt, of which `left` rows count; power: of row col (eight bits).  `heads`: the columns with a head.
   // `early` is called when the reads of the first 16 rows (and of all keys) have returned.
-  auto tile = [&](const char* kt, float power, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
+  auto tile = [&](char* kt, float power, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
     f32x16 s;
     float pw[16];
-    logits(kt, power, s, pw);
-    VT vf[PV];
-#pragma unroll
-    for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
+    // (the powers pass through the tile's first positional values, which have been read by then: 16 of them a row)
+    auto powers = [&](int e) {
+      if (e == 0) *(float*)(kt + (col >> 4) * RB + DVL + 4 * (col & 15)) = power;
+      const int r = 2 * e + 4 * half;
+      return (const f32x4*)(kt + (e >> 3) * RB + DVL + 4 * (r & 15));
+    };
+    logits(kt, s, pw, powers);
     if (left < PD_KT) {  // rows past the end: no weight (a real branch)
       asm volatile("");
 #pragma unroll
@@ -534,26 +594,18 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         if (8 * (e >> 2) + 4 * half + (e & 3) >= left) s[e] = -INFINITY;
     }
     float corr;
-    if (softmax_refs(s, power, heads, corr) && !first) rescale(corr);  // (nothing is there yet at the first tile)
+    if (softmax_refs(s, pw, heads, corr) && !first) rescale(corr);  // (nothing is there yet at the first tile)
 #pragma unroll
     for (int e = 0; e < 16; ++e) softmax_exp(s, pw, e);
 #pragma unroll
     for (int q = 0; q < 8; ++q) softmax_pack(s, q);
     const Weights w = weights(s);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int j = 0; j < 2 * NC; ++j) {
-      product(j, vf[j % PV], w);
-      if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
-      __builtin_amdgcn_sched_barrier(0);
+    weighted(kt, w, [&](int j) __attribute__((always_inline)) {
       if (j == NC) {
         mfma_a_done(acc);  // (no branch, where the compiler may move registers, before the products' waits)
         early();
       }
-    }
-    mfma_a_done(acc);
-    // every read of the tile has returned before copies may overwrite it
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    });
   };
   // the reference and sum of the state, as a merge of states takes them
   auto reference = [&] { return E4M3 ? m_run - E8_BIAS : m_run; };
@@ -579,32 +631,29 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   if (on_shared) {
     // ---- shared rows: pieces of four query blocks ----
     // This wavefront's part of a tile's copies: 8 rows (WIDE) or half of 16, its lanes' source offsets in a table in LDS.
-    int* table = plan_x + 16;
+    int* table = plan_x + 16;  // row (times 4) << 16 | bytes from its start
     for (int u = tid; u < 64 * TL::PERIOD; u += 64 * PD_WAVES) {
       const int r = u / CHR, pc = u % CHR;
-      table[u] = 16 * (r * CHR + (pc ^ TL::swz(r)));
+      table[u] = r << 18 | 16 * (pc ^ TL::swz(r));
     }
     constexpr int NJ = TL::WIDE ? TL::PERIOD : (TL::PERIOD + 1) / 2;
-    const int row0 = TL::WIDE ? 8 * wave : 16 * (wave >> 1);
+    const int row0 = TL::WIDE ? 8 * wave : 16 * (wave >> 1), flip = TL::WIDE && (wave & 1) ? TL::XOR8 : 0;
     auto copy_of = [&](int j) { return TL::WIDE ? j : min(2 * j + (wave & 1), TL::PERIOD - 1); };
     const uint32_t tiles_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tiles) + row0 * RB;
-    auto issue = [&](int buf, uint64_t at, bool together) __attribute__((always_inline)) {
-      const uint32_t lds = __builtin_amdgcn_readfirstlane(tiles_lds + buf * TL::BYTES);
-      const int flip = TL::WIDE && (wave & 1) ? TL::XOR8 : 0;
-      if (together) {
-        uint64_t base = row_address(at, row0);
-        asm volatile("s_nop 4" : "+s"(base));  // (vector ALU to scalar register to memory operation)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) copy_s(base, (uint32_t)(table[64 * copy_of(j) + lane] ^ flip), lds + 1024 * copy_of(j));
-      } else {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const uint32_t off = (uint32_t)(table[64 * copy_of(j) + lane] ^ flip), r = off / RB;
-          const int from = row0 + (int)r;
-          const uint64_t src = (uint64_t)(uint32_t)__shfl((int)(uint32_t)at, from, 64) | (uint64_t)(uint32_t)__shfl((int)(uint32_t)(at >> 32), from, 64) << 32;
-          dma16((const bf16_t*)(uintptr_t)(src + (off - r * RB)), (bf16_t*)(tiles + buf * TL::BYTES + row0 * RB + 1024 * copy_of(j)));
-        }
-      }
+    // copy j of a tile whose row col is at `at`, in three parts (each waits for the LDS reads of the one before)
+    struct Copy {
+      int from;
+      uint32_t lo, hi;
+    };
+    auto copy_offset = [&](Copy& c, int j) __attribute__((always_inline)) { c.from = (table[64 * copy_of(j) + lane] ^ flip) + (row0 << 18); };
+    auto copy_row = [&](Copy& c, uint64_t at) __attribute__((always_inline)) {
+      c.lo = (uint32_t)__builtin_amdgcn_ds_bpermute(c.from >> 16, (int)(uint32_t)at);
+      c.hi = (uint32_t)__builtin_amdgcn_ds_bpermute(c.from >> 16, (int)(uint32_t)(at >> 32));
+    };
+    auto copy_issue = [&](const Copy& c, int j, int buf) __attribute__((always_inline)) {
+      const uint64_t src = ((uint64_t)c.hi << 32 | c.lo) + (uint32_t)(c.from & 0xffff);
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(tiles_lds + buf * TL::BYTES) + 1024 * copy_of(j);
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "{m0}"(dst) : "memory");
     };
     const int* ahead = table + 64 * TL::PERIOD + wave * (E4M3 ? 512 : 256);
     const uint32_t ahead_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ahead);
@@ -635,37 +684,43 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       // the compiler would wait for: a wait names how many operations of the later tiles may be under way.
       bool bad = false;
       auto ask = [&](int j) __attribute__((always_inline)) {  // (the last tile's entries again past the end)
-        dma4(a.table + (int64_t)b0 * a.max_pages + (min(j, q_hi - 1) * PD_KT + col) / a.page_size, ahead_lds + 256 * (j & 3));
+        dma4(a.table + (int64_t)b0 * a.max_pages + page_of(a, min(j, q_hi - 1) * PD_KT + col), ahead_lds + 256 * (j & 3));
       };
-      auto copy = [&](int j, int page) __attribute__((always_inline)) {
+      auto locate = [&](int j, int page) __attribute__((always_inline)) {  // tile j's rows (the last tile's again past the end)
         uint64_t power_at = 0;
         bool out;
-        const uint64_t at = address(j * PD_KT + col, page, out, power_at);
+        const uint64_t at = address(min(j, q_hi - 1) * PD_KT + col, page, out, power_at);
         bad |= out;
         if constexpr (E4M3) dma4((const void*)(uintptr_t)power_at, ahead_lds + 1024 + 256 * (j & 3));
-        issue(j & 3, at, whole16);
+        return at;
       };
-      constexpr int OPS = NJ + (E4M3 ? 2 : 1);  // of copy() and ask()
-      auto power_of = [&](int j) { return E4M3 ? __int_as_float(ahead[256 + 64 * (j & 3) + lane]) : 1.f; };
+      constexpr int OPS = NJ + (E4M3 ? 2 : 1);  // operations of a tile: its copies, its powers, table entries
+      auto copy = [&](int j, int page) __attribute__((always_inline)) {
+        const uint64_t at = locate(j, page);
+#pragma unroll
+        for (int c = 0; c < NJ; ++c) {
+          Copy k;
+          copy_offset(k, c);
+          copy_row(k, at);
+          copy_issue(k, c, j & 3);
+        }
+      };
+      auto powers_of = [&](int j) { return [=](int e) { return (const f32x4*)(ahead + 256 + 64 * (j & 3) + 2 * e + 4 * half); }; };
       const int page0 = entry(b0, i * PD_KT + col), page1 = entry(b0, min(i + 1, q_hi - 1) * PD_KT + col),
                 page2 = entry(b0, min(i + 2, q_hi - 1) * PD_KT + col);
       __syncthreads();  // (the buffers are free)
       copy(i, page0);
       begin(x);
       wait_vm<0>();
-      if (i + 1 < q_hi) {
-        copy(i + 1, page1);
-        ask(i + 3);
-      }
-      if (i + 2 < q_hi) {
-        copy(i + 2, page2);
-        ask(i + 4);
-      }
+      copy(i + 1, page1);
+      ask(i + 3);
+      copy(i + 2, page2);
+      ask(i + 4);
       __syncthreads();
       f32x16 s;
-      float pw[16], corr, pow_now = power_of(i);
-      logits(tiles + (i & 3) * TL::BYTES, pow_now, s, pw);
-      softmax_refs(s, pow_now, heads, corr);
+      float pw[16], corr;
+      logits(tiles + (i & 3) * TL::BYTES, s, pw, powers_of(i));
+      softmax_refs(s, pw, heads, corr);
       bool move = false;  // (nothing is there yet at the first tile)
 #pragma unroll
       for (int e = 0; e < 16; ++e) softmax_exp(s, pw, e);
@@ -674,55 +729,40 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       Weights w = weights(s);
       for (; i + 1 < q_hi; ++i) {
         pin(acc);
-        if (i + 2 < q_hi) wait_vm<OPS>();
-        else wait_vm<0>();
+        wait_vm<OPS>();  // (the tile after the next one's may be under way)
         __syncthreads();
-        if (i + 3 < q_hi) {
-          copy(i + 3, ahead[64 * ((i + 3) & 3) + lane]);
-          ask(i + 5);
-        }
-        pow_now = power_of(i + 1);
-        logits(tiles + ((i + 1) & 3) * TL::BYTES, pow_now, s, pw);
-        const char* kt = tiles + (i & 3) * TL::BYTES;
-        VT vf[PV];
-#pragma unroll
-        for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
+        int page = ahead[64 * ((i + 3) & 3) + lane];
+        logits(tiles + ((i + 1) & 3) * TL::BYTES, s, pw, powers_of(i + 1));
         if (move) rescale(corr);
-        __builtin_amdgcn_sched_barrier(0);
-        constexpr int K = 16 / NC;  // exponentials a step
-#pragma unroll
-        for (int j = 0; j < 2 * NC; ++j) {
-          product(j, vf[j % PV], w);
-          if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
-          if (j == 0) move = softmax_refs(s, pow_now, heads, corr);
+        constexpr int ST = 2 * NC, K = 16 / NC;  // steps, exponentials a step
+        Copy c[NJ];
+        uint64_t at = 0;
+        weighted(tiles + (i & 3) * TL::BYTES, w, [&](int j) __attribute__((always_inline)) {
+          if (j == 0) move = softmax_refs(s, pw, heads, corr);
 #pragma unroll
           for (int k = 0; k < K; ++k) {
             const int e = (j - 1) * K + k;
             if (e >= 0 && e < 16) softmax_exp(s, pw, e);
             if (e >= 16 && e < 24) softmax_pack(s, e - 16);
           }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        mfma_a_done(acc);
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // (every read of the tile has returned)
+          // the tile three ahead is asked for between the products
+          if (j == 1) at = locate(i + 3, page);
+          if (j == 2) ask(i + 5);
+#pragma unroll
+          for (int k = 0; k < NJ; ++k) {
+            // (an LDS read's result is asked for some steps behind it)
+            constexpr int LAG = ST >= 32 ? 3 : 1;
+            const int when = 2 + 2 * LAG + k * (ST - 2 - 2 * LAG) / NJ;
+            if (j == when - 2 * LAG) copy_offset(c[k], k);
+            if (j == when - LAG) copy_row(c[k], at);
+            if (j == when) copy_issue(c[k], k, (i + 3) & 3);
+          }
+        });
         w = weights(s);
       }
-      {
-        const char* kt = tiles + (i & 3) * TL::BYTES;
-        VT vf[PV];
-#pragma unroll
-        for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
-        if (move) rescale(corr);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int j = 0; j < 2 * NC; ++j) {
-          product(j, vf[j % PV], w);
-          if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        mfma_a_done(acc);
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-      }
+      if (move) rescale(corr);
+      weighted(tiles + (i & 3) * TL::BYTES, w, [](int) {});
+      wait_vm<0>();  // (copies past the end)
       any_bad = bad;
       store((int64_t)4 * piece + wave, wave < nx && h0 + col < a.H);
     }
@@ -1020,6 +1060,10 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   LatentDev a;
   a.pool = (const char*)d.c.pool; a.table = d.c.table; a.n_pages = d.c.n_pages; a.page_size = d.c.page_size;
   a.max_pages = d.c.max_pages;
+  // with 2^(shift - 1) < page_size <= 2^shift: 2^(31 + shift) / page_size rounded up, off by less than 1 / page_size in a quotient
+  a.div_shift = 0;
+  while (((int64_t)1 << a.div_shift) < d.c.page_size) ++a.div_shift;
+  a.div_mul = (uint32_t)((((uint64_t)1 << (31 + a.div_shift)) + d.c.page_size - 1) / d.c.page_size);
   a.page_bytes = p.e4m3 ? E4m3Page(d.c.page_size, d.rkv, d.dr).bytes : (int64_t)d.c.page_size * DK * 2;
   a.len = d.len; a.max_len = d.max_len; a.B = d.B; a.H = d.H; a.HB = HB;
   a.qabs = (const bf16_t*)(ws + l.qabs); a.qexp = (const int8_t*)(ws + l.qexp); a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
