@@ -14,7 +14,7 @@ work on them.  One model step over some sequences is a ``Batch``::
 The pools hold bf16 rows or, with ``format="e4m3"``, rows whose latents take eight bits (about half
 the bytes, so twice the tokens and a quicker decoding; a latent is off by up to 2^-4 of itself).
 Forked sequences share pages: a step of single tokens made with ``share=True`` attends to the
-pages that neighbours in the batch have in common once for all of them.
+pages that neighbours in the batch have in common once for all of them, where that is quicker.
 
 All device work is enqueued on the current HIP stream; calls from more than one stream are the
 caller's to order (the layers of a batch share its workspace).
@@ -143,10 +143,10 @@ class PageAllocator:
         return list(moved.items())
 
 
-def shared_prefixes(table: np.ndarray, page_size: int, least_rows: int) -> list[tuple[int, int, int]]:
+def shared_prefixes(table: np.ndarray, page_size: int) -> list[tuple[int, int, int]]:
     """Groups (first sequence, sequences, shared rows) of neighbours in a page table whose rows begin
     with the same pages.  A sequence joins its neighbour's group unless fewer rows would then be spared
-    (those of all but one); a group has two sequences at least, and shares least_rows at least."""
+    (those of all but one); a group has two sequences at least."""
     if len(table) < 2:
         return []
     differ = (table[1:] != table[:-1]) | (table[1:] < 0)
@@ -157,10 +157,28 @@ def shared_prefixes(table: np.ndarray, page_size: int, least_rows: int) -> list[
         if n and (i == first + 1 or (i - first) * min(n, pages) >= (i - first - 1) * pages):
             pages = n if i == first + 1 else min(n, pages)
             continue
-        if i - first >= 2 and pages * page_size >= least_rows:
+        if i - first >= 2:
             groups.append((first, i - first, pages * page_size))
         first = i
     return groups
+
+
+def worth_sharing(groups, n_heads: int, format: str) -> list[tuple[int, int, int]]:
+    """Those of a step's groups whose rows are to be read once for all: the others, and every group of a step
+    in which too few rows would be spared, are quicker apart, where the caches serve what is read again.
+
+    Whole calls, us apart / shared (groups x sequences, shared rows each; 64 rows of their own), bf16, the 8B
+    layer: 1 x 8, 4096 rows 32 / 46; 16 x 4, 8192 120 / 85; 8 x 8, 16384 202 / 126; 2 x 3, 131072
+    164 / 125; 1 x 64, 2048 50 / 51, 8192 93 / 82; 1 x 128, 4096 80 / 96, 16384 222 / 229; 1 x 192, 16384
+    468 / 307; 1 x 256, 4096 145 / 166, 16384 433 / 474; 32 x 2, 16384 212 / 226.  The 0.5B one: 8 x 8, 4096
+    37 / 38; 1 x 64, 4096 34 / 41; 32 x 4, 4096 60 / 52; 8 x 8, 16384 99 / 73.  e4m3 rows, half as many bytes,
+    gain less: the 8B layer 8 x 8, 16384 127 / 115, 7 x 6, 20032 109 / 113, 1 x 64, 8192 81 / 78; the
+    0.5B one 8 x 8, 16384 78 / 76, 1 x 64, 8192 50 / 53."""
+    least, rows = (3, 1 << (17 if n_heads > 32 else 18)) if format == "bf16" else (8, 1 << 18)
+    if format != "bf16" and n_heads <= 32:
+        return []
+    groups = [g for g in groups if g[1] >= least and (g[1] <= 64 or g[2] >= 16384)]
+    return groups if sum((n - 1) * shared for _, n, shared in groups) >= rows else []
 
 
 class PagedLatentCache:
@@ -268,7 +286,8 @@ class PagedLatentCache:
         """A step that adds counts[i] >= 1 tokens to seqs[i]: pages are reserved (and shared ones
         copied).  One batch is open at a time.  Sequences past 2^31 - 1 tokens are refused with nothing
         changed.  share: where every sequence has one new token, pages that neighbours in seqs have in
-        common are attended to once for all of them (put forks of one sequence next to each other)."""
+        common are attended to once for all of them, if that is quicker (``worth_sharing``; put forks of
+        one sequence next to each other)."""
         self._closed()
         step = Batch(self, list(seqs), [int(c) for c in counts], share)
         self.alloc.extend(step.seqs, step.counts, self._copy)
@@ -284,10 +303,6 @@ class PagedLatentCache:
 class Batch:
     """One model step over some sequences of a PagedLatentCache: the packed new tokens of
     sequence i follow those of sequence i - 1."""
-
-    # Rows that a group has to share to be worth it: 4 sequences of the 8B layer behind 64 shared rows 23 us
-    # shared and 22 apart, behind 256 24 and 28
-    SHARE_ROWS = 128
 
     def __init__(self, cache: PagedLatentCache, seqs, counts, share: bool = False):
         if not seqs or len(seqs) != len(counts) or any(c < 1 for c in counts):
@@ -311,7 +326,7 @@ class Batch:
             row[:len(a.pages[s])] = a.pages[s]
         if self.share:
             # (pages in common are full: a shared page that is not has been copied)
-            self.groups = shared_prefixes(table, a.page_size, self.SHARE_ROWS)
+            self.groups = worth_sharing(shared_prefixes(table, a.page_size), self.cache.cfg.n_heads, self.cache.format)
         zero = [0]
         # one upload: offsets, starts, offsets of the cached rows, lengths, the table
         parts = [np.cumsum(zero + counts), before, np.cumsum(zero + after), after, table.ravel()]

@@ -6,7 +6,7 @@ import pytest
 
 from oracle import cache_e4m3_oracle as EO
 from oracle import paged_oracle as PO
-from paper_2607_27269_amd import configs
+from paper_2607_27269_amd import configs, paged
 from test_gpu_paged import REL, bf16, up
 
 pytestmark = pytest.mark.gpu
@@ -70,10 +70,11 @@ class Model:
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("name,ps", [("05b", 16), ("1b", 7), ("8b", 32)])
-def test_samples_of_prompts(name, ps, fmt):
+def test_samples_of_prompts(name, ps, fmt, monkeypatch):
     """Two prompts, samples of each side by side in steps that share their pages, a sequence of its own
     between them; sequences that end, compaction, drafts of several tokens."""
     print(f"[serving] {name} {fmt}, pages of {ps}", flush=True)
+    monkeypatch.setattr(paged, "worth_sharing", lambda groups, n_heads, format: groups)   # (short prompts)
     m = Model(name, fmt, n_pages=150, ps=ps, seed=ps)
     a, alone, b = m.add(), m.add(), m.add()
     m.step([a, alone, b], [200, 3, 150])

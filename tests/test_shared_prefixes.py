@@ -6,7 +6,8 @@ import pytest
 import torch
 
 from paper_2607_27269_amd import _lib as L
-from paper_2607_27269_amd.paged import Batch, PagedLatentCache, shared_prefixes
+from paper_2607_27269_amd import paged
+from paper_2607_27269_amd.paged import PagedLatentCache, shared_prefixes, worth_sharing
 from test_paged_steps import grown, host_cache
 
 
@@ -29,12 +30,26 @@ def table(*rows):
     ([[-1, -1], [-1, -1]], []),
 ])
 def test_groups_of_a_table(rows, groups):
-    assert shared_prefixes(table(*rows), 16, 1) == groups
+    assert shared_prefixes(table(*rows), 16) == groups
 
 
-def test_few_shared_rows_are_not_worth_it():
-    t = table([1, 2, 3], [1, 2, 4])
-    assert shared_prefixes(t, 16, 33) == [] and shared_prefixes(t, 16, 32) == [(0, 2, 32)]
+@pytest.mark.parametrize("groups,heads,format,kept", [
+    ([], 128, "bf16", []),
+    ([(0, 9, 16384)], 128, "bf16", [(0, 9, 16384)]),          # 2^17 rows spared
+    ([(0, 9, 16368)], 128, "bf16", []),
+    ([(0, 9, 16384)], 16, "bf16", []),
+    ([(0, 9, 32768)], 16, "bf16", [(0, 9, 32768)]),
+    ([(0, 2, 1 << 20)], 128, "bf16", []),                     # pairs do not count
+    ([(0, 2, 1 << 20), (2, 5, 16384), (9, 5, 16384)], 128, "bf16", [(2, 5, 16384), (9, 5, 16384)]),
+    ([(0, 64, 8192)], 128, "bf16", [(0, 64, 8192)]),
+    ([(0, 65, 8192)], 128, "bf16", []),                       # large groups behind few rows
+    ([(0, 200, 16384)], 128, "bf16", [(0, 200, 16384)]),
+    ([(0, 17, 16384)], 128, "e4m3", [(0, 17, 16384)]),
+    ([(0, 7, 1 << 17)], 128, "e4m3", []),
+    ([(0, 17, 16384)], 32, "e4m3", []),
+])
+def test_what_is_worth_sharing(groups, heads, format, kept):
+    assert worth_sharing(groups, heads, format) == kept
 
 
 def test_the_first_and_last_rows_hold_for_any_table():
@@ -44,7 +59,7 @@ def test_the_first_and_last_rows_hold_for_any_table():
         t = rng.integers(0, 2, (rng.integers(1, 12), rng.integers(1, 6))).astype(np.int32)
         t[rng.random(t.shape) < 0.05] = -1
         end = 0
-        for first, n, rows in shared_prefixes(t, 4, 1):
+        for first, n, rows in shared_prefixes(t, 4):
             assert first >= end and n >= 2 and rows % 4 == 0
             end = first + n
             part = t[first:end, :rows // 4]
@@ -53,10 +68,11 @@ def test_the_first_and_last_rows_hold_for_any_table():
 
 
 @pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libmlarecon.so not built")
-def test_a_step_shares_full_pages_only():
+def test_a_step_shares_full_pages_only(monkeypatch):
     """Forks of a sequence with a partly filled last page: each that grows has its own copy of that page;
     sequences between two groups are a group without shared rows."""
     c = host_cache(200, 16)
+    monkeypatch.setattr(paged, "worth_sharing", lambda groups, n_heads, format: groups)
     a = grown(c, 16 * 9 + 3)
     b = c.alloc.fork(a)
     alone = grown(c, 20)
@@ -74,6 +90,10 @@ def test_a_step_shares_full_pages_only():
     assert not step.groups
     step.abandon()
     step = c.batch([alone, a, b], [1] * 3)
+    assert not step.groups
+    step.abandon()
+    monkeypatch.undo()
+    step = c.batch([a, b], [1] * 2, share=True)                 # too few
     assert not step.groups
     step.abandon()
 
