@@ -434,8 +434,8 @@ int mla_recon_prefill_e4m3(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
                            void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Decoding for sequences that begin with the same rows (samples of one prompt, users behind one system
- * prompt): as mla_recon_decode_paged, but the shared rows are read once for a group (of three sequences with
- * rows or more; two are quicker apart).
+ * prompt): as mla_recon_decode_paged, but the shared rows are read once for a group (of three blocks of 32 heads or
+ * more, over its sequences with rows: two are quicker apart).
  * Group g is the sequences group_offsets[g] .. group_offsets[g + 1] - 1; the first shared_len[g] rows
  * of each of them are the same values, in the same pages or in copies of them.  Which of the copies
  * is read is not defined.  Sequences of no group, and rows behind the shared ones, are read for

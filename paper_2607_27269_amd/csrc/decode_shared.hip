@@ -138,9 +138,10 @@ __device__ void make_plan(const LatentDev& a) {
   int quads = 0, items = 0, total_q, total_i, longest = 0;
   for (int g = g_lo; g < g_hi; ++g) {
     const int lo = min(max(a.group_off[g], 0), a.B), n = max(min(max(a.group_off[g + 1], 0), a.B) - lo, 0) * a.HB;
-    // (two sequences gain nothing: 32 pairs of the 8B layer behind 16384 rows of bf16 212 us apart and 226 shared, of
-    // e4m3 138 and 193; 2 x 3 behind 131072 164 and 125, 100 and 106)
-    const int t = agent_load(group_cnt + g) >= 3 ? agent_load(group_min + g) / PD_KT : 0;
+    // (two blocks gain nothing: 32 pairs of the 8B layer behind 16384 rows of bf16 212 us apart and 226 shared, of
+    // e4m3 138 and 193; 2 x 3 sequences behind 131072 164 and 125, 100 and 106; with 64 heads 16 pairs behind 16384
+    // 160 and 134, 127 and 115)
+    const int t = agent_load(group_cnt + g) * (int64_t)a.HB >= 3 ? agent_load(group_min + g) / PD_KT : 0;
     int32_t* d = a.group + GROUP_INTS * g;
     d[G_QUADS] = (n + 3) / 4;
     __hip_atomic_store(d + G_TILES, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -201,8 +202,9 @@ __device__ void make_plan(const LatentDev& a) {
     int32_t* d = a.group + GROUP_INTS * g;
     d[G_FIRST] = first;
     d[G_PIECES] = (d[G_TILES] + hi - 1) / hi;
-    first += d[G_QUADS] * d[G_PIECES];
-    if (first > a.max_pieces) d[G_PIECES] = 0;  // (of decreasing offsets: no slots)
+    const int64_t end = first + (int64_t)d[G_QUADS] * d[G_PIECES];
+    if (first < 0 || end > a.max_pieces) d[G_PIECES] = 0;  // (of decreasing offsets: no slots)
+    first = (int)min(end, (int64_t)a.max_pieces);
   }
   if (tid == 0) {
     a.tile_off[a.B * a.HB] = total;

@@ -163,22 +163,26 @@ def shared_prefixes(table: np.ndarray, page_size: int) -> list[tuple[int, int, i
     return groups
 
 
-def worth_sharing(groups, n_heads: int, format: str) -> list[tuple[int, int, int]]:
+def worth_sharing(groups, cfg, format: str) -> list[tuple[int, int, int]]:
     """Those of a step's groups whose rows are to be read once for all: the others, and every group of a step
-    in which too few rows would be spared, are quicker apart, where the caches serve what is read again.
+    in which too few bytes would be spared (those of all sequences but one of each group), are quicker apart,
+    where the caches serve what is read again.
 
-    Whole calls, us apart / shared (groups x sequences, shared rows each; 64 rows of their own), bf16, the 8B
-    layer: 1 x 8, 4096 rows 32 / 46; 16 x 4, 8192 120 / 85; 8 x 8, 16384 202 / 126; 2 x 3, 131072
-    164 / 125; 1 x 64, 2048 50 / 51, 8192 93 / 82; 1 x 128, 4096 80 / 96, 16384 222 / 229; 1 x 192, 16384
-    468 / 307; 1 x 256, 4096 145 / 166, 16384 433 / 474; 32 x 2, 16384 212 / 226.  The 0.5B one: 8 x 8, 4096
-    37 / 38; 1 x 64, 4096 34 / 41; 32 x 4, 4096 60 / 52; 8 x 8, 16384 99 / 73.  e4m3 rows, half as many bytes,
-    gain less: the 8B layer 8 x 8, 16384 127 / 115, 7 x 6, 20032 109 / 113, 1 x 64, 8192 81 / 78; the
-    0.5B one 8 x 8, 16384 78 / 76, 1 x 64, 8192 50 / 53."""
-    least, rows = (3, 1 << (17 if n_heads > 32 else 18)) if format == "bf16" else (8, 1 << 18)
-    if format != "bf16" and n_heads <= 32:
+    Whole calls, us apart / shared (groups x sequences, shared rows each; 64 rows of their own).  bf16, the
+    8B layer (1152 bytes a row): 1 x 8, 4096 rows 32 / 46; 8 x 8, 4096 73 / 62; 16 x 4, 8192 120 / 85; 8 x 8, 16384
+    202 / 126; 32 x 2, 16384 212 / 226; 2 x 3, 131072 164 / 125; 1 x 64, 2048 50 / 51, 8192 93 / 82; 1 x 128, 4096
+    80 / 96, 16384 222 / 229; 1 x 192, 16384 468 / 307; 1 x 256, 4096 145 / 166, 16384 433 / 474.  The 0.5B one
+    (576 bytes): 8 x 8, 4096 37 / 38; 1 x 64, 4096 34 / 41; 32 x 4, 4096 60 / 52; 8 x 8, 16384 99 / 73.  e4m3 rows,
+    about half as many bytes, gain less: the 8B layer 7 x 6, 20032 109 / 113; 4 x 16, 8192 82 / 79; 8 x 8, 16384
+    127 / 115; the 0.5B one 1 x 64, 8192 50 / 53; 8 x 8, 16384 78 / 76.  With more than 32 heads a row is
+    worked on longer once it is read (64 heads: 8 x 8, 4096 83 / 94; 16 x 3, 8192 120 / 135)."""
+    if cfg.n_heads > 32:
         return []
+    row, least, spared = cfg.kv_rank + 2 * cfg.rope_dim + 4, 8, 288 << 20
+    if format == "bf16":
+        row, least, spared = 2 * (cfg.kv_rank + cfg.rope_dim), 3, 144 << 20
     groups = [g for g in groups if g[1] >= least and (g[1] <= 64 or g[2] >= 16384)]
-    return groups if sum((n - 1) * shared for _, n, shared in groups) >= rows else []
+    return groups if sum((n - 1) * rows for _, n, rows in groups) * row >= spared else []
 
 
 class PagedLatentCache:
@@ -265,7 +269,8 @@ class PagedLatentCache:
 
     def read(self, layer: int, seq: int, start: int = 0, count: int | None = None) -> torch.Tensor:
         """Cached rows start .. start + count - 1 of a sequence (default: all from start), as one bf16 tensor
-        [count, r_kv + d_rope] = [c^KV | k^PE rotated]: for another cache, or a look at what is stored."""
+        [count, r_kv + d_rope] = [c^KV | k^PE rotated]: for another cache, or a look at what is stored.  Up to
+        8388608 rows a call."""
         have = self.alloc.length[seq]
         count = have - start if count is None else int(count)
         if start < 0 or count < 0 or start + count > have:
@@ -326,7 +331,11 @@ class Batch:
             row[:len(a.pages[s])] = a.pages[s]
         if self.share:
             # (pages in common are full: a shared page that is not has been copied)
-            self.groups = worth_sharing(shared_prefixes(table, a.page_size), self.cache.cfg.n_heads, self.cache.format)
+            self.groups = worth_sharing(shared_prefixes(table, a.page_size), self.cache.cfg, self.cache.format)
+            # (a step of more rows than the call for groups takes is still decoded, apart)
+            if self.groups and L.mla_recon_decode_shared_workspace_size(self.ccfg, self.cache._format, self.max_len,
+                                                                        len(seqs)) == 0:
+                self.groups = []
         zero = [0]
         # one upload: offsets, starts, offsets of the cached rows, lengths, the table
         parts = [np.cumsum(zero + counts), before, np.cumsum(zero + after), after, table.ravel()]

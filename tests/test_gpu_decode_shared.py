@@ -151,6 +151,42 @@ def test_one_large_group(fmt):
 
 
 @FORMATS
+@pytest.mark.parametrize("n", [1, 3])
+def test_the_longest_sequences(n, fmt):
+    """2^31 - 1 rows, of two pages again and again, all of one weight (zero queries).  A wavefront's sums of the
+    weights and of the latents (1, 2 and 3; 2^21 rows) are whole numbers below 2^24, so only the output rounds."""
+    import torch
+    from paper_2607_27269_amd import _lib as L
+    rows, ps = 2**31 - 1, 1 << 16
+    lay = (E4m3Layer if fmt else Layer)(shape("tiny"), [2 * ps], ps, seed=n)
+    rkv = lay.cfg.kv_rank
+    for name in ("codes", "power"):                              # (made again of the rows below)
+        if fmt:
+            delattr(lay, name)
+    lay.pool[..., :rkv] = np.random.default_rng(n).integers(1, 4, lay.pool[..., :rkv].shape)
+    lay.upload()
+    table = np.tile(lay.table[:1, :2], (n, rows // ps // 2 + 1))[:, :rows // ps + 1]
+    first, second = (lay.pool[lay.table[0, k], :, :rkv] for k in (0, 1))
+    mean = (2**14 * (first.sum(0) + second.sum(0)) - second[-1]) / rows   # 2^15 pages, of the last all rows but one
+    q = torch.zeros(n, lay.cfg.n_heads, lay.cfg.nope_dim + lay.cfg.rope_dim, dtype=torch.bfloat16, device="cuda")
+    o = torch.empty(n, lay.cfg.n_heads, lay.cfg.head_dim, dtype=torch.bfloat16, device="cuda")
+    d_table, lens, off, shared = ints(table), ints([rows] * n), ints([0, n]), ints([rows])
+    cfg, cache = L.make_cfg(lay.cfg.replace(batch=n, seq=1)), L.PagedCache(
+        lay.d_pool.data_ptr(), d_table.data_ptr(), len(lay.d_pool), ps, table.shape[1])
+    size = L.mla_recon_decode_shared_workspace_size(cfg, int(fmt), rows, 1)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    L.mla_recon_decode_shared(cfg, q.data_ptr(), cache, int(fmt), rows, lens.data_ptr(), 1, off.data_ptr(),
+                              shared.data_ptr(), lay.d_Wuk.data_ptr(), lay.d_Wuv.data_ptr(), o.data_ptr(), ws.data_ptr(),
+                              size, torch.cuda.current_stream().cuda_stream)
+    per = lay.cfg.n_heads // lay.cfg.s_kv_groups
+    want = (lay.Wuv @ mean).reshape(lay.cfg.s_kv_groups, -1)
+    got = o.double().cpu().numpy()
+    for h in range(lay.cfg.n_heads):                             # the output's rounding, and the latents' second part's
+        ref = want[h // per]
+        assert np.linalg.norm(got[:, h] - ref, axis=-1).max() <= (2.0 ** -8 + 2.0 ** -15) * np.linalg.norm(ref), h
+
+
+@FORMATS
 def test_bad_pages(fmt):
     """A shared row on no page: NaN for the group; a row of one sequence's own: for that one."""
     lay, lens, off = make("1b", fmt, [3, 3], [128, 128], [40], 32, seed=8)

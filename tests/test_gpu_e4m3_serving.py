@@ -74,7 +74,7 @@ def test_samples_of_prompts(name, ps, fmt, monkeypatch):
     """Two prompts, samples of each side by side in steps that share their pages, a sequence of its own
     between them; sequences that end, compaction, drafts of several tokens."""
     print(f"[serving] {name} {fmt}, pages of {ps}", flush=True)
-    monkeypatch.setattr(paged, "worth_sharing", lambda groups, n_heads, format: groups)   # (short prompts)
+    monkeypatch.setattr(paged, "worth_sharing", lambda groups, cfg, format: groups)   # (short prompts)
     m = Model(name, fmt, n_pages=150, ps=ps, seed=ps)
     a, alone, b = m.add(), m.add(), m.add()
     m.step([a, alone, b], [200, 3, 150])

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2607_27269_amd import _lib as L
-from paper_2607_27269_amd import paged
+from paper_2607_27269_amd import configs, paged
 from paper_2607_27269_amd.paged import PagedLatentCache, shared_prefixes, worth_sharing
 from test_paged_steps import grown, host_cache
 
@@ -33,23 +33,25 @@ def test_groups_of_a_table(rows, groups):
     assert shared_prefixes(table(*rows), 16) == groups
 
 
-@pytest.mark.parametrize("groups,heads,format,kept", [
-    ([], 128, "bf16", []),
-    ([(0, 9, 16384)], 128, "bf16", [(0, 9, 16384)]),          # 2^17 rows spared
-    ([(0, 9, 16368)], 128, "bf16", []),
-    ([(0, 9, 16384)], 16, "bf16", []),
-    ([(0, 9, 32768)], 16, "bf16", [(0, 9, 32768)]),
-    ([(0, 2, 1 << 20)], 128, "bf16", []),                     # pairs do not count
-    ([(0, 2, 1 << 20), (2, 5, 16384), (9, 5, 16384)], 128, "bf16", [(2, 5, 16384), (9, 5, 16384)]),
-    ([(0, 64, 8192)], 128, "bf16", [(0, 64, 8192)]),
-    ([(0, 65, 8192)], 128, "bf16", []),                       # large groups behind few rows
-    ([(0, 200, 16384)], 128, "bf16", [(0, 200, 16384)]),
-    ([(0, 17, 16384)], 128, "e4m3", [(0, 17, 16384)]),
-    ([(0, 7, 1 << 17)], 128, "e4m3", []),
-    ([(0, 17, 16384)], 32, "e4m3", []),
+@pytest.mark.parametrize("groups,name,format,kept", [
+    ([], 3, "bf16", []),
+    ([(0, 9, 16384)], 3, "bf16", [(0, 9, 16384)]),            # 2^17 rows spared, of 1152 bytes
+    ([(0, 9, 16368)], 3, "bf16", []),
+    ([(0, 9, 16384)], 1, "bf16", []),                         # of 576 bytes
+    ([(0, 9, 32768)], 1, "bf16", [(0, 9, 32768)]),
+    ([(0, 2, 1 << 20)], 3, "bf16", []),                       # pairs do not count
+    ([(0, 2, 1 << 20), (2, 5, 16384), (9, 5, 16384)], 3, "bf16", [(2, 5, 16384), (9, 5, 16384)]),
+    ([(0, 64, 8192)], 3, "bf16", [(0, 64, 8192)]),
+    ([(0, 65, 8192)], 3, "bf16", []),                         # large groups behind few rows
+    ([(0, 200, 16384)], 3, "bf16", [(0, 200, 16384)]),
+    ([(0, 31, 16384)], 3, "e4m3", [(0, 31, 16384)]),          # of 644 bytes
+    ([(0, 28, 16384)], 3, "e4m3", []),
+    ([(0, 7, 1 << 17)], 3, "e4m3", []),
 ])
-def test_what_is_worth_sharing(groups, heads, format, kept):
-    assert worth_sharing(groups, heads, format) == kept
+def test_what_is_worth_sharing(groups, name, format, kept):
+    cfg = configs.get(name)
+    assert worth_sharing(groups, cfg, format) == kept
+    assert worth_sharing(groups, cfg.replace(n_heads=64), format) == []
 
 
 def test_the_first_and_last_rows_hold_for_any_table():
@@ -72,7 +74,7 @@ def test_a_step_shares_full_pages_only(monkeypatch):
     """Forks of a sequence with a partly filled last page: each that grows has its own copy of that page;
     sequences between two groups are a group without shared rows."""
     c = host_cache(200, 16)
-    monkeypatch.setattr(paged, "worth_sharing", lambda groups, n_heads, format: groups)
+    monkeypatch.setattr(paged, "worth_sharing", lambda groups, cfg, format: groups)
     a = grown(c, 16 * 9 + 3)
     b = c.alloc.fork(a)
     alone = grown(c, 20)
@@ -98,7 +100,21 @@ def test_a_step_shares_full_pages_only(monkeypatch):
     step.abandon()
 
 
+@pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libmlarecon.so not built")
+def test_steps_too_large_for_groups_are_decoded_apart(monkeypatch):
+    """More rows than decode_shared numbers (2^35 over all blocks of 32 heads): the step is served as without sharing."""
+    monkeypatch.setattr(paged, "worth_sharing", lambda groups, cfg, format: groups)
+    c = host_cache(3000, 1 << 16, configs.get(3).replace(n_heads=64, batch=1, seq=1))
+    a = grown(c, 1 << 26)
+    seqs = [a] + [c.alloc.fork(a) for _ in range(299)]          # (full pages: each grows into one of its own)
+    ccfg = L.make_cfg(c.cfg.replace(batch=300))
+    assert L.mla_recon_decode_shared_workspace_size(ccfg, 0, (1 << 26) + 1, 1) == 0
+    assert L.mla_recon_decode_paged_workspace_size(ccfg, (1 << 26) + 1) > 0
+    step = c.batch(seqs, [1] * 300, share=True)
+    assert not step.groups and step._workspace_bytes() > 0
+    step.abandon()
+
+
 def test_unknown_formats_are_refused():
-    from paper_2607_27269_amd import configs
     with pytest.raises(ValueError):
         PagedLatentCache(configs.get(1), 1, 4, 16, format="fp8")
