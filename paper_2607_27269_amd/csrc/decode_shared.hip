@@ -19,8 +19,9 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // of the matrix products, its state belongs to a wavefront, tiles have 32 rows.  Here the rows of
 // a sequence may begin with ones that its group shares, and there are two lists of tiles:
 //
-// * own rows: the tiles of all query blocks behind what they share, cut as in paged_attn.hip (a wavefront
-//   on a run of its own tiles);
+// * own rows: the tiles of all query blocks behind what they share.  A wavefront works on a run of tiles of its
+//   own; the four of a workgroup are in the same block's rows and join their states, or, where there are too many
+//   blocks for that, the list is cut into equal runs as in paged_attn.hip;
 // * shared rows: a group's query blocks in fours ("quads"), for each quad the tiles of the shared rows.
 //   A workgroup takes a run of these items; its four wavefronts have a query block each and one tile in
 //   LDS for all of them, which is then read from memory once for four blocks and once from the
@@ -47,12 +48,15 @@ struct LatentDev {
   int n_groups, max_pieces;
   const int32_t* group_off;
   const int32_t* shared_len;
-  int32_t* head;          // [3]: pieces of the shared rows, workgroups for them, tiles of own rows
+  int32_t* head;          // [4]: pieces of the shared rows, workgroups for them, tiles of own rows, and of a
+                          // wavefront at most where each workgroup is in one block's (else 0)
   int32_t* start;         // [B]: rows that the sequence shares, a multiple of PD_KT
   int32_t* tile_off;      // [B HB + 1]: first tile of each block's own rows
+  int32_t* wg_off;        // [B HB + 1]: first workgroup of each block's own rows, if each is in one block's
   int32_t* member;        // [B]: the sequence's group if it has shared rows, else -1
   int32_t* group;         // [n_groups][GROUP_INTS]
-  int32_t* scratch;       // [3 n_groups]
+  int32_t* lens;          // [B]: lengths, within [0, max_len]
+  int32_t* scratch;       // [5 n_groups + 1]
 };
 
 __device__ __forceinline__ int len_of(const LatentDev& a, int b) { return min(max(a.len[b], 0), a.max_len); }
@@ -75,27 +79,43 @@ __device__ __forceinline__ int page_of(const LatentDev& a, int p) {
 }
 
 // ---- the plan -------------------------------------------------------------------------
-// Sum over the threads before this one, and over all (NT threads).
+// Sums over the threads before this one, and over all (NT threads), of N values at once.
+template <int NT, int N>
+__device__ __forceinline__ void scan_before(int (&v)[N], int (&total)[N]) {
+  __shared__ int sums[N][NT / 64];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  int upto[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) upto[k] = v[k];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int o = __shfl_up(upto[k], d, 64);
+      if (lane >= d) upto[k] += o;
+    }
+  __syncthreads();
+  if (lane == 63)
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums[k][wave] = upto[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    v[k] = upto[k] - v[k];
+    total[k] = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < wave) v[k] += sums[k][w];
+      total[k] += sums[k][w];
+    }
+  }
+}
 template <int NT>
 __device__ __forceinline__ int scan_before(int mine, int& total) {
-  __shared__ int sums[NT / 64];
-  const int lane = threadIdx.x & 63, wave = wave_id();
-  int upto = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int v = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += v;
-  }
-  __syncthreads();
-  if (lane == 63) sums[wave] = upto;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) {
-    if (w < wave) upto += sums[w];
-    total += sums[w];
-  }
-  return upto - mine;
+  int v[1] = {mine}, t[1];
+  scan_before<NT>(v, t);
+  total = t[0];
+  return v[0];
 }
 
 __device__ __forceinline__ int agent_load(const int32_t* p) {
@@ -103,84 +123,112 @@ __device__ __forceinline__ int agent_load(const int32_t* p) {
 }
 
 // One workgroup of NT threads.  Group offsets that decrease give a plan of no meaning whose indexes
-// are in range.
+// are in range.  Bound by latency: what is looked at again lies in LDS for up to 512 sequences and 256 groups
+// (from memory each look took its round trip: 5.5 us of this launch for one sequence, 4.4 from LDS; 8.4 and 5.9
+// for a group of four).
 template <int NT>
-__device__ void make_plan(const LatentDev& a) {
+__device__ void make_plan(const LatentDev& a, int rkv) {
   const int tid = threadIdx.x, G = a.n_groups;
-  // per group: the shared rows that all its sequences have, how many have rows, and the first that has
-  constexpr int IN_LDS = 512;
-  __shared__ int32_t group_lds[3 * IN_LDS];
-  int32_t *group_min = G <= IN_LDS ? group_lds : a.scratch, *group_cnt = group_min + G, *group_seq = group_cnt + G;
-  for (int g = tid; g < G; g += NT) {
+  constexpr int LDS_G = 256, LDS_B = 512;
+  __shared__ int32_t group_lds[5 * LDS_G + 1], seq_lds[3 * LDS_B];
+  const bool g_lds = G <= LDS_G, b_lds = a.B <= LDS_B;
+  int32_t* tmp = g_lds ? group_lds : a.scratch;
+  // per group: the shared rows that all its sequences have, how many have rows, and the first that has; its tiles, its first
+  // sequence
+  int32_t *group_min = tmp, *group_cnt = tmp + G, *group_seq = tmp + 2 * G, *group_tiles = tmp + 3 * G, *group_off = tmp + 4 * G;
+  int32_t *lens = b_lds ? seq_lds : a.lens, *member = b_lds ? seq_lds + LDS_B : a.member, *start = b_lds ? seq_lds + 2 * LDS_B : a.start;
+  for (int g = tid; g <= G && G > 0; g += NT) {
+    group_off[g] = a.group_off[g];
+    if (g == G) break;
     __hip_atomic_store(group_min + g, min(max(a.shared_len[g], 0), a.max_len), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(group_cnt + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(group_seq + g, a.B, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  __threadfence();
+  for (int b = tid; b < a.B; b += NT) lens[b] = len_of(a, b);
   __syncthreads();
   for (int b = tid; b < a.B; b += NT) {
     int g = -1;
-    const int n = len_of(a, b);
+    const int n = lens[b];
     if (G > 0 && n > 0) {
-      g = sequence_of(a.group_off, G, b);
-      if (b < a.group_off[g] || b >= a.group_off[g + 1]) g = -1;
+      g = sequence_of(group_off, G, b);
+      if (b < group_off[g] || b >= group_off[g + 1]) g = -1;
     }
-    a.member[b] = g;
+    member[b] = g;
     if (g >= 0) {
       atomicMin(group_min + g, n);
       atomicAdd(group_cnt + g, 1);
       atomicMin(group_seq + g, b);
     }
   }
-  __threadfence();
   __syncthreads();
   const int run = (G + NT - 1) / NT, g_lo = min(tid * run, G), g_hi = min(g_lo + run, G);
-  int quads = 0, items = 0, total_q, total_i, longest = 0;
+  auto first_of = [&](int g) { return min(max(group_off[g], 0), a.B); };
+  auto blocks_of = [&](int g) { return max(first_of(g + 1) - first_of(g), 0) * a.HB; };
+  auto quads_of = [&](int g) { return (blocks_of(g) + 3) / 4; };
+  int both[2] = {0, 0}, totals[2];  // quads, and their tiles
   for (int g = g_lo; g < g_hi; ++g) {
-    const int lo = min(max(a.group_off[g], 0), a.B), n = max(min(max(a.group_off[g + 1], 0), a.B) - lo, 0) * a.HB;
     // (two blocks gain nothing: 32 pairs of the 8B layer behind 16384 rows of bf16 212 us apart and 226 shared, of
     // e4m3 138 and 193; 2 x 3 sequences behind 131072 164 and 125, 100 and 106; with 64 heads 16 pairs behind 16384
     // 160 and 134, 127 and 115)
     const int t = agent_load(group_cnt + g) * (int64_t)a.HB >= 3 ? agent_load(group_min + g) / PD_KT : 0;
-    int32_t* d = a.group + GROUP_INTS * g;
-    d[G_QUADS] = (n + 3) / 4;
-    __hip_atomic_store(d + G_TILES, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    d[G_X0] = lo * a.HB;
-    d[G_BLOCKS] = n;
-    d[G_SEQ] = agent_load(group_seq + g);
+    group_tiles[g] = t;
     if (t > 0) {
-      quads += (n + 3) / 4;
-      items += (n + 3) / 4 * t;
-      longest = max(longest, t);
+      both[0] += quads_of(g);
+      both[1] += quads_of(g) * t;
     }
   }
-  scan_before<NT>(quads, total_q);
-  scan_before<NT>(items, total_i);
-  __threadfence();
-  __syncthreads();
+  scan_before<NT>(both, totals);
+  const int total_q = totals[0], total_i = totals[1];
   // own rows
   const int runb = (a.B + NT - 1) / NT, b_lo = min(tid * runb, a.B), b_hi = min(b_lo + runb, a.B);
   int mine = 0, total;
   for (int b = b_lo; b < b_hi; ++b) {
-    const int g = a.member[b], n = len_of(a, b), t = g >= 0 ? agent_load(a.group + GROUP_INTS * g + G_TILES) : 0;
-    a.start[b] = min(t * PD_KT, n);
-    if (t == 0) a.member[b] = -1;
-    mine += tiles_of(n - min(t * PD_KT, n)) * a.HB;
+    const int g = member[b], n = lens[b], t = g >= 0 ? group_tiles[g] : 0;
+    a.start[b] = start[b] = min(t * PD_KT, n);
+    a.member[b] = t == 0 ? -1 : g;
+    mine += tiles_of(n - start[b]) * a.HB;
   }
   int at = scan_before<NT>(mine, total);
   for (int b = b_lo; b < b_hi; ++b) {
-    const int n = tiles_of(len_of(a, b) - a.start[b]);
+    const int n = tiles_of(lens[b] - start[b]);
     for (int h = 0; h < a.HB; ++h, at += n) a.tile_off[b * a.HB + h] = at;
+  }
+  // Own rows, each workgroup in one block's: the least number of tiles a wavefront for which there are enough
+  // workgroups, if that is not much more than equal runs need.  Equal runs cross blocks: every wavefront
+  // then writes a state, or two, where here the workgroup writes one (of 512 values 64 KB, which the merge reads
+  // again), and loads a block's queries more often.  Whole calls over e4m3 rows, equal runs / this, us: 512 values: 41 sequences of 1024
+  // rows 39 / 32, of 4096 53 / 45, 250 of 2048 143 / 115, 200 of 4096 (24 tiles a wavefront / 32) 175 / 156,
+  // 250 of 8192 (59 / 64) 316 / 273; 256 values: 250 of 512 35 / 30, 100 of 4096 (13 / 16) 44 / 46, 200 of 4096
+  // (24 / 32) 71 / 79.  Equal runs for 260 of 2048: 149 (512 values; 256 of them 116).
+  const int n_s = shared_workgroups(a.nwg, total_i, total), n_p = max(a.nwg - n_s, 1);
+  const int least = (ListCut(total, n_p).share + PD_WAVES - 1) / PD_WAVES, more = rkv >= 512 ? least / 3 + 2 : 1;
+  constexpr int TRIES = 6;
+  auto tried = [&](int k) { return least + more * k / (TRIES - 1); };
+  int wanted[TRIES] = {}, sums[TRIES], per_wave = 0, wgs = 0;
+  for (int b = b_lo; b < b_hi; ++b) {
+    const int n = tiles_of(lens[b] - start[b]);
+#pragma unroll
+    for (int k = 0; k < TRIES; ++k) wanted[k] += (n + PD_WAVES * tried(k) - 1) / (PD_WAVES * tried(k)) * a.HB;
+  }
+  scan_before<NT>(wanted, sums);
+#pragma unroll
+  for (int k = TRIES - 1; k >= 0; --k)
+    if (sums[k] <= n_p) {
+      per_wave = tried(k);
+      wgs = wanted[k];
+    }
+  if (per_wave > 0) {
+    for (int b = b_lo; b < b_hi; ++b) {
+      const int n = (tiles_of(lens[b] - start[b]) + PD_WAVES * per_wave - 1) / (PD_WAVES * per_wave);
+      for (int h = 0; h < a.HB; ++h, wgs += n) a.wg_off[b * a.HB + h] = wgs;
+    }
+    if (b_lo < a.B && b_hi == a.B) a.wg_off[a.B * a.HB] = wgs;
   }
   // The shared rows' workgroups take a piece each: the least number of tiles a piece for which there are enough of
   // them (with more quads than workgroups a quad is a piece).
-  const int n_s = shared_workgroups(a.nwg, total_i, total);
   auto pieces_at = [&](int t) {
     int n = 0, sum;
-    for (int g = g_lo; g < g_hi; ++g) {
-      const int32_t* d = a.group + GROUP_INTS * g;
-      n += d[G_QUADS] * ((d[G_TILES] + t - 1) / t);
-    }
+    for (int g = g_lo; g < g_hi; ++g) n += quads_of(g) * ((group_tiles[g] + t - 1) / t);
     scan_before<NT>(n, sum);
     return sum;
   };
@@ -196,14 +244,19 @@ __device__ void make_plan(const LatentDev& a) {
   }
   hi = max(hi, 1);
   int count = 0, pieces;
-  for (int g = g_lo; g < g_hi; ++g) count += a.group[GROUP_INTS * g + G_QUADS] * ((a.group[GROUP_INTS * g + G_TILES] + hi - 1) / hi);
+  for (int g = g_lo; g < g_hi; ++g) count += quads_of(g) * ((group_tiles[g] + hi - 1) / hi);
   int first = scan_before<NT>(count, pieces);
   for (int g = g_lo; g < g_hi; ++g) {
+    const int of = (group_tiles[g] + hi - 1) / hi;
+    const int64_t end = first + (int64_t)quads_of(g) * of;
     int32_t* d = a.group + GROUP_INTS * g;
     d[G_FIRST] = first;
-    d[G_PIECES] = (d[G_TILES] + hi - 1) / hi;
-    const int64_t end = first + (int64_t)d[G_QUADS] * d[G_PIECES];
-    if (first < 0 || end > a.max_pieces) d[G_PIECES] = 0;  // (of decreasing offsets: no slots)
+    d[G_QUADS] = quads_of(g);
+    d[G_PIECES] = first < 0 || end > a.max_pieces ? 0 : of;  // (0: of decreasing offsets, no slots)
+    d[G_TILES] = group_tiles[g];
+    d[G_X0] = first_of(g) * a.HB;
+    d[G_BLOCKS] = blocks_of(g);
+    d[G_SEQ] = agent_load(group_seq + g);
     first = (int)min(end, (int64_t)a.max_pieces);
   }
   if (tid == 0) {
@@ -211,6 +264,7 @@ __device__ void make_plan(const LatentDev& a) {
     a.head[0] = min(pieces, a.max_pieces);
     a.head[1] = n_s;
     a.head[2] = total;
+    a.head[3] = per_wave;
   }
 }
 
@@ -220,7 +274,7 @@ template <bool E4M3>
 __global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev a, const bf16_t* q, const bf16_t* Wuk,
                                                                       int hpg, int dn, int dr, int rkv) {
   if (blockIdx.x == 0) {
-    make_plan<PREP_THREADS>(a);
+    make_plan<PREP_THREADS>(a, rkv);
     return;
   }
   const int nx = rkv / 64, ny = (a.B * hpg + 31) / 32, k = blockIdx.x - 1;
@@ -773,22 +827,45 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   }
 
   // ---- own rows: a run of tiles a wavefront ----
-  const ListCut cut(total_p, a.nwg - n_s);
-  const int t_lo = cut.lo(wg), t_hi = cut.hi(wg), per = cut.per_wave(wg);
-  if (t_lo >= t_hi) return;
+  const bool in_one = __builtin_amdgcn_readfirstlane(a.head[3]) > 0;
   const int64_t slot0 = (int64_t)4 * a.max_pieces;  // (behind the shared rows')
-  for (int x = tid; x < VB; x += 64 * PD_WAVES) {
-    const int lo = a.tile_off[x], hi = a.tile_off[x + 1];
+  int t_lo, t_hi, per;
+  if (in_one) {
+    if (wg >= __builtin_amdgcn_readfirstlane(a.wg_off[VB])) return;
+    for (int x = tid; x < VB; x += 64 * PD_WAVES) {
+      const int lo = a.wg_off[x], hi = a.wg_off[x + 1];
+      if (lo <= wg && wg < hi) {
+        const int at = a.tile_off[x], n = a.tile_off[x + 1] - at;
 #pragma unroll
-    for (int w = 0; w < PD_WAVES; ++w) {
-      const int t = t_lo + w * per;
-      if (t < t_hi && lo <= t && t < hi) {
-        plan_x[w] = x;
-        plan_at[w] = lo;
+        for (int w = 0; w < PD_WAVES; ++w) {
+          plan_x[w] = x;
+          plan_at[w] = at;
+        }
+        plan_at[PD_WAVES] = at + (int)((int64_t)n * (wg - lo) / (hi - lo));
+        plan_at[PD_WAVES + 1] = at + (int)((int64_t)n * (wg + 1 - lo) / (hi - lo));
       }
     }
+    __syncthreads();
+    t_lo = __builtin_amdgcn_readfirstlane(plan_at[PD_WAVES]);
+    t_hi = __builtin_amdgcn_readfirstlane(plan_at[PD_WAVES + 1]);
+    per = (t_hi - t_lo + PD_WAVES - 1) / PD_WAVES;
+  } else {
+    const ListCut cut(total_p, a.nwg - n_s);
+    t_lo = cut.lo(wg), t_hi = cut.hi(wg), per = cut.per_wave(wg);
+    if (t_lo >= t_hi) return;
+    for (int x = tid; x < VB; x += 64 * PD_WAVES) {
+      const int lo = a.tile_off[x], hi = a.tile_off[x + 1];
+#pragma unroll
+      for (int w = 0; w < PD_WAVES; ++w) {
+        const int t = t_lo + w * per;
+        if (t < t_hi && lo <= t && t < hi) {
+          plan_x[w] = x;
+          plan_at[w] = lo;
+        }
+      }
+    }
+    __syncthreads();
   }
-  __syncthreads();
   const int t_first = t_lo + wave * per;
   int T = t_first;                                 // this wavefront's run: tiles [T, T_end)
   const int T_end = min(T + per, t_hi);
@@ -950,7 +1027,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     float* buf = (float*)tiles;
     float M = -INFINITY, L = 0.f, f[PD_WAVES];
     const int hj = 32 * (x_first % a.HB);
-    const int64_t row = (slot0 + (int64_t)PD_WAVES * wg + x_first) * 32 + col;
+    const int64_t row = (slot0 + (in_one ? (int64_t)wg : (int64_t)PD_WAVES * wg + x_first)) * 32 + col;
     float* po = a.part_o + row * DVL + 4 * half;
 #pragma unroll
     for (int ph = 0; ph < PH; ++ph) {
@@ -1001,12 +1078,17 @@ struct LatentStates {
   int n = 0, first = 0, step = 0;  // of the shared rows' states: the first slot, and from piece to piece
 };
 struct LatentWhere {
-  const int32_t *head, *tile_off, *member, *group;
+  const int32_t *head, *tile_off, *wg_off, *member, *group;
   int HB, nwg, max_pieces;
   __device__ __forceinline__ LatentStates states(int b, int h) const {
     const int x = b * HB + h / 32;
     LatentStates s;
-    s.own = States(ListCut(head[2], max(nwg - head[1], 1)), x, tile_off[x], tile_off[x + 1]);
+    if (head[3] > 0) {
+      s.own.at0 = wg_off[x];
+      s.own.n = s.own.n0 = wg_off[x + 1] - s.own.at0;
+    } else {
+      s.own = States(ListCut(head[2], max(nwg - head[1], 1)), x, tile_off[x], tile_off[x + 1]);
+    }
     s.n = s.own.n;
     const int g = member[b];
     if (g >= 0) {
@@ -1041,7 +1123,7 @@ SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_gro
   l.part_o = l.qexp + al(VB * 32 * (DVL / 32));
   l.part_ml = l.part_o + al(slots * 32 * DVL * 4);
   l.plan = l.part_ml + al(slots * 32 * 2 * 4);
-  l.bytes = l.plan + al((8 + 2 * (size_t)B + VB + 1 + (GROUP_INTS + 3) * (size_t)n_groups) * 4);
+  l.bytes = l.plan + al((8 + 3 * (size_t)B + 2 * (VB + 1) + (GROUP_INTS + 5) * (size_t)n_groups + 1) * 4);
   return l;
 }
 
@@ -1076,7 +1158,9 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.head = at; at += 8;
   a.start = at; at += d.B;
   a.member = at; at += d.B;
+  a.lens = at; at += d.B;
   a.tile_off = at; at += VB + 1;
+  a.wg_off = at; at += VB + 1;
   a.group = at; at += GROUP_INTS * p.n_groups;
   a.scratch = at;
   prof_begin(KC_ELEM, s);
@@ -1099,7 +1183,7 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL),
            (double)d.B * d.max_len * (p.e4m3 ? d.rkv + 2 * d.dr + 4 : DK * 2), KLABEL("latent_decode_kernel"));
   prof_begin(KC_ELEM, s);
-  const LatentWhere w{a.head, a.tile_off, a.member, a.group, HB, l.nwg, l.max_pieces};
+  const LatentWhere w{a.head, a.tile_off, a.wg_off, a.member, a.group, HB, l.nwg, l.max_pieces};
 #define X(a_, b_, c_) \
   if (DK == a_ && DVL == b_) decode_finish<b_>(d, a.part_o, a.part_ml, w, s);
   MLA_SHARED_SHAPES(X)
