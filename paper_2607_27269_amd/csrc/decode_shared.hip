@@ -28,7 +28,17 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 //   caches for the group's other quads.
 //
 // The workgroups are divided between the lists by their tiles.  A tile of one block's own rows and
-// an item of four blocks cost a workgroup about the same: the first waits for its copy.
+// an item of four blocks cost a workgroup about the same: the first waits for its copy (64 sequences of the 8B layer
+// behind 8192 shared rows, 400 of their own: 70 us; with own tiles counted as 3/4, 2/3, 1/2: 71, 76, 87).
+//
+// Three launches: the absorbed queries with the plan, the attention, the merge with W_UV.  Measured (whole calls; 5.2 TB/s
+// is a large copy's rate, 1444 TFLOP/s a large bf16 product's):
+//   e4m3, 64 sequences to 4096 rows, 32 heads of 512 + 64   63 us (7.0 + 50 + 8.7; the rows alone 33)
+//   e4m3, 41 ragged ones to 16001                           44    (5.6 + 30 + 10.6; 14)
+//   e4m3, one of 300, 14 heads of 256 + 32                  17    (4.5 + 9.0 + 3.9)
+//   bf16, 64 behind 8192 shared rows                        87    (8.5 + 70 + 16.6; operations alone 26)
+//   e4m3, 45 in 7 groups behind 20000                       89    (8.2 + 72 + 17.5; 23)
+//   bf16, 4 behind 1000, 14 heads                           20    (6.0 + 9.8 + 4.4)
 struct LatentDev {
   const char* pool;
   const int32_t* table;
@@ -196,10 +206,10 @@ __device__ void make_plan(const LatentDev& a, int rkv) {
   // Own rows, each workgroup in one block's: the least number of tiles a wavefront for which there are enough
   // workgroups, if that is not much more than equal runs need.  Equal runs cross blocks: every wavefront
   // then writes a state, or two, where here the workgroup writes one (of 512 values 64 KB, which the merge reads
-  // again), and loads a block's queries more often.  Whole calls over e4m3 rows, equal runs / this, us: 512 values: 41 sequences of 1024
-  // rows 39 / 32, of 4096 53 / 45, 250 of 2048 143 / 115, 200 of 4096 (24 tiles a wavefront / 32) 175 / 156,
-  // 250 of 8192 (59 / 64) 316 / 273; 256 values: 250 of 512 35 / 30, 100 of 4096 (13 / 16) 44 / 46, 200 of 4096
-  // (24 / 32) 71 / 79.  Equal runs for 260 of 2048: 149 (512 values; 256 of them 116).
+  // again), and loads a block's queries more often.  Whole calls over e4m3 rows, equal runs / this, us: 512 values: 41
+  // sequences of 1024 rows 39 / 31, of 4096 53 / 45, 250 of 2048 143 / 114, 200 of 4096 (24 tiles a wavefront / 32)
+  // 175 / 154, 250 of 8192 (59 / 64) 316 / 273; 256 values: 250 of 512 35 / 30, 100 of 4096 (13 / 16) 44 / 46, 200
+  // of 4096 (24 / 32) 71 / 79.
   const int n_s = shared_workgroups(a.nwg, total_i, total), n_p = max(a.nwg - n_s, 1);
   const int least = (ListCut(total, n_p).share + PD_WAVES - 1) / PD_WAVES, more = rkv >= 512 ? least / 3 + 2 : 1;
   constexpr int TRIES = 6;
@@ -321,8 +331,8 @@ __device__ __forceinline__ void dma4(const void* src, uint32_t lds) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(lds) : "memory");
 }
 
-// A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r) (paged_attn.hip).  S^T reads 16 bytes of 16 consecutive rows, which take
-// different banks; the transposing reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16:
+// A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r)
+// (paged_attn.hip).  S^T reads 16 bytes of 16 consecutive rows, which take different banks; the transposing reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16:
 // 32 bytes of four rows).  In eight bits the rows of those that share banks differ in bits 1 and 3 where two
 // rows span the banks (640 bytes), which go to chunk bits 1 and 2.
 template <int DK, int DVL, bool E4M3>
@@ -352,13 +362,27 @@ struct LatentTile {
 // and divided by the same power, so that the logit is multiplied by it last.
 constexpr float E8_SLACK = 7.f, E8_BIAS = 8.f;
 
+// In bf16 the absorbed queries are bf16 (as in the paged decoding): their rounding, 2^-9 of each, is most of the
+// error, 2.8e-3 to 3.3e-3 of the output's norm where the output's own rounding is 1.7e-3, and e4m3 with fp16 queries
+// 1.7e-3 in all.
+//
+// What bounds it.  Own rows: the stream of the rows (in eight bits 20 KB a wavefront and tile, 3.4 TB/s over the
+// kernel) behind a fixed 9 us (launch, plan, queries, first tile), then the states.  Shared rows: a tile costs a
+// workgroup 3.2 us in bf16, of which its products take about half (100 of 32 cycles a wavefront at the 1.5 to 1.9 GHz that
+// such a loop runs at), the softmax and the copies' addresses run between them, and the reads of four wavefronts keep
+// LDS as busy as S^T's products the matrix cores.  Ahead of that 9 us as above; behind it the states, 64 KB a
+// block and piece (12 us for 56 MB; the merge reads them again, 16 us).
+// Tried for the shared rows and not kept: tiles made fp16 once for all wavefronts, with fp16 queries and one operand for
+// P (68 products for 100): 78 us for 70 in bf16, 71 for 72 in e4m3, LDS being read and written once more a tile;
+// operands read further ahead (PF 7, PV 6 to 8), no change.  (With P V after its own tile's softmax, and pieces that
+// crossed quads: 77.)
 template <int DK, int DVL, bool E4M3, int OCC>
 __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(LatentDev a) {
   using TL = LatentTile<DK, DVL, E4M3>;
   using QT = typename std::conditional<E4M3, f16x8, bf16x8>::type;
   constexpr int RB = TL::RB, CHR = TL::CHR, DR = DK - DVL;
   constexpr int NL = DVL / 16, NR = DR / 16, NC = DVL / 32;
-  constexpr int PF = E4M3 ? 5 : 5, PV = E4M3 ? 5 : 3;  // operand reads in flight ahead of the products of S, and of P V
+  constexpr int PF = 5, PV = E4M3 ? 5 : 3;  // operand reads in flight ahead of the products of S, and of P V
   static_assert(DVL % 128 == 0 && DR % 16 == 0, "decode shape");
   // In eight bits a wavefront has two tiles, all of the LDS at 576 values; what is small lies in a second tile: of
   // wavefront 0 (the plan, before the copies) and of the wavefront itself (reference and sum, after its tiles).

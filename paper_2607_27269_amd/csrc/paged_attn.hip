@@ -530,7 +530,8 @@ namespace {
 // that is not finite, has a latent of 2^72 or more or lies on no page becomes zeros with a NaN positional
 // key: its values and non-positional key are 0 and its logits NaN, for exactly the queries that see it.
 // Rows of no sequence become zeros.  Bound by memory (14083 rows of 576 values 10.9 us, 4.4 TB/s) and, for
-// few rows, by three dependent loads (77 rows 3.4 us).
+// few rows, by three dependent loads (77 rows 3.4 us).  E4M3: the values that the rows stand for, exact in bf16;
+// 15349 rows 15.4 us.
 constexpr int GATHER_EXP = 64;  // largest |e|
 constexpr int GATHER_TOP = 127 + GATHER_EXP + 8;  // exponent field of the first latent too large
 struct GatherDev {
