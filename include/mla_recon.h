@@ -447,7 +447,8 @@ int mla_recon_prefill_e4m3(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
  *   shared_len    device int32 [n_groups]
  * Everything else as for mla_recon_decode_paged, but batch ceil(n_heads / 32) max_len is at most 2^35.  ws 16-byte aligned, of
  * mla_recon_decode_shared_workspace_size bytes (0 = unsupported or invalid) for this cfg, max_len and
- * n_groups, or of those for more sequences, groups or a larger max_len. */
+ * n_groups, or of those for more sequences, groups or a larger max_len.  (From 16 blocks of 32 heads in all on it
+ * has room for the shared rows, up to 256 MiB.) */
 size_t mla_recon_decode_shared_workspace_size(const mla_recon_cfg *cfg, int32_t format, int32_t max_len,
                                               int32_t n_groups);
 int mla_recon_decode_shared(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,

@@ -17,15 +17,16 @@ namespace mla {
 // kk][half][head][8]: a matrix operand is 1 KB in one piece there.
 // ABS_F16: fp16 for the decoding over an eight-bit cache, as [b][block of heads][step][half][head][8]: step 2 i + e
 // of half h holds latents 32 i + 16 h + 8 e + 0..7.  32 latents of a head are brought to [2^8, 2^9) by a power of
-// two, whose exponent is written to exps [b][block of heads][head][rkv / 32]; the rotary part stays bf16.
+// two, whose exponent is written to exps [b][block of heads][head][rkv / 32]; the rotary part is written in bf16, as by
+// ABS_FRAG.  ABS_BOTH: ABS_FRAG and ABS_F16.
 constexpr int ABS_LD = 96;  // LDS row stride: 4 rows of a transposing read on distinct banks
 constexpr int ABS_DN = 192;
-enum AbsorbOut { ABS_ROWS, ABS_FRAG, ABS_F16 };
+enum AbsorbOut { ABS_ROWS, ABS_FRAG, ABS_F16, ABS_BOTH };
 constexpr int ABS_MIN_EXP = -126, ABS_MAX_EXP = 120;
 template <AbsorbOut OUT>
 __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const bf16_t* __restrict__ Wuk,
-                                             bf16_t* __restrict__ qabs, int8_t* __restrict__ exps, int B, int H,
-                                             int HP, int hpg, int dn, int dr, int rkv, int bx, int by, int g) {
+                                             bf16_t* __restrict__ qabs, bf16_t* __restrict__ qabs16,
+                                             int8_t* __restrict__ exps, int B, int H, int HP, int hpg, int dn, int dr, int rkv, int bx, int by, int g) {
   __shared__ __attribute__((aligned(16))) bf16_t Ws[ABS_DN * ABS_LD];
   const int c0 = 64 * bx, r0 = 32 * by;
   const int DK = rkv + dr, dq = dn + dr, tid = threadIdx.x;
@@ -85,7 +86,7 @@ __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           lds_operand_tr(Ws, ABS_LD, 32 * wave, 16 * kk + 8 * half, 16 * kk + 8 * half + 4), qf[kk], acc,
           0, 0, 0);
-  if constexpr (OUT == ABS_F16) {
+  if constexpr (OUT == ABS_F16 || OUT == ABS_BOTH) {
     float top = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(acc[e]));
@@ -94,11 +95,12 @@ __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const
     const float down = __uint_as_float((uint32_t)(127 - t) << 23);
     if (rr >= rows) return;
     if (half == 0) exps[qi * (rkv / 32) + i] = (int8_t)t;
+    bf16_t* to = qabs16 + ((int64_t)(rc / hpg) * (HP / 32) + head / 32) * rkv * 32 + head % 32 * 8;
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4)
-      *(u32x2*)(qabs + fi + (2 * i + (e4 & 1)) * 512 + (e4 >> 1) * 256 + 4 * half) =
+      *(u32x2*)(to + (2 * i + (e4 & 1)) * 512 + (e4 >> 1) * 256 + 4 * half) =
           u32x2{pack2h(acc[4 * e4] * down, acc[4 * e4 + 1] * down), pack2h(acc[4 * e4 + 2] * down, acc[4 * e4 + 3] * down)};
-    return;
+    if constexpr (OUT == ABS_F16) return;
   }
   if (rr >= rows) return;
 #pragma unroll

@@ -89,7 +89,7 @@ __global__ __launch_bounds__(128) void absorb_kernel(const bf16_t* __restrict__ 
                                                      const bf16_t* __restrict__ Wuk,
                                                      bf16_t* __restrict__ qabs, int B, int H, int HP,
                                                      int hpg, int dn, int dr, int rkv) {
-  absorb_block<OUT>(q, Wuk, qabs, nullptr, B, H, HP, hpg, dn, dr, rkv, blockIdx.x, blockIdx.y, blockIdx.z);
+  absorb_block<OUT>(q, Wuk, qabs, nullptr, nullptr, B, H, HP, hpg, dn, dr, rkv, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 template <int DK, int DVL>

@@ -1,5 +1,7 @@
 // Absorbed-form decoding over a paged latent cache of either format, for sequences some of which begin
 // with the same rows.
+#include <type_traits>
+
 #include "absorb.h"
 #include "attn_common.h"
 #include "cache_rows.h"
@@ -13,7 +15,7 @@ namespace {
 size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // Attention is that of paged_attn.hip: a block of 32 heads of a sequence (32 queries) is one column block
 // of the matrix products, its state belongs to a wavefront, tiles have 32 rows.  Here the rows of
@@ -25,18 +27,20 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // * shared rows: a group's query blocks in fours ("quads"), for each quad the tiles of the shared rows.
 //   A workgroup takes a run of these items; its four wavefronts have a query block each and one tile in
 //   LDS for all of them, which is then read from memory once for four blocks and once from the
-//   caches for the group's other quads.
+//   caches for the group's other quads.  For large groups the tiles are images that the launch before has
+//   made: in fp16 with a power of two a row, in the order in which LDS holds them.
 //
 // The workgroups are divided between the lists by their tiles.  A tile of one block's own rows and
 // an item of four blocks cost a workgroup about the same: the first waits for its copy (64 sequences of the 8B layer
-// behind 8192 shared rows, 400 of their own: 70 us; with own tiles counted as 3/4, 2/3, 1/2: 71, 76, 87).
+// behind 8192 shared rows, 400 of their own, bf16, without images: 70 us; with own tiles counted as 3/4, 2/3, 1/2:
+// 71, 76, 87; with images 62, as 3/4 70, as 4/3 and 3/2 62).
 //
 // Three launches: the absorbed queries with the plan, the attention, the merge with W_UV.  Measured (whole calls; 5.2 TB/s
 // is a large copy's rate, 1444 TFLOP/s a large bf16 product's):
 //   e4m3, 64 sequences to 4096 rows, 32 heads of 512 + 64   63 us (7.0 + 50 + 8.7; the rows alone 33)
 //   e4m3, 41 ragged ones to 16001                           44    (5.6 + 30 + 10.6; 14)
 //   e4m3, one of 300, 14 heads of 256 + 32                  17    (4.5 + 9.0 + 3.9)
-//   bf16, 64 behind 8192 shared rows                        87    (8.5 + 70 + 16.6; operations alone 26)
+//   bf16, 64 behind 8192 shared rows                        86    (13 + 63 + 16.8; operations alone 26)
 //   e4m3, 45 in 7 groups behind 20000                       89    (8.2 + 72 + 17.5; 23)
 //   bf16, 4 behind 1000, 14 heads                           20    (6.0 + 9.8 + 4.4)
 struct LatentDev {
@@ -48,8 +52,12 @@ struct LatentDev {
   int64_t page_bytes;
   const int32_t* len;
   int max_len, B, H, HB;  // HB: blocks of 32 heads
-  const bf16_t* qabs;     // [B HB][DK / 16][64 lanes][8], bf16 or (e4m3, the latents) fp16
-  const int8_t* qexp;     // e4m3: [B HB][32][DVL / 32], exponents of the queries' powers of two
+  const bf16_t* qabs;     // [B HB][DK / 16][64 lanes][8], bf16; not the latents of an e4m3 cache
+  const bf16_t* qabs16;   // the latents in fp16 (absorb.h; [B HB][DVL / 16][64 lanes][8]): of an e4m3 cache, or for images
+  const int8_t* qexp;     // [B HB][32][DVL / 32], exponents of their powers of two
+  char* images;           // [n_groups][image_tiles] tiles of the shared rows, as LDS holds them, in fp16
+  float* image_powers;    // [n_groups][image_tiles][32]
+  int image_tiles;
   float* part_o;          // [slot][32][DVL], not normalised
   float* part_ml;         // [slot][32][2]: reference (log2), sum
   float sl2;
@@ -278,20 +286,6 @@ __device__ void make_plan(const LatentDev& a, int rkv) {
   }
 }
 
-// The absorbed queries (absorb.h), and one workgroup, the first, for the plan.
-constexpr int PREP_THREADS = 128;
-template <bool E4M3>
-__global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev a, const bf16_t* q, const bf16_t* Wuk,
-                                                                      int hpg, int dn, int dr, int rkv) {
-  if (blockIdx.x == 0) {
-    make_plan<PREP_THREADS>(a, rkv);
-    return;
-  }
-  const int nx = rkv / 64, ny = (a.B * hpg + 31) / 32, k = blockIdx.x - 1;
-  absorb_block<E4M3 ? ABS_F16 : ABS_FRAG>(q, Wuk, (bf16_t*)a.qabs, (int8_t*)a.qexp, a.B, a.H, 32 * a.HB, hpg, dn, dr,
-                                          rkv, k % nx, k / nx % ny, k / nx / ny);
-}
-
 // ---- attention ------------------------------------------------------------------------
 // The products here have no wait for operands: these come from LDS, or were converted a product before
 // (tests/test_latent_waits.py looks at the built code).
@@ -352,46 +346,163 @@ struct LatentTile {
   static constexpr int XOR8 = 16 * (E4M3 ? 4 : 1);  // what 8 rows further do to an offset (WIDE)
 };
 
-// Eight bits.  A latent is its e4m3 value c times its row's power 2^e.  The products take c (exact in fp16): logits are
-// multiplied by 2^e (before the positional part is added), and a row's weight in the weighted latents is
+// The absorbed queries (absorb.h), one workgroup, the first, for the plan, and the images of the shared rows' tiles.
+constexpr int PREP_THREADS = 128;
+// Tile t of group g as LDS holds it (LatentTile of 16 bits), the latents in fp16: what its members with rows all
+// have, read through the first of them (the plan uses as much of it as it finds).  Sixteen lanes a row.  Bound by
+// latency (lengths, page numbers, rows): 8192 rows of 1152 bytes make the launch 13 us, without images 8.5.
+template <int DK, int DVL, bool E4M3>
+__device__ __forceinline__ void image_tile(const LatentDev& a, int g, int t) {
+  using FT = LatentTile<DK, DVL, false>;
+  constexpr int NQ = DVL / 128, RB = LatentTile<DK, DVL, E4M3>::RB;
+  __shared__ int least, first;
+  const int tid = threadIdx.x, l = tid & 15;
+  if (tid == 0) {
+    least = min(max(a.shared_len[g], 0), a.max_len);
+    first = a.B;
+  }
+  __syncthreads();
+  const int lo = max(a.group_off[g], 0), hi = min(a.group_off[g + 1], a.B);
+  for (int b = lo + tid; b < hi; b += PREP_THREADS) {
+    const int n = len_of(a, b);
+    if (n > 0) {
+      atomicMin(&least, n);
+      atomicMin(&first, b);
+    }
+  }
+  __syncthreads();
+  if (first >= a.B || t >= least / PD_KT) return;
+  char* image = a.images + ((int64_t)g * a.image_tiles + t) * FT::BYTES;
+  // (everything is asked for before anything is used: a row after the other took a round trip each)
+  constexpr int ROWS = PD_KT / 8;
+  const char* from[ROWS];
+  bool bad[ROWS];
+  float power[ROWS];
+  u32x4 v[ROWS][NQ], pe[ROWS];
+  int page[ROWS];
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) page[k] = a.table[(int64_t)first * a.max_pages + page_of(a, t * PD_KT + 8 * k + (tid >> 4))];
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    const int p = t * PD_KT + 8 * k + (tid >> 4), row = p - page_of(a, p) * a.page_size;
+    bad[k] = page[k] < 0 || page[k] >= a.n_pages;
+    const char* at = a.pool + (bad[k] ? 0 : page[k]) * a.page_bytes;
+    from[k] = at + (int64_t)row * RB;
+    if constexpr (E4M3) power[k] = *(const float*)(at + (int64_t)a.page_size * RB + 4 * (int64_t)row);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      if constexpr (E4M3) {
+        const u32x2 w = *(const u32x2*)(from[k] + 8 * (16 * q + l));
+        v[k][q] = u32x4{w[0], w[1], 0u, 0u};
+      } else {
+        v[k][q] = *(const u32x4*)(from[k] + 16 * (16 * q + l));
+      }
+    }
+    if (l < (DK - DVL) / 8) pe[k] = *(const u32x4*)(from[k] + (E4M3 ? DVL : 2 * DVL) + 16 * l);
+  }
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    const int r = 8 * k + (tid >> 4);
+    if constexpr (E4M3) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) v[k][q] = __builtin_bit_cast(u32x4, e4m3_to_f16(v[k][q][0], v[k][q][1]));
+    } else {
+      u16x2 top = {0, 0};
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[k][q][e] & 0x7fff7fffu));
+      int m = max((int)top[0], (int)top[1]);
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) m = max(m, __shfl_xor(m, d, 64));
+      const int e2 = min(max((m >> 7) - 141, E4M3_MIN_EXP), E4M3_MAX_EXP);  // (bits 7 .. 14: the exponent)
+      const float down = power_of_two(-e2);
+      power[k] = power_of_two(e2);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[k][q][e] = pack2h(__uint_as_float(v[k][q][e] << 16) * down, __uint_as_float(v[k][q][e] & 0xffff0000u) * down);
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) *(u32x4*)(image + r * FT::RB + 16 * ((16 * q + l) ^ FT::swz(r))) = v[k][q];
+    if (l < (DK - DVL) / 8) *(u32x4*)(image + r * FT::RB + 16 * ((DVL / 8 + l) ^ FT::swz(r))) = pe[k];
+    // (a row on no page: NaN for whoever sees it)
+    if (l == 0) a.image_powers[((int64_t)g * a.image_tiles + t) * PD_KT + r] = bad[k] ? NAN : power[k];
+  }
+}
+// DK 0: no images.
+template <bool E4M3, int DK, int DVL>
+__global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev a, const bf16_t* q, const bf16_t* Wuk,
+                                                                      int hpg, int dn, int dr, int rkv) {
+  if (blockIdx.x == 0) {
+    make_plan<PREP_THREADS>(a, rkv);
+    return;
+  }
+  int k = blockIdx.x - 1;
+  if constexpr (DK > 0) {  // (the images first: they take longer)
+    if (k < a.n_groups * a.image_tiles) {
+      image_tile<DK, DVL, E4M3>(a, k / a.image_tiles, k % a.image_tiles);
+      return;
+    }
+    k -= a.n_groups * a.image_tiles;
+  }
+  const int nx = rkv / 64, ny = (a.B * hpg + 31) / 32;
+  constexpr AbsorbOut OUT = E4M3 ? ABS_F16 : DK == 0 ? ABS_FRAG : ABS_BOTH;
+  absorb_block<OUT>(q, Wuk, (bf16_t*)a.qabs, (bf16_t*)a.qabs16, (int8_t*)a.qexp, a.B, a.H, 32 * a.HB, hpg, dn, dr, rkv,
+                    k % nx, k / nx % ny, k / nx / ny);
+}
+
+// How a tile's latents enter the products.
+// * AS_BF16 (a bf16 cache): as they are, with bf16 queries and the weights as two bf16 operands.
+// * AS_E8 (an e4m3 cache): the e4m3 values, made fp16 as they are read.
+// * AS_F16 (images of shared rows): fp16, made by the launch before of e4m3 values, or of bf16 values divided by a
+//   power of two of the row (its largest to [2^14, 2^15)): exact down to 2^-31 of the row's largest.
+// In the last two a latent is c times its row's power 2^e.  The products take c: logits are multiplied by 2^e
+// (before the positional part is added), and a row's weight in the weighted latents is
 // p 2^e = 2^(x + e - m) with x the logit in log2 units and m the running maximum of x + e over the rows.  So weights
 // are at most 2^(SLACK + BIAS) < 2^16 and fp16 holds them with 11 bits down to 2^-22 of the largest (their
 // rounding is an eighth of bf16's, and one operand does where bf16 takes two).  The sum of the p = 2^(x - m) is in
 // fp32, whose range holds them down to 2^-14 of the largest even beside the largest power, 2^120.
 // Absorbed queries are fp16 too, each head's brought to [2^8, 2^9) by a power of two; the rotary part is bf16
 // and divided by the same power, so that the logit is multiplied by it last.
+enum LatentAs { AS_BF16, AS_E8, AS_F16 };
+template <int V>
+using As = std::integral_constant<int, V>;
 constexpr float E8_SLACK = 7.f, E8_BIAS = 8.f;
 
-// In bf16 the absorbed queries are bf16 (as in the paged decoding): their rounding, 2^-9 of each, is most of the
-// error, 2.8e-3 to 3.3e-3 of the output's norm where the output's own rounding is 1.7e-3, and e4m3 with fp16 queries
-// 1.7e-3 in all.
+// As AS_BF16 the absorbed queries are bf16 (as in the paged decoding): their rounding, 2^-9 of each, is most of the
+// error, 2.7e-3 to 3.3e-3 of the output's norm where the output's own rounding is 1.7e-3; with fp16 queries, as AS_E8
+// and AS_F16, it is 1.7e-3 in all.
 //
 // What bounds it.  Own rows: the stream of the rows (in eight bits 20 KB a wavefront and tile, 3.4 TB/s over the
 // kernel) behind a fixed 9 us (launch, plan, queries, first tile), then the states.  Shared rows: a tile costs a
-// workgroup 3.2 us in bf16, of which its products take about half (100 of 32 cycles a wavefront at the 1.5 to 1.9 GHz that
-// such a loop runs at), the softmax and the copies' addresses run between them, and the reads of four wavefronts keep
-// LDS as busy as S^T's products the matrix cores.  Ahead of that 9 us as above; behind it the states, 64 KB a
-// block and piece (12 us for 56 MB; the merge reads them again, 16 us).
-// Tried for the shared rows and not kept: tiles made fp16 once for all wavefronts, with fp16 queries and one operand for
-// P (68 products for 100): 78 us for 70 in bf16, 71 for 72 in e4m3, LDS being read and written once more a tile;
-// operands read further ahead (PF 7, PV 6 to 8), no change.  (With P V after its own tile's softmax, and pieces that
-// crossed quads: 77.)
-template <int DK, int DVL, bool E4M3, int OCC>
+// workgroup 3.2 us in bf16, of which its products take about half (100 of 32 cycles a wavefront at the 1.5 to 1.9 GHz
+// that such a loop runs at), 2 us of an image (68 products, and no addresses to make); the softmax and the copies
+// run between the products, and the reads of four wavefronts keep LDS as busy as S^T's products the matrix cores.
+// Ahead of that 9 us as above; behind it the states, 64 KB a block and piece (12 us for 56 MB; the merge reads
+// them again, 16 us).
+// Tried for the shared rows and not kept: tiles made fp16 by each workgroup, once for its wavefronts: 78 us for 70 in
+// bf16, 71 for 72 in e4m3, LDS being read and written once more a tile; operands read further ahead (PF 7, PV 6
+// to 8), no change.  (With P V after its own tile's softmax, and pieces that crossed quads, 77.)
+template <int DK, int DVL, bool E4M3, int OCC, bool IMAGES>
 __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(LatentDev a) {
   using TL = LatentTile<DK, DVL, E4M3>;
-  using QT = typename std::conditional<E4M3, f16x8, bf16x8>::type;
+  using FT = LatentTile<DK, DVL, false>;  // of images
+  constexpr int OWN = E4M3 ? AS_E8 : AS_BF16, SHARED = IMAGES ? AS_F16 : OWN;
   constexpr int RB = TL::RB, CHR = TL::CHR, DR = DK - DVL;
   constexpr int NL = DVL / 16, NR = DR / 16, NC = DVL / 32;
-  constexpr int PF = 5, PV = E4M3 ? 5 : 3;  // operand reads in flight ahead of the products of S, and of P V
+  constexpr int PF = 5;  // operand reads in flight ahead of the products of S
   static_assert(DVL % 128 == 0 && DR % 16 == 0, "decode shape");
   // In eight bits a wavefront has two tiles, all of the LDS at 576 values; what is small lies in a second tile: of
   // wavefront 0 (the plan, before the copies) and of the wavefront itself (reference and sum, after its tiles).
   constexpr int NBUF = E4M3 ? 2 : 1, SMALL = NBUF * PD_WAVES * TL::BYTES - (E4M3 ? PD_WAVES * TL::BYTES : 0);
   // (the plan's, the offsets of the shared rows' copies, each wavefront's page table entries and powers of four tiles)
   constexpr int TABLE = 64 + TL::PERIOD * 256 + PD_WAVES * (E4M3 ? 2048 : 1024);
-  __shared__ __attribute__((aligned(1024))) char tiles[NBUF * PD_WAVES * TL::BYTES + (E4M3 ? 0 : 1024 + TABLE)];
-  int* plan_x = (int*)(tiles + SMALL + (E4M3 ? 0 : 1024));  // [PD_WAVES], then plan_at
-  int* plan_at = plan_x + PD_WAVES;
+  constexpr int ALL = NBUF * PD_WAVES * TL::BYTES + (E4M3 ? 0 : 1024 + TABLE);
+  // (images: four tiles, the plan's, each wavefront's powers of four tiles)
+  constexpr int IMAGE_ALL = IMAGES ? 4 * FT::BYTES + 64 + PD_WAVES * 1024 : 0;
+  __shared__ __attribute__((aligned(1024))) char tiles[ALL > IMAGE_ALL ? ALL : IMAGE_ALL];
   auto ml = [&](int w) { return (float*)(tiles + SMALL + w * (E4M3 ? TL::BYTES : 256)); };  // [2][32]
 
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
@@ -400,27 +511,31 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   const int n_s = __builtin_amdgcn_readfirstlane(a.head[1]);
   const bool on_shared = (int)blockIdx.x < n_s;
   const int wg = on_shared ? xcd_remap(blockIdx.x, n_s) : (int)blockIdx.x - n_s;
+  int* plan_x = (int*)(tiles + (IMAGES && on_shared ? 4 * FT::BYTES : SMALL + (E4M3 ? 0 : 1024)));  // [PD_WAVES], then plan_at
+  int* plan_at = plan_x + PD_WAVES;
 
   // ---- what both lists use ----
   // lane offsets in a tile: S^T's operand (chunk 2 i + half of row col, i % 4 = 0..3), V^T's
-  int kb[4];
+  int kb[4], vb[4];
+  auto offsets = [&](auto as) __attribute__((always_inline)) {
+    using T = typename std::conditional<as() == AS_E8, TL, FT>::type;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) kb[j] = col * RB + 16 * ((2 * j + half) ^ TL::swz(col));
-  int vb[4];
-  if constexpr (E4M3) {  // rows 4 half + 0..3, 8 + 4 half + 0..3, latents 16 ((lane / 16) % 2) + 8 (lane % 2) (+ 32 j)
-    const int i = (lane & 15) >> 1, r = 4 * half + (i & 3) + 8 * (i >> 2);
+    for (int j = 0; j < 4; ++j) kb[j] = col * T::RB + 16 * ((2 * j + half) ^ T::swz(col));
+    if constexpr (as() == AS_E8) {  // rows 4 half + 0..3, 8 + 4 half + 0..3, latents 16 ((lane / 16) % 2) + 8 (lane % 2) (+ 32 j)
+      const int i = (lane & 15) >> 1, r = 4 * half + (i & 3) + 8 * (i >> 2);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) vb[j] = r * RB + 16 * ((2 * j + (lane >> 4 & 1)) ^ TL::swz(r)) + 8 * (lane & 1);
-  } else {  // [8 more rows][32 latents further]: rows 4 half + (lane % 16) / 4, latents 16 ((lane / 16) % 2) + 4 (lane % 4)
+      for (int j = 0; j < 4; ++j) vb[j] = r * T::RB + 16 * ((2 * j + (lane >> 4 & 1)) ^ T::swz(r)) + 8 * (lane & 1);
+    } else {  // [8 more rows][32 latents further]: rows 4 half + (lane % 16) / 4, latents 16 ((lane / 16) % 2) + 4 (lane % 4)
 #pragma unroll
-    for (int h8 = 0; h8 < 2; ++h8)
+      for (int h8 = 0; h8 < 2; ++h8)
 #pragma unroll
-      for (int odd = 0; odd < 2; ++odd) {
-        const int r = 8 * h8 + 4 * half + ((lane & 15) >> 2);
-        const int d = 32 * odd + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        vb[2 * h8 + odd] = r * RB + 16 * ((d >> 3) ^ TL::swz(r)) + 2 * (d & 7);
-      }
-  }
+        for (int odd = 0; odd < 2; ++odd) {
+          const int r = 8 * h8 + 4 * half + ((lane & 15) >> 2);
+          const int d = 32 * odd + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          vb[2 * h8 + odd] = r * T::RB + 16 * ((d >> 3) ^ T::swz(r)) + 2 * (d & 7);
+        }
+    }
+  };
   // the row at position p of sequence b (the last of the tile's again past the end, which gets no weight)
   auto entry = [&](int b, int p) { return a.table[(int64_t)b * a.max_pages + page_of(a, p)]; };
   auto address = [&](int p, int page, bool& bad, uint64_t& power) {
@@ -443,19 +558,27 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   };
 
   // ---- a wavefront's state: 32 queries ----
-  QT qf[NL];             // this lane's head as B operand fragments
+  u32x4 qf[NL];          // this lane's head as B operand fragments, bf16 or fp16
   bf16x8 qr[NR];
   float sl2 = a.sl2;     // logits to log2 units (eight bits: times what the fragments were divided by)
   f32x16 acc[NC];
   float m_run, l_run;
   bool any_bad;
-  auto begin = [&](int x) __attribute__((always_inline)) {
+  auto begin = [&](auto as, int x) __attribute__((always_inline)) {
     const bf16_t* src = a.qabs + (int64_t)x * 32 * DK + 8 * lane;
 #pragma unroll
-    for (int s = 0; s < NL; ++s) qf[s] = *(const QT*)(src + 512 * s);
-#pragma unroll
     for (int s = 0; s < NR; ++s) qr[s] = *(const bf16x8*)(src + 512 * (NL + s));
-    if constexpr (E4M3) {  // one power for the head's queries
+    if constexpr (as() == AS_BF16) {
+#pragma unroll
+      for (int s = 0; s < NL; ++s) qf[s] = *(const u32x4*)(src + 512 * s);
+    } else {
+      // stored step 2 i + e of half h has latents 32 i + 16 h + 8 e .., which are what one LDS read of e4m3 values
+      // gives; of fp16 values step k of half h takes latents 16 k + 8 h ..
+      const bf16_t* src16 = a.qabs16 + (int64_t)x * 32 * DVL;
+#pragma unroll
+      for (int s = 0; s < NL; ++s)
+        qf[s] = *(const u32x4*)(as() == AS_E8 ? src16 + 512 * s + 8 * lane : src16 + 512 * (s / 2 * 2 + half) + 256 * (s % 2) + 8 * col);
+      // one power for the head's queries
       const int8_t* e = a.qexp + ((int64_t)x * 32 + col) * NC;
       int t[NC], top = ABS_MIN_EXP;
 #pragma unroll
@@ -482,9 +605,11 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       for (int i = 0; i < NC; ++i) {
         const _Float16 f = (_Float16)power_of_two(min(max(t[i] - top, -30), 15));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          qf[2 * i][k] *= f;
-          qf[2 * i + 1][k] *= f;
+        for (int s = 2 * i; s < 2 * i + 2; ++s) {
+          f16x8 v = __builtin_bit_cast(f16x8, qf[s]);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] *= f;
+          qf[s] = __builtin_bit_cast(u32x4, v);
         }
       }
     }
@@ -496,42 +621,43 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     l_run = 0.f;
     any_bad = false;
   };
-  // S^T of the tile at kt.  Eight bits: the rows' powers are in it; pw takes those of the rows of s
+  // S^T of the tile at kt.  AS_E8, AS_F16: the rows' powers are in it; pw takes those of the rows of s
   // (8 (e / 4) + 4 half + e % 4) from powers(e), the address of four of them, once the tile's last read is asked for.
-  auto logits = [&](const char* kt, f32x16& s, float (&pw)[16], auto powers) __attribute__((always_inline)) {
+  auto logits = [&](auto as, const char* kt, f32x16& s, float (&pw)[16], auto powers) __attribute__((always_inline)) {
+    auto take_powers = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x4 v4 = *powers(e);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) pw[e + k] = v4[k];
+      }
+    };
     auto kread = [&](int i) { return *(const u32x4*)(kt + kb[i % 4] + 128 * (i / 4)); };
     u32x4 raw[PF];  // (pinned: the compiler would read each operand right before its product and wait for it)
 #pragma unroll
     for (int j = 0; j < PF; ++j) raw[j] = kread(j);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (E4M3) {
+    if constexpr (as() == AS_E8) {
       f16x8 k0 = e4m3_to_f16(raw[0][0], raw[0][1]), k1 = e4m3_to_f16(raw[0][2], raw[0][3]);
       asm volatile("" : "+v"(k0));
       operand_written(k1);
 #pragma unroll
       for (int i = 0; i < NL / 2; ++i) {
         const u32x4 v = raw[(i + 1) % PF];
-        if (i == 0) pv_first(s, k0, qf[0]);
-        else pv_next(s, k0, qf[2 * i]);
+        if (i == 0) pv_first(s, k0, __builtin_bit_cast(f16x8, qf[0]));
+        else pv_next(s, k0, __builtin_bit_cast(f16x8, qf[2 * i]));
         if (i + 1 < NL / 2) {
           k0 = e4m3_to_f16(v[0], v[1]);
           operand_written(k0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        pv_next(s, k1, qf[2 * i + 1]);
+        pv_next(s, k1, __builtin_bit_cast(f16x8, qf[2 * i + 1]));
         if (i + 1 < NL / 2) {
           k1 = e4m3_to_f16(v[2], v[3]);
           operand_written(k1);
         }
         if (i + PF < NL / 2 + NR) raw[i % PF] = kread(i + PF);
-        if (i == NL / 2 - 2) {
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const f32x4 v4 = *powers(e);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) pw[e + k] = v4[k];
-          }
-        }
+        if (i == NL / 2 - 2) take_powers();
         __builtin_amdgcn_sched_barrier(0);
       }
       mfma_v_done(s);
@@ -543,12 +669,28 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         pv_next(s, __builtin_bit_cast(bf16x8, raw[(NL / 2 + j) % PF]), qr[j]);
       }
       static_assert(NR <= PF - 1, "the positional part is read before the powers are");
+    } else if constexpr (as() == AS_F16) {
+#pragma unroll
+      for (int kk = 0; kk < NL; ++kk) {
+        const f16x8 k = __builtin_bit_cast(f16x8, raw[kk % PF]);
+        if (kk == 0) pv_first(s, k, __builtin_bit_cast(f16x8, qf[0]));
+        else pv_next(s, k, __builtin_bit_cast(f16x8, qf[kk]));
+        if (kk + PF < NL + NR) raw[kk % PF] = kread(kk + PF);
+        if (kk == NL - 3) take_powers();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mfma_v_done(s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] *= pw[e];
+      operand_written(s);
+#pragma unroll
+      for (int j = 0; j < NR; ++j) pv_next(s, __builtin_bit_cast(bf16x8, raw[(NL + j) % PF]), qr[j]);
     } else {
 #pragma unroll
       for (int kk = 0; kk < NL + NR; ++kk) {
         const bf16x8 k = __builtin_bit_cast(bf16x8, raw[kk % PF]);
-        if (kk == 0) pv_first(s, k, qf[0]);
-        else pv_next(s, k, kk < NL ? qf[kk % NL] : qr[kk - NL < 0 ? 0 : kk - NL]);
+        if (kk == 0) pv_first(s, k, __builtin_bit_cast(bf16x8, qf[0]));
+        else pv_next(s, k, kk < NL ? __builtin_bit_cast(bf16x8, qf[kk % NL]) : qr[kk - NL < 0 ? 0 : kk - NL]);
         if (kk + PF < NL + NR) raw[kk % PF] = kread(kk + PF);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -556,17 +698,16 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     mfma_v_done(s);
   };
   // V^T operand of step j = NC u + c: latents 32 c .., rows 16 u + {4 half.., 8 + 4 half..}
-  auto vread = [&](const char* kt, int j) {
+  auto vread = [&](auto as, const char* kt, int j) {
     const int c = j % NC, u = j / NC;
-    if constexpr (E4M3) {
+    if constexpr (as() == AS_E8) {
       return lds_read_tr8(kt + vb[c % 4] + 128 * (c / 4) + 16 * RB * u);
     } else {
-      const char* p = kt + 16 * RB * u + 128 * (c / 2);
+      const char* p = kt + 16 * FT::RB * u + 128 * (c / 2);
       const u32x2 lo = lds_read_tr4((const bf16_t*)(p + vb[c & 1])), hi = lds_read_tr4((const bf16_t*)(p + vb[2 + (c & 1)]));
-      return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
   };
-  using VT = typename std::conditional<E4M3, u32x2, bf16x8>::type;
   // A tile's weights as matrix operands: fp16, or two bf16 values each (rounded, and what that lost: a rounding of
   // P alone would add as much error as that of the output)
   struct Weights {
@@ -574,29 +715,34 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   };
   // P V of the tile at kt; step(j) is called behind the products of step j.  Operands are read PV steps ahead and
   // converted one.
-  auto weighted = [&](const char* kt, const Weights& w, auto step) __attribute__((always_inline)) {
-    VT vf[PV];
+  auto weighted = [&](auto as, const char* kt, const Weights& w, auto step) __attribute__((always_inline)) {
+    constexpr int PV = as() == AS_E8 ? 5 : 3;
+    decltype(vread(as, kt, 0)) vf[PV];
 #pragma unroll
-    for (int j = 0; j < PV; ++j) vf[j] = vread(kt, j);
+    for (int j = 0; j < PV; ++j) vf[j] = vread(as, kt, j);
     f16x8 v;
-    if constexpr (E4M3) {
+    if constexpr (as() == AS_E8) {
       v = e4m3_to_f16(vf[0][0], vf[0][1]);
       operand_written(v);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < 2 * NC; ++j) {
-      if constexpr (E4M3) {
+      if constexpr (as() == AS_E8) {
         pa_next(acc[j % NC], v, __builtin_bit_cast(f16x8, w.hi[j / NC]));
-        if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
+        if (j + PV < 2 * NC) vf[j % PV] = vread(as, kt, j + PV);
         if (j + 1 < 2 * NC) {
           v = e4m3_to_f16(vf[(j + 1) % PV][0], vf[(j + 1) % PV][1]);
           operand_written(v);
         }
       } else {
-        pa_next(acc[j % NC], vf[j % PV], __builtin_bit_cast(bf16x8, w.hi[j / NC]));
-        pa_next(acc[j % NC], vf[j % PV], __builtin_bit_cast(bf16x8, w.lo[j / NC]));
-        if (j + PV < 2 * NC) vf[j % PV] = vread(kt, j + PV);
+        if constexpr (as() == AS_F16) {
+          pa_next(acc[j % NC], __builtin_bit_cast(f16x8, vf[j % PV]), __builtin_bit_cast(f16x8, w.hi[j / NC]));
+        } else {
+          pa_next(acc[j % NC], __builtin_bit_cast(bf16x8, vf[j % PV]), __builtin_bit_cast(bf16x8, w.hi[j / NC]));
+          pa_next(acc[j % NC], __builtin_bit_cast(bf16x8, vf[j % PV]), __builtin_bit_cast(bf16x8, w.lo[j / NC]));
+        }
+        if (j + PV < 2 * NC) vf[j % PV] = vread(as, kt, j + PV);
       }
       step(j);
       __builtin_amdgcn_sched_barrier(0);
@@ -608,15 +754,15 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   // The softmax of a tile in steps that can be spread over the products of another: the references first (they move only
   // when the tile's maximum exceeds one by more than the slack; returns whether the weighted latents are
   // to be multiplied by corr), then 16 exponentials, then 8 pairs of operands.
-  auto softmax_refs = [&](const f32x16& s, const float (&pw)[16], uint64_t heads, float& corr) __attribute__((always_inline)) {
+  auto softmax_refs = [&](auto as, const f32x16& s, const float (&pw)[16], uint64_t heads, float& corr) __attribute__((always_inline)) {
     float my = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e)  // (a power's exponent from its bits; that of a row never written counts as -80)
-      my = fmaxf(my, E4M3 ? __builtin_fmaf((float)max(__float_as_uint(pw[e]), (uint32_t)(127 + E4M3_MIN_EXP) << 23), 0x1p-23f, s[e] * sl2) : s[e]);
+      my = fmaxf(my, as() != AS_BF16 ? __builtin_fmaf((float)max(__float_as_uint(pw[e]), (uint32_t)(127 + E4M3_MIN_EXP) << 23), 0x1p-23f, s[e] * sl2) : s[e]);
     my = pair_max32(my);
-    if constexpr (E4M3) my -= 127.f;
+    if constexpr (as() != AS_BF16) my -= 127.f;
     else my *= sl2;
-    const bool move = (__ballot(my > m_run + (E4M3 ? E8_SLACK : PD_SLACK)) & heads) != 0;
+    const bool move = (__ballot(my > m_run + (as() != AS_BF16 ? E8_SLACK : PD_SLACK)) & heads) != 0;
     // (no branch: products may be under way)
     const float m_new = move ? fmaxf(m_run, my) : m_run;
     corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
@@ -624,15 +770,15 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     l_run *= corr;
     return move;
   };
-  auto softmax_exp = [&](f32x16& s, const float (&pw)[16], int e) __attribute__((always_inline)) {
-    const float ref = (m_run == -INFINITY ? 0.f : m_run) - (E4M3 ? E8_BIAS : 0.f);
+  auto softmax_exp = [&](auto as, f32x16& s, const float (&pw)[16], int e) __attribute__((always_inline)) {
+    const float ref = (m_run == -INFINITY ? 0.f : m_run) - (as() != AS_BF16 ? E8_BIAS : 0.f);
     s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -ref));
     l_run += s[e];
-    if constexpr (E4M3) s[e] *= pw[e];
+    if constexpr (as() != AS_BF16) s[e] *= pw[e];
   };
-  auto softmax_pack = [&](f32x16& s, int q) __attribute__((always_inline)) {  // (in place: weights() takes them)
+  auto softmax_pack = [&](auto as, f32x16& s, int q) __attribute__((always_inline)) {  // (in place: weights() takes them)
     const float p0 = s[2 * q], p1 = s[2 * q + 1];
-    if constexpr (E4M3) {
+    if constexpr (as() != AS_BF16) {
       s[2 * q] = __uint_as_float(pack2h(p0, p1));
     } else {
       const uint32_t h = pack2bf(p0, p1);
@@ -640,14 +786,14 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       s[2 * q + 1] = __uint_as_float(pack2bf(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u)));
     }
   };
-  auto weights = [&](const f32x16& s) __attribute__((always_inline)) {
+  auto weights = [&](auto as, const f32x16& s) __attribute__((always_inline)) {
     Weights w;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       w.hi[q / 4][q % 4] = __float_as_uint(s[2 * q]);
       w.lo[q / 4][q % 4] = __float_as_uint(s[2 * q + 1]);
     }
-    if constexpr (!E4M3) asm volatile("" : "+v"(w.lo[0]), "+v"(w.lo[1]));
+    if constexpr (as() == AS_BF16) asm volatile("" : "+v"(w.lo[0]), "+v"(w.lo[1]));
     asm volatile("" : "+v"(w.hi[0]));
     operand_written(w.hi[1]);
     return w;
@@ -659,6 +805,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   // One tile at kt, of which `left` rows count; power: of row col (eight bits).  `heads`: the columns with a head.
   // `early` is called when the reads of the first 16 rows (and of all keys) have returned.
   auto tile = [&](char* kt, float power, int left, uint64_t heads, bool first, auto early) __attribute__((always_inline)) {
+    constexpr As<OWN> as;
     f32x16 s;
     float pw[16];
     // (the powers pass through the tile's first positional values, which have been read by then: 16 of them a row)
@@ -667,7 +814,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       const int r = 2 * e + 4 * half;
       return (const f32x4*)(kt + (e >> 3) * RB + DVL + 4 * (r & 15));
     };
-    logits(kt, s, pw, powers);
+    logits(as, kt, s, pw, powers);
     if (left < PD_KT) {  // rows past the end: no weight (a real branch)
       asm volatile("");
 #pragma unroll
@@ -675,13 +822,13 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
         if (8 * (e >> 2) + 4 * half + (e & 3) >= left) s[e] = -INFINITY;
     }
     float corr;
-    if (softmax_refs(s, pw, heads, corr) && !first) rescale(corr);  // (nothing is there yet at the first tile)
+    if (softmax_refs(as, s, pw, heads, corr) && !first) rescale(corr);  // (nothing is there yet at the first tile)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) softmax_exp(s, pw, e);
+    for (int e = 0; e < 16; ++e) softmax_exp(as, s, pw, e);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) softmax_pack(s, q);
-    const Weights w = weights(s);
-    weighted(kt, w, [&](int j) __attribute__((always_inline)) {
+    for (int q = 0; q < 8; ++q) softmax_pack(as, s, q);
+    const Weights w = weights(as, s);
+    weighted(as, kt, w, [&](int j) __attribute__((always_inline)) {
       if (j == NC) {
         mfma_a_done(acc);  // (no branch, where the compiler may move registers, before the products' waits)
         early();
@@ -689,12 +836,12 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     });
   };
   // the reference and sum of the state, as a merge of states takes them
-  auto reference = [&] { return E4M3 ? m_run - E8_BIAS : m_run; };
+  auto reference = [&](auto as) { return as() != AS_BF16 ? m_run - E8_BIAS : m_run; };
   auto sum = [&] {
     return any_bad ? NAN : pair_sum32(l_run);  // (a row on no page)
   };
-  auto store = [&](int64_t slot, bool has_head) __attribute__((always_inline)) {
-    const float l = sum(), m = reference();
+  auto store = [&](auto as, int64_t slot, bool has_head) __attribute__((always_inline)) {
+    const float l = sum(), m = reference(as);
     if (!has_head) return;
     const int64_t row = slot * 32 + col;
     float* po = a.part_o + row * DVL + 4 * half;  // lane (head col, half) holds latents 32 c + 8 g + 4 half + 0..3
@@ -711,9 +858,11 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
 
   if (on_shared) {
     // ---- shared rows: pieces of four query blocks ----
+    constexpr As<SHARED> as;
+    offsets(as);
     // This wavefront's part of a tile's copies: 8 rows (WIDE) or half of 16, its lanes' source offsets in a table in LDS.
     int* table = plan_x + 16;  // row (times 4) << 16 | bytes from its start
-    for (int u = tid; u < 64 * TL::PERIOD; u += 64 * PD_WAVES) {
+    for (int u = tid; !IMAGES && u < 64 * TL::PERIOD; u += 64 * PD_WAVES) {
       const int r = u / CHR, pc = u % CHR;
       table[u] = r << 18 | 16 * (pc ^ TL::swz(r));
     }
@@ -761,96 +910,146 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       const int h0 = 32 * (x % a.HB);
       const uint64_t heads = __ballot(h0 + col < a.H);
       // Tile i: P V while the softmax of the next tile runs between the products.  Copies are asked for three tiles
-      // ahead (four buffers) and the page table's entries two tiles before that, all of it without a register that
-      // the compiler would wait for: a wait names how many operations of the later tiles may be under way.
-      bool bad = false;
-      auto ask = [&](int j) __attribute__((always_inline)) {  // (the last tile's entries again past the end)
-        dma4(a.table + (int64_t)b0 * a.max_pages + page_of(a, min(j, q_hi - 1) * PD_KT + col), ahead_lds + 256 * (j & 3));
-      };
-      auto locate = [&](int j, int page) __attribute__((always_inline)) {  // tile j's rows (the last tile's again past the end)
-        uint64_t power_at = 0;
-        bool out;
-        const uint64_t at = address(min(j, q_hi - 1) * PD_KT + col, page, out, power_at);
-        bad |= out;
-        if constexpr (E4M3) dma4((const void*)(uintptr_t)power_at, ahead_lds + 1024 + 256 * (j & 3));
-        return at;
-      };
-      constexpr int OPS = NJ + (E4M3 ? 2 : 1);  // operations of a tile: its copies, its powers, table entries
-      auto copy = [&](int j, int page) __attribute__((always_inline)) {
-        const uint64_t at = locate(j, page);
-#pragma unroll
-        for (int c = 0; c < NJ; ++c) {
-          Copy k;
-          copy_offset(k, c);
-          copy_row(k, at);
-          copy_issue(k, c, j & 3);
-        }
-      };
-      auto powers_of = [&](int j) { return [=](int e) { return (const f32x4*)(ahead + 256 + 64 * (j & 3) + 2 * e + 4 * half); }; };
-      const int page0 = entry(b0, i * PD_KT + col), page1 = entry(b0, min(i + 1, q_hi - 1) * PD_KT + col),
-                page2 = entry(b0, min(i + 2, q_hi - 1) * PD_KT + col);
-      __syncthreads();  // (the buffers are free)
-      copy(i, page0);
-      begin(x);
-      wait_vm<0>();
-      copy(i + 1, page1);
-      ask(i + 3);
-      copy(i + 2, page2);
-      ask(i + 4);
-      __syncthreads();
-      f32x16 s;
-      float pw[16], corr;
-      logits(tiles + (i & 3) * TL::BYTES, s, pw, powers_of(i));
-      softmax_refs(s, pw, heads, corr);
-      bool move = false;  // (nothing is there yet at the first tile)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) softmax_exp(s, pw, e);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) softmax_pack(s, q);
-      Weights w = weights(s);
-      for (; i + 1 < q_hi; ++i) {
-        pin(acc);
-        wait_vm<OPS>();  // (the tile after the next one's may be under way)
+      // ahead (four buffers; spread(step of P V, tile) does it between the products), without a register that the
+      // compiler would wait for: a wait names how many operations of the later tiles may be under way.
+      auto pipeline = [&](auto ops, auto powers_of, auto before, auto spread) __attribute__((always_inline)) {
+        constexpr int BYTES = IMAGES ? FT::BYTES : TL::BYTES;
+        auto buffer = [&](int j) { return tiles + (j & 3) * BYTES; };
         __syncthreads();
-        int page = ahead[64 * ((i + 3) & 3) + lane];
-        logits(tiles + ((i + 1) & 3) * TL::BYTES, s, pw, powers_of(i + 1));
+        f32x16 s;
+        float pw[16], corr;
+        logits(as, buffer(i), s, pw, powers_of(i));
+        softmax_refs(as, s, pw, heads, corr);
+        bool move = false;  // (nothing is there yet at the first tile)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) softmax_exp(as, s, pw, e);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) softmax_pack(as, s, q);
+        Weights w = weights(as, s);
+        pin(acc);
+        for (; i + 1 < q_hi; ++i) {
+          pin(acc);
+          wait_vm<decltype(ops)::value>();  // (the tile after the next one's may be under way)
+          __syncthreads();
+          before(i + 3);
+          logits(as, buffer(i + 1), s, pw, powers_of(i + 1));
+          if (move) rescale(corr);
+          constexpr int K = 16 / NC;  // exponentials a step
+          weighted(as, buffer(i), w, [&](int j) __attribute__((always_inline)) {
+            if (j == 0) move = softmax_refs(as, s, pw, heads, corr);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+              const int e = (j - 1) * K + k;
+              if (e >= 0 && e < 16) softmax_exp(as, s, pw, e);
+              if (e >= 16 && e < 24) softmax_pack(as, s, e - 16);
+            }
+            spread(j, i + 3);
+          });
+          w = weights(as, s);
+        }
+        pin(acc);
         if (move) rescale(corr);
-        constexpr int ST = 2 * NC, K = 16 / NC;  // steps, exponentials a step
+        weighted(as, buffer(i), w, [](int) {});
+        wait_vm<0>();  // (copies past the end)
+      };
+      constexpr int ST = 2 * NC;  // steps of P V
+      bool bad = false;
+      if constexpr (IMAGES) {
+        // 1 KB after the other, in fours for the wavefronts; the tile's powers for each wavefront
+        constexpr int CH = FT::BYTES / 1024, NI = (CH + PD_WAVES - 1) / PD_WAVES;
+        const uint64_t image = (uint64_t)(uintptr_t)a.images + (uint64_t)g * a.image_tiles * FT::BYTES;
+        const float* powers = a.image_powers + (int64_t)g * a.image_tiles * PD_KT;
+        const float* ring = (const float*)(plan_x + 16) + 256 * wave;
+        const uint32_t ring_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ring);
+        const uint32_t base_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tiles);
+        auto copy = [&](int j, int c) __attribute__((always_inline)) {  // (the last tile's again past the end)
+          const int at = __builtin_amdgcn_readfirstlane(min(j, q_hi - 1)), k = min(PD_WAVES * c + wave, CH - 1);
+          copy_s(image + (uint64_t)at * FT::BYTES + 1024 * k, 16 * lane,
+                 __builtin_amdgcn_readfirstlane(base_lds + (j & 3) * FT::BYTES + 1024 * k));
+        };
+        auto copy_powers = [&](int j) __attribute__((always_inline)) {
+          dma4(powers + min(j, q_hi - 1) * (int64_t)PD_KT + col, __builtin_amdgcn_readfirstlane(ring_lds + 256 * (j & 3)));
+        };
+        auto copy_all = [&](int j) __attribute__((always_inline)) {
+          copy_powers(j);
+#pragma unroll
+          for (int c = 0; c < NI; ++c) copy(j, c);
+        };
+        __syncthreads();  // (the buffers are free)
+        copy_all(i);
+        begin(as, x);
+        wait_vm<0>();
+        copy_all(i + 1);
+        copy_all(i + 2);
+        pipeline(As<NI + 1>(), [&](int j) { return [=](int e) { return (const f32x4*)(ring + 64 * (j & 3) + 2 * e + 4 * half); }; },
+                 [](int) {},
+                 [&](int j, int next) __attribute__((always_inline)) {
+                   if (j == 1) copy_powers(next);
+#pragma unroll
+                   for (int c = 0; c < NI; ++c)
+                     if (j == 1 + c * (ST - 1) / NI) copy(next, c);
+                 });
+      } else {
+        // the page table's entries two tiles before the copies
+        auto ask = [&](int j) __attribute__((always_inline)) {  // (the last tile's entries again past the end)
+          dma4(a.table + (int64_t)b0 * a.max_pages + page_of(a, min(j, q_hi - 1) * PD_KT + col), ahead_lds + 256 * (j & 3));
+        };
+        auto locate = [&](int j, int page) __attribute__((always_inline)) {  // tile j's rows (the last tile's again past the end)
+          uint64_t power_at = 0;
+          bool out;
+          const uint64_t at = address(min(j, q_hi - 1) * PD_KT + col, page, out, power_at);
+          bad |= out;
+          if constexpr (E4M3) dma4((const void*)(uintptr_t)power_at, ahead_lds + 1024 + 256 * (j & 3));
+          return at;
+        };
+        using Ops = As<NJ + (E4M3 ? 2 : 1)>;  // of a tile: its copies, its powers, table entries
+        auto copy = [&](int j, int page) __attribute__((always_inline)) {
+          const uint64_t at = locate(j, page);
+#pragma unroll
+          for (int c = 0; c < NJ; ++c) {
+            Copy k;
+            copy_offset(k, c);
+            copy_row(k, at);
+            copy_issue(k, c, j & 3);
+          }
+        };
+        auto powers_of = [&](int j) { return [=](int e) { return (const f32x4*)(ahead + 256 + 64 * (j & 3) + 2 * e + 4 * half); }; };
+        const int page0 = entry(b0, i * PD_KT + col), page1 = entry(b0, min(i + 1, q_hi - 1) * PD_KT + col),
+                  page2 = entry(b0, min(i + 2, q_hi - 1) * PD_KT + col);
+        __syncthreads();  // (the buffers are free)
+        copy(i, page0);
+        begin(as, x);
+        wait_vm<0>();
+        copy(i + 1, page1);
+        ask(i + 3);
+        copy(i + 2, page2);
+        ask(i + 4);
         Copy c[NJ];
+        int page = 0;
         uint64_t at = 0;
-        weighted(tiles + (i & 3) * TL::BYTES, w, [&](int j) __attribute__((always_inline)) {
-          if (j == 0) move = softmax_refs(s, pw, heads, corr);
+        pipeline(Ops(), powers_of, [&](int next) __attribute__((always_inline)) { page = ahead[64 * (next & 3) + lane]; },
+                 [&](int j, int next) __attribute__((always_inline)) {
+                   if (j == 1) at = locate(next, page);
+                   if (j == 2) ask(next + 2);
 #pragma unroll
-          for (int k = 0; k < K; ++k) {
-            const int e = (j - 1) * K + k;
-            if (e >= 0 && e < 16) softmax_exp(s, pw, e);
-            if (e >= 16 && e < 24) softmax_pack(s, e - 16);
-          }
-          // the tile three ahead is asked for between the products
-          if (j == 1) at = locate(i + 3, page);
-          if (j == 2) ask(i + 5);
-#pragma unroll
-          for (int k = 0; k < NJ; ++k) {
-            // (an LDS read's result is asked for some steps behind it)
-            constexpr int LAG = ST >= 32 ? 3 : 1;
-            const int when = 2 + 2 * LAG + k * (ST - 2 - 2 * LAG) / NJ;
-            if (j == when - 2 * LAG) copy_offset(c[k], k);
-            if (j == when - LAG) copy_row(c[k], at);
-            if (j == when) copy_issue(c[k], k, (i + 3) & 3);
-          }
-        });
-        w = weights(s);
+                   for (int k = 0; k < NJ; ++k) {
+                     // (an LDS read's result is asked for some steps behind it)
+                     constexpr int LAG = ST >= 32 ? 3 : 1;
+                     const int when = 2 + 2 * LAG + k * (ST - 2 - 2 * LAG) / NJ;
+                     if (j == when - 2 * LAG) copy_offset(c[k], k);
+                     if (j == when - LAG) copy_row(c[k], at);
+                     if (j == when) copy_issue(c[k], k, next & 3);
+                   }
+                 });
       }
-      if (move) rescale(corr);
-      weighted(tiles + (i & 3) * TL::BYTES, w, [](int) {});
-      wait_vm<0>();  // (copies past the end)
       any_bad = bad;
-      store((int64_t)4 * piece + wave, wave < nx && h0 + col < a.H);
+      store(as, (int64_t)4 * piece + wave, wave < nx && h0 + col < a.H);
     }
     return;
   }
 
   // ---- own rows: a run of tiles a wavefront ----
+  offsets(As<OWN>());
   const bool in_one = __builtin_amdgcn_readfirstlane(a.head[3]) > 0;
   const int64_t slot0 = (int64_t)4 * a.max_pieces;  // (behind the shared rows')
   int t_lo, t_hi, per;
@@ -974,7 +1173,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     int x2 = x, b2 = b, s2 = s0, n2 = n, seq2 = seq0;  // the block after it
     const int seg_begin = T, h0 = 32 * (x % a.HB);
     const uint64_t heads = __ballot(h0 + col < a.H);  // (columns without a head move no reference)
-    begin(x);  // (a wavefront without tiles, in a joined share, has an empty state)
+    begin(As<OWN>(), x);  // (a wavefront without tiles, in a joined share, has an empty state)
     for (; T < seg_end; ++T) {
       any_bad |= bad;
       const int t = T - seq0, left = n - s0 - t * PD_KT;
@@ -1029,7 +1228,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     }
 
     if (!joined) {  // leaving the block: its state
-      store(slot0 + (int64_t)PD_WAVES * wg + wave + x, h0 + col < a.H);
+      store(As<OWN>(), slot0 + (int64_t)PD_WAVES * wg + wave + x, h0 + col < a.H);
       x = x2;
       b = b2;
       s0 = s2;
@@ -1043,7 +1242,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     // through LDS: every wavefront writes its part, then sums a quarter of it
     constexpr int PH = E4M3 ? 4 : 2, NH = NC / PH;
     static_assert(PD_WAVES * NH * 4096 <= PD_WAVES * TL::BYTES, "a part of every state fits the (first) tiles");
-    const float l = sum(), ref = reference();
+    const float l = sum(), ref = reference(As<OWN>());
     if (half == 0) {
       ml(wave)[col] = ref;
       ml(wave)[32 + col] = l;
@@ -1131,9 +1330,18 @@ struct LatentWhere {
 };
 
 struct SharedLayout {
-  size_t qabs, qexp, part_o, part_ml, plan, bytes;
-  int max_pieces, nwg;
+  size_t qabs, qabs16, qexp, part_o, part_ml, plan, images, image_powers, bytes;
+  int max_pieces, nwg, image_tiles;  // (0: without images)
 };
+// Images of the shared rows' tiles, at most 256 MiB of them, for groups of 16 blocks of heads and more on the
+// average.  Whole calls without and with them, us (groups x sequences, shared rows each; 64 of their own), the 8B
+// layer: bf16 8 x 8, 4096 rows 62 / 67; 1 x 8, 16384 53 / 54; 1 x 16, 4096 51 / 49; 4 x 16, 4096 61 / 62; 1 x 32, 16384 82 / 77;
+// 4 x 32, 4096 93 / 88; 1 x 64, 16384 125 / 113; 1 x 256, 8192 272 / 232; e4m3 8 x 8, 4096 60 / 62; 4 x 16, 4096
+// 60 / 59; 1 x 64, 16384 115 / 103; 1 x 256, 8192 245 / 209; the 0.5B one, 1 x 64, 1024 30 / 32, 16384 74 / 71.
+// The workspace has room for as many tiles as the largest number of such groups has, so that it grows with
+// sequences, rows and groups.
+constexpr int IMAGE_BLOCKS = 16;
+constexpr size_t IMAGE_BYTES = (size_t)256 << 20;
 SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_groups) {
   const size_t HB = (H + 31) / 32, VB = B * HB;
   SharedLayout l;
@@ -1142,12 +1350,18 @@ SharedLayout shared_layout(int B, int H, int DK, int DVL, int max_len, int n_gro
   // a piece a workgroup, or a quad a piece (the plan stays below both)
   l.max_pieces = n_groups == 0 ? 0 : (int)(VB / 4 + n_groups > (size_t)l.nwg ? VB / 4 + n_groups : l.nwg);
   const size_t slots = 4 * ((size_t)l.nwg + l.max_pieces) + VB;
+  const size_t tile = PD_KT * (2 * (size_t)DK + 4), row_tiles = (max_len + (size_t)PD_KT - 1) / PD_KT;
+  const size_t room = n_groups == 0 ? 0 : std::min(IMAGE_BYTES / tile, VB / IMAGE_BLOCKS * row_tiles);
+  l.image_tiles = n_groups > 0 && (size_t)n_groups * IMAGE_BLOCKS <= VB && n_groups * row_tiles <= room ? (int)row_tiles : 0;
   l.qabs = 0;
-  l.qexp = l.qabs + al(VB * 32 * DK * 2);
+  l.qabs16 = l.qabs + al(VB * 32 * DK * 2);
+  l.qexp = l.qabs16 + al(VB * 32 * DVL * 2);
   l.part_o = l.qexp + al(VB * 32 * (DVL / 32));
   l.part_ml = l.part_o + al(slots * 32 * DVL * 4);
   l.plan = l.part_ml + al(slots * 32 * 2 * 4);
-  l.bytes = l.plan + al((8 + 3 * (size_t)B + 2 * (VB + 1) + (GROUP_INTS + 5) * (size_t)n_groups + 1) * 4);
+  l.images = l.plan + al((8 + 3 * (size_t)B + 2 * (VB + 1) + (GROUP_INTS + 5) * (size_t)n_groups + 1) * 4);
+  l.image_powers = l.images + al(room * PD_KT * 2 * DK);
+  l.bytes = l.image_powers + al(room * PD_KT * 4);
   return l;
 }
 
@@ -1175,7 +1389,8 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.div_mul = (uint32_t)((((uint64_t)1 << (31 + a.div_shift)) + d.c.page_size - 1) / d.c.page_size);
   a.page_bytes = p.e4m3 ? E4m3Page(d.c.page_size, d.rkv, d.dr).bytes : (int64_t)d.c.page_size * DK * 2;
   a.len = d.len; a.max_len = d.max_len; a.B = d.B; a.H = d.H; a.HB = HB;
-  a.qabs = (const bf16_t*)(ws + l.qabs); a.qexp = (const int8_t*)(ws + l.qexp); a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
+  a.qabs = (const bf16_t*)(ws + l.qabs); a.qabs16 = (const bf16_t*)(ws + l.qabs16);
+  a.qexp = (const int8_t*)(ws + l.qexp); a.part_o = (float*)(ws + l.part_o); a.part_ml = (float*)(ws + l.part_ml);
   a.sl2 = d.scale * attn::LOG2E; a.nwg = l.nwg;
   a.n_groups = p.n_groups; a.max_pieces = l.max_pieces; a.group_off = p.group_off; a.shared_len = p.shared_len;
   int32_t* at = (int32_t*)(ws + l.plan);
@@ -1187,20 +1402,37 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.wg_off = at; at += VB + 1;
   a.group = at; at += GROUP_INTS * p.n_groups;
   a.scratch = at;
+  a.images = ws + l.images; a.image_powers = (float*)(ws + l.image_powers); a.image_tiles = l.image_tiles;
+  const bool images = l.image_tiles > 0;
   prof_begin(KC_ELEM, s);
-  const int64_t grid = 1 + (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
-  if (p.e4m3)
-    latent_prepare_kernel<true><<<(unsigned)grid, PREP_THREADS, 0, s>>>(a, (const bf16_t*)d.q, (const bf16_t*)d.Wuk, d.hpg, d.dn, d.dr, d.rkv);
-  else
-    latent_prepare_kernel<false><<<(unsigned)grid, PREP_THREADS, 0, s>>>(a, (const bf16_t*)d.q, (const bf16_t*)d.Wuk, d.hpg, d.dn, d.dr, d.rkv);
+  const int64_t grid = 1 + (int64_t)p.n_groups * l.image_tiles + (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
+#define PREP(e_, a_, b_)                                                                                      \
+  latent_prepare_kernel<e_, a_, b_><<<(unsigned)grid, PREP_THREADS, 0, s>>>(a, (const bf16_t*)d.q, (const bf16_t*)d.Wuk, \
+                                                                           d.hpg, d.dn, d.dr, d.rkv)
+  if (!images && p.e4m3) PREP(true, 0, 0);
+  else if (!images) PREP(false, 0, 0);
+#define X(a_, b_, c_)                              \
+  else if (DK == a_ && DVL == b_) {                \
+    if (p.e4m3) PREP(true, a_, b_);                \
+    else PREP(false, a_, b_);                      \
+  }
+  MLA_SHARED_SHAPES(X)
+#undef X
+#undef PREP
   prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dn * d.rkv, (double)d.B * d.H * (d.rkv + d.dr + d.dn + d.dr) * 2,
            KLABEL("latent_prepare_kernel"));
   // algorithmic work at full lengths
   prof_begin(KC_ATTN_FWD, s);
-#define X(a_, b_, c_)                                                                                      \
-  if (DK == a_ && DVL == b_) {                                                                             \
-    if (p.e4m3) latent_decode_kernel<a_, b_, true, c_><<<l.nwg, 64 * PD_WAVES, 0, s>>>(a);                 \
-    else latent_decode_kernel<a_, b_, false, c_><<<l.nwg, 64 * PD_WAVES, 0, s>>>(a);                       \
+#define X(a_, b_, c_)                                                                      \
+  if (DK == a_ && DVL == b_) {                                                             \
+    constexpr int C_ = c_;                                                                 \
+    auto run = [&](auto e, auto i) {                                                       \
+      latent_decode_kernel<a_, b_, e(), C_, i()><<<l.nwg, 64 * PD_WAVES, 0, s>>>(a);       \
+    };                                                                                     \
+    if (p.e4m3 && images) run(std::true_type(), std::true_type());                         \
+    else if (p.e4m3) run(std::true_type(), std::false_type());                             \
+    else if (images) run(std::false_type(), std::true_type());                             \
+    else run(std::false_type(), std::false_type());                                        \
   }
   MLA_SHARED_SHAPES(X)
 #undef X

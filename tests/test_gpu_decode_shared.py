@@ -150,6 +150,79 @@ def test_one_large_group(fmt):
     d.guard()
 
 
+# Groups of 16 blocks of 32 heads and more on the average: the shared rows' tiles are made fp16 by the launch before.
+@FORMATS
+@pytest.mark.parametrize("name,members,shared,ps", [
+    ("tiny", [17], [300], 7), ("05b", [16, 20], [1000, 95], 16), ("05b", [2, 40, 0, 30], [500, 64, 77, 31], 100),
+    ("1b", [40], [129], 24), ("8b", [33], [700], 64)])
+def test_large_groups(name, members, shared, ps, fmt):
+    print(f"[shared] {name} {members} x {shared} page {ps} {'e4m3' if fmt else 'bf16'}", flush=True)
+    lay, lens, off = make(name, fmt, members, shared, [1, 40, 3, 70, 32], ps, seed=ps)
+    q = lay.queries(len(lens))
+    d = Shared(lay, q, lens, max(lens), off, shared, fmt)
+    check_decode(lay, q, lens, d())
+    d.guard()
+
+
+@FORMATS
+def test_large_groups_of_many_heads(fmt):
+    lay, lens, off = make("05b", fmt, [5, 6], [200, 64], [7, 33], 16, seed=21, n_heads=128, s_kv_groups=8, n_kv_groups=8)
+    q = lay.queries(len(lens))
+    check_decode(lay, q, lens, Shared(lay, q, lens, max(lens), off, [200, 64], fmt)())
+
+
+@FORMATS
+def test_large_groups_with_short_members_and_bad_pages(fmt):
+    """Sequences with fewer rows than the group shares, without rows (whose table is not looked at), and a shared
+    row on no page: NaN for its group alone."""
+    lay, lens, off = make("8b", fmt, [20, 20], [200, 128], [1, 30], 16, seed=22)
+    q = lay.queries(40)
+    now = [0, 190, 201, 64, 201] + lens[5:]                     # (of 201, 230, 201, 230, .. rows that there are)
+    lay.table[0] = 10**6
+    lay.d_table.copy_(ints(lay.table))
+    check_decode(lay, q, now, Shared(lay, q, now, 231, off, [200, 128], fmt)())
+    check_decode(lay, q, [0] * 40, Shared(lay, q, [0] * 40, 231, off, [200, 128], fmt)())
+    check_decode(lay, q, now, Shared(lay, q, now, 231, off, [-5, 2**31 - 1], fmt)(), only=set(range(20)))
+    lay.table[20:, 1] = -1
+    lay.d_table.copy_(ints(lay.table))
+    got = Shared(lay, q, now, 231, off, [200, 128], fmt)()
+    check_decode(lay, q, now, got, only=set(range(20)))
+    assert np.isnan(got[20:].float().cpu().numpy()).all()
+
+
+@FORMATS
+def test_large_groups_of_rows_of_very_different_sizes(fmt):
+    """Powers from 2^-30 to 2^30, and rows of zeros, among the shared rows; queries small enough that the logits
+    stay moderate."""
+    lay, lens, off = make("1b", fmt, [18], [160], [5, 40], 16, seed=23)
+    q = lay.queries(18)
+    q[..., :lay.cfg.nope_dim] = bf16(q[..., :lay.cfg.nope_dim] * 2.0 ** -32)
+    for p in range(160):
+        at = lay.table[0, p // 16], p % 16
+        row = bf16(lay.pool[at][:512] * (0.0 if p % 7 == 0 else 2.0 ** lay.rng.integers(-30, 31)))
+        if fmt:
+            lay.edit(*at, row)
+        else:
+            lay.pool[at][:512] = row
+    lay.upload()
+    check_decode(lay, q, lens, Shared(lay, q, lens, max(lens), off, [160], fmt)())
+
+
+@FORMATS
+def test_large_groups_non_finite_rows_stay_in_their_group(fmt):
+    lay, lens, off = make("05b", fmt, [18, 18], [96, 96], [5, 40], 16, seed=24)
+    at = lay.table[0, 2], 3
+    if fmt:
+        lay.edit(*at, np.where(np.arange(256) == 9, np.inf, lay.pool[at][:256]))
+    else:
+        lay.pool[at][9] = np.inf
+    lay.upload()
+    q = lay.queries(36)
+    got = Shared(lay, q, lens, max(lens), off, [96, 96], fmt)()
+    check_decode(lay, q, lens, got, only=set(range(18, 36)))
+    assert np.isnan(got[:18].float().cpu().numpy()).any(axis=(1, 2)).all()
+
+
 @FORMATS
 @pytest.mark.parametrize("n", [1, 3])
 def test_the_longest_sequences(n, fmt):
@@ -210,6 +283,31 @@ def test_large_logits(fmt):
             lay.pool[lay.table[b, p // 16], p % 16, 128 + b] = 8.0 if p == where else 4.0
     lay.upload()
     check_decode(lay, q, lens, Shared(lay, q, lens, 136, off, [96], fmt)())
+
+
+@FORMATS
+def test_large_groups_repeat_their_bits_and_follow_their_arrays_in_a_graph(fmt):
+    import torch
+    lay, lens, off = make("05b", fmt, [20, 16], [160, 96], [30, 1, 65], 32, seed=25)
+    q = lay.queries(36)
+    d = Shared(lay, q, lens, 300, off, [160, 96], fmt)
+    first = d().clone()
+    d.ws.fill_(0x7B)
+    assert torch.equal(d(), first)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        d()
+    for k, (now, o, s) in enumerate(((lens, off, [160, 96]), ([100] * 20 + [90] * 16, off, [100, 90]),
+                                     (lens, [0, 2, 20], [160, 160]), ([0] * 36, off, [160, 96]), (lens, [0, 0, 0], [5, 5]))):
+        d.lens.copy_(ints(now)), d.off.copy_(ints(o)), d.shared.copy_(ints(s))
+        d.o.fill_(3.0)
+        graph.replay()
+        got = d.o.clone()
+        torch.cuda.synchronize()
+        d.o.fill_(5.0)
+        assert torch.equal(d(), got), k
+        check_decode(lay, q, now, got)
 
 
 @FORMATS

@@ -63,13 +63,14 @@ def test_latent_decode_products_are_waited_for(tmp_path):
             for part in re.split(r"^<", text, flags=re.M)[1:]:
                 name, _, body = part.partition(">:")
                 kernels[name] = [l.split("//")[0] for l in body.splitlines() if l.strip()]
-    assert len(kernels) == 6, sorted(kernels)       # each width of rows in each format
+    assert len(kernels) == 12, sorted(kernels)      # each width of rows in each format, with and without images
     for name, lines in kernels.items():
         bad, products = violations(lines)
-        dk, dvl, e4m3 = (int(v) for v in re.search(r"ILi(\d+)ELi(\d+)ELb(\d)E", name).groups())
+        dk, dvl, e4m3, images = (int(v) for v in re.search(r"ILi(\d+)ELi(\d+)ELb(\d)ELi\dELb(\d)E", name).groups())
         print(f"[waits] {name}: {products} products, {len(lines)} instructions")
         # S once for own rows, twice for shared ones (the first tile's stands before the loop); P V likewise (the last
-        # tile's stands behind it)
-        assert products == 3 * (dk // 16 + (dvl // 16 if e4m3 else dvl // 8)) and not bad, (name, products, bad[:5])
+        # tile's stands behind it), with two products a piece where the weights are bf16
+        own, fp16 = dk // 16 + (dvl // 16 if e4m3 else dvl // 8), dk // 16 + dvl // 16
+        assert products == own + 2 * (fp16 if images else own) and not bad, (name, products, bad[:5])
         late = written_late(lines)
         assert not late, (name, late[:5])
