@@ -170,18 +170,19 @@ def worth_sharing(groups, cfg, format: str) -> list[tuple[int, int, int]]:
 
     Whole calls, us apart / shared (groups x sequences, shared rows each; 64 rows of their own).  bf16, the
     8B layer (1152 bytes a row): 1 x 8, 4096 rows 32 / 46; 8 x 8, 4096 73 / 62; 16 x 4, 8192 120 / 85; 8 x 8, 16384
-    202 / 126; 32 x 2, 16384 212 / 226; 2 x 3, 131072 164 / 125; 1 x 64, 2048 50 / 51, 8192 93 / 82; 1 x 128, 4096
-    80 / 96, 16384 222 / 229; 1 x 192, 16384 468 / 307; 1 x 256, 4096 145 / 166, 16384 433 / 474.  The 0.5B one
+    202 / 126; 32 x 2, 16384 212 / 226; 2 x 3, 131072 164 / 125; 1 x 64, 2048 48 / 51, 8192 92 / 75; 1 x 128, 4096
+    78 / 85, 8192 125 / 120; 1 x 192, 16384 454 / 256; 1 x 256, 4096 140 / 145, 16384 419 / 391.  The 0.5B one
     (576 bytes): 8 x 8, 4096 37 / 38; 1 x 64, 4096 34 / 41; 32 x 4, 4096 60 / 52; 8 x 8, 16384 99 / 73.  e4m3 rows,
-    about half as many bytes, gain less: the 8B layer 7 x 6, 20032 109 / 113; 4 x 16, 8192 82 / 79; 8 x 8, 16384
-    127 / 115; the 0.5B one 1 x 64, 8192 50 / 53; 8 x 8, 16384 78 / 76.  With more than 32 heads a row is
-    worked on longer once it is read (64 heads: 8 x 8, 4096 83 / 94; 16 x 3, 8192 120 / 135)."""
+    about half as many bytes, gain less: the 8B layer 7 x 6, 20032 109 / 113; 1 x 32, 16384 70 / 72; 1 x 64, 8192
+    71 / 70, 16384 110 / 103; 1 x 192, 8192 200 / 144; the 0.5B one 1 x 64, 8192 48 / 49; 1 x 128, 16384 128 / 117.
+    With more than 32 heads a row is worked on longer once it is read (64 heads: 8 x 8, 4096 83 / 94; 16 x 3,
+    8192 120 / 135)."""
     if cfg.n_heads > 32:
         return []
-    row, least, spared = cfg.kv_rank + 2 * cfg.rope_dim + 4, 8, 288 << 20
+    row, least, spared = cfg.kv_rank + 2 * cfg.rope_dim + 4, 16, 384 << 20
     if format == "bf16":
         row, least, spared = 2 * (cfg.kv_rank + cfg.rope_dim), 3, 144 << 20
-    groups = [g for g in groups if g[1] >= least and (g[1] <= 64 or g[2] >= 16384)]
+    groups = [g for g in groups if g[1] >= least and (g[1] <= 64 or g[2] >= 8192)]
     return groups if sum((n - 1) * rows for _, n, rows in groups) * row >= spared else []
 
 

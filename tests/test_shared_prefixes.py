@@ -42,11 +42,11 @@ def test_groups_of_a_table(rows, groups):
     ([(0, 2, 1 << 20)], 3, "bf16", []),                       # pairs do not count
     ([(0, 2, 1 << 20), (2, 5, 16384), (9, 5, 16384)], 3, "bf16", [(2, 5, 16384), (9, 5, 16384)]),
     ([(0, 64, 8192)], 3, "bf16", [(0, 64, 8192)]),
-    ([(0, 65, 8192)], 3, "bf16", []),                         # large groups behind few rows
-    ([(0, 200, 16384)], 3, "bf16", [(0, 200, 16384)]),
-    ([(0, 31, 16384)], 3, "e4m3", [(0, 31, 16384)]),          # of 644 bytes
-    ([(0, 28, 16384)], 3, "e4m3", []),
-    ([(0, 7, 1 << 17)], 3, "e4m3", []),
+    ([(0, 65, 8176)], 3, "bf16", []),                         # large groups behind few rows
+    ([(0, 200, 8192)], 3, "bf16", [(0, 200, 8192)]),
+    ([(0, 41, 16384)], 3, "e4m3", [(0, 41, 16384)]),          # of 644 bytes
+    ([(0, 38, 16384)], 3, "e4m3", []),
+    ([(0, 15, 1 << 18)], 3, "e4m3", []),
 ])
 def test_what_is_worth_sharing(groups, name, format, kept):
     cfg = configs.get(name)
