@@ -165,6 +165,19 @@ def test_large_groups(name, members, shared, ps, fmt):
 
 
 @FORMATS
+def test_large_groups_of_too_many_rows_for_a_copy(fmt):
+    """The same groups where max_len allows more shared rows than the workspace has room for."""
+    lay, lens, off = make("tiny", fmt, [17], [300], [1, 40], 64, seed=20)
+    lay.table = np.pad(lay.table, ((0, 0), (0, (1 << 20) // 64)), constant_values=-1)
+    lay.upload()
+    q = lay.queries(17)
+    d = Shared(lay, q, lens, 1 << 20, off, [300], fmt)
+    check_decode(lay, q, lens, d())
+    d.guard()
+    check_decode(lay, q, lens, Shared(lay, q, lens, 1 << 15, off, [300], fmt)())
+
+
+@FORMATS
 def test_large_groups_of_many_heads(fmt):
     lay, lens, off = make("05b", fmt, [5, 6], [200, 64], [7, 33], 16, seed=21, n_heads=128, s_kv_groups=8, n_kv_groups=8)
     q = lay.queries(len(lens))
