@@ -13,6 +13,7 @@ namespace mla {
 // H = 32, r_kv = 512; one round of small workgroups), fp32 accumulation.  Measured with the
 // rotary copy: 64 sequences 26 -> 7.1 us, one sequence 13.6 -> 4.1 us (a vector-ALU product and
 // a copy launch before).
+// Ws: ABS_LDS elements of LDS.
 // ABS_FRAG: qabs in the order in which the paged decoding reads it, [b][block of 32 heads][16-wide step
 // kk][half][head][8]: a matrix operand is 1 KB in one piece there.
 // ABS_F16: fp16 for the decoding over an eight-bit cache, as [b][block of heads][step][half][head][8]: step 2 i + e
@@ -21,13 +22,13 @@ namespace mla {
 // ABS_FRAG.  ABS_BOTH: ABS_FRAG and ABS_F16.
 constexpr int ABS_LD = 96;  // LDS row stride: 4 rows of a transposing read on distinct banks
 constexpr int ABS_DN = 192;
+constexpr int ABS_LDS = ABS_DN * ABS_LD;  // elements of LDS, 16-byte aligned
 enum AbsorbOut { ABS_ROWS, ABS_FRAG, ABS_F16, ABS_BOTH };
 constexpr int ABS_MIN_EXP = -126, ABS_MAX_EXP = 120;
 template <AbsorbOut OUT>
 __device__ __forceinline__ void absorb_block(const bf16_t* __restrict__ q, const bf16_t* __restrict__ Wuk,
                                              bf16_t* __restrict__ qabs, bf16_t* __restrict__ qabs16,
-                                             int8_t* __restrict__ exps, int B, int H, int HP, int hpg, int dn, int dr, int rkv, int bx, int by, int g) {
-  __shared__ __attribute__((aligned(16))) bf16_t Ws[ABS_DN * ABS_LD];
+                                             int8_t* __restrict__ exps, bf16_t* Ws, int B, int H, int HP, int hpg, int dn, int dr, int rkv, int bx, int by, int g) {
   const int c0 = 64 * bx, r0 = 32 * by;
   const int DK = rkv + dr, dq = dn + dr, tid = threadIdx.x;
   const int lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;

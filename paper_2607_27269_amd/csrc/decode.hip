@@ -89,7 +89,8 @@ __global__ __launch_bounds__(128) void absorb_kernel(const bf16_t* __restrict__ 
                                                      const bf16_t* __restrict__ Wuk,
                                                      bf16_t* __restrict__ qabs, int B, int H, int HP,
                                                      int hpg, int dn, int dr, int rkv) {
-  absorb_block<OUT>(q, Wuk, qabs, nullptr, nullptr, B, H, HP, hpg, dn, dr, rkv, blockIdx.x, blockIdx.y, blockIdx.z);
+  __shared__ __attribute__((aligned(16))) bf16_t lds[ABS_LDS];
+  absorb_block<OUT>(q, Wuk, qabs, nullptr, nullptr, lds, B, H, HP, hpg, dn, dr, rkv, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 template <int DK, int DVL>

@@ -40,7 +40,7 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 //   e4m3, 64 sequences to 4096 rows, 32 heads of 512 + 64   63 us (7.0 + 50 + 8.7; the rows alone 33)
 //   e4m3, 41 ragged ones to 16001                           44    (5.6 + 30 + 10.6; 14)
 //   e4m3, one of 300, 14 heads of 256 + 32                  17    (4.5 + 9.0 + 3.9)
-//   bf16, 64 behind 8192 shared rows                        86    (13 + 63 + 16.8; operations alone 26)
+//   bf16, 64 behind 8192 shared rows                        85    (13 + 62 + 16.8; operations alone 26)
 //   e4m3, 45 in 7 groups behind 20000                       89    (8.2 + 72 + 17.5; 23)
 //   bf16, 4 behind 1000, 14 heads                           20    (6.0 + 9.8 + 4.4)
 struct LatentDev {
@@ -145,16 +145,18 @@ __device__ __forceinline__ int agent_load(const int32_t* p) {
 // (from memory each look took its round trip: 5.5 us of this launch for one sequence, 4.4 from LDS; 8.4 and 5.9
 // for a group of four).
 template <int NT>
-__device__ void make_plan(const LatentDev& a, int rkv) {
+__device__ void make_plan(const LatentDev& a, int rkv, int32_t* lds) {
   const int tid = threadIdx.x, G = a.n_groups;
   constexpr int LDS_G = 256, LDS_B = 512;
-  __shared__ int32_t group_lds[5 * LDS_G + 1], seq_lds[3 * LDS_B];
+  static_assert((5 * LDS_G + 1 + 3 * LDS_B) * 4 <= ABS_LDS * 2, "in the LDS of the absorbed queries");
+  int32_t *group_lds = lds, *seq_lds = lds + 5 * LDS_G + 1;
   const bool g_lds = G <= LDS_G, b_lds = a.B <= LDS_B;
   int32_t* tmp = g_lds ? group_lds : a.scratch;
   // per group: the shared rows that all its sequences have, how many have rows, and the first that has; its tiles, its first
   // sequence
   int32_t *group_min = tmp, *group_cnt = tmp + G, *group_seq = tmp + 2 * G, *group_tiles = tmp + 3 * G, *group_off = tmp + 4 * G;
-  int32_t *lens = b_lds ? seq_lds : a.lens, *member = b_lds ? seq_lds + LDS_B : a.member, *start = b_lds ? seq_lds + 2 * LDS_B : a.start;
+  int32_t *lens = b_lds ? seq_lds : a.lens, *member = b_lds ? seq_lds + LDS_B : a.member;
+  int32_t* start = b_lds ? seq_lds + 2 * LDS_B : a.start;
   for (int g = tid; g <= G && G > 0; g += NT) {
     group_off[g] = a.group_off[g];
     if (g == G) break;
@@ -326,9 +328,10 @@ __device__ __forceinline__ void dma4(const void* src, uint32_t lds) {
 }
 
 // A tile in LDS: 32 rows of CHR 16-byte chunks without padding, chunk c of row r at c ^ swz(r)
-// (paged_attn.hip).  S^T reads 16 bytes of 16 consecutive rows, which take different banks; the transposing reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16:
-// 32 bytes of four rows).  In eight bits the rows of those that share banks differ in bits 1 and 3 where two
-// rows span the banks (640 bytes), which go to chunk bits 1 and 2.
+// (paged_attn.hip).  S^T reads 16 bytes of 16 consecutive rows, which take different banks; the transposing
+// reads 16 bytes of rows {0..3, 8..11} (+ 4) at two neighbouring chunks (bf16: 32 bytes of four rows).  In
+// eight bits the rows of those that share banks differ in bits 1 and 3 where two rows span the banks (640
+// bytes), which go to chunk bits 1 and 2.
 template <int DK, int DVL, bool E4M3>
 struct LatentTile {
   static constexpr int RB = E4M3 ? DVL + 2 * (DK - DVL) : 2 * DK;  // bytes of a row
@@ -357,12 +360,12 @@ __device__ __forceinline__ void image_tile(const LatentDev& a, int g, int t) {
   constexpr int NQ = DVL / 128, RB = LatentTile<DK, DVL, E4M3>::RB;
   __shared__ int least, first;
   const int tid = threadIdx.x, l = tid & 15;
+  const int lo = max(a.group_off[g], 0), hi = min(a.group_off[g + 1], a.B), shared = min(max(a.shared_len[g], 0), a.max_len);
   if (tid == 0) {
-    least = min(max(a.shared_len[g], 0), a.max_len);
+    least = shared;
     first = a.B;
   }
   __syncthreads();
-  const int lo = max(a.group_off[g], 0), hi = min(a.group_off[g + 1], a.B);
   for (int b = lo + tid; b < hi; b += PREP_THREADS) {
     const int n = len_of(a, b);
     if (n > 0) {
@@ -435,8 +438,9 @@ __device__ __forceinline__ void image_tile(const LatentDev& a, int g, int t) {
 template <bool E4M3, int DK, int DVL>
 __global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev a, const bf16_t* q, const bf16_t* Wuk,
                                                                       int hpg, int dn, int dr, int rkv) {
+  __shared__ __attribute__((aligned(16))) bf16_t lds[ABS_LDS];
   if (blockIdx.x == 0) {
-    make_plan<PREP_THREADS>(a, rkv);
+    make_plan<PREP_THREADS>(a, rkv, (int32_t*)lds);
     return;
   }
   int k = blockIdx.x - 1;
@@ -449,8 +453,8 @@ __global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev 
   }
   const int nx = rkv / 64, ny = (a.B * hpg + 31) / 32;
   constexpr AbsorbOut OUT = E4M3 ? ABS_F16 : DK == 0 ? ABS_FRAG : ABS_BOTH;
-  absorb_block<OUT>(q, Wuk, (bf16_t*)a.qabs, (bf16_t*)a.qabs16, (int8_t*)a.qexp, a.B, a.H, 32 * a.HB, hpg, dn, dr, rkv,
-                    k % nx, k / nx % ny, k / nx / ny);
+  absorb_block<OUT>(q, Wuk, (bf16_t*)a.qabs, (bf16_t*)a.qabs16, (int8_t*)a.qexp, lds, a.B, a.H, 32 * a.HB, hpg, dn, dr,
+                    rkv, k % nx, k / nx % ny, k / nx / ny);
 }
 
 // How a tile's latents enter the products.
@@ -577,7 +581,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       const bf16_t* src16 = a.qabs16 + (int64_t)x * 32 * DVL;
 #pragma unroll
       for (int s = 0; s < NL; ++s)
-        qf[s] = *(const u32x4*)(as() == AS_E8 ? src16 + 512 * s + 8 * lane : src16 + 512 * (s / 2 * 2 + half) + 256 * (s % 2) + 8 * col);
+        qf[s] = *(const u32x4*)(as() == AS_E8 ? src16 + 512 * s + 8 * lane
+                                              : src16 + 512 * (s / 2 * 2 + half) + 256 * (s % 2) + 8 * col);
       // one power for the head's queries
       const int8_t* e = a.qexp + ((int64_t)x * 32 + col) * NC;
       int t[NC], top = ABS_MIN_EXP;
@@ -758,7 +763,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     float my = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e)  // (a power's exponent from its bits; that of a row never written counts as -80)
-      my = fmaxf(my, as() != AS_BF16 ? __builtin_fmaf((float)max(__float_as_uint(pw[e]), (uint32_t)(127 + E4M3_MIN_EXP) << 23), 0x1p-23f, s[e] * sl2) : s[e]);
+      my = fmaxf(my, as() == AS_BF16 ? s[e]
+                                     : __builtin_fmaf((float)max(__float_as_uint(pw[e]), (uint32_t)(127 + E4M3_MIN_EXP) << 23),
+                                                      0x1p-23f, s[e] * sl2));
     my = pair_max32(my);
     if constexpr (as() != AS_BF16) my -= 127.f;
     else my *= sl2;
@@ -875,7 +882,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       int from;
       uint32_t lo, hi;
     };
-    auto copy_offset = [&](Copy& c, int j) __attribute__((always_inline)) { c.from = (table[64 * copy_of(j) + lane] ^ flip) + (row0 << 18); };
+    auto copy_offset = [&](Copy& c, int j) __attribute__((always_inline)) {
+      c.from = (table[64 * copy_of(j) + lane] ^ flip) + (row0 << 18);
+    };
     auto copy_row = [&](Copy& c, uint64_t at) __attribute__((always_inline)) {
       c.lo = (uint32_t)__builtin_amdgcn_ds_bpermute(c.from >> 16, (int)(uint32_t)at);
       c.hi = (uint32_t)__builtin_amdgcn_ds_bpermute(c.from >> 16, (int)(uint32_t)(at >> 32));
@@ -1383,7 +1392,8 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   LatentDev a;
   a.pool = (const char*)d.c.pool; a.table = d.c.table; a.n_pages = d.c.n_pages; a.page_size = d.c.page_size;
   a.max_pages = d.c.max_pages;
-  // with 2^(shift - 1) < page_size <= 2^shift: 2^(31 + shift) / page_size rounded up, off by less than 1 / page_size in a quotient
+  // with 2^(shift - 1) < page_size <= 2^shift: 2^(31 + shift) / page_size rounded up, off by less than 1 / page_size
+  // in a quotient
   a.div_shift = 0;
   while (((int64_t)1 << a.div_shift) < d.c.page_size) ++a.div_shift;
   a.div_mul = (uint32_t)((((uint64_t)1 << (31 + a.div_shift)) + d.c.page_size - 1) / d.c.page_size);
@@ -1405,7 +1415,8 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   a.images = ws + l.images; a.image_powers = (float*)(ws + l.image_powers); a.image_tiles = l.image_tiles;
   const bool images = l.image_tiles > 0;
   prof_begin(KC_ELEM, s);
-  const int64_t grid = 1 + (int64_t)p.n_groups * l.image_tiles + (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
+  const int64_t grid = 1 + (int64_t)p.n_groups * l.image_tiles +
+                       (int64_t)(d.rkv / 64) * ((d.B * (int64_t)d.hpg + 31) / 32) * (d.H / d.hpg);
 #define PREP(e_, a_, b_)                                                                                      \
   latent_prepare_kernel<e_, a_, b_><<<(unsigned)grid, PREP_THREADS, 0, s>>>(a, (const bf16_t*)d.q, (const bf16_t*)d.Wuk, \
                                                                            d.hpg, d.dn, d.dr, d.rkv)
