@@ -59,6 +59,16 @@ __device__ __forceinline__ void acc_scale(f32x16& v, float f) {
   }
 }
 
+// 2^d, d <= 0, the factor of a state whose reference moves up by -d.  A sum of weights may be as large as 2^126 where its rows'
+// powers of two are small (decode_shared.hip), and what 2^d, which fp32 holds down to 2^-126, makes of it still count:
+// half of d at a time.  (Past d = -252 a sum is below 2^-126, the weighted latents past -126.)
+struct StateFactor {
+  float h;
+  __device__ __forceinline__ explicit StateFactor(float d) : h(__builtin_amdgcn_exp2f(0.5f * d)) {}
+  __device__ __forceinline__ float value() const { return h * h; }
+  __device__ __forceinline__ float sum(float l) const { return l * h * h; }
+};
+
 // 1 KB from a uniform address plus the lanes' offsets to the LDS byte address `lds`
 __device__ __forceinline__ void copy_s(uint64_t sbase, uint32_t voff, uint32_t lds) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
@@ -168,14 +178,15 @@ __global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* _
     float m1 = M;
 #pragma unroll
     for (int u = 0; u < U; ++u) m1 = fmaxf(m1, ml[u][0]);
-    const float ref = m1 == -INFINITY ? 0.f : m1, c = __builtin_amdgcn_exp2f(M - ref);
-    v *= c;
-    L *= c;
+    const float ref = m1 == -INFINITY ? 0.f : m1;
+    const StateFactor c(M - ref);
+    v *= c.value();
+    L = c.sum(L);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const float w = __builtin_amdgcn_exp2f(ml[u][0] - ref);
-      v += x[u] * w;
-      L += ml[u][1] * w;
+      const StateFactor w(ml[u][0] - ref);
+      v += x[u] * w.value();
+      L += w.sum(ml[u][1]);
     }
     M = m1;
   }
@@ -197,9 +208,9 @@ __global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* _
       L = 0.f;
 #pragma unroll
       for (int k = 0; k < NSLOT; ++k) {
-        const float f = __builtin_amdgcn_exp2f(sm[col][k] - ref);
-        v += *(const f32x4*)&red[grp + k][4 * cg] * f;
-        L += sl[col][k] * f;
+        const StateFactor f(sm[col][k] - ref);
+        v += *(const f32x4*)&red[grp + k][4 * cg] * f.value();
+        L += f.sum(sl[col][k]);
       }
     }
     v *= L == 0.f ? 0.f : 1.f / L;  // (NaN stays NaN)

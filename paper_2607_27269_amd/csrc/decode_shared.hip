@@ -467,7 +467,9 @@ __global__ __launch_bounds__(PREP_THREADS) void latent_prepare_kernel(LatentDev 
 // p 2^e = 2^(x + e - m) with x the logit in log2 units and m the running maximum of x + e over the rows.  So weights
 // are at most 2^(SLACK + BIAS) < 2^16 and fp16 holds them with 11 bits down to 2^-22 of the largest (their
 // rounding is an eighth of bf16's, and one operand does where bf16 takes two).  The sum of the p = 2^(x - m) is in
-// fp32, whose range holds them down to 2^-14 of the largest even beside the largest power, 2^120.
+// fp32, whose range holds them down to 2^-14 of the largest even beside the largest power, 2^120, and up to 2^88 each
+// for rows of the smallest, 2^-80.  What a reference that moves multiplies the sum by may be as small as 2^-200 (rows
+// of zeros, then some of 2^120) while the product counts: StateFactor.
 // Absorbed queries are fp16 too, each head's brought to [2^8, 2^9) by a power of two; the rotary part is bf16
 // and divided by the same power, so that the logit is multiplied by it last.
 enum LatentAs { AS_BF16, AS_E8, AS_F16 };
@@ -771,10 +773,16 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     else my *= sl2;
     const bool move = (__ballot(my > m_run + (as() != AS_BF16 ? E8_SLACK : PD_SLACK)) & heads) != 0;
     // (no branch: products may be under way)
-    const float m_new = move ? fmaxf(m_run, my) : m_run;
-    corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+    const float m_new = move ? fmaxf(m_run, my) : m_run, d = m_run - (m_new == -INFINITY ? 0.f : m_new);
+    if constexpr (as() != AS_BF16) {
+      const StateFactor f(d);
+      corr = f.value();
+      l_run = f.sum(l_run);
+    } else {
+      corr = __builtin_amdgcn_exp2f(d);
+      l_run *= corr;
+    }
     m_run = m_new;
-    l_run *= corr;
     return move;
   };
   auto softmax_exp = [&](auto as, f32x16& s, const float (&pw)[16], int e) __attribute__((always_inline)) {
@@ -1270,8 +1278,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
 #pragma unroll
         for (int w = 0; w < PD_WAVES; ++w) {
           const float mw = ml(w)[col];
-          f[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
-          L += ml(w)[32 + col] * f[w];
+          const StateFactor of(mw == -INFINITY ? mw : mw - M);
+          f[w] = of.value();
+          L += of.sum(ml(w)[32 + col]);
         }
       }
 #pragma unroll
