@@ -422,7 +422,9 @@ int mla_recon_cache_read(const mla_recon_cfg *cfg, const mla_paged_cache *cache,
 /* mla_recon_decode_paged and mla_recon_prefill_paged over a cache of format MLA_CACHE_E4M3: the same
  * arguments and rules, with workspaces of their own sizes; decoding takes batch ceil(n_heads / 32) max_len up
  * to 2^35.  (Beside rows with latents of 2^118 and more, softmax weights below 2^-14 of the largest may
- * be lost.) */
+ * be lost.  Absorbed queries are fp16 with powers of two: what is below 2^-24 of a head's largest counts as zero, as
+ * do those of a head that are all below 2^-104; a head with some above and all below 2^-88 has positional logits up to
+ * 2^31, before the scale.) */
 size_t mla_recon_decode_e4m3_workspace_size(const mla_recon_cfg *cfg, int32_t max_len);
 int mla_recon_decode_e4m3(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
                           int32_t max_len, const int32_t *lengths, const void *Wuk, const void *Wuv,

@@ -597,7 +597,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
           top = max(top, t[i + k]);
         }
       }
-      top = min(max(top, -64), 100);  // (the positional part is divided by it)
+      // the positional part is divided by it: logits of that part alone hold up to 2^31 beside small absorbed queries,
+      // and beside none (or all below 2^-104, which count as zeros) up to fp32's range
+      top = top < -112 ? 0 : max(top, -96);
       sl2 = a.sl2 * power_of_two(top);
       const float down = power_of_two(-top);
 #pragma unroll
@@ -610,7 +612,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       }
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const _Float16 f = (_Float16)power_of_two(min(max(t[i] - top, -30), 15));
+        const _Float16 f = (_Float16)power_of_two(min(max(t[i] - top, -30), 0));  // (below 2^-24: zero)
 #pragma unroll
         for (int s = 2 * i; s < 2 * i + 2; ++s) {
           f16x8 v = __builtin_bit_cast(f16x8, qf[s]);
@@ -760,14 +762,19 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   };
   // The softmax of a tile in steps that can be spread over the products of another: the references first (they move only
   // when the tile's maximum exceeds one by more than the slack; returns whether the weighted latents are
-  // to be multiplied by corr), then 16 exponentials, then 8 pairs of operands.
-  auto softmax_refs = [&](auto as, const f32x16& s, const float (&pw)[16], uint64_t heads, float& corr) __attribute__((always_inline)) {
+  // to be multiplied by corr), then 16 exponentials, then 8 pairs of operands.  With powers a weight must stay below
+  // 2^16, so that logits are rounded to log2 units once: a fused product, not rounded, may exceed a large maximum's
+  // rounded one by 2^7 and more.
+  auto softmax_refs = [&](auto as, f32x16& s, const float (&pw)[16], uint64_t heads, float& corr) __attribute__((always_inline)) {
+#pragma clang fp contract(off)
     float my = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)  // (a power's exponent from its bits; that of a row never written counts as -80)
+    for (int e = 0; e < 16; ++e) {  // (a power's exponent from its bits; that of a row never written counts as -80)
+      if constexpr (as() != AS_BF16) s[e] *= sl2;
       my = fmaxf(my, as() == AS_BF16 ? s[e]
                                      : __builtin_fmaf((float)max(__float_as_uint(pw[e]), (uint32_t)(127 + E4M3_MIN_EXP) << 23),
-                                                      0x1p-23f, s[e] * sl2));
+                                                      0x1p-23f, s[e]));
+    }
     my = pair_max32(my);
     if constexpr (as() != AS_BF16) my -= 127.f;
     else my *= sl2;
@@ -787,7 +794,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   };
   auto softmax_exp = [&](auto as, f32x16& s, const float (&pw)[16], int e) __attribute__((always_inline)) {
     const float ref = (m_run == -INFINITY ? 0.f : m_run) - (as() != AS_BF16 ? E8_BIAS : 0.f);
-    s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -ref));
+    s[e] = __builtin_amdgcn_exp2f(as() == AS_BF16 ? __builtin_fmaf(s[e], sl2, -ref) : s[e] - ref);
     l_run += s[e];
     if constexpr (as() != AS_BF16) s[e] *= pw[e];
   };
