@@ -11,6 +11,11 @@ constexpr int PD_KT = 32;         // rows per tile
 constexpr int PD_WAVES = 4;
 constexpr float PD_SLACK = 8.f;   // log2 units the running reference maximum may lag
 constexpr int PD_CUS = 256;
+// Tiles that a wavefront sums before its state is put down and the next begins.  An fp32 sum of n values of one size is off by
+// up to n 2^-25 of itself, in one direction where they are equal: of 4096 tiles 2^-12 (a weighted latent, two additions
+// a tile) and 2^-13 (the weights, first a tile's).  (Of one sequence of 2^31 - 1 rows alike, 65536 tiles a wavefront and each
+// weight added by itself, 0.7 %; of three behind as many shared rows 5 %.)  States are joined up to a thousand times: 2^-15 more.
+constexpr int PD_RUN = 4096;
 
 __device__ __forceinline__ int tiles_of(int n) { return (int)(((uint32_t)n + PD_KT - 1) / PD_KT); }  // (n up to 2^31 - 1)
 // The list's cut: tiles per workgroup (at least one for each wavefront), and the part of
@@ -59,6 +64,19 @@ __device__ __forceinline__ void acc_scale(f32x16& v, float f) {
   }
 }
 
+// elements 4 g .. of accumulation registers, which stay where they are
+__device__ __forceinline__ f32x4 acc_read4(const f32x16& v, int g) {
+  f32x4 o;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float x = v[4 * g + k];
+    float t;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(t) : "a"(x));
+    o[k] = t;
+  }
+  return o;
+}
+
 // 2^d, d <= 0, the factor of a state whose reference moves up by -d.  A sum of weights may be as large as 2^126 where its rows'
 // powers of two are small (decode_shared.hip), and what 2^d, which fp32 holds down to 2^-126, makes of it still count:
 // half of d at a time.  (Past d = -252 a sum is below 2^-126, the weighted latents past -126.)
@@ -85,10 +103,10 @@ __device__ __forceinline__ void copy_s(uint64_t sbase, uint32_t voff, uint32_t l
 constexpr int PF_THREADS = 1024;
 
 // Where the states of the sequence with tiles [t0, t1) are: n of them, the first n0 in the slots
-// of its first workgroup (one if that is joined), one for each workgroup inside, the last in those
-// of its last workgroup.
+// of its first workgroup (one if that is joined), one for each workgroup inside (or one for each of its
+// wavefronts, if their shares are longer than PD_RUN), the last in those of its last workgroup.
 struct States {
-  int n = 0, n0 = 0, mid = 0, at0 = 0, at_mid = 0, at1 = 0;
+  int n = 0, n0 = 0, mid = 0, step = PD_WAVES, at0 = 0, at_mid = 0, at1 = 0;
   States() = default;
   __device__ __forceinline__ States(const ListCut& cut, int b, int t0, int t1) {
     if (t1 <= t0) return;
@@ -99,6 +117,10 @@ struct States {
     n = n0;
     if (w1 > w0) {
       mid = w1 - w0 - 1;
+      if (cut.per_wave(w0 + 1) > PD_RUN && mid > 0) {
+        mid *= PD_WAVES;
+        step = 1;
+      }
       at_mid = PD_WAVES * (w0 + 1) + b;
       n += mid + part(cut, w1, t0, t1, v);
       at1 = PD_WAVES * w1 + v + b;
@@ -107,14 +129,14 @@ struct States {
   __device__ __forceinline__ static int part(const ListCut& cut, int w, int t0, int t1, int& v) {
     const int lo = cut.lo(w), hi = cut.hi(w), per = cut.per_wave(w);
     v = 0;
-    if (t0 <= lo && hi <= t1) return 1;  // joined
+    if (t0 <= lo && hi <= t1 && per <= PD_RUN) return 1;  // joined
     v = (max(t0, lo) - lo) / per;
     return (min(t1, hi) - 1 - lo) / per - v + 1;
   }
   __device__ __forceinline__ int slot(int k) const {
     if (k < n0) return at0 + k;
     k -= n0;
-    if (k < mid) return at_mid + PD_WAVES * k;
+    if (k < mid) return at_mid + step * k;
     return at1 + k - mid;
   }
 };

@@ -23,12 +23,14 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 //
 // * own rows: the tiles of all query blocks behind what they share.  A wavefront works on a run of tiles of its
 //   own; the four of a workgroup are in the same block's rows and join their states, or, where there are too many
-//   blocks for that, the list is cut into equal runs as in paged_attn.hip;
+//   blocks or tiles for that, the list is cut into equal runs as in paged_attn.hip;
 // * shared rows: a group's query blocks in fours ("quads"), for each quad the tiles of the shared rows.
 //   A workgroup takes a run of these items; its four wavefronts have a query block each and one tile in
 //   LDS for all of them, which is then read from memory once for four blocks and once from the
 //   caches for the group's other quads.  For large groups the tiles are images that the launch before has
 //   made: in fp16 with a power of two a row, in the order in which LDS holds them.
+//
+// Behind PD_RUN tiles of a run or a piece the state is put down, joined to that in its slot, and the next begins at zero.
 //
 // The workgroups are divided between the lists by their tiles.  A tile of one block's own rows and
 // an item of four blocks cost a workgroup about the same: the first waits for its copy (64 sequences of the 8B layer
@@ -233,7 +235,7 @@ __device__ void make_plan(const LatentDev& a, int rkv, int32_t* lds) {
   scan_before<NT>(wanted, sums);
 #pragma unroll
   for (int k = TRIES - 1; k >= 0; --k)
-    if (sums[k] <= n_p) {
+    if (sums[k] <= n_p && tried(k) <= PD_RUN) {  // (longer runs take equal shares, and put states down on their way)
       per_wave = tried(k);
       wgs = wanted[k];
     }
@@ -568,7 +570,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   bf16x8 qr[NR];
   float sl2 = a.sl2;     // logits to log2 units (eight bits: times what the fragments were divided by)
   f32x16 acc[NC];
-  float m_run, l_run;
+  float m_run, l_run, l_tile;  // (l_tile: the sum of a tile's weights, in order of e)
   bool any_bad;
   auto begin = [&](auto as, int x) __attribute__((always_inline)) {
     const bf16_t* src = a.qabs + (int64_t)x * 32 * DK + 8 * lane;
@@ -795,7 +797,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   auto softmax_exp = [&](auto as, f32x16& s, const float (&pw)[16], int e) __attribute__((always_inline)) {
     const float ref = (m_run == -INFINITY ? 0.f : m_run) - (as() != AS_BF16 ? E8_BIAS : 0.f);
     s[e] = __builtin_amdgcn_exp2f(as() == AS_BF16 ? __builtin_fmaf(s[e], sl2, -ref) : s[e] - ref);
-    l_run += s[e];
+    l_tile = e == 0 ? s[0] : l_tile + s[e];
+    if (e == 15) l_run += l_tile;
     if constexpr (as() != AS_BF16) s[e] *= pw[e];
   };
   auto softmax_pack = [&](auto as, f32x16& s, int q) __attribute__((always_inline)) {  // (in place: weights() takes them)
@@ -862,16 +865,33 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   auto sum = [&] {
     return any_bad ? NAN : pair_sum32(l_run);  // (a row on no page)
   };
-  auto store = [&](auto as, int64_t slot, bool has_head) __attribute__((always_inline)) {
-    const float l = sum(), m = reference(as);
+  // first: whether the slot has no state yet; else this one is joined to it
+  auto store = [&](auto as, int64_t slot, bool has_head, bool first) __attribute__((always_inline)) {
+    float l = sum(), m = reference(as);
     if (!has_head) return;
     const int64_t row = slot * 32 + col;
     float* po = a.part_o + row * DVL + 4 * half;  // lane (head col, half) holds latents 32 c + 8 g + 4 half + 0..3
+    if (first) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(f32x4*)(po + 32 * c + 8 * g) = f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+        for (int g = 0; g < 4; ++g)
+          *(f32x4*)(po + 32 * c + 8 * g) = f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+    } else {
+      const float m0 = a.part_ml[2 * row], l0 = a.part_ml[2 * row + 1], top = fmaxf(m, m0), ref = top == -INFINITY ? 0.f : top;
+      const StateFactor f(m - ref), f0(m0 - ref);
+      l = f.sum(l) + f0.sum(l0);
+      m = top;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4* at = (f32x4*)(po + 32 * c + 8 * g);
+          *at = acc_read4(acc[c], g) * f.value() + *at * f0.value();  // (or the compiler moves and spills accumulators)
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     if (half == 0) {
       a.part_ml[2 * row] = m;
       a.part_ml[2 * row + 1] = l;
@@ -912,7 +932,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     const int* ahead = table + 64 * TL::PERIOD + wave * (E4M3 ? 512 : 256);
     const uint32_t ahead_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ahead);
     const int pieces = __builtin_amdgcn_readfirstlane(a.head[0]);
-    for (int piece = wg; piece < pieces; piece += n_s) {
+    for (int piece = wg, done = 0; piece < pieces;) {  // (done: tiles of the piece that are behind a state)
       if (tid == 0) plan_x[0] = -1;
       __syncthreads();
       for (int g = tid; g < a.n_groups; g += 64 * PD_WAVES) {
@@ -921,14 +941,17 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       }
       __syncthreads();
       const int g = __builtin_amdgcn_readfirstlane(plan_x[0]);
-      if (g < 0) continue;
+      if (g < 0) {
+        piece += n_s;
+        continue;
+      }
       const int32_t* d = a.group + GROUP_INTS * g;
       const int quads = __builtin_amdgcn_readfirstlane(d[G_QUADS]), of = __builtin_amdgcn_readfirstlane(d[G_PIECES]);
       const int nt = __builtin_amdgcn_readfirstlane(d[G_TILES]), k = piece - __builtin_amdgcn_readfirstlane(d[G_FIRST]);
       const int q = k % quads, pp = k / quads;
       const int x0 = __builtin_amdgcn_readfirstlane(d[G_X0]) + 4 * q, nx = min(__builtin_amdgcn_readfirstlane(d[G_BLOCKS]) - 4 * q, 4);
-      const int q_hi = (int)((int64_t)nt * (pp + 1) / of);
-      int i = (int)((int64_t)nt * pp / of);
+      int i = (int)((int64_t)nt * pp / of) + done;
+      const int i_hi = (int)((int64_t)nt * (pp + 1) / of), q_hi = min(i + PD_RUN, i_hi);
       // (a wavefront without a block works on the last one's, and stores nothing)
       const int b0 = __builtin_amdgcn_readfirstlane(d[G_SEQ]), x = x0 + min(wave, nx - 1);
       const int h0 = 32 * (x % a.HB);
@@ -1067,7 +1090,12 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
                  });
       }
       any_bad = bad;
-      store(as, (int64_t)4 * piece + wave, wave < nx && h0 + col < a.H);
+      store(as, (int64_t)4 * piece + wave, wave < nx && h0 + col < a.H, done == 0);
+      done += PD_RUN;
+      if (q_hi == i_hi) {
+        piece += n_s;
+        done = 0;
+      }
     }
     return;
   }
@@ -1130,7 +1158,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
   }
   // whether the share lies in one block's rows (the same in every wavefront)
   const int x_first = __builtin_amdgcn_readfirstlane(plan_x[0]);
-  const bool joined = t_hi <= __builtin_amdgcn_readfirstlane(a.tile_off[x_first + 1]);
+  const bool joined = per <= PD_RUN && t_hi <= __builtin_amdgcn_readfirstlane(a.tile_off[x_first + 1]);
 
   char* kt = tiles + wave * TL::BYTES;
   const uint32_t kt_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)kt);
@@ -1192,8 +1220,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     return;
   }
 
-  do {  // a block's part of the run
-    const int seg_end = min(T_end, seq0 + nt);
+  do {  // a block's part of the run, PD_RUN tiles of it at most
+    const int block_end = seq0 + nt, seg_end = min(min(T_end, block_end), T + PD_RUN);
     int x2 = x, b2 = b, s2 = s0, n2 = n, seq2 = seq0;  // the block after it
     const int seg_begin = T, h0 = 32 * (x % a.HB);
     const uint64_t heads = __ballot(h0 + col < a.H);  // (columns without a head move no reference)
@@ -1205,7 +1233,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
       int page = 0, p2 = 0;
       const bool more = T + 1 < T_end;
       if (more) {
-        if (T + 1 == seg_end) {
+        if (T + 1 == block_end) {
           seq2 += nt;
           do sequence(++x2, b2, s2, n2);
           while (n2 - s2 == 0);
@@ -1252,7 +1280,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     }
 
     if (!joined) {  // leaving the block: its state
-      store(As<OWN>(), slot0 + (int64_t)PD_WAVES * wg + wave + x, h0 + col < a.H);
+      store(As<OWN>(), slot0 + (int64_t)PD_WAVES * wg + wave + x, h0 + col < a.H, seg_begin == max(seq0, t_first));
       x = x2;
       b = b2;
       s0 = s2;

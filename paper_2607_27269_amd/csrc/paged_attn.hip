@@ -28,7 +28,8 @@ size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 // * Where a wavefront leaves a sequence it stores the state to slot (wavefront + sequence), which
 //   nobody else has: along the list one of the two grows from state to state.  Where the whole
 //   share lies in one sequence the four states are joined through LDS first and only one is stored
-//   (with long sequences a quarter of the traffic).
+//   (with long sequences a quarter of the traffic).  Behind every PD_RUN tiles of a sequence the state is put
+//   down too, joined to that in the slot, and the next begins at zero.
 // * S^T = K Q^T has the row in the MFMA row and the head in its column, so a lane owns one head's
 //   state, and the accumulator of S^T is, after the exponential, the B operand of O^T = V^T P^T
 //   (the order of the rows inside a K step is the same on both sides).  V^T comes from the same
@@ -141,7 +142,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
   __syncthreads();
   if (t_lo >= t_hi) return;
 
-  int T = t_lo + wave * per;                       // this wavefront's run: tiles [T, T_end)
+  const int t_first = t_lo + wave * per;
+  int T = t_first;                                 // this wavefront's run: tiles [T, T_end)
   const int T_end = min(T + per, t_hi);
   int b = 0, seq0 = 0, n = 0, nt = 0;              // the current sequence: first tile, rows, tiles
   if (T < T_end) {
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
   }
   // whether the share lies in one sequence (the same in every wavefront)
   const int b_first = __builtin_amdgcn_readfirstlane(plan_b[0]);
-  const bool joined = t_hi <= __builtin_amdgcn_readfirstlane(plan_at[0]) + tiles_of(__builtin_amdgcn_readfirstlane(decode_len(a, b_first)));
+  const bool joined = per <= PD_RUN && t_hi <= __builtin_amdgcn_readfirstlane(plan_at[0]) + tiles_of(__builtin_amdgcn_readfirstlane(decode_len(a, b_first)));
 
   const uint64_t heads = __ballot(h0 + col < a.H);  // (columns without a head move no reference)
   bf16_t* kt = tiles[wave];
@@ -244,8 +246,8 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
   if (T < T_end) issue_rows(address(T - seq0, n, entry(b, T - seq0, n), bad));
   else if (!joined) return;
 
-  do {  // a sequence's part of the run
-    const int seg_end = min(T_end, seq0 + nt);
+  do {  // a sequence's part of the run, PD_RUN tiles of it at most
+    const int seq_end = seq0 + nt, seg_end = min(min(T_end, seq_end), T + PD_RUN);
     int b2 = b, n2 = n, seq2 = seq0;  // the sequence after it
     const int seg_begin = T;
     any_bad = false;
@@ -263,7 +265,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
       // the tile after this one: the next of the sequence, or the first of the next that has rows
       int page = 0;
       if (T + 1 < T_end) {
-        if (T + 1 == seg_end) {
+        if (T + 1 == seq_end) {
           seq2 += nt;
           do n2 = __builtin_amdgcn_readfirstlane(decode_len(a, ++b2));
           while (n2 == 0);
@@ -324,6 +326,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
       // P as two bf16 operands, rounded and what that lost: a rounding of P alone would add as much
       // error as that of the output, and the second products hide behind the copies
       bf16x8 pf[2], pl[2];
+      float l_tile = 0.f;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         u32x4 w, w2;
@@ -331,13 +334,14 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
         for (int q = 0; q < 4; ++q) {
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q], a.sl2, -m_use));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * u + 2 * q + 1], a.sl2, -m_use));
-          l_run += p0 + p1;
+          l_tile += p0 + p1;
           w[q] = pack2bf(p0, p1);
           w2[q] = pack2bf(p0 - __uint_as_float(w[q] << 16), p1 - __uint_as_float(w[q] & 0xffff0000u));
         }
         pf[u] = __builtin_bit_cast(bf16x8, w);
         pl[u] = __builtin_bit_cast(bf16x8, w2);
       }
+      l_run += l_tile;
       __builtin_amdgcn_sched_barrier(0);
       // the next tile's first 16 rows are asked for as soon as those of this one have been read (LDS
       // reads return in order: that of step NC is there), the others behind the last read
@@ -368,18 +372,34 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
       }
     }
 
-    if (!joined) {  // leaving the sequence: its state
-      const float l = any_bad ? NAN : pair_sum32(l_run);  // (a row on no page)
+    if (!joined) {  // leaving the sequence, or PD_RUN tiles of it behind: its state
+      float l = any_bad ? NAN : pair_sum32(l_run);  // (a row on no page)
       if (h0 + col < a.H) {
         const int64_t row = ((int64_t)PD_WAVES * wg + wave + b) * a.HP + h0 + col;
         // lane (head col, half) holds latents 32 c + 8 g + 4 half + 0..3
         float* po = a.part_o + row * DVL + 4 * half;
+        if (seg_begin == max(seq0, t_first)) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+          for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *(f32x4*)(po + 32 * c + 8 * g) =
-                f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+            for (int g = 0; g < 4; ++g)
+              *(f32x4*)(po + 32 * c + 8 * g) =
+                  f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+        } else {  // joined to the one that is there
+          const float m0 = a.part_ml[2 * row], l0 = a.part_ml[2 * row + 1], top = fmaxf(m_run, m0), ref = top == -INFINITY ? 0.f : top;
+          const StateFactor f(m_run - ref), f0(m0 - ref);
+          l = f.sum(l) + f0.sum(l0);
+          m_run = top;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              f32x4* at = (f32x4*)(po + 32 * c + 8 * g);
+              *at = acc_read4(acc[c], g) * f.value() + *at * f0.value();
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
         if (half == 0) {
           a.part_ml[2 * row] = m_run;
           a.part_ml[2 * row + 1] = l;
