@@ -79,12 +79,13 @@ __device__ __forceinline__ f32x4 acc_read4(const f32x16& v, int g) {
 
 // 2^d, d <= 0, the factor of a state whose reference moves up by -d.  A sum of weights may be as large as 2^126 where its rows'
 // powers of two are small (decode_shared.hip), and what 2^d, which fp32 holds down to 2^-126, makes of it still count:
-// half of d at a time.  (Past d = -252 a sum is below 2^-126, the weighted latents past -126.)
+// half of d at a time.  (Past d = -252 a sum is below 2^-126, the weighted latents past -126.)  POWERS: whether there are such.
+template <bool POWERS>
 struct StateFactor {
-  float h;
-  __device__ __forceinline__ explicit StateFactor(float d) : h(__builtin_amdgcn_exp2f(0.5f * d)) {}
-  __device__ __forceinline__ float value() const { return h * h; }
-  __device__ __forceinline__ float sum(float l) const { return l * h * h; }
+  float f;
+  __device__ __forceinline__ explicit StateFactor(float d) : f(__builtin_amdgcn_exp2f(POWERS ? 0.5f * d : d)) {}
+  __device__ __forceinline__ float value() const { return POWERS ? f * f : f; }
+  __device__ __forceinline__ float sum(float l) const { return POWERS ? l * f * f : l * f; }
 };
 
 // 1 KB from a uniform address plus the lanes' offsets to the LDS byte address `lds`
@@ -143,6 +144,7 @@ struct States {
 
 // Where the states are: of the paged decoding, in slots of HP heads.
 struct ListWhere {
+  static constexpr bool POWERS = false;
   const int32_t* tile_off;
   int B, HP, nwg;
   __device__ __forceinline__ States states(int b, int head) const {
@@ -201,12 +203,12 @@ __global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* _
 #pragma unroll
     for (int u = 0; u < U; ++u) m1 = fmaxf(m1, ml[u][0]);
     const float ref = m1 == -INFINITY ? 0.f : m1;
-    const StateFactor c(M - ref);
+    const StateFactor<Where::POWERS> c(M - ref);
     v *= c.value();
     L = c.sum(L);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const StateFactor w(ml[u][0] - ref);
+      const StateFactor<Where::POWERS> w(ml[u][0] - ref);
       v += x[u] * w.value();
       L += w.sum(ml[u][1]);
     }
@@ -230,7 +232,7 @@ __global__ __launch_bounds__(PF_THREADS) void paged_finish_kernel(const float* _
       L = 0.f;
 #pragma unroll
       for (int k = 0; k < NSLOT; ++k) {
-        const StateFactor f(sm[col][k] - ref);
+        const StateFactor<Where::POWERS> f(sm[col][k] - ref);
         v += *(const f32x4*)&red[grp + k][4 * cg] * f.value();
         L += f.sum(sl[col][k]);
       }

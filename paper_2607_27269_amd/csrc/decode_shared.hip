@@ -783,14 +783,9 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
     const bool move = (__ballot(my > m_run + (as() != AS_BF16 ? E8_SLACK : PD_SLACK)) & heads) != 0;
     // (no branch: products may be under way)
     const float m_new = move ? fmaxf(m_run, my) : m_run, d = m_run - (m_new == -INFINITY ? 0.f : m_new);
-    if constexpr (as() != AS_BF16) {
-      const StateFactor f(d);
-      corr = f.value();
-      l_run = f.sum(l_run);
-    } else {
-      corr = __builtin_amdgcn_exp2f(d);
-      l_run *= corr;
-    }
+    const StateFactor<as() != AS_BF16> f(d);
+    corr = f.value();
+    l_run = f.sum(l_run);
     m_run = m_new;
     return move;
   };
@@ -879,7 +874,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
           *(f32x4*)(po + 32 * c + 8 * g) = f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
     } else {
       const float m0 = a.part_ml[2 * row], l0 = a.part_ml[2 * row + 1], top = fmaxf(m, m0), ref = top == -INFINITY ? 0.f : top;
-      const StateFactor f(m - ref), f0(m0 - ref);
+      const StateFactor<as() != AS_BF16> f(m - ref), f0(m0 - ref);
       l = f.sum(l) + f0.sum(l0);
       m = top;
 #pragma unroll
@@ -1313,7 +1308,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void latent_decode_kernel(Laten
 #pragma unroll
         for (int w = 0; w < PD_WAVES; ++w) {
           const float mw = ml(w)[col];
-          const StateFactor of(mw == -INFINITY ? mw : mw - M);
+          const StateFactor<E4M3> of(mw == -INFINITY ? mw : mw - M);
           f[w] = of.value();
           L += of.sum(ml(w)[32 + col]);
         }
@@ -1353,7 +1348,9 @@ struct LatentStates {
   States own;
   int n = 0, first = 0, step = 0;  // of the shared rows' states: the first slot, and from piece to piece
 };
+template <bool POWERS_>
 struct LatentWhere {
+  static constexpr bool POWERS = POWERS_;
   const int32_t *head, *tile_off, *wg_off, *member, *group;
   int HB, nwg, max_pieces;
   __device__ __forceinline__ LatentStates states(int b, int h) const {
@@ -1494,9 +1491,14 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL),
            (double)d.B * d.max_len * (p.e4m3 ? d.rkv + 2 * d.dr + 4 : DK * 2), KLABEL("latent_decode_kernel"));
   prof_begin(KC_ELEM, s);
-  const LatentWhere w{a.head, a.tile_off, a.wg_off, a.member, a.group, HB, l.nwg, l.max_pieces};
-#define X(a_, b_, c_) \
-  if (DK == a_ && DVL == b_) decode_finish<b_>(d, a.part_o, a.part_ml, w, s);
+  auto where = [&](auto powers) {
+    return LatentWhere<powers()>{a.head, a.tile_off, a.wg_off, a.member, a.group, HB, l.nwg, l.max_pieces};
+  };
+#define X(a_, b_, c_)                                                                                  \
+  if (DK == a_ && DVL == b_) {                                                                         \
+    if (p.e4m3 || images) decode_finish<b_>(d, a.part_o, a.part_ml, where(std::true_type()), s);       \
+    else decode_finish<b_>(d, a.part_o, a.part_ml, where(std::false_type()), s);                       \
+  }
   MLA_SHARED_SHAPES(X)
 #undef X
   prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dv * d.rkv, ((double)l.nwg + d.B) * d.H * (DVL + 2) * 4,

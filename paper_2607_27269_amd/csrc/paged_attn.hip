@@ -387,7 +387,7 @@ __global__ __launch_bounds__(64 * PD_WAVES, OCC) void paged_decode_kernel(PagedD
                   f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
         } else {  // joined to the one that is there
           const float m0 = a.part_ml[2 * row], l0 = a.part_ml[2 * row + 1], top = fmaxf(m_run, m0), ref = top == -INFINITY ? 0.f : top;
-          const StateFactor f(m_run - ref), f0(m0 - ref);
+          const StateFactor<false> f(m_run - ref), f0(m0 - ref);
           l = f.sum(l) + f0.sum(l0);
           m_run = top;
 #pragma unroll
