@@ -424,7 +424,7 @@ int mla_recon_cache_read(const mla_recon_cfg *cfg, const mla_paged_cache *cache,
  * to 2^35.  (Beside rows with latents of 2^118 and more, softmax weights below 2^-14 of the largest may
  * be lost.  Absorbed queries are fp16 with powers of two: what is below 2^-24 of a head's largest counts as zero, as
  * do those of a head that are all below 2^-104; a head with some above and all below 2^-88 has positional logits up to
- * 2^31, before the scale.) */
+ * 2^31, before the scale.  Logits past 2^23, two of them within 8 of each other, may give NaN.) */
 size_t mla_recon_decode_e4m3_workspace_size(const mla_recon_cfg *cfg, int32_t max_len);
 int mla_recon_decode_e4m3(const mla_recon_cfg *cfg, const void *q, const mla_paged_cache *cache,
                           int32_t max_len, const int32_t *lengths, const void *Wuk, const void *Wuv,
@@ -447,6 +447,12 @@ int mla_recon_prefill_e4m3(const mla_recon_cfg *cfg, const void *q, int32_t n_q,
  *   n_groups      number of groups, 0 to batch; with 0 the two arrays may be NULL
  *   group_offsets device int32 [n_groups + 1], not decreasing, within [0, batch]
  *   shared_len    device int32 [n_groups]
+ * Whether that is quicker than decoding each sequence for itself is the caller's to decide: where the caches hold
+ * what is read again it is not (8 sequences of the 8B layer behind 4096 rows 46 us, apart 32; 64 behind 8192 75 and 92).
+ * In a call whose groups have 16 blocks of 32 heads and more on the average, and 32-row tiles of max_len rows for each
+ * group within 256 MiB, the shared rows are multiplied in fp16 with fp16 absorbed queries (errors of 1.7e-3 of the
+ * norm, where bf16 queries give 3e-3), with what mla_recon_decode_e4m3 says of them; latents of a bf16 cache below
+ * 2^-94 lose bits there and those below 2^-104 count as zero.
  * Everything else as for mla_recon_decode_paged, but batch ceil(n_heads / 32) max_len is at most 2^35.  ws 16-byte aligned, of
  * mla_recon_decode_shared_workspace_size bytes (0 = unsupported or invalid) for this cfg, max_len and
  * n_groups, or of those for more sequences, groups or a larger max_len.  (From 16 blocks of 32 heads in all on it

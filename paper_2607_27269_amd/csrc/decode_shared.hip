@@ -37,14 +37,16 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 // behind 8192 shared rows, 400 of their own, bf16, without images: 70 us; with own tiles counted as 3/4, 2/3, 1/2:
 // 71, 76, 87; with images 62, as 3/4 70, as 4/3 and 3/2 62).
 //
-// Three launches: the absorbed queries with the plan, the attention, the merge with W_UV.  Measured (whole calls; 5.2 TB/s
-// is a large copy's rate, 1444 TFLOP/s a large bf16 product's):
-//   e4m3, 64 sequences to 4096 rows, 32 heads of 512 + 64   63 us (7.0 + 50 + 8.7; the rows alone 33)
-//   e4m3, 41 ragged ones to 16001                           44    (5.6 + 30 + 10.6; 14)
-//   e4m3, one of 300, 14 heads of 256 + 32                  17    (4.5 + 9.0 + 3.9)
-//   bf16, 64 behind 8192 shared rows                        85    (13 + 62 + 16.8; operations alone 26)
-//   e4m3, 45 in 7 groups behind 20000                       89    (8.2 + 72 + 17.5; 23)
-//   bf16, 4 behind 1000, 14 heads                           20    (6.0 + 9.8 + 4.4)
+// Three launches: the absorbed queries with the plan, the attention, the merge with W_UV.  Measured: whole calls, beside
+// them the launches as the profiler shows them (with it attached all are longer, so that they add up to more), what the
+// rows' bytes (at a large copy's 5.2 TB/s) or the operations (at a large product's 1444 TFLOP/s) need alone, and decoding
+// each sequence for itself:
+//   e4m3, 64 sequences to 4096 rows, 32 heads of 512 + 64   64 us (7.0, 50, 9.0;   33)
+//   e4m3, 41 ragged ones to 16001                           44    (5.6, 30, 10.7;  14)
+//   e4m3, one of 300, 14 heads of 256 + 32                  17    (4.5, 10, 3.9;   0)
+//   bf16, 64 behind 8192 shared rows                        86    (12, 64, 17.0;   26; apart 87)
+//   e4m3, 45 in 7 groups behind 20000                       89    (7.9, 73, 17.8;  23; apart 71)
+//   bf16, 4 behind 1000, 14 heads                           20    (6.4, 10, 4.3;   0;  apart 17)
 struct LatentDev {
   const char* pool;
   const int32_t* table;
@@ -1471,9 +1473,13 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   MLA_SHARED_SHAPES(X)
 #undef X
 #undef PREP
-  prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dn * d.rkv, (double)d.B * d.H * (d.rkv + d.dr + d.dn + d.dr) * 2,
+  // work at full lengths (the device alone knows the others): images of all rows that there is room for, and
+  // every row read for each sequence
+  const double row_bytes = p.e4m3 ? d.rkv + 2 * d.dr + 4 : DK * 2;
+  prof_end(KC_ELEM, s, 2.0 * d.B * d.H * d.dn * d.rkv,
+           (double)d.B * d.H * (d.rkv + d.dr + d.dn + d.dr) * 2 +
+               (double)p.n_groups * l.image_tiles * PD_KT * (row_bytes + DK * 2 + 4),
            KLABEL("latent_prepare_kernel"));
-  // algorithmic work at full lengths
   prof_begin(KC_ATTN_FWD, s);
 #define X(a_, b_, c_)                                                                      \
   if (DK == a_ && DVL == b_) {                                                             \
@@ -1489,7 +1495,7 @@ hipError_t decode_shared(const DecodeShared& p, hipStream_t s) {
   MLA_SHARED_SHAPES(X)
 #undef X
   prof_end(KC_ATTN_FWD, s, 2.0 * d.B * d.H * (double)d.max_len * (DK + DVL),
-           (double)d.B * d.max_len * (p.e4m3 ? d.rkv + 2 * d.dr + 4 : DK * 2), KLABEL("latent_decode_kernel"));
+           (double)d.B * d.max_len * row_bytes, KLABEL("latent_decode_kernel"));
   prof_begin(KC_ELEM, s);
   auto where = [&](auto powers) {
     return LatentWhere<powers()>{a.head, a.tile_off, a.wg_off, a.member, a.group, HB, l.nwg, l.max_pieces};
